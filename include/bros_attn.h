@@ -124,6 +124,91 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
                   int32_t block_size, int32_t dtype, void* stream);
 
 /*
+ * bros_qkv_append / bros_qkv_append_q8 -- a step's projected rows on their way to
+ * the attention: per-head norms, position rotation, and the write of bros_kv_write,
+ * in one pass.
+ *
+ * Stands before bros_kv_write's step: that call takes rows that are ready to be
+ * cached, this one takes them as the projection leaves them. For every new token
+ * t of sequence s at logical position p (cu_new, pos0 as in bros_kv_write), and
+ * every head row x of its q and k:
+ *     n = x * rsqrt(mean(x^2) + eps) * w            with the norm's weights w, else n = x
+ *     for pair i of the first rotary_dim dims, (a, b) its two values of n:
+ *         a' = a cos - b sin,   b' = b cos + a sin,
+ *         cos = table[r][i],    sin = table[r][rotary_dim / 2 + i]
+ * with r the position of the pair: p, or rope_pos[x][t] for the axis x that holds
+ * pair i. Dims from rotary_dim on are not rotated. q_out[t][h] gets the q rows;
+ * the k rows, and the v rows unchanged, go to the token's slot. Arithmetic is
+ * fp32, rounded once (to the rows' type, or to 8 bits).
+ *
+ *   q, k, v  : rows of new tokens, [num_new_tokens] times num_q_heads or
+ *              num_kv_heads rows of head_dim values, contiguous within a token;
+ *              q_stride, k_stride, v_stride elements from a token to the next
+ *              (three views of one projection's output, or three tensors). dtype
+ *              is theirs, that of the norm's weights and of q_out.
+ *   q_out    : [num_new_tokens][num_q_heads][head_dim]; may be q itself where q's
+ *              tokens are contiguous. q and q_out NULL: no q rows (num_q_heads 0).
+ *   norm     : NULL: none. A weight that is NULL leaves its rows without a norm.
+ *   rope     : NULL: no rotation.
+ *   rope_pos : int32 [axes][num_new_tokens], device; NULL (one axis only): the
+ *              logical position. Both structs are HOST memory, read during the call.
+ *
+ * bros_qkv_append stores into pools of the rows' type; bros_qkv_append_q8 into an
+ * 8-bit pool: k_pool and v_pool hold e4m3 codes, one byte each, [num_blocks]
+ * [num_kv_heads][16][head_dim], and kv_scales, uint8 [num_blocks][num_kv_heads]
+ * [2][16], the scales of the K rows and of the V rows, one byte e + 127 per slot for
+ * the scale 2^e. A row's e is the least integer, within -100 .. 120, with
+ * max |x| <= 448 * 2^e over its finite values; a code is x * 2^-e rounded to the
+ * nearest e4m3 value, ties to even; infinities and NaNs are stored as NaN. The
+ * scale belongs to the slot, as the row does: two requests may share a block.
+ *
+ * A token in no sequence's range is left alone: its q_out row keeps what it held,
+ * nothing is stored (rows of padding behind cu_new[num_seqs]). A token with a
+ * rotation position outside [0, table_rows) gets zero q rows and is not stored. A
+ * token without a valid table entry gets its q rows and is not stored.
+ *
+ * Errors as bros_kv_write; also BROS_E_SHAPE for a stride below a token's rows or
+ * one that is not a multiple of 16 bytes, q without q_out, more than 2^31 - 1 head
+ * rows, a rotary_dim outside 16 .. head_dim or not a multiple of 16, axes outside
+ * 1 .. 4, axes without rope_pos, or sections that do not add up to rotary_dim / 2.
+ */
+enum bros_rope_pairs { BROS_ROPE_HALF = 0,       /* pair i: dims i and i + rotary_dim / 2 */
+                       BROS_ROPE_ADJACENT = 1 }; /* pair i: dims 2 i and 2 i + 1          */
+typedef struct bros_rope {
+  const float* table;    /* device fp32 [table_rows][rotary_dim], 16-byte aligned: cosines of the pairs, then sines */
+  int32_t table_rows;
+  int32_t rotary_dim;    /* multiple of 16, 16 .. head_dim */
+  int32_t pairs;         /* bros_rope_pairs */
+  int32_t axes;          /* 1 .. 4 rows of rope_pos */
+  int32_t sections[4];   /* axes > 1: pairs of each axis, the first pairs axis 0's, adding up to rotary_dim / 2 */
+} bros_rope;
+typedef struct bros_qk_norm {
+  const void* q_weight;  /* device [head_dim] of the rows' type, 16-byte aligned, or NULL */
+  const void* k_weight;
+  float eps;
+} bros_qk_norm;
+int bros_qkv_append(void* q_out, const void* q, const void* k, const void* v,
+                    int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                    int32_t num_new_tokens, int32_t num_q_heads,
+                    const bros_qk_norm* norm, const bros_rope* rope, const int32_t* rope_pos,
+                    void* k_pool, void* v_pool, int32_t num_blocks,
+                    const int32_t* block_tables, int32_t max_blocks_per_seq,
+                    const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                    const int32_t* pos0, const int32_t* cu_new,
+                    int32_t num_seqs, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t block_size, int32_t dtype, void* stream);
+int bros_qkv_append_q8(void* q_out, const void* q, const void* k, const void* v,
+                       int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                       int32_t num_new_tokens, int32_t num_q_heads,
+                       const bros_qk_norm* norm, const bros_rope* rope, const int32_t* rope_pos,
+                       void* k_pool, void* v_pool, uint8_t* kv_scales, int32_t num_blocks,
+                       const int32_t* block_tables, int32_t max_blocks_per_seq,
+                       const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                       const int32_t* pos0, const int32_t* cu_new,
+                       int32_t num_seqs, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, int32_t dtype, void* stream);
+
+/*
  * bros_attn_decode -- one query row per sequence over its whole paged context.
  *
  * Defines: the decode attention of Sec. 2.1 (the new token attends to the
@@ -325,6 +410,32 @@ int bros_kv_scatter(const void* k_in, const void* v_in,
                     void* k_pool, void* v_pool, int32_t num_blocks,
                     int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
                     int32_t dtype, void* stream);
+
+/*
+ * bros_kv_gather_q8 / bros_kv_scatter_q8 / bros_kv_read_q8 -- slots of an 8-bit pool.
+ *
+ * Gather and scatter are bros_kv_gather and bros_kv_scatter for the pools of
+ * bros_qkv_append_q8: the codes of slot i to or from k_out[i][h][:] / v_out[i][h][:]
+ * (one byte a value), and its scale bytes to or from scales[i][h][0] (K) and [1] (V),
+ * uint8 [num_slots][num_kv_heads][2]. Bytes move unchanged, so a row that comes back
+ * is the row that went, in any slot. Read gives the values the slots stand for,
+ * code * 2^e, exact (from 2^128 on infinite), in BROS_BF16 or BROS_F32: [num_slots][num_kv_heads][head_dim] each
+ * (for a pool of that type, through bros_kv_scatter, on another instance).
+ * Ids, their limits and the errors as for bros_kv_gather and bros_kv_scatter: an id
+ * outside the pool gives zeros, and is skipped by the scatter.
+ */
+int bros_kv_gather_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                      const int32_t* slot_ids, int32_t num_slots,
+                      void* k_out, void* v_out, uint8_t* scales_out,
+                      int32_t num_kv_heads, int32_t head_dim, int32_t block_size, void* stream);
+int bros_kv_scatter_q8(const void* k_in, const void* v_in, const uint8_t* scales_in,
+                       const int32_t* slot_ids, int32_t num_slots,
+                       void* k_pool, void* v_pool, uint8_t* kv_scales, int32_t num_blocks,
+                       int32_t num_kv_heads, int32_t head_dim, int32_t block_size, void* stream);
+int bros_kv_read_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                    const int32_t* slot_ids, int32_t num_slots,
+                    void* k_out, void* v_out,
+                    int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype, void* stream);
 
 /*
  * bros_copy_dma -- an asynchronous copy of `bytes` bytes on a copy (SDMA)

@@ -11,3 +11,6 @@ from .paged_attention import (  # noqa: F401
 from .checkpoint import (  # noqa: F401
     slot_ids, kv_gather, kv_scatter, overwritten_peer_tokens,
 )
+from .append import (  # noqa: F401
+    E4M3, NAN_CODE, rotate, norm, row_exponents, encode, decode_rows,
+)

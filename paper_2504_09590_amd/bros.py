@@ -23,6 +23,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbros_att
 BROS_F32, BROS_BF16 = 0, 1
 BROS_RT, BROS_BE = 0, 1
 BROS_WS_DECODE, BROS_WS_PREFILL = 0, 1
+BROS_ROPE_HALF, BROS_ROPE_ADJACENT = 0, 1
 STATUS = {0: "BROS_OK", -1: "BROS_E_NULL", -2: "BROS_E_SHAPE", -3: "BROS_E_DTYPE",
           -4: "BROS_E_UNSUPPORTED", -5: "BROS_E_WORKSPACE", -6: "BROS_E_HIP", -7: "BROS_E_TABLE",
           -8: "BROS_E_NOMEM"}
@@ -34,13 +35,23 @@ EXPORTED = ["bros_status_str", "bros_last_error", "bros_abi_version", "bros_kv_w
             "bros_mgr_create", "bros_mgr_destroy", "bros_mgr_add_request", "bros_mgr_release", "bros_mgr_grow",
             "bros_mgr_restore", "bros_mgr_query", "bros_mgr_table", "bros_mgr_free_blocks", "bros_mgr_validate", "bros_mgr_available",
             "bros_mgr_entries_needed", "bros_mgr_preemption_table", "bros_schedule", "bros_next_batch_size",
-            "bros_mgr_grow_batch", "bros_mgr_plan_bound", "bros_schedule_pulled", "bros_set_decode_kernel_events"]
+            "bros_mgr_grow_batch", "bros_mgr_plan_bound", "bros_schedule_pulled", "bros_set_decode_kernel_events",
+            "bros_qkv_append", "bros_qkv_append_q8", "bros_kv_gather_q8", "bros_kv_scatter_q8", "bros_kv_read_q8"]
 
 
 class BrosError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
         self.status = status
+
+
+class _Rope(ctypes.Structure):     # bros_rope
+    _fields_ = [("table", ctypes.c_void_p), ("table_rows", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4)]
+
+
+class _QkNorm(ctypes.Structure):   # bros_qk_norm
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
 def _load() -> ctypes.CDLL:
@@ -84,6 +95,19 @@ def _load() -> ctypes.CDLL:
     lib.bros_slot_ids.restype = ctypes.c_int
     lib.bros_copy_dma.argtypes = [P, P, Z, P]
     lib.bros_copy_dma.restype = ctypes.c_int
+    L = ctypes.c_int64
+    rows = [P, P, P, P, L, L, L, I, I, ctypes.POINTER(_QkNorm), ctypes.POINTER(_Rope), P]
+    meta = [I, P, I, P, P, I, P, P, I, I, I, I, I, P]
+    lib.bros_qkv_append.argtypes = rows + [P, P] + meta
+    lib.bros_qkv_append.restype = ctypes.c_int
+    lib.bros_qkv_append_q8.argtypes = rows + [P, P, P] + meta
+    lib.bros_qkv_append_q8.restype = ctypes.c_int
+    lib.bros_kv_gather_q8.argtypes = [P, P, P, I, P, I, P, P, P, I, I, I, P]
+    lib.bros_kv_gather_q8.restype = ctypes.c_int
+    lib.bros_kv_scatter_q8.argtypes = [P, P, P, P, I, P, P, P, I, I, I, I, P]
+    lib.bros_kv_scatter_q8.restype = ctypes.c_int
+    lib.bros_kv_read_q8.argtypes = [P, P, P, I, P, I, P, P, I, I, I, I, P]
+    lib.bros_kv_read_q8.restype = ctypes.c_int
     from . import manager as _m   # host block manager and scheduler signatures
     _m.declare(lib)
     return lib
@@ -156,6 +180,177 @@ def bros_kv_write(k_new, v_new, k_pool, v_pool, block_tables, dir, cls, pos0, cu
                              _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls),
                              _dir_mode(dir, block_tables), _ptr(pos0), _ptr(cu_new), int(cu_new.shape[0]) - 1, hkv, d, bs,
                              _dtype_code(k_pool), _stream(stream)))
+
+
+class Rope:
+    """A position rotation for bros_qkv_append: `table` float32 [positions][rotary_dim]
+    on the device, the cosines of the pairs, then the sines (rope.rope_table builds
+    one). `pairs` says which dims a pair has; `sections`, for positions with
+    several axes, how many pairs each axis turns. Made once and kept."""
+
+    def __init__(self, table, pairs: int = BROS_ROPE_HALF, sections=None):
+        if table.dtype != torch.float32 or table.dim() != 2:
+            raise ValueError("the table must be a float32 tensor [positions][rotary_dim]")
+        sections = () if sections is None else tuple(int(x) for x in sections)
+        if len(sections) > 4:
+            raise ValueError(f"{len(sections)} sections; at most 4")
+        self.table = table
+        self.axes = max(len(sections), 1)
+        self._c = _Rope(_ptr(table), int(table.shape[0]), int(table.shape[1]), int(pairs), self.axes,
+                        (ctypes.c_int32 * 4)(*sections))
+        self.ref = ctypes.byref(self._c)
+
+
+class QkNorm:
+    """Weights (one value per dim of a head, of the rows' type) and epsilon of the
+    norms of q and k rows for bros_qkv_append; a weight of None: no norm. Made
+    once and kept."""
+
+    def __init__(self, q_weight, k_weight, eps: float = 1e-6):
+        self.weights = [w for w in (q_weight, k_weight) if w is not None]
+        if any(w.dim() != 1 or w.dtype != self.weights[0].dtype for w in self.weights):
+            raise ValueError("weights must be vectors of one type")
+        self._c = _QkNorm(_ptr(q_weight), _ptr(k_weight), float(eps))
+        self.ref = ctypes.byref(self._c)
+
+
+def _on_device(*tensors) -> None:
+    """Every tensor (None aside) lies on the current device, where the kernel runs."""
+    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            raise ValueError(f"a tensor is on {t.device}, not on the current device")
+
+
+def _check_meta(rows: int, block_tables, dir, cls, *offsets) -> None:
+    """Metadata tensors of `rows` sequences: types and lengths."""
+    if block_tables.dtype != torch.int32 or block_tables.dim() != 2 or block_tables.shape[0] != rows:
+        raise ValueError(f"block_tables must be int32 [{rows}][max_blocks]")
+    if dir is not None and (dir.dtype != torch.int8 or dir.shape[0] != rows):
+        raise ValueError(f"dir must be int8 with {rows} rows")
+    _dir_mode(dir, block_tables)
+    if cls is not None and (cls.dtype != torch.uint8 or cls.shape[0] != rows):
+        raise ValueError(f"cls must be uint8 [{rows}]")
+    for t, n in offsets:
+        if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n:
+            raise ValueError(f"an offset or length array must be int32 [{n}]")
+
+
+def _token_rows(t, name: str, tokens: int, like):
+    """Address and elements between tokens of rows [tokens][heads][head_dim], contiguous within a token."""
+    if t.dim() != 3 or t.shape[0] != tokens or t.dtype != like.dtype or t.shape[2] != like.shape[2]:
+        raise ValueError(f"{name} must be [{tokens}][heads][{like.shape[2]}] {like.dtype}")
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{name}'s heads must be contiguous within a token")
+    # (one token's stride, or none's, is never used)
+    return t.data_ptr(), (t.stride(0) if tokens > 1 else t.shape[1] * t.shape[2])
+
+
+def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm, pools):
+    nb, hkv, bs, _ = pools[0].shape
+    tn, d = int(k.shape[0]), int(k.shape[2])
+    kp, ks = _token_rows(k, "k", tn, k)
+    vp, vs = _token_rows(v, "v", tn, k)
+    if k.shape[1] != hkv or v.shape[1] != hkv:
+        raise ValueError(f"k and v must have the pool's {hkv} heads")
+    qp, qs, hq = None, 0, 0
+    if q is not None:
+        qp, qs = _token_rows(q, "q", tn, k)
+        hq = int(q.shape[1])
+        if q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out must have q's shape and type")
+    if norm is not None and any(w.dtype != k.dtype or w.shape[0] != d for w in norm.weights):
+        raise ValueError(f"norm weights must be [{d}] {k.dtype}")
+    if rope_pos is not None:
+        if rope is None:
+            raise ValueError("rope_pos without a rotation")
+        if rope_pos.dtype != torch.int32 or rope_pos.numel() != rope.axes * tn:
+            raise ValueError(f"rope_pos must be int32 [{rope.axes}][{tn}]")
+    S = int(cu_new.shape[0]) - 1
+    _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
+    _on_device(*pools, q_out if q is not None else None, q, k, v, block_tables, dir, cls, pos0, cu_new, rope_pos,
+               None if rope is None else rope.table, *(() if norm is None else norm.weights))
+    head = (_ptr(q_out) if q is not None else None, qp, kp, vp, qs, ks, vs, tn, hq,
+            None if norm is None else norm.ref, None if rope is None else rope.ref, _ptr(rope_pos))
+    tail = (nb, _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls), _dir_mode(dir, block_tables),
+            _ptr(pos0), _ptr(cu_new), S, hkv, d, bs, _dtype_code(k))
+    return head, tail
+
+
+def bros_qkv_append(q_out, q, k, v, k_pool, v_pool, block_tables, dir, cls, pos0, cu_new, rope=None, rope_pos=None,
+                    norm=None, stream=None):
+    """Norms and position rotation of new tokens' q and k rows; q to q_out, k and v to
+    their slots of the pools. q, k, v: [Tn][heads][D], contiguous within a token (views
+    of one projection's output will do); q and q_out None: k and v alone."""
+    if k.dtype != k_pool.dtype or v_pool.dtype != k_pool.dtype or v_pool.shape != k_pool.shape:
+        raise ValueError(f"rows are {k.dtype}, the pools {k_pool.dtype} and {v_pool.dtype}")
+    head, tail = _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm, (k_pool, v_pool))
+    _check(LIB.bros_qkv_append(*head, _ptr(k_pool), _ptr(v_pool), *tail, _stream(stream)))
+
+
+def _eight_bit(k_pool, v_pool, kv_scales):
+    """Checks an 8-bit pool: codes of one byte and [num_blocks][Hkv][2][16] scale bytes."""
+    nb, hkv, bs, d = k_pool.shape
+    if k_pool.element_size() != 1 or v_pool.element_size() != 1 or v_pool.shape != k_pool.shape:
+        raise ValueError("an 8-bit pool holds one byte per value, k and v alike")
+    if kv_scales.element_size() != 1 or tuple(kv_scales.shape) != (nb, hkv, 2, bs):
+        raise ValueError(f"kv_scales must be uint8 [{nb}][{hkv}][2][{bs}]")
+    return nb, hkv, bs, d
+
+
+def bros_qkv_append_q8(q_out, q, k, v, k_pool, v_pool, kv_scales, block_tables, dir, cls, pos0, cu_new, rope=None,
+                       rope_pos=None, norm=None, stream=None):
+    """bros_qkv_append into an 8-bit pool: e4m3 codes [nb][Hkv][16][D] (uint8 or
+    float8_e4m3fn) and scale bytes [nb][Hkv][2][16]."""
+    _eight_bit(k_pool, v_pool, kv_scales)
+    head, tail = _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm,
+                              (k_pool, v_pool, kv_scales))
+    _check(LIB.bros_qkv_append_q8(*head, _ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), *tail, _stream(stream)))
+
+
+def _dense(n: int, pools, ids, rows, scales=None, one_byte=True) -> None:
+    """Dense sides of a move of n slots: [>= n][Hkv][D] each, scales [>= n][Hkv][2], on the
+    current device or in pinned host memory."""
+    hkv, d = pools[0].shape[1], pools[0].shape[3]
+    if n < 0 or (ids is not None and (ids.dtype != torch.int32 or ids.numel() < n)):
+        raise ValueError(f"slot_ids must be int32 and hold {n} ids")
+    for t in rows:
+        if t.shape[0] < n or tuple(t.shape[1:]) != (hkv, d) or (one_byte and t.element_size() != 1):
+            raise ValueError(f"a dense buffer must hold [{n}][{hkv}][{d}]" + (" bytes" if one_byte else ""))
+    if scales is not None and (scales.shape[0] < n or tuple(scales.shape[1:]) != (hkv, 2) or scales.element_size() != 1):
+        raise ValueError(f"the scales must hold [{n}][{hkv}][2] bytes")
+    _on_device(ids, *pools, *(t for t in (*rows, scales) if t is not None and (t.is_cuda or not t.is_pinned())))
+
+
+def bros_kv_gather_q8(k_pool, v_pool, kv_scales, slot_ids, k_out, v_out, scales_out, num_slots: int | None = None,
+                      stream=None):
+    """Codes and scale bytes of an 8-bit pool's slots into dense [n][Hkv][D] and [n][Hkv][2] buffers."""
+    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
+    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
+    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_out, v_out), scales_out)
+    _check(LIB.bros_kv_gather_q8(_ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb, _ptr(slot_ids), n, _ptr(k_out),
+                                 _ptr(v_out), _ptr(scales_out), hkv, d, bs, _stream(stream)))
+
+
+def bros_kv_scatter_q8(k_in, v_in, scales_in, slot_ids, k_pool, v_pool, kv_scales, num_slots: int | None = None,
+                       stream=None):
+    """Dense codes and scale bytes back into an 8-bit pool's slots; ids outside the pool are skipped."""
+    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
+    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
+    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_in, v_in), scales_in)
+    _check(LIB.bros_kv_scatter_q8(_ptr(k_in), _ptr(v_in), _ptr(scales_in), _ptr(slot_ids), n, _ptr(k_pool),
+                                  _ptr(v_pool), _ptr(kv_scales), nb, hkv, d, bs, _stream(stream)))
+
+
+def bros_kv_read_q8(k_pool, v_pool, kv_scales, slot_ids, k_out, v_out, num_slots: int | None = None, stream=None):
+    """The values of an 8-bit pool's slots into dense [n][Hkv][D] tensors (bfloat16 or float32)."""
+    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
+    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
+    if k_out.dtype != v_out.dtype:
+        raise ValueError("k_out and v_out must have one type")
+    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_out, v_out), one_byte=False)
+    _check(LIB.bros_kv_read_q8(_ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb, _ptr(slot_ids), n, _ptr(k_out),
+                               _ptr(v_out), hkv, d, bs, _dtype_code(k_out), _stream(stream)))
 
 
 def bros_set_decode_kernel_events(before=None, after=None):

@@ -57,6 +57,131 @@ float resolve_scale(float scale, int head_dim) {
   return s * 1.4426950408889634f;   // log2(e): the kernels use base-2 exponentials
 }
 
+// bros_qkv_append and, with scales (`eight`), bros_qkv_append_q8.
+int qkv_append(const char* fn, bool eight, void* q_out, const void* q, const void* k, const void* v,
+               int64_t q_stride, int64_t k_stride, int64_t v_stride, int32_t num_new_tokens, int32_t num_q_heads,
+               const bros_qk_norm* norm, const bros_rope* rope, const int32_t* rope_pos,
+               void* k_pool, void* v_pool, uint8_t* kv_scales, int32_t num_blocks,
+               const int32_t* block_tables, int32_t max_blocks_per_seq, const int8_t* dir, const uint8_t* cls,
+               int32_t dir_per_entry, const int32_t* pos0, const int32_t* cu_new, int32_t num_seqs,
+               int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {
+  int group = 0;
+  int st = check_shapes(fn, num_kv_heads, num_kv_heads, head_dim, block_size, dtype, &group);
+  if (st) return st;
+  if (num_new_tokens < 0 || num_seqs < 0 || num_q_heads < 0)
+    return fail(BROS_E_SHAPE, "%s: negative count (tokens=%d seqs=%d Hq=%d)", fn, num_new_tokens, num_seqs, num_q_heads);
+  if (num_kv_heads > 16384 || num_q_heads > 16384)
+    return fail(BROS_E_UNSUPPORTED, "%s: %d query and %d KV heads; at most 16384", fn, num_q_heads, num_kv_heads);
+  bros::AppendArgs a{};
+  if (rope != nullptr) {
+    if (rope->rotary_dim < 16 || rope->rotary_dim > head_dim || rope->rotary_dim % 16 != 0)
+      return fail(BROS_E_SHAPE, "%s: rotary_dim %d is not a multiple of 16 in 16 .. %d", fn, rope->rotary_dim, head_dim);
+    if (rope->pairs != BROS_ROPE_HALF && rope->pairs != BROS_ROPE_ADJACENT)
+      return fail(BROS_E_SHAPE, "%s: pairs %d is neither BROS_ROPE_HALF nor BROS_ROPE_ADJACENT", fn, rope->pairs);
+    if (rope->axes < 1 || rope->axes > 4) return fail(BROS_E_SHAPE, "%s: %d axes; 1 to 4", fn, rope->axes);
+    if (rope->table_rows <= 0) return fail(BROS_E_SHAPE, "%s: table_rows %d must be positive", fn, rope->table_rows);
+    if (rope->table == nullptr) return fail(BROS_E_NULL, "%s: rope->table is NULL", fn);
+    if (!aligned(rope->table, 16)) return fail(BROS_E_SHAPE, "%s: rope->table is not 16-byte aligned", fn);
+    if (rope->axes > 1 && rope_pos == nullptr) return fail(BROS_E_SHAPE, "%s: %d axes but rope_pos is NULL", fn, rope->axes);
+    if (!aligned(rope_pos, 4)) return fail(BROS_E_SHAPE, "%s: rope_pos is not 4-byte aligned", fn);
+    // first pair behind each of the axes 0, 1 and 2 (one axis holds all pairs)
+    const int32_t half = rope->rotary_dim / 2;
+    int64_t end = rope->axes == 1 ? half : 0;
+    for (int x = 0; x < 4; ++x) {
+      if (rope->axes > 1 && x < rope->axes) {
+        if (rope->sections[x] < 0) return fail(BROS_E_SHAPE, "%s: sections[%d] is negative", fn, x);
+        end += rope->sections[x];
+      }
+      if (x < 3) a.axis_end[x] = (int32_t)std::min<int64_t>(end, half);
+    }
+    if (end != half)
+      return fail(BROS_E_SHAPE, "%s: sections add up to %lld, not rotary_dim / 2 = %d", fn, (long long)end, half);
+    a.rope_table = rope->table;
+    a.rope_pos = rope_pos;
+    a.table_rows = rope->table_rows;
+    a.rotary_dim = rope->rotary_dim;
+    a.adjacent = rope->pairs;
+    a.axes = rope->axes;
+  }
+  if ((q == nullptr) != (q_out == nullptr)) return fail(BROS_E_NULL, "%s: give both q and q_out, or neither", fn);
+  if (q != nullptr && num_q_heads == 0) return fail(BROS_E_SHAPE, "%s: q rows but num_q_heads is 0", fn);
+  const int32_t hq = q == nullptr ? 0 : num_q_heads;
+  if ((int64_t)num_new_tokens * (hq + 2 * (int64_t)num_kv_heads) > 0x7fffffffLL)
+    return fail(BROS_E_SHAPE, "%s: more than 2^31 - 1 head rows", fn);
+  if (num_new_tokens == 0) return ok();
+  if (num_seqs == 0) return fail(BROS_E_SHAPE, "%s: %d new tokens but no sequences", fn, num_new_tokens);
+  if (!k || !v || !k_pool || !v_pool || !pos0 || !cu_new || (eight && !kv_scales))
+    return fail(BROS_E_NULL, "%s: a tensor or offset pointer is NULL", fn);
+  st = check_meta(fn, block_tables, max_blocks_per_seq, dir, cls, dir_per_entry, num_blocks);
+  if (st) return st;
+  const int64_t per16 = dtype == BROS_BF16 ? 8 : 4;   // elements of 16 bytes
+  const auto bad_stride = [&](int64_t stride, int32_t heads) {
+    return stride < (int64_t)heads * head_dim || stride % per16 != 0 || stride > (1LL << 40);
+  };
+  if ((q && bad_stride(q_stride, hq)) || bad_stride(k_stride, num_kv_heads) || bad_stride(v_stride, num_kv_heads))
+    return fail(BROS_E_SHAPE, "%s: a stride (q %lld, k %lld, v %lld) is below a token's rows or not a multiple of 16 bytes", fn,
+                (long long)q_stride, (long long)k_stride, (long long)v_stride);
+  if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
+      !aligned(kv_scales, 16) || (norm && (!aligned(norm->q_weight, 16) || !aligned(norm->k_weight, 16))))
+    return fail(BROS_E_SHAPE, "%s: tensors must be 16-byte aligned", fn);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  if (norm != nullptr) {
+    a.q_norm = norm->q_weight;
+    a.k_norm = norm->k_weight;
+    a.eps = norm->eps;
+  }
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  a.kv_scales = eight ? kv_scales : nullptr;
+  a.block_tables = block_tables;
+  a.dir = dir;
+  a.cls = cls;
+  a.pos0 = pos0;
+  a.cu_new = cu_new;
+  a.dir_per_entry = dir_per_entry;
+  a.num_new_tokens = num_new_tokens;
+  a.num_seqs = num_seqs;
+  a.num_blocks = num_blocks;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.num_q_heads = hq;
+  a.num_kv_heads = num_kv_heads;
+  return launch_status(fn, bros::launch_append(a, dtype == BROS_BF16, static_cast<hipStream_t>(stream)));
+}
+
+// Checks of the three calls on slots of an 8-bit pool; sets *a.
+int check_move_q8(const char* fn, const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                  const int32_t* slot_ids, int32_t num_slots, const void* k_dense, const void* v_dense,
+                  const uint8_t* scales_dense, bool with_scales, int32_t num_kv_heads, int32_t head_dim,
+                  int32_t block_size, int32_t dtype, bros::KvMoveQ8Args* a) {
+  int group = 0;
+  const int st = check_shapes(fn, num_kv_heads, num_kv_heads, head_dim, block_size, dtype, &group);
+  if (st) return st;
+  if (num_kv_heads > 16384) return fail(BROS_E_UNSUPPORTED, "%s: %d KV heads; at most 16384", fn, num_kv_heads);
+  if (num_slots < 0) return fail(BROS_E_SHAPE, "%s: negative num_slots %d", fn, num_slots);
+  if (num_slots == 0) return BROS_OK;
+  if (num_blocks <= 0) return fail(BROS_E_SHAPE, "%s: num_blocks %d must be positive", fn, num_blocks);
+  if (!k_pool || !v_pool || !kv_scales || !k_dense || !v_dense || !slot_ids || (with_scales && !scales_dense))
+    return fail(BROS_E_NULL, "%s: a pool, dense buffer, scales or slot_ids pointer is NULL", fn);
+  if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(kv_scales, 16) || !aligned(k_dense, 16) ||
+      !aligned(v_dense, 16) || !aligned(slot_ids, 4))
+    return fail(BROS_E_SHAPE, "%s: tensors must be 16-byte aligned", fn);
+  *a = bros::KvMoveQ8Args{const_cast<void*>(k_pool), const_cast<void*>(v_pool), const_cast<uint8_t*>(kv_scales),
+                          const_cast<void*>(k_dense), const_cast<void*>(v_dense), const_cast<uint8_t*>(scales_dense),
+                          slot_ids, num_slots, num_blocks, num_kv_heads};
+  return BROS_OK;
+}
+
+int move_q8_status(const char* fn, int32_t num_slots, hipError_t e) {
+  if (e == hipErrorInvalidValue) return fail(BROS_E_SHAPE, "%s: %d slots make a grid too large", fn, num_slots);
+  return launch_status(fn, e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -402,6 +527,75 @@ int bros_kv_scatter(const void* k_in, const void* v_in,
                     int32_t dtype, void* stream) {
   return kv_move("bros_kv_scatter", false, k_pool, v_pool, num_blocks, slot_ids, num_slots,
                  const_cast<void*>(k_in), const_cast<void*>(v_in), num_kv_heads, head_dim, block_size, dtype, stream);
+}
+
+int bros_qkv_append(void* q_out, const void* q, const void* k, const void* v,
+                    int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                    int32_t num_new_tokens, int32_t num_q_heads,
+                    const bros_qk_norm* norm, const bros_rope* rope, const int32_t* rope_pos,
+                    void* k_pool, void* v_pool, int32_t num_blocks,
+                    const int32_t* block_tables, int32_t max_blocks_per_seq,
+                    const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                    const int32_t* pos0, const int32_t* cu_new,
+                    int32_t num_seqs, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t block_size, int32_t dtype, void* stream) {
+  return qkv_append("bros_qkv_append", false, q_out, q, k, v, q_stride, k_stride, v_stride, num_new_tokens, num_q_heads,
+                    norm, rope, rope_pos, k_pool, v_pool, nullptr, num_blocks, block_tables, max_blocks_per_seq, dir, cls,
+                    dir_per_entry, pos0, cu_new, num_seqs, num_kv_heads, head_dim, block_size, dtype, stream);
+}
+
+int bros_qkv_append_q8(void* q_out, const void* q, const void* k, const void* v,
+                       int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                       int32_t num_new_tokens, int32_t num_q_heads,
+                       const bros_qk_norm* norm, const bros_rope* rope, const int32_t* rope_pos,
+                       void* k_pool, void* v_pool, uint8_t* kv_scales, int32_t num_blocks,
+                       const int32_t* block_tables, int32_t max_blocks_per_seq,
+                       const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                       const int32_t* pos0, const int32_t* cu_new,
+                       int32_t num_seqs, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, int32_t dtype, void* stream) {
+  return qkv_append("bros_qkv_append_q8", true, q_out, q, k, v, q_stride, k_stride, v_stride, num_new_tokens, num_q_heads,
+                    norm, rope, rope_pos, k_pool, v_pool, kv_scales, num_blocks, block_tables, max_blocks_per_seq, dir, cls,
+                    dir_per_entry, pos0, cu_new, num_seqs, num_kv_heads, head_dim, block_size, dtype, stream);
+}
+
+int bros_kv_gather_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                      const int32_t* slot_ids, int32_t num_slots,
+                      void* k_out, void* v_out, uint8_t* scales_out,
+                      int32_t num_kv_heads, int32_t head_dim, int32_t block_size, void* stream) {
+  const char* fn = "bros_kv_gather_q8";
+  bros::KvMoveQ8Args a{};
+  const int st = check_move_q8(fn, k_pool, v_pool, kv_scales, num_blocks, slot_ids, num_slots, k_out, v_out, scales_out,
+                               true, num_kv_heads, head_dim, block_size, BROS_BF16, &a);
+  if (st) return st;
+  if (num_slots == 0) return ok();
+  return move_q8_status(fn, num_slots, bros::launch_kv_move_q8(a, true, static_cast<hipStream_t>(stream)));
+}
+
+int bros_kv_scatter_q8(const void* k_in, const void* v_in, const uint8_t* scales_in,
+                       const int32_t* slot_ids, int32_t num_slots,
+                       void* k_pool, void* v_pool, uint8_t* kv_scales, int32_t num_blocks,
+                       int32_t num_kv_heads, int32_t head_dim, int32_t block_size, void* stream) {
+  const char* fn = "bros_kv_scatter_q8";
+  bros::KvMoveQ8Args a{};
+  const int st = check_move_q8(fn, k_pool, v_pool, kv_scales, num_blocks, slot_ids, num_slots, k_in, v_in, scales_in,
+                               true, num_kv_heads, head_dim, block_size, BROS_BF16, &a);
+  if (st) return st;
+  if (num_slots == 0) return ok();
+  return move_q8_status(fn, num_slots, bros::launch_kv_move_q8(a, false, static_cast<hipStream_t>(stream)));
+}
+
+int bros_kv_read_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                    const int32_t* slot_ids, int32_t num_slots,
+                    void* k_out, void* v_out,
+                    int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {
+  const char* fn = "bros_kv_read_q8";
+  bros::KvMoveQ8Args a{};
+  const int st = check_move_q8(fn, k_pool, v_pool, kv_scales, num_blocks, slot_ids, num_slots, k_out, v_out, nullptr,
+                               false, num_kv_heads, head_dim, block_size, dtype, &a);
+  if (st) return st;
+  if (num_slots == 0) return ok();
+  return move_q8_status(fn, num_slots, bros::launch_kv_read_q8(a, dtype == BROS_BF16, static_cast<hipStream_t>(stream)));
 }
 
 int bros_set_decode_kernel_events(void* before, void* after) {

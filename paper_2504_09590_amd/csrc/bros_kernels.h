@@ -25,6 +25,43 @@ struct KvWriteArgs {
   int32_t num_kv_heads;
 };
 
+// New rows with their norms and rotation (append.hip): q rows to q_out, k and v
+// rows to their slots. Null norm weights: no norm. rope_table null (rotary_dim 0): no rotation.
+struct AppendArgs {
+  const void* q;              // null: no q rows (num_q_heads 0)
+  const void* k;
+  const void* v;
+  int64_t q_stride;           // elements from one token's rows to the next's
+  int64_t k_stride;
+  int64_t v_stride;
+  void* q_out;
+  const void* q_norm;         // [128] each, of the rows' type
+  const void* k_norm;
+  float eps;
+  const float* rope_table;    // [table_rows][rotary_dim]: cosines of the pairs, then sines
+  const int32_t* rope_pos;    // [axes][num_new_tokens], or null: the logical position
+  int32_t table_rows;
+  int32_t rotary_dim;
+  int32_t adjacent;           // pairs (2 i, 2 i + 1) instead of (i, i + rotary_dim / 2)
+  int32_t axes;               // 1..4 rows of rope_pos
+  int32_t axis_end[3];        // first pair behind axes 0, 1 and 2
+  void* k_pool;
+  void* v_pool;
+  uint8_t* kv_scales;         // [num_blocks][Hkv][2][16], or null: the pool is of the rows' type
+  const int32_t* block_tables;
+  const int8_t* dir;
+  const uint8_t* cls;
+  const int32_t* pos0;
+  const int32_t* cu_new;
+  int32_t dir_per_entry;      // dir is [S][max_blocks_per_seq] (else [S])
+  int32_t num_new_tokens;
+  int32_t num_seqs;
+  int32_t num_blocks;
+  int32_t max_blocks_per_seq;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+};
+
 // Decode rows (cu_q == nullptr): row r is sequence r with context ctx_lens[r].
 // For the fp32 prefill chunks (cu_q != nullptr): row r belongs to the sequence s
 // with cu_q[s] <= r < cu_q[s+1] and sees the first ctx_lens[s] - (cu_q[s+1] -
@@ -113,6 +150,21 @@ struct KvMoveArgs {
   int32_t row_bytes;      // head_dim * element bytes (a multiple of 16)
 };
 
+// Rows of an 8-bit pool by slot id: codes and scales to or from dense buffers, or
+// their values into dense buffers (scales_dense unused).
+struct KvMoveQ8Args {
+  void* k_pool;           // (only read by gather and read)
+  void* v_pool;
+  uint8_t* kv_scales;     // [num_blocks][Hkv][2][16]
+  void* k_dense;
+  void* v_dense;
+  uint8_t* scales_dense;  // [num_slots][Hkv][2]
+  const int32_t* slot_ids;
+  int32_t num_slots;
+  int32_t num_blocks;
+  int32_t num_kv_heads;
+};
+
 // Decode planning shared by the launcher and the workspace query.
 struct DecodePlan {
   int32_t split_blocks;
@@ -126,6 +178,9 @@ void set_decode_workspace(DecodeArgs& a, void* ws, bool bf16);
 
 hipError_t launch_kv_write(const KvWriteArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_kv_move(const KvMoveArgs& a, bool gather, hipStream_t stream);
+hipError_t launch_append(const AppendArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_kv_move_q8(const KvMoveQ8Args& a, bool gather, hipStream_t stream);
+hipError_t launch_kv_read_q8(const KvMoveQ8Args& a, bool bf16, hipStream_t stream);
 hipError_t launch_decode(DecodeArgs a, int group, bool bf16, hipStream_t stream);
 hipError_t launch_prefill_f32(const DecodeArgs& a, int group, hipStream_t stream);
 // The bf16 decode of short contexts or few segments (decode_short.hip): whether

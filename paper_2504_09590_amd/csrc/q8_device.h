@@ -1,0 +1,64 @@
+// Device helpers of the 8-bit cache: rows of 128 values held as e4m3 codes with
+// one power-of-two scale 2^e per slot and KV head, kept as the byte e + 127.
+//
+// e is the least integer with max |x| <= 448 * 2^e over the row's finite values
+// (448 is the largest e4m3 value), so nothing saturates; a code is x * 2^-e
+// rounded to the nearest e4m3 value, ties to even. e4m3 is a floating format: a
+// finer scale than a power of two would gain no relative precision, and with it a
+// value code * 2^e is exact in bf16 and the conversion to bf16 applies it for
+// nothing. One scale per slot, because the slot is what a request owns here: two
+// requests fill a block from its two ends, and single slots are checkpointed,
+// overwritten and put back, so a scale of a whole block would have two writers.
+#pragma once
+
+#include "bros_device.h"
+
+namespace bros {
+namespace q8 {
+
+typedef unsigned v2u_t __attribute__((ext_vector_type(2)));
+typedef unsigned v4u_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2_t;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float float2_t;
+
+// Exponents a row may take. Below, 2^e times the smallest code would leave the
+// normal range of bf16; above, no finite fp32 row reaches.
+constexpr int kMinExp = -100, kMaxExp = 120;
+constexpr uint32_t kNaNBits = 0x7fc00000u;
+
+// Scale exponent of a row whose largest finite magnitude is amax (448 = 1.75 * 2^8).
+__device__ __forceinline__ int row_exponent(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return min(max(e, kMinExp), kMaxExp);
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// |x| where x is finite, else 0 (infinities and NaNs take no part in the scale).
+__device__ __forceinline__ float finite_magnitude(float x) {
+  const float m = fabsf(x);
+  return m < INFINITY ? m : 0.0f;
+}
+// Four e4m3 codes of x * mul (mul = 2^-e); a value that is not finite becomes the NaN code.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float mul) {
+  const auto v = [&](float x) { return fabsf(x) < INFINITY ? x * mul : __uint_as_float(kNaNBits); };
+  int r = 0;
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(v(a), v(b), r, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(v(c), v(d), r, true);
+  return (uint32_t)r;
+}
+
+// The values of a scale byte and of codes.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// Two codes (the low or the high half of w) times the scale, as bf16 (exact).
+template <bool HI>
+__device__ __forceinline__ uint32_t values2_bf16(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {   // round to nearest even
+  const float2_t f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+}
+
+}  // namespace q8
+}  // namespace bros
