@@ -412,6 +412,26 @@ int bros_kv_scatter(const void* k_in, const void* v_in,
                     int32_t dtype, void* stream);
 
 /*
+ * bros_attn_decode_q8 -- bros_attn_decode over an 8-bit pool.
+ *
+ * The keys and values are those that the codes and scales of bros_qkv_append_q8
+ * stand for; everything else, head groups, directions, contexts, max_ctx, scale
+ * and empty rows, is as in bros_attn_decode. bf16 q and out only
+ * (BROS_E_UNSUPPORTED otherwise); sums and softmax statistics are fp32.
+ *
+ *   workspace    : as for bros_attn_decode, at least bros_attn_workspace_size(
+ *                  BROS_WS_DECODE, BROS_BF16, ...) bytes, 16-byte aligned.
+ */
+int bros_attn_decode_q8(void* out, const void* q,
+                        const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                        const int32_t* block_tables, int32_t max_blocks_per_seq,
+                        const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                        int32_t max_ctx, int32_t num_seqs, int32_t num_q_heads,
+                        int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                        float scale, int32_t dtype, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
  * bros_kv_gather_q8 / bros_kv_scatter_q8 / bros_kv_read_q8 -- slots of an 8-bit pool.
  *
  * Gather and scatter are bros_kv_gather and bros_kv_scatter for the pools of

@@ -36,7 +36,8 @@ EXPORTED = ["bros_status_str", "bros_last_error", "bros_abi_version", "bros_kv_w
             "bros_mgr_restore", "bros_mgr_query", "bros_mgr_table", "bros_mgr_free_blocks", "bros_mgr_validate", "bros_mgr_available",
             "bros_mgr_entries_needed", "bros_mgr_preemption_table", "bros_schedule", "bros_next_batch_size",
             "bros_mgr_grow_batch", "bros_mgr_plan_bound", "bros_schedule_pulled", "bros_set_decode_kernel_events",
-            "bros_qkv_append", "bros_qkv_append_q8", "bros_kv_gather_q8", "bros_kv_scatter_q8", "bros_kv_read_q8"]
+            "bros_qkv_append", "bros_qkv_append_q8", "bros_kv_gather_q8", "bros_kv_scatter_q8", "bros_kv_read_q8",
+            "bros_attn_decode_q8"]
 
 
 class BrosError(RuntimeError):
@@ -102,6 +103,8 @@ def _load() -> ctypes.CDLL:
     lib.bros_qkv_append.restype = ctypes.c_int
     lib.bros_qkv_append_q8.argtypes = rows + [P, P, P] + meta
     lib.bros_qkv_append_q8.restype = ctypes.c_int
+    lib.bros_attn_decode_q8.argtypes = [P, P, P, P, P, I, P, I, P, P, I, P, I, I, I, I, I, I, F, I, P, Z, P]
+    lib.bros_attn_decode_q8.restype = ctypes.c_int
     lib.bros_kv_gather_q8.argtypes = [P, P, P, I, P, I, P, P, P, I, I, I, P]
     lib.bros_kv_gather_q8.restype = ctypes.c_int
     lib.bros_kv_scatter_q8.argtypes = [P, P, P, P, I, P, P, P, I, I, I, I, P]
@@ -306,6 +309,29 @@ def bros_qkv_append_q8(q_out, q, k, v, k_pool, v_pool, kv_scales, block_tables, 
     head, tail = _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm,
                               (k_pool, v_pool, kv_scales))
     _check(LIB.bros_qkv_append_q8(*head, _ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), *tail, _stream(stream)))
+
+
+def _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens, workspace, *offsets):
+    """Checks what the two attentions over an 8-bit pool share."""
+    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
+    if q.dim() != 3 or q.shape[2] != d or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError(f"q and out must be [rows][Hq][{d}] of one type")
+    S = int(ctx_lens.shape[0])
+    _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *offsets)
+    _on_device(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens, workspace, *(t for t, _ in offsets))
+    return nb, hkv, bs, d, S, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def bros_attn_decode_q8(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens, max_ctx: int,
+                        scale: float = 0.0, workspace=None, stream=None):
+    """bros_attn_decode over an 8-bit pool (bfloat16 q and out, the bf16 decode's workspace)."""
+    nb, hkv, bs, d, S, ws_bytes = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens, workspace)
+    if q.shape[0] != S:
+        raise ValueError(f"{q.shape[0]} query rows for {S} sequences")
+    _check(LIB.bros_attn_decode_q8(_ptr(out), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb,
+                                   _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls),
+                                   _dir_mode(dir, block_tables), _ptr(ctx_lens), int(max_ctx), S, int(q.shape[1]), hkv, d,
+                                   bs, float(scale), _dtype_code(q), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def _dense(n: int, pools, ids, rows, scales=None, one_byte=True) -> None:

@@ -103,6 +103,13 @@ struct DecodeArgs {
   float scale_log2;       // softmax scale * log2(e)
 };
 
+// An 8-bit pool: codes [num_blocks][Hkv][16][128] each, scale bytes [num_blocks][Hkv][2][16].
+struct Q8Pool {
+  const uint8_t* k;
+  const uint8_t* v;
+  const uint8_t* scales;
+};
+
 struct PrefillArgs {
   void* out;
   const void* q;
@@ -178,6 +185,10 @@ void set_decode_workspace(DecodeArgs& a, void* ws, bool bf16);
 
 hipError_t launch_kv_write(const KvWriteArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_kv_move(const KvMoveArgs& a, bool gather, hipStream_t stream);
+// bf16 rows over an 8-bit pool (a.k_pool and a.v_pool unused), with the bf16 decode's workspace.
+hipError_t launch_decode_q8(DecodeArgs a, Q8Pool pool, int group, hipStream_t stream);
+// Folds the partials of pieces (n_split_max to a segment): segments of more than split_blocks blocks.
+hipError_t launch_decode_pieces_merge(const DecodeArgs& a, int group, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_kv_move_q8(const KvMoveQ8Args& a, bool gather, hipStream_t stream);
 hipError_t launch_kv_read_q8(const KvMoveQ8Args& a, bool bf16, hipStream_t stream);

@@ -256,6 +256,13 @@ __global__ __launch_bounds__(kThreads) void decode_short_merge_kernel(DecodeArgs
 }
 
 template <int G>
+hipError_t launch_merge_group(const DecodeArgs& a, hipStream_t stream) {
+  const int64_t segments = (int64_t)a.num_rows * a.num_kv_heads;
+  hipLaunchKernelGGL(decode_short_merge_kernel<G>, dim3((unsigned)segments), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int G>
 hipError_t launch_short_group(DecodeArgs a, hipStream_t stream, hipEvent_t between) {
   const int64_t segments = (int64_t)a.num_rows * a.num_kv_heads;
   for (int64_t s0 = 0; s0 < segments; s0 += kMaxSegmentsPerLaunch) {
@@ -269,8 +276,7 @@ hipError_t launch_short_group(DecodeArgs a, hipStream_t stream, hipEvent_t betwe
     if (e != hipSuccess) return e;
   }
   if (a.n_split_max <= 1) return hipSuccess;
-  hipLaunchKernelGGL(decode_short_merge_kernel<G>, dim3((unsigned)segments), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  return launch_merge_group<G>(a, stream);
 }
 
 }  // namespace dm
@@ -287,6 +293,16 @@ bool plan_decode_short(DecodeArgs& a, hipStream_t stream) {
   const int64_t slots = (int64_t)a.num_rows * a.num_q_heads + (int64_t)kDecodeGroupSlots * std::min(a.num_q_heads, 8);
   return plan_short_decode(segments, a.num_q_heads / a.num_kv_heads, blocks, stream_compute_units(stream), slots,
                            &a.split_blocks, &a.n_split_max);
+}
+
+hipError_t launch_decode_pieces_merge(const DecodeArgs& a, int group, hipStream_t stream) {
+  switch (group) {
+    case 1: return dm::launch_merge_group<1>(a, stream);
+    case 2: return dm::launch_merge_group<2>(a, stream);
+    case 4: return dm::launch_merge_group<4>(a, stream);
+    case 8: return dm::launch_merge_group<8>(a, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 hipError_t launch_decode_short(const DecodeArgs& a, int group, hipStream_t stream, hipEvent_t between) {

@@ -181,3 +181,42 @@ def test_rope_table():
         rope_table(4, 33, device="cpu")
     with pytest.raises(ValueError):
         rope_table(4, 32, inv_freq=[1.0, 2.0], device="cpu")
+
+
+def decode(**kw):
+    a = dict(out=FAKE, q=FAKE, k=FAKE, v=FAKE, s=FAKE, nb=10, bt=FAKE, maxb=4, dir=FAKE, cls=None, dpe=0, ctx=FAKE, max_ctx=64,
+             S=2, hq=8, hkv=2, d=128, bs=16, scale=0.0, dtype=1, ws=FAKE, wsb=1 << 40)
+    a.update(kw)
+    return bros.LIB.bros_attn_decode_q8(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=0), UNSUPPORTED), (dict(dtype=7), DTYPE), (dict(d=64), UNSUPPORTED), (dict(bs=32), UNSUPPORTED),
+    (dict(hq=6, hkv=4), SHAPE), (dict(hq=48), UNSUPPORTED), (dict(out=None), NULL), (dict(q=None), NULL), (dict(k=None), NULL),
+    (dict(v=None), NULL), (dict(s=None), NULL), (dict(ctx=None), NULL), (dict(bt=None), NULL), (dict(dir=None), NULL),
+    (dict(dpe=2), SHAPE), (dict(S=-1), SHAPE), (dict(max_ctx=-1), SHAPE), (dict(nb=0), SHAPE), (dict(maxb=0), SHAPE),
+    (dict(out=FAKE + 4), SHAPE), (dict(s=FAKE + 4), SHAPE), (dict(S=2 ** 20, max_ctx=2 ** 31 - 1), SHAPE), (dict(ws=None), -5),
+    (dict(wsb=16), -5), (dict(ws=FAKE + 4), -5),
+])
+def test_decode_rejects(kw, code):
+    assert decode(**kw) == code
+    assert bros.LIB.bros_last_error().decode() != ""
+
+
+def test_decode_of_no_sequences():
+    assert decode(S=0, out=None, q=None, ws=None) == 0
+
+
+def test_decode_binding_refuses():
+    q, pool = rows(2, 8), torch.zeros((4, 2, 16, 128), dtype=torch.uint8)
+    scales, bt = torch.zeros((4, 2, 2, 16), dtype=torch.uint8), torch.zeros((2, 3), dtype=torch.int32)
+    d, ctx = torch.ones(2, dtype=torch.int8), torch.ones(2, dtype=torch.int32)
+    for args, says in (((q, q, pool, pool, scales, bt, d, None, ctx, 16), "current device"),
+                       ((q, q[:1], pool, pool, scales, bt, d, None, ctx, 16), "of one type"),
+                       ((q.float(), q, pool, pool, scales, bt, d, None, ctx, 16), "of one type"),
+                       ((q, q, pool.bfloat16(), pool, scales, bt, d, None, ctx, 16), "one byte"),
+                       ((q, q, pool, pool, scales[:, :1], bt, d, None, ctx, 16), "kv_scales"),
+                       ((q, q, pool, pool, scales, bt[:1], d, None, ctx, 16), "block_tables"),
+                       ((q, q, pool, pool, scales, bt, d, None, ctx.long(), 16), "length")):
+        with pytest.raises(ValueError, match=says):
+            bros.bros_attn_decode_q8(*args)
