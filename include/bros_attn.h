@@ -432,6 +432,26 @@ int bros_attn_decode_q8(void* out, const void* q,
                         void* stream);
 
 /*
+ * bros_attn_prefill_chunk_q8 -- bros_attn_prefill_chunk over an 8-bit pool.
+ *
+ * The chunks' own keys and values are in the pool already (bros_qkv_append_q8), in
+ * 8 bits like the rest. Everything but the pool is as in the bf16
+ * bros_attn_prefill_chunk: rows, causal limits, max_q_len, max_ctx, and the
+ * workspace (optional up to max_ctx 32768, required beyond; sizes by
+ * bros_attn_workspace_size(BROS_WS_PREFILL, BROS_BF16, ...)). Rows behind
+ * cu_q[num_seqs] keep what out held. bf16 q and out only.
+ */
+int bros_attn_prefill_chunk_q8(void* out, const void* q, const int32_t* cu_q,
+                               int32_t num_q_tokens, int32_t max_q_len,
+                               const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                               const int32_t* block_tables, int32_t max_blocks_per_seq,
+                               const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                               int32_t max_ctx, int32_t num_seqs, int32_t num_q_heads,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                               float scale, int32_t dtype, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
  * bros_kv_gather_q8 / bros_kv_scatter_q8 / bros_kv_read_q8 -- slots of an 8-bit pool.
  *
  * Gather and scatter are bros_kv_gather and bros_kv_scatter for the pools of

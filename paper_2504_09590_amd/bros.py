@@ -37,7 +37,7 @@ EXPORTED = ["bros_status_str", "bros_last_error", "bros_abi_version", "bros_kv_w
             "bros_mgr_entries_needed", "bros_mgr_preemption_table", "bros_schedule", "bros_next_batch_size",
             "bros_mgr_grow_batch", "bros_mgr_plan_bound", "bros_schedule_pulled", "bros_set_decode_kernel_events",
             "bros_qkv_append", "bros_qkv_append_q8", "bros_kv_gather_q8", "bros_kv_scatter_q8", "bros_kv_read_q8",
-            "bros_attn_decode_q8"]
+            "bros_attn_decode_q8", "bros_attn_prefill_chunk_q8"]
 
 
 class BrosError(RuntimeError):
@@ -105,6 +105,8 @@ def _load() -> ctypes.CDLL:
     lib.bros_qkv_append_q8.restype = ctypes.c_int
     lib.bros_attn_decode_q8.argtypes = [P, P, P, P, P, I, P, I, P, P, I, P, I, I, I, I, I, I, F, I, P, Z, P]
     lib.bros_attn_decode_q8.restype = ctypes.c_int
+    lib.bros_attn_prefill_chunk_q8.argtypes = [P, P, P, I, I, P, P, P, I, P, I, P, P, I, P, I, I, I, I, I, I, F, I, P, Z, P]
+    lib.bros_attn_prefill_chunk_q8.restype = ctypes.c_int
     lib.bros_kv_gather_q8.argtypes = [P, P, P, I, P, I, P, P, P, I, I, I, P]
     lib.bros_kv_gather_q8.restype = ctypes.c_int
     lib.bros_kv_scatter_q8.argtypes = [P, P, P, P, I, P, P, P, I, I, I, I, P]
@@ -332,6 +334,18 @@ def bros_attn_decode_q8(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cl
                                    _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls),
                                    _dir_mode(dir, block_tables), _ptr(ctx_lens), int(max_ctx), S, int(q.shape[1]), hkv, d,
                                    bs, float(scale), _dtype_code(q), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def bros_attn_prefill_chunk_q8(out, q, cu_q, max_q_len: int, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens,
+                               max_ctx: int, scale: float = 0.0, workspace=None, stream=None):
+    """bros_attn_prefill_chunk over an 8-bit pool (bfloat16 q and out, the bf16 prefill's workspace)."""
+    nb, hkv, bs, d, S, ws_bytes = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
+                                                workspace, (cu_q, int(ctx_lens.shape[0]) + 1))
+    _check(LIB.bros_attn_prefill_chunk_q8(_ptr(out), _ptr(q), _ptr(cu_q), int(q.shape[0]), int(max_q_len), _ptr(k_pool),
+                                          _ptr(v_pool), _ptr(kv_scales), nb, _ptr(block_tables),
+                                          int(block_tables.shape[1]), _ptr(dir), _ptr(cls), _dir_mode(dir, block_tables),
+                                          _ptr(ctx_lens), int(max_ctx), S, int(q.shape[1]), hkv, d, bs, float(scale),
+                                          _dtype_code(q), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def _dense(n: int, pools, ids, rows, scales=None, one_byte=True) -> None:

@@ -537,6 +537,66 @@ int bros_attn_decode_q8(void* out, const void* q,
   return launch_status(fn, bros::launch_decode_q8(a, pool, group, static_cast<hipStream_t>(stream)));
 }
 
+int bros_attn_prefill_chunk_q8(void* out, const void* q, const int32_t* cu_q,
+                               int32_t num_q_tokens, int32_t max_q_len,
+                               const void* k_pool, const void* v_pool, const uint8_t* kv_scales, int32_t num_blocks,
+                               const int32_t* block_tables, int32_t max_blocks_per_seq,
+                               const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                               int32_t max_ctx, int32_t num_seqs, int32_t num_q_heads,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                               float scale, int32_t dtype, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  const char* fn = "bros_attn_prefill_chunk_q8";
+  int group = 0;
+  int st = check_shapes(fn, num_q_heads, num_kv_heads, head_dim, block_size, dtype, &group);
+  if (st) return st;
+  if (dtype != BROS_BF16) return fail(BROS_E_UNSUPPORTED, "%s: bf16 queries only", fn);
+  if (num_seqs < 0 || num_q_tokens < 0 || max_q_len < 0 || max_ctx < 0)
+    return fail(BROS_E_SHAPE, "%s: negative count (seqs=%d tokens=%d max_q_len=%d max_ctx=%d)", fn, num_seqs, num_q_tokens, max_q_len, max_ctx);
+  if (num_seqs == 0 || num_q_tokens == 0) return ok();
+  if (max_q_len == 0) return fail(BROS_E_SHAPE, "%s: max_q_len is 0 with %d query rows", fn, num_q_tokens);
+  max_q_len = std::min(max_q_len, num_q_tokens);   // (a loose bound must not size the grid)
+  if (!out || !q || !cu_q || !k_pool || !v_pool || !kv_scales || !ctx_lens)
+    return fail(BROS_E_NULL, "%s: a tensor, scale or length pointer is NULL", fn);
+  st = check_meta(fn, block_tables, max_blocks_per_seq, dir, cls, dir_per_entry, num_blocks);
+  if (st) return st;
+  if (!aligned(out, 16) || !aligned(q, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(kv_scales, 16))
+    return fail(BROS_E_SHAPE, "%s: tensors must be 16-byte aligned", fn);
+  const bool whole_table = max_ctx <= bros::kPrefillWholeTableCtx;
+  if (!whole_table) {
+    if ((long long)num_q_tokens * num_kv_heads * ((max_ctx + 15LL) / 16) > 0x7fffffffLL)
+      return fail(BROS_E_SHAPE, "%s: more than 2^31 (row, KV head, block) tiles", fn);
+    const size_t need = bros::decode_workspace_bytes(num_q_tokens, num_q_heads, max_ctx, true);
+    if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))
+      return fail(BROS_E_WORKSPACE, "%s: workspace of %zu bytes (16-byte aligned) required, got %zu at %p", fn, need, workspace_bytes, workspace);
+  }
+  bros::PrefillArgs a{};
+  a.out = out;
+  a.q = q;
+  a.cu_q = cu_q;
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  a.block_tables = block_tables;
+  a.dir = dir;
+  a.cls = cls;
+  a.dir_per_entry = dir_per_entry;
+  a.ctx_lens = ctx_lens;
+  a.num_q_tokens = num_q_tokens;
+  a.num_seqs = num_seqs;
+  a.num_blocks = num_blocks;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.max_ctx = max_ctx;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  const int qt = bros::prefill_positions_per_tile(group);
+  a.tiles_per_seq = (int32_t)(((int64_t)max_q_len + qt - 1) / qt);
+  a.scale_log2 = resolve_scale(scale, head_dim);
+  const long long total = (long long)num_seqs * num_kv_heads * a.tiles_per_seq;
+  if (total > 0x7fffffffLL - 1024) return fail(BROS_E_SHAPE, "%s: grid of %lld workgroups too large", fn, total);
+  if (aligned(workspace, 16)) bros::set_prefill_workspace(a, workspace, workspace_bytes, whole_table);
+  return launch_status(fn, bros::launch_prefill_q8(a, kv_scales, group, (int)total, static_cast<hipStream_t>(stream)));
+}
+
 static int kv_move(const char* fn, bool gather, void* k_pool, void* v_pool, int32_t num_blocks,
                    const int32_t* slot_ids, int32_t num_slots, void* k_dense, void* v_dense,
                    int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {

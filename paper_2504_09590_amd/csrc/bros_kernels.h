@@ -189,6 +189,13 @@ hipError_t launch_kv_move(const KvMoveArgs& a, bool gather, hipStream_t stream);
 hipError_t launch_decode_q8(DecodeArgs a, Q8Pool pool, int group, hipStream_t stream);
 // Folds the partials of pieces (n_split_max to a segment): segments of more than split_blocks blocks.
 hipError_t launch_decode_pieces_merge(const DecodeArgs& a, int group, hipStream_t stream);
+// bf16 rows over an 8-bit pool (a.k_pool and a.v_pool its codes).
+hipError_t launch_prefill_q8(PrefillArgs a, const uint8_t* scales, int group, int num_tiles_total, hipStream_t stream);
+// How the matrix-core prefill's grid is laid out: sets a.num_cus (0: no unit is
+// split) and a.xcd_cus, gives the workgroups, and tells whether tables run through
+// the LDS ring. And the merge that follows where a.num_cus > 0.
+bool plan_prefill_launch(PrefillArgs& a, int num_units, hipStream_t stream, long long* grid);
+hipError_t launch_prefill_merge(const PrefillArgs& a, int group, int num_units, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_kv_move_q8(const KvMoveQ8Args& a, bool gather, hipStream_t stream);
 hipError_t launch_kv_read_q8(const KvMoveQ8Args& a, bool bf16, hipStream_t stream);

@@ -86,8 +86,10 @@ bool prefill_needs_ring(int32_t max_ctx, int32_t max_blocks_per_seq) {
   return max_ctx > kPrefillWholeTableCtx && max_blocks_per_seq > kMaxTableLds;
 }
 
-template <int G>
-hipError_t launch_group(PrefillArgs a, int num_units, hipStream_t stream) {
+}  // namespace pf
+
+bool plan_prefill_launch(PrefillArgs& a, int num_units, hipStream_t stream, long long* grid) {
+  using namespace pf;
   // Split only when the units leave compute units idle: with a unit or more
   // per compute unit, splitting measured no faster (1000 rows on 4000 tokens,
   // 256 units: 96 us whole, 100 split).
@@ -117,11 +119,27 @@ hipError_t launch_group(PrefillArgs a, int num_units, hipStream_t stream) {
     if (cus == stream_compute_units(nullptr) && cus % kXcds == 0) a.xcd_cus = cus / kXcds;
   }
   // ranks beyond the units: at most 2 num_cus / Hkv more pieces than items
-  const long long grid = (long long)num_units + 2 * a.num_cus;
+  *grid = (long long)num_units + 2 * a.num_cus;
+  return prefill_needs_ring(a.max_ctx, a.max_blocks_per_seq);
+}
+
+namespace pf {
+
+template <int G>
+hipError_t launch_merge_group(const PrefillArgs& a, int num_units, hipStream_t stream) {
+  // four workgroups per split (item, KV head); split items x Hkv <= num_units
+  hipLaunchKernelGGL(prefill_merge_kernel<G>, dim3((unsigned)(4 * num_units)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int G>
+hipError_t launch_group(PrefillArgs a, int num_units, hipStream_t stream) {
+  long long grid = 0;
+  const bool ring = plan_prefill_launch(a, num_units, stream, &grid);
   // (block, KV head) rows of 4 KiB: 32-bit offsets reach them all below 2^20 rows
   const bool off32 = (int64_t)a.num_blocks * a.num_kv_heads <= (int64_t)1 << 20;
   const dim3 g((unsigned)grid), b(kThreads);
-  if (prefill_needs_ring(a.max_ctx, a.max_blocks_per_seq)) {
+  if (ring) {
     if (off32)
       hipLaunchKernelGGL((prefill_mfma_kernel<G, true, true>), g, b, 0, stream, a);
     else
@@ -134,9 +152,7 @@ hipError_t launch_group(PrefillArgs a, int num_units, hipStream_t stream) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.num_cus == 0) return e;
-  // four workgroups per split (item, KV head); split items x Hkv <= num_units
-  hipLaunchKernelGGL(prefill_merge_kernel<G>, dim3((unsigned)(4 * num_units)), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  return launch_merge_group<G>(a, num_units, stream);
 }
 
 }  // namespace pf
@@ -169,6 +185,16 @@ void set_prefill_workspace(PrefillArgs& a, void* ws, size_t bytes, bool whole) {
   a.ws_o = static_cast<float*>(ws);
   a.ws_ml = a.ws_o + rows * kHeadDim;
   a.ws_list = reinterpret_cast<int32_t*>(a.ws_ml + rows * 2);
+}
+
+hipError_t launch_prefill_merge(const PrefillArgs& a, int group, int num_units, hipStream_t stream) {
+  switch (group) {
+    case 1: return pf::launch_merge_group<1>(a, num_units, stream);
+    case 2: return pf::launch_merge_group<2>(a, num_units, stream);
+    case 4: return pf::launch_merge_group<4>(a, num_units, stream);
+    case 8: return pf::launch_merge_group<8>(a, num_units, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 hipError_t launch_prefill_mfma(PrefillArgs a, int group, int num_tiles_total, hipStream_t stream) {

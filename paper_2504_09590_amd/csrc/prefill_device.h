@@ -78,6 +78,7 @@
 
 #include "bros_device.h"
 #include "bros_kernels.h"
+#include "q8_device.h"
 
 #include <limits.h>
 #include <math.h>
@@ -585,9 +586,16 @@ __device__ __forceinline__ int paired_id(const PrefillArgs& a, int b, int grid) 
 // are a ring over the piece (any context length) instead of the whole table
 // (contexts up to kPrefillWholeTableCtx); the step loop then carries one more
 // scalar test per four tiles, which is why short contexts keep their own variant.
-template <int G, bool kOff32, bool kRing>
+//
+// kQ8: the pools hold 8-bit codes and `scales` their scales (q8_device.h). Each wave
+// reads its eight rows of a K and a V tile into registers, 16 codes a lane, two steps
+// before it turns them into bf16 values and writes them to the rings, a step before
+// they are used: 16 conversions and four LDS writes a wave and step, where the 16-bit
+// rows go to LDS by themselves. From there on a step is the same.
+template <int G, bool kOff32, bool kRing, bool kQ8 = false>
 __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8_t* s_kring, uint8_t* s_vring,
-                                             int* s_first_bad_p, int* s_tbl, int8_t* s_dir) {
+                                             int* s_first_bad_p, int* s_tbl, int8_t* s_dir,
+                                             const uint8_t* scales = nullptr) {
   constexpr int QT = kRows / G;   // positions per unit
   constexpr int kSlotBytes = kTileBytes;
   const int tid = threadIdx.x;
@@ -719,6 +727,59 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     }
   };
 
+  // 8-bit rows: lane l holds codes 16 (l % 8) .. + 15 of the wave's row l / 8, the two
+  // 16-byte chunks 2 (l % 8), + 1 of the bf16 row. Batch b (K of tile b + 1, V of tile b)
+  // sits in set b % 2 from step b - 3 to step b - 1.
+  struct Staged {
+    v4u_t k, v;
+    uint32_t ks, vs;
+  };
+  [[maybe_unused]] Staged sets[2];
+  [[maybe_unused]] const int q8_row = lane >> 3, q8_c = lane & 7;
+  [[maybe_unused]] const uint32_t q8_off = (uint32_t)((my_slot0 + q8_row) * kHeadDim + 16 * q8_c);
+  auto fetch_q8 = [&](int idx, const void* pool, int which, v4u_t& codes, uint32_t& scale) __attribute__((always_inline)) {
+    const uint8_t* p = static_cast<const uint8_t*>(pool);
+    const uint32_t so = (uint32_t)(kBlockSize * which + my_slot0 + q8_row);
+    if constexpr (kOff32) {
+      codes = *reinterpret_cast<const v4u_t*>(p + (((uint32_t)idx << 11) + q8_off));
+      scale = scales[((uint32_t)idx << 5) + so];
+    } else {
+      const size_t r = (size_t)__builtin_amdgcn_readfirstlane(idx);
+      codes = *reinterpret_cast<const v4u_t*>(p + r * (kBlockSize * kHeadDim) + q8_off);
+      scale = (scales + r * (2 * kBlockSize))[so];
+    }
+  };
+  auto put_q8 = [&](const v4u_t& codes, uint32_t scale, uint8_t* ring, bool keep) __attribute__((always_inline)) {
+    const int row = 8 * rg + q8_row;   // tile row
+    const float f = q8::scale_of(scale);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v4u_t w = {q8::values2_bf16<false>(codes[2 * h], f), q8::values2_bf16<true>(codes[2 * h], f),
+                 q8::values2_bf16<false>(codes[2 * h + 1], f), q8::values2_bf16<true>(codes[2 * h + 1], f)};
+      if (!keep) w = v4u_t{0u, 0u, 0u, 0u};
+      *reinterpret_cast<v4u_t*>(ring + row * kRowBytes + (((2 * q8_c + h) ^ swz(row)) << 4)) = w;
+    }
+  };
+  // Whether this lane's row of tile j is context (by what LDS holds of the table).
+  auto context_q8 = [&](int j) __attribute__((always_inline)) -> bool {
+    const int b = 2 * (kb + j) + my_bt;
+    const int dirv = s_dir[at(b)];
+    return dirv != 0 && b * kBlockSize + slot_of_offset(my_slot0 + q8_row, dirv) < ctx;
+  };
+  auto fetch_batch = [&](int b, Staged& st) __attribute__((always_inline)) {
+    fetch_q8(own(b + 1), a.k_pool, 0, st.k, st.ks);
+    fetch_q8(own(b), a.v_pool, 1, st.v, st.vs);
+  };
+  // At the start of step ii: batch ii + 1 goes to the rings, and batch ii + 3 is
+  // requested into its set. (The slots written were last read two steps ago.)
+  auto turn_q8 = [&](int ii, Staged& st, auto fixc) __attribute__((always_inline)) {
+    bool keep = true;
+    if constexpr (decltype(fixc)::value) keep = context_q8(ii + 1);
+    put_q8(st.k, st.ks, s_kring + ((ii + 2) & (kSlots - 1)) * kSlotBytes, true);
+    put_q8(st.v, st.vs, s_vring + ((ii + 1) & (kSlots - 1)) * kSlotBytes, keep);
+    fetch_batch(ii + 3, st);
+  };
+
   // K operand (S^T = K Q^T, d-step c): tile row mrow, logical chunk 2c + half.
   const int k_sw = swz(mrow);
   const int k_lane = mrow * kRowBytes + (((half ^ k_sw) & 1) << 4);
@@ -827,6 +888,53 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     for (int dt = 0; dt < 4; ++dt)
       o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[dt]), pf[c2], o[dt], 0, 0, 0);
   };
+  // PV of a tile with keys that not every row sees, 8-bit cache: a row that does not
+  // see a key must not meet a NaN there (0 * NaN), and the chunk's own rows of a
+  // 16-bit cache cannot be told apart either, but here a NaN is what an infinity was
+  // stored as. Values that are not finite are taken out of V, and the rows that see
+  // one get their NaN from a product of ones: marks of such values, marks of seen keys.
+  [[maybe_unused]] auto pv_guarded = [&](v4u_t (&v0)[4], v4u_t (&v1)[4], const bf16x8_t (&pf)[2], const floatx16& cur)
+      __attribute__((always_inline)) {
+    constexpr uint32_t kLo = 0x7f80u, kHi = 0x7f800000u;
+    bool bad = false;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bad |= (v0[dt][i] & kLo) == kLo || (v0[dt][i] & kHi) == kHi;
+        bad |= (v1[dt][i] & kLo) == kLo || (v1[dt][i] & kHi) == kHi;
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(bad) != 0) {
+      v4u_t seen[2];
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          seen[c2][i] = (cur[8 * c2 + 2 * i] == -INFINITY ? 0u : 0x3f80u) | (cur[8 * c2 + 2 * i + 1] == -INFINITY ? 0u : 0x3f800000u);
+      }
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        floatx16 hit = {};
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) {
+          v4u_t& w = c2 ? v1[dt] : v0[dt];
+          v4u_t mark;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = (w[i] & kLo) == kLo ? 0xffffu : 0u, hi = (w[i] & kHi) == kHi ? 0xffff0000u : 0u;
+            mark[i] = (lo | hi) & 0x3f803f80u;
+            w[i] &= ~(lo | hi);
+          }
+          hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(mark), as_bf16x8(seen[c2]), hit, 0, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[dt][j] = hit[j] > 0.0f ? __uint_as_float(0x7fc00000u) : o[dt][j];
+      }
+    }
+    pv(v0, pf, 0);
+    pv(v1, pf, 1);
+  };
   // Rare (lazy max).
   auto rescale_o = [&]() __attribute__((always_inline)) {
     if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
@@ -850,6 +958,8 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   auto step = [&](const uint8_t* sk, const uint8_t* sv, int next_tile, auto has_next, auto mask_next,
                   const floatx16& in, floatx16& out) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(has_next)::value;
+    // (the current tile may have keys that not every row sees, but for the main loop's)
+    constexpr bool GUARD = kQ8 && (!NEXT || decltype(mask_next)::value);
     v4u_t kv[8];
     v4u_t vv0[4], vv1[4];
     if constexpr (NEXT) k_operands(sk, kv);
@@ -858,8 +968,12 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     if constexpr (NEXT) scores(kv, out);
     probs(pf, in);
     v_operands(sv, 1, vv1);
-    pv(vv0, pf, 0);
-    pv(vv1, pf, 1);
+    if constexpr (GUARD) {
+      pv_guarded(vv0, vv1, pf, in);
+    } else {
+      pv(vv0, pf, 0);
+      pv(vv1, pf, 1);
+    }
     if constexpr (NEXT) mask_max(out, mask_next, next_tile);
   };
   // After step ii: wait for batch ii + 1 (K of step ii + 2, V of step ii + 1),
@@ -886,9 +1000,17 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   auto own0 = [&](int j) -> int { return entry(2 * (kb + j) + my_bt); };
   const int e0 = own0(0);
   const int w0 = own0(1), w1 = own0(2), w2 = own0(3), w3 = own0(4);
-  issue(e0, kpool, s_kring);
-  issue(w0, kpool, s_kring + 1 * kSlotBytes);
-  issue(e0, vpool, s_vring);
+  [[maybe_unused]] v4u_t k0_codes;
+  [[maybe_unused]] uint32_t k0_scale;
+  if constexpr (kQ8) {
+    fetch_q8(e0, a.k_pool, 0, k0_codes, k0_scale);
+    fetch_q8(w0, a.k_pool, 0, sets[0].k, sets[0].ks);
+    fetch_q8(e0, a.v_pool, 1, sets[0].v, sets[0].vs);
+  } else {
+    issue(e0, kpool, s_kring);
+    issue(w0, kpool, s_kring + 1 * kSlotBytes);
+    issue(e0, vpool, s_vring);
+  }
   // Tiles below `plain_tiles` need no mask: every key is context, sits behind
   // a valid table entry and is visible to every row of the unit. The first
   // invalid entry of the piece comes from the staging pass, while the first
@@ -926,10 +1048,18 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   __syncthreads();
   const int first_bad = __builtin_amdgcn_readfirstlane((*s_first_bad_p));
   const int plain_tiles = min(full_below / kKeys, first_bad / 2);
-  // Everything so far, Q included: a wait the compiler sees, so it knows the
-  // Q registers are ready and adds no wait of its own later.
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-  fixup_v(0, s_vring);
+  if constexpr (kQ8) {
+    put_q8(k0_codes, k0_scale, s_kring, true);
+    put_q8(sets[0].k, sets[0].ks, s_kring + kSlotBytes, true);
+    put_q8(sets[0].v, sets[0].vs, s_vring, context_q8(0));
+    fetch_batch(1, sets[1]);
+    fetch_batch(2, sets[0]);
+  } else {
+    // Everything so far, Q included: a wait the compiler sees, so it knows the
+    // Q registers are ready and adds no wait of its own later.
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    fixup_v(0, s_vring);
+  }
   lds_barrier();
   {
     v4u_t kv[8];
@@ -938,13 +1068,15 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     if (kb >= plain_tiles) mask_max(sa, std::true_type{}, kb);
     else mask_max(sa, std::false_type{}, kb);
   }
-  lds_barrier();   // K slot 0 is free again
-  issue(w1, kpool, s_kring + 2 * kSlotBytes);
-  issue(w0, vpool, s_vring + 1 * kSlotBytes);
-  issue(w2, kpool, s_kring + 3 * kSlotBytes);
-  issue(w1, vpool, s_vring + 2 * kSlotBytes);
-  issue(w3, kpool, s_kring);
-  issue(w2, vpool, s_vring + 3 * kSlotBytes);
+  if constexpr (!kQ8) {
+    lds_barrier();   // K slot 0 is free again
+    issue(w1, kpool, s_kring + 2 * kSlotBytes);
+    issue(w0, vpool, s_vring + 1 * kSlotBytes);
+    issue(w2, kpool, s_kring + 3 * kSlotBytes);
+    issue(w1, vpool, s_vring + 2 * kSlotBytes);
+    issue(w3, kpool, s_kring);
+    issue(w2, vpool, s_vring + 3 * kSlotBytes);
+  }
 
   // ---- Steps. Before step i: batch i (K of step i + 1, V of step i) is in
   // LDS, batches i + 1 .. i + 3 are in flight. The steady state (this wave has
@@ -975,14 +1107,17 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     constexpr int u = decltype(uc)::value;
     if (ii + 1 >= n_plain) return false;
     if constexpr (u == 0) refill();   // (u and ii agree mod 4)
-    const int ik = own(ii + 5);
+    int ik = 0;
+    if constexpr (kQ8) turn_q8(ii, sets[(u + 1) % 2], std::false_type{});
+    else ik = own(ii + 5);
     // step ii reads buffer ii % 2 and fills the other (u and ii agree mod 4)
     if constexpr (u % 2 == 0)
       step(kr + ((u + 1) % kSlots) * kSlotBytes, vr + u * kSlotBytes, 0, std::true_type{}, std::false_type{}, sa, sb);
     else
       step(kr + ((u + 1) % kSlots) * kSlotBytes, vr + u * kSlotBytes, 0, std::true_type{}, std::false_type{}, sb, sa);
     rescale_o();
-    advance(ii, u, ik, iv, std::false_type{});
+    if constexpr (kQ8) lds_barrier();
+    else advance(ii, u, ik, iv, std::false_type{});
     iv = ik;
     ++ii;
     return true;
@@ -995,20 +1130,31 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     const int sl = ii & (kSlots - 1);
     const int sl1 = (sl + 1) & (kSlots - 1);
     refill();
-    const int ik = own(ii + 5);
+    int ik = 0;
+    if constexpr (kQ8) {
+      if (ii & 1) turn_q8(ii, sets[0], std::true_type{});
+      else turn_q8(ii, sets[1], std::true_type{});
+    } else {
+      ik = own(ii + 5);
+    }
     step(kr + sl1 * kSlotBytes, vr + sl * kSlotBytes, kb + ii + 1, std::true_type{}, std::true_type{}, sa, sb);
     sa = sb;
     rescale_o();
-    advance(ii, sl, ik, iv, std::true_type{});
+    if constexpr (kQ8) lds_barrier();
+    else advance(ii, sl, ik, iv, std::true_type{});
     iv = ik;
   }
   // The last tile (no next tile to score).
   if (ii < n_kt) {
     const int sl = ii & (kSlots - 1);
-    const int ik = own(ii + 5);
-    step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb);
-    advance(ii, sl, ik, iv, std::true_type{});
-    iv = ik;
+    if constexpr (kQ8) {
+      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb);
+    } else {
+      const int ik = own(ii + 5);
+      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb);
+      advance(ii, sl, ik, iv, std::true_type{});
+      iv = ik;
+    }
     ++ii;
   }
   wait_vmem<0>();

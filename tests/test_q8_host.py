@@ -220,3 +220,40 @@ def test_decode_binding_refuses():
                        ((q, q, pool, pool, scales, bt, d, None, ctx.long(), 16), "length")):
         with pytest.raises(ValueError, match=says):
             bros.bros_attn_decode_q8(*args)
+
+
+def prefill(**kw):
+    a = dict(out=FAKE, q=FAKE, cu_q=FAKE, n=64, max_q=32, k=FAKE, v=FAKE, s=FAKE, nb=10, bt=FAKE, maxb=4, dir=FAKE, cls=None, dpe=0,
+             ctx=FAKE, max_ctx=64, S=2, hq=8, hkv=2, d=128, bs=16, scale=0.0, dtype=1, ws=None, wsb=0)
+    a.update(kw)
+    return bros.LIB.bros_attn_prefill_chunk_q8(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=0), UNSUPPORTED), (dict(dtype=7), DTYPE), (dict(d=64), UNSUPPORTED), (dict(bs=32), UNSUPPORTED),
+    (dict(hq=6, hkv=4), SHAPE), (dict(hq=48), UNSUPPORTED), (dict(out=None), NULL), (dict(q=None), NULL), (dict(cu_q=None), NULL),
+    (dict(k=None), NULL), (dict(v=None), NULL), (dict(s=None), NULL), (dict(ctx=None), NULL), (dict(bt=None), NULL),
+    (dict(dir=None), NULL), (dict(dpe=2), SHAPE), (dict(S=-1), SHAPE), (dict(n=-1), SHAPE), (dict(max_q=0), SHAPE),
+    (dict(max_ctx=-1), SHAPE), (dict(nb=0), SHAPE), (dict(maxb=0), SHAPE), (dict(out=FAKE + 4), SHAPE), (dict(s=FAKE + 4), SHAPE),
+    (dict(max_ctx=40000), -5), (dict(max_ctx=40000, ws=FAKE, wsb=100), -5), (dict(n=2 ** 30, max_ctx=2 ** 31 - 1), SHAPE),
+    (dict(n=2 ** 31 - 1, max_q=2 ** 31 - 1, S=2 ** 20), SHAPE),
+])
+def test_prefill_rejects(kw, code):
+    assert prefill(**kw) == code
+    assert bros.LIB.bros_last_error().decode() != ""
+
+
+def test_prefill_of_nothing():
+    assert prefill(S=0, out=None) == 0 and prefill(n=0, q=None) == 0
+
+
+def test_prefill_binding_refuses():
+    q, pool = rows(5, 8), torch.zeros((4, 2, 16, 128), dtype=torch.uint8)
+    scales, bt = torch.zeros((4, 2, 2, 16), dtype=torch.uint8), torch.zeros((2, 3), dtype=torch.int32)
+    d, ctx, cu = torch.ones(2, dtype=torch.int8), torch.ones(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for args, says in (((q, q, cu, 5, pool, pool, scales, bt, d, None, ctx, 16), "current device"),
+                       ((q, q, cu[:2], 5, pool, pool, scales, bt, d, None, ctx, 16), "offset"),
+                       ((q[:4], q, cu, 5, pool, pool, scales, bt, d, None, ctx, 16), "of one type"),
+                       ((q, q, cu, 5, pool, pool, scales.int(), bt, d, None, ctx, 16), "kv_scales")):
+        with pytest.raises(ValueError, match=says):
+            bros.bros_attn_prefill_chunk_q8(*args)
