@@ -57,11 +57,10 @@ def encode(x):
     e = row_exponents(x)
     z = x / 2.0 ** e[..., None].astype(np.float64)
     mag = np.abs(np.where(np.isfinite(z), z, 0.0))
-    vals = E4M3[:NAN_CODE]                       # ascending; code c is even where its last mantissa bit is 0
-    hi = np.clip(np.searchsorted(vals, mag), 0, NAN_CODE - 1)
-    lo = np.maximum(hi - 1, 0)
-    d_hi, d_lo = np.abs(vals[hi] - mag), np.abs(mag - vals[lo])
-    code = np.where(d_lo < d_hi, lo, np.where(d_hi < d_lo, hi, np.where(lo % 2 == 0, lo, hi)))
+    # spacing 2^(x - 3) in [2^x, 2^(x + 1)), 2^-9 below 2^-6; the number of steps is rounded
+    # half to even, and from the 8th on counts through the binades as the code does
+    x = np.where(mag > 0, np.maximum(np.frexp(mag)[1] - 1, -6), -6)
+    code = np.rint(np.ldexp(mag, 3 - x)).astype(np.int64) + 8 * (x + 6)
     code = np.where(np.signbit(z), code + 128, code)
     code = np.where(np.isfinite(x), code, NAN_CODE)
     return code.astype(np.uint8), (e + 127).astype(np.uint8)

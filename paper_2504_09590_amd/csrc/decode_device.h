@@ -84,11 +84,13 @@ __device__ __forceinline__ int32_t load_uniform(const int32_t* p, size_t i) {
   return ((scalar_i32_ptr)p)[i];   // address-space cast: C-style only
 }
 
-// Tiles of one row: KV heads x blocks of its visible context.
+// Tiles of one row: KV heads x blocks of its visible context (or, here and below,
+// other runs of kTokens positions that a caller takes as its tiles).
+template <int kTokens = kBlockSize>
 __device__ __forceinline__ int row_tiles(const DecodeArgs& a, int row) {
   int s, ctx;
   resolve_row(a, row, s, ctx);
-  return ctx > 0 ? a.num_kv_heads * ((ctx + kBlockSize - 1) / kBlockSize) : 0;
+  return ctx > 0 ? a.num_kv_heads * ((ctx + kTokens - 1) / kTokens) : 0;
 }
 
 // Prefix of tiles over rows in LDS: entry c is the first tile of row c * chunk
@@ -98,6 +100,7 @@ __device__ __forceinline__ int row_tiles(const DecodeArgs& a, int row) {
 // in its own entry; a scan within each wave and one across the waves (one
 // barrier) gives every thread its start, and the thread turns its entries
 // into prefixes. `s_scan` holds kThreads / kWave ints.
+template <int kTokens = kBlockSize>
 [[maybe_unused]] static __device__ int build_tile_prefix(const DecodeArgs& a, int* s_pre, int* s_scan, int chunk, int nch) {
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1), w = tid / kWave;
@@ -106,7 +109,7 @@ __device__ __forceinline__ int row_tiles(const DecodeArgs& a, int row) {
   int mine = 0;
   for (int c = c0; c < c1; ++c) {
     int t = 0;
-    for (int r = c * chunk; r < min(a.num_rows, (c + 1) * chunk); ++r) t += row_tiles(a, r);
+    for (int r = c * chunk; r < min(a.num_rows, (c + 1) * chunk); ++r) t += row_tiles<kTokens>(a, r);
     s_pre[c] = t;   // (this thread's entry: its count for now)
     mine += t;
   }
@@ -135,7 +138,7 @@ __device__ __forceinline__ int row_tiles(const DecodeArgs& a, int row) {
         int rr = run;
         for (int r = c * chunk; r < min(a.num_rows, (c + 1) * chunk); ++r) {
           a.ws_rows[r] = rr;
-          rr += row_tiles(a, r);
+          rr += row_tiles<kTokens>(a, r);
         }
       }
     }
@@ -154,12 +157,13 @@ struct Cursor {
   int row, s, ctx, nblk, dirv, g, b;
 };
 
+template <int kTokens = kBlockSize>
 __device__ __forceinline__ void enter_row(const DecodeArgs& a, int row, Cursor& c) {
   c.row = row;
   resolve_row(a, row, c.s, c.ctx);
-  c.nblk = c.ctx > 0 ? (c.ctx + kBlockSize - 1) / kBlockSize : 0;
+  c.nblk = c.ctx > 0 ? (c.ctx + kTokens - 1) / kTokens : 0;
   // Only the tail block has slots outside the context: its entry's direction.
-  c.dirv = entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, c.s, c.nblk > 0 ? c.nblk - 1 : 0);
+  c.dirv = kTokens != kBlockSize ? 1 : entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, c.s, c.nblk > 0 ? c.nblk - 1 : 0);
   c.row = __builtin_amdgcn_readfirstlane(c.row);
   c.s = __builtin_amdgcn_readfirstlane(c.s);
   c.ctx = __builtin_amdgcn_readfirstlane(c.ctx);
@@ -169,6 +173,7 @@ __device__ __forceinline__ void enter_row(const DecodeArgs& a, int row, Cursor& 
 
 // Next tile in (row, KV head, block) order; rows without context have no tiles.
 // Only called while tiles remain in the worker's range, so a row exists.
+template <int kTokens = kBlockSize>
 __device__ __forceinline__ void advance(const DecodeArgs& a, Cursor& c) {
   if (++c.b < c.nblk) return;
   c.b = 0;
@@ -177,18 +182,19 @@ __device__ __forceinline__ void advance(const DecodeArgs& a, Cursor& c) {
   int row = c.row;
   do {
     ++row;
-    enter_row(a, row, c);
+    enter_row<kTokens>(a, row, c);
   } while (c.nblk == 0 && row + 1 < a.num_rows);
 }
 
 // Tile t (< total): binary search over the chunk prefix, then rows of the chunk.
+template <int kTokens = kBlockSize>
 [[maybe_unused]] static __device__ void locate(const DecodeArgs& a, const int* s_pre, int chunk, int nch, int t, Cursor& c) {
   int ch = upper_index(s_pre, nch + 1, t);
   ch = min(ch, nch - 1);
   int base = s_pre[ch];
   int row = ch * chunk;
   for (;;) {
-    enter_row(a, row, c);
+    enter_row<kTokens>(a, row, c);
     const int n = c.nblk * a.num_kv_heads;
     if (t < base + n || row + 1 >= a.num_rows) break;
     base += n;

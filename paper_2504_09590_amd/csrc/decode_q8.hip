@@ -12,6 +12,133 @@
 namespace bros {
 namespace dq {
 
+// Pairs whose loads a wave of the even split keeps in flight (register sets).
+constexpr int kDepth = 2;
+
+// One wave of a worker of the even split (decode_q8_even_kernel): head `hh` of the
+// H heads of the pairs [t0, t0 + n) in (row, group of H KV heads, pair) order
+// (n >= 1). a.num_kv_heads counts the groups; `wid` names the worker's partials.
+template <int G, int H>
+__device__ __forceinline__ void even_worker(const DecodeArgs& a, const Q8Pool& pool, const int* s_pre, int chunk, int nch,
+                                            int wid, int hh, int t0, int n, const dm::Shares& shares) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int grp = lane >> 4;
+  const int col = lane & 15;
+  const bool head_lane = col < G;
+  const int groups = a.num_kv_heads;
+  const int nkv = groups * H;
+  const int Hq = a.num_q_heads;
+
+  // Where a pair lies: its cursor, and its blocks' pool tiles (tile g of block 0 in
+  // place of one that is not there: masked whole).
+  struct Pair {
+    dm::Cursor c;
+    size_t tile[2];
+    bool ok[2];
+  };
+  auto entries = [&](Pair& p) {
+    const int nb = (p.c.ctx + kBlockSize - 1) / kBlockSize;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int b = 2 * p.c.b + x;
+      const int e = load_uniform(a.block_tables, (size_t)p.c.s * a.max_blocks_per_seq + min(b, nb - 1));
+      p.ok[x] = b < nb && e >= 0 && e < a.num_blocks;
+      p.tile[x] = (size_t)(p.ok[x] ? e : 0) * nkv + (p.c.g * H + hh);
+    }
+  };
+  auto first_head = [&](const Pair& p) -> size_t { return (size_t)p.c.row * Hq + (p.c.g * H + hh) * G; };   // of q and out
+  v4u_t qf[4];
+  KRegs k_[kDepth];
+  VRegs v_[kDepth];
+  Running run;
+  run.clear();
+
+  Pair cur[kDepth + 2];   // cur[d]: pair i + d (entries are read one pair before their loads issue)
+  dm::locate<kPairSlots>(a, s_pre, chunk, nch, t0, cur[0].c);
+  entries(cur[0]);
+  issue_k(pool, cur[0].tile[0], cur[0].tile[1], grp, col, k_[0]);
+  load_q<G>(a.q, first_head(cur[0]), grp, col, qf);
+  issue_v(pool, cur[0].tile[0], cur[0].tile[1], grp, col, v_[0]);
+  bool whole = cur[0].c.b == 0;   // this wave saw the segment's first pair
+#pragma unroll
+  for (int d = 1; d <= kDepth; ++d) {
+    cur[d] = cur[d - 1];
+    if (d < n) {
+      dm::advance<kPairSlots>(a, cur[d].c);
+      entries(cur[d]);
+    }
+    if (d < kDepth) {
+      issue_k(pool, cur[d].tile[0], cur[d].tile[1], grp, col, k_[d]);
+      issue_v(pool, cur[d].tile[0], cur[d].tile[1], grp, col, v_[d]);
+    }
+  }
+  cur[kDepth + 1] = cur[kDepth];
+
+  // Pair i, its rows in (k, v).
+  auto body = [&](int i, KRegs& k, VRegs& v) __attribute__((always_inline)) {
+    Pair& p = cur[0];
+    cur[kDepth + 1] = cur[kDepth];
+    if (i + kDepth + 1 < n) {
+      dm::advance<kPairSlots>(a, cur[kDepth + 1].c);
+      entries(cur[kDepth + 1]);
+    }
+    float s[8];
+    const PairScales ps = pair_scales(v.scales);
+    pair_scores(k, qf, ps, a.scale_log2, s);
+    const bool last = p.c.b == p.c.nblk - 1;
+    const bool seg_end = last || i + 1 == n;
+    if (i + 1 == n) {
+      // the cut list: the segment this worker started and leaves unfinished, and the
+      // worker that holds its last pair
+      const bool starts_cut = whole && !last;
+      if (lane == 0 && hh == 0) {
+        a.ws_cut[2 * wid] = starts_cut ? p.c.row * groups + p.c.g : -1;
+        a.ws_cut[2 * wid + 1] = starts_cut ? shares.holder(t0 + i + (p.c.nblk - 1 - p.c.b)) : -1;
+      }
+    }
+    // (past the share the last pair's rows are read again: no branch)
+    issue_k(pool, cur[kDepth].tile[0], cur[kDepth].tile[1], grp, col, k);
+    if (i + 1 < n && seg_end) load_q<G>(a.q, first_head(cur[1]), grp, col, qf);
+    VRows rows = exchange(v, ps);
+    if (!p.ok[0] || !p.ok[1] || last) mask_pair(a, p.c.row, p.c.ctx, 2 * p.c.b, p.ok, grp, s, rows);
+    run.fold(s, rows, head_lane);
+    // (V's registers are free before the fold, but requested there they come no sooner
+    // and everything takes longer: 848 us against 832 in the case above)
+    asm volatile("" ::: "memory");
+    issue_v(pool, cur[kDepth].tile[0], cur[kDepth].tile[1], grp, col, v);
+
+    if (seg_end) {
+      const float l_head = run.total();
+      const bool direct = whole && last;   // the whole segment was this wave's
+      if (head_lane) {
+        if (direct) {
+          const float inv = l_head > 0.0f ? 1.0f / l_head : 0.0f;
+          run.store_bf16(static_cast<uint16_t*>(a.out) + (first_head(p) + col) * kHeadDim, grp, inv);
+        } else {
+          const size_t slot = (((size_t)p.c.row * groups + p.c.g + wid) * H + hh) * G + col;   // partial (run + worker)
+          run.store(a.ws_acc + slot * kHeadDim, grp);
+          if (grp == 0) {
+            a.ws_ml[2 * slot] = run.m_ref;
+            a.ws_ml[2 * slot + 1] = l_head;
+          }
+        }
+      }
+      run.clear();
+      whole = true;
+    }
+#pragma unroll
+    for (int d = 0; d <= kDepth; ++d) cur[d] = cur[d + 1];
+  };
+#pragma clang loop unroll(disable)
+  for (int i = 0; i < n; i += kDepth) {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if (i + d >= n) break;
+      body(i + d, k_[d], v_[d]);
+    }
+  }
+}
+
 // Blocks [sp S, (sp + 1) S) of segment seg0 + blockIdx.x, S = split_blocks (even) and
 // sp = blockIdx.y: the whole segment when it has no more than S blocks, else a
 // partial in slot (segment * n_split_max + sp) * G + head.
@@ -38,8 +165,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   const int n = b1 > first ? (b1 - first + 2 * kWaves - 1) / (2 * kWaves) : 0;
 
   v4u_t qf[4];
-  KRegs k[2];
-  VRegs v[2];
+  KRegs k;
+  VRegs v;
   Running run;
   run.clear();
 
@@ -57,13 +184,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     bool ok[2];
     size_t tile[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      tile[x] = entry(0, x, ok[x]);
-      issue_k(pool, tile[x], grp, col, k[x]);
-    }
+    for (int x = 0; x < 2; ++x) tile[x] = entry(0, x, ok[x]);
+    issue_k(pool, tile[0], tile[1], grp, col, k);
     load_q<G>(a.q, (size_t)row * Hq + g * G, grp, col, qf);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) issue_v(pool, tile[x], grp, col, v[x]);
+    issue_v(pool, tile[0], tile[1], grp, col, v);
 #pragma clang loop unroll(disable)
     for (int i = 0; i < n; ++i) {
       const int b = first + 2 * kWaves * i;
@@ -71,33 +195,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
       for (int x = 0; x < 2; ++x) tile[x] = entry(i + 1, x, next_ok[x]);
       float s[8];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const floatx4_t sc = block_scores(k[x], qf);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[4 * x + r] = sc[r] * a.scale_log2;
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) issue_k(pool, tile[x], grp, col, k[x]);   // the K registers are free
-      if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > ctx) mask_pair(a, row, ctx, b, ok, grp, s, v);
-      run.fold(s, v, head_lane);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        issue_v(pool, tile[x], grp, col, v[x]);   // the V registers are free
-        ok[x] = next_ok[x];
-      }
+      const PairScales ps = pair_scales(v.scales);
+      pair_scores(k, qf, ps, a.scale_log2, s);
+      issue_k(pool, tile[0], tile[1], grp, col, k);   // the K registers are free
+      VRows rows = exchange(v, ps);
+      issue_v(pool, tile[0], tile[1], grp, col, v);   // and V's
+      if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > ctx) mask_pair(a, row, ctx, b, ok, grp, s, rows);
+      run.fold(s, rows, head_lane);
+      ok[0] = next_ok[0];
+      ok[1] = next_ok[1];
     }
   }
 
   // The waves' results.
   const float l_head = run.total();
   if (head_lane) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float* o = &s_o[w][col][32 * grp + 8 * r];
-      *reinterpret_cast<floatx4_t*>(o) = floatx4_t{run.acc[0][r], run.acc[1][r], run.acc[2][r], run.acc[3][r]};
-      *reinterpret_cast<floatx4_t*>(o + 4) = floatx4_t{run.acc[4][r], run.acc[5][r], run.acc[6][r], run.acc[7][r]};
-    }
+    run.store(s_o[w][col], grp);
     if (grp == 0) {
       s_m[w][col] = run.m_ref;
       s_l[w][col] = l_head;
@@ -133,14 +246,126 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   }
 }
 
+// The even split. A run is the pairs of H neighbouring KV heads of a row, and a worker
+// H waves, one per head: the worker takes an equal contiguous share of all pairs in
+// (row, group of heads, pair) order, its waves walk it side by side. A block's rows of
+// H heads lie side by side in the pool, so the waves' reads of a block meet in 2 H KiB
+// of it, and in the H heads' 32 H bytes of scales, where one head's tile alone is 2 KiB.
+// Runs cut between workers leave partials in slot ((run + worker) * H + head) * G +
+// head-in-group, unique as both are in order; the merge folds them.
+template <int G, int H>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void decode_q8_even_kernel(DecodeArgs a, Q8Pool pool) {
+  __shared__ int s_pre[kMaxRowsLds + 1];
+  __shared__ int s_scan[kWaves];
+  constexpr int W = kWaves / H;   // workers of a workgroup
+  const int chunk = (a.num_rows + kMaxRowsLds - 1) / kMaxRowsLds;
+  const int nch = (a.num_rows + chunk - 1) / chunk;
+  const int total = dm::build_tile_prefix<kPairSlots>(a, s_pre, s_scan, chunk, nch);
+  const dm::Shares shares(a, total);
+  const int workers = shares.workers;
+  const int wave = wave_id_uniform();
+  const int hh = wave % H;
+  // (fewer workers than the grid holds are spread over the workgroups)
+  const int wid = workers < a.num_workers ? wave / H * gridDim.x + blockIdx.x : blockIdx.x * W + wave / H;
+  if (wid >= workers) {
+    if (hh == 0 && (threadIdx.x & (kWave - 1)) == 0) a.ws_cut[2 * wid] = -1;   // idle: nothing to merge
+    return;
+  }
+  int t0 = shares.start(wid), t1 = shares.start(wid + 1);
+  asm volatile("" : "+v"(t0), "+v"(t1));
+  even_worker<G, H>(a, pool, s_pre, chunk, nch, wid, hh, t0, t1 - t0, shares);
+}
+
+// The merge: workgroup w folds the run that worker w started and left unfinished (its
+// entry of the cut list names the run and the worker of its last pair), o = sum_i
+// 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over the partials of the workers between. A thread takes
+// two dims of one head per pass. Workgroups behind the workers' write the zeros of
+// rows without context, one wave a row.
+constexpr int kRound = 8;   // partials requested at once
+
+template <int HG>   // query heads of a run
+__global__ __launch_bounds__(kThreads) void decode_q8_merge_kernel(DecodeArgs a) {
+  const int w = blockIdx.x;
+  if (w >= a.num_workers) {
+    const int row = (w - a.num_workers) * kWaves + wave_id_uniform();
+    if (row >= a.num_rows) return;
+    int s, ctx;
+    resolve_row(a, row, s, ctx);
+    if (ctx > 0) return;
+    uint32_t* z = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + (size_t)row * a.num_q_heads * kHeadDim);
+    for (int i = threadIdx.x & (kWave - 1); i < a.num_q_heads * kHeadDim / 2; i += kWave) z[i] = 0u;
+    return;
+  }
+  const int run = load_uniform(a.ws_cut, 2 * (size_t)w);
+  if (run < 0) return;
+  const int w1 = load_uniform(a.ws_cut, 2 * (size_t)w + 1);
+  const int n = w1 - w + 1;
+  const size_t slot0 = ((size_t)run + w) * HG;
+  for (int i = threadIdx.x; i < HG * (kHeadDim / 2); i += kThreads) {
+    const int h = i / (kHeadDim / 2), d = 2 * (i % (kHeadDim / 2));
+    const float2* ml = reinterpret_cast<const float2*>(a.ws_ml) + slot0 + h;
+    const float* acc = a.ws_acc + (slot0 + h) * kHeadDim + d;
+    float M = kNoMax, L = 0.0f, A0 = 0.0f, A1 = 0.0f;
+    for (int c = 0; c < n; c += kRound) {   // indices clamped in range
+      float2 x[kRound], v[kRound];
+#pragma unroll
+      for (int u = 0; u < kRound; ++u) {
+        const int j = min(c + u, n - 1);
+        x[u] = ml[(size_t)j * HG];
+        v[u] = *reinterpret_cast<const float2*>(acc + (size_t)j * HG * kHeadDim);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int u = 0; u < kRound; ++u) Mn = fmaxf(Mn, x[u].x);
+      const float alpha = fast_exp2(M - Mn);
+      L *= alpha;
+      A0 *= alpha;
+      A1 *= alpha;
+      M = Mn;
+#pragma unroll
+      for (int u = 0; u < kRound; ++u) {
+        // (a round's padding adds zero by selection: the partial it repeats may hold a NaN)
+        const bool use = c + u < n;
+        const float wt = use ? fast_exp2(x[u].x - M) : 0.0f;
+        L = fmaf(use ? x[u].y : 0.0f, wt, L);
+        A0 = fmaf(use ? v[u].x : 0.0f, wt, A0);
+        A1 = fmaf(use ? v[u].y : 0.0f, wt, A1);
+      }
+    }
+    const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+    // (a run's heads are neighbours, and runs are in the order of rows and heads)
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + ((size_t)run * HG + h) * kHeadDim + d) =
+        q8::pack2_bf16(A0 * inv, A1 * inv);
+  }
+}
+
+template <int G, int H>
+hipError_t launch_even(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot, int cus) {
+  // (the workspace's partials: a slot per query row and kDecodeGroupSlots groups of heads)
+  const int wgs = std::min(workgroups_per_cu(reinterpret_cast<const void*>(&decode_q8_even_kernel<G, H>), kThreads, slot) * cus,
+                           kDecodeGroupSlots / kWaves);
+  a.num_kv_heads /= H;
+  a.num_workers = wgs * (kWaves / H);
+  hipLaunchKernelGGL((decode_q8_even_kernel<G, H>), dim3(wgs), dim3(kThreads), 0, stream, a, pool);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(decode_q8_merge_kernel<G * H>, dim3(a.num_workers + (a.num_rows + kWaves - 1) / kWaves), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
 constexpr long long kMaxSegmentsPerLaunch = 1 << 23;   // (a launch's threads must stay below 2^32)
 
 template <int G>
-hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream) {
+hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot) {
   const int64_t segments = (int64_t)a.num_rows * a.num_kv_heads;
   const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(((int64_t)a.max_ctx + 15) / 16, a.max_blocks_per_seq));
   const int64_t slots = (int64_t)a.num_rows * a.num_q_heads + (int64_t)kDecodeGroupSlots * std::min(a.num_q_heads, 8);
   const int64_t cus = stream_compute_units(stream);
+  if (segments * ((blocks + 1) / 2) >= 64 * cus) {
+    if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot, (int)cus);
+    if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot, (int)cus);
+    return launch_even<G, 1>(a, pool, stream, slot, (int)cus);
+  }
   int64_t want = std::min<int64_t>((4 * cus + segments - 1) / segments, slots / (segments * G));
   want = std::max<int64_t>(1, std::min<int64_t>(want, (blocks + 7) / 8));
   const int64_t per = ((blocks + want - 1) / want + 7) / 8 * 8;
@@ -159,10 +384,10 @@ hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream) {
 
 hipError_t launch_decode_q8(DecodeArgs a, Q8Pool pool, int group, hipStream_t stream) {
   switch (group) {
-    case 1: return dq::launch_group<1>(a, pool, stream);
-    case 2: return dq::launch_group<2>(a, pool, stream);
-    case 4: return dq::launch_group<4>(a, pool, stream);
-    case 8: return dq::launch_group<8>(a, pool, stream);
+    case 1: return dq::launch_group<1>(a, pool, stream, 8);
+    case 2: return dq::launch_group<2>(a, pool, stream, 9);
+    case 4: return dq::launch_group<4>(a, pool, stream, 10);
+    case 8: return dq::launch_group<8>(a, pool, stream, 11);
     default: return hipErrorInvalidValue;
   }
 }

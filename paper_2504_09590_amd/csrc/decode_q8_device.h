@@ -5,19 +5,26 @@
 // block, and the softmax weights never move between lanes. Lane l = 16 grp + col:
 //   S^T[slot][head] = K[slot][:] . q[head][:]         mfma 16x16x32, four a block
 //   O^T[dim][head] += V^T[dim][slot] P^T[slot][head]  mfma 16x16x32, eight a pair
-// In the C layout of the first product lane l holds the scores of slots 4 grp ..
-// 4 grp + 3 of head col; the 32 slots of a pair are ordered so that the four of the
-// first block and the four of the second are the eight the second product wants in
-// that lane. K: the lane reads row col, dims 16 grp .. + 15 and 64 + 16 grp .. + 15 (the
-// contraction's order of dims is free, q uses the same). V: rows 4 grp + j, dims
-// 8 col .. + 7, and output row m of product t is dim 8 m + t, so lane l ends up with
-// dims 32 grp .. 32 grp + 31 of head col.
+// In the C layout of the first product lane l holds the scores of four K rows for head
+// col, and which slots these are is free (slot_of): those whose V rows the lane has.
+// The 32 slots of a pair are ordered so that the four of the first block and the four of
+// the second are the eight the second product wants in that lane.
 //
-// Codes become bf16 values in registers, two per instruction, which multiplies by
-// the row's scale on the way: exact, so what follows is the 16-bit decode of the
-// values the cache stands for. A pair costs a wave 64 such conversions and 32 byte
-// permutations for 8 KiB of codes; at the rate HBM delivers them a SIMD has about
-// 2900 cycles for a pair, and all of a step's instructions take about a third of that.
+// Codes become bf16 values in registers, two per instruction (exact; V's scale is
+// applied on the way, K's to the scores, a power of two either way), so what follows
+// is the 16-bit decode of the values the cache stands for.
+//
+// What bounds a step is how the memory system takes its reads: with all arithmetic
+// taken out it runs no faster (288 rows of 256 to 16384 tokens, 64 / 8 heads: 852 us
+// without, 834 with). Fewer load instructions and reads that lie together help:
+//   K: the lane reads row slot_of(col / 4, col % 4), dims 16 grp .. + 15 and 64 + 16 grp ..
+//      + 15 (the contraction's order of dims is free, q uses the same).
+//   V: an instruction reads eight rows of a block, 1 KiB: lane (grp, col) reads 16 codes,
+//      chunk col % 8, of rows 2 grp + col / 8 and 8 + 2 grp + col / 8; lanes col and col + 8
+//      then swap halves, so that both have 8 codes of the four rows, dims 16 (col % 8) +
+//      8 (col / 8) .. + 7. Output row m of product t is that of lane col = m, plus t, so lane
+//      l ends up with dims run_dim(grp) + 16 r + t of head col.
+//   Scales: one instruction for both blocks' K and V.
 #pragma once
 
 #include "decode_device.h"
@@ -35,30 +42,42 @@ constexpr int kPairSlots = 2 * kBlockSize;           // slots of a step
 constexpr int kTileBytes = kBlockSize * kHeadDim;    // codes of one (block, KV head), K or V
 constexpr int kScaleBytes = 2 * kBlockSize;          // its scales, K then V
 
-// The registers of one block of a step.
+// What a wave has read of a pair.
 struct KRegs {
-  v4u_t lo, hi;    // row col: dims 16 grp .., 64 + 16 grp ..
-  uint32_t scale;  // the row's scale byte
+  v4u_t lo[2], hi[2];   // per block, row col: dims 16 grp .., 64 + 16 grp ..
 };
 struct VRegs {
-  v2u_t row[4];    // rows 4 grp + j: dims 8 col ..
-  uint32_t scale;  // their scale bytes
+  v4u_t row[2][2];      // per block, rows 8 i + 2 grp + col / 8: dims 16 (col % 8) ..
+  uint32_t scales;      // lane col % 8 = 4 x + 2 w + i: block x's scale bytes of slots 8 i + 2 grp, + 1, K (w = 0) or V
 };
 
-__device__ __forceinline__ v4u_t load16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const v4u_t*>(p)); }
-__device__ __forceinline__ v2u_t load8(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const v2u_t*>(p)); }
+// Slot of the r-th score of a lane of group grp.
+__device__ __forceinline__ int slot_of(int grp, int r) { return 8 * (r >> 1) + 2 * grp + (r & 1); }
 
-__device__ __forceinline__ void issue_k(const Q8Pool& p, size_t tile, int grp, int col, KRegs& k) {
-  const uint8_t* b = p.k + tile * kTileBytes + (uint32_t)(col * kHeadDim + 16 * grp);
-  k.lo = load16(b);
-  k.hi = load16(b + 64);
-  k.scale = p.scales[tile * kScaleBytes + (uint32_t)col];
-}
-__device__ __forceinline__ void issue_v(const Q8Pool& p, size_t tile, int grp, int col, VRegs& v) {
-  const uint8_t* b = p.v + tile * kTileBytes + (uint32_t)(4 * grp * kHeadDim + 8 * col);
+// First of the four runs of 8 dims a lane holds of the output, 16 apart.
+__device__ __forceinline__ int run_dim(int grp) { return 64 * (grp & 1) + 8 * (grp >> 1); }
+
+__device__ __forceinline__ v4u_t load16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const v4u_t*>(p)); }
+
+// tile0, tile1: the (block, KV head) rows of the pair's two blocks, uniform.
+__device__ __forceinline__ void issue_k(const Q8Pool& p, size_t tile0, size_t tile1, int grp, int col, KRegs& k) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v.row[j] = load8(b + j * kHeadDim);
-  v.scale = *reinterpret_cast<const uint32_t*>(p.scales + tile * kScaleBytes + (uint32_t)(kBlockSize + 4 * grp));
+  for (int x = 0; x < 2; ++x) {
+    const uint8_t* b = p.k + (x ? tile1 : tile0) * kTileBytes + (uint32_t)(slot_of(col >> 2, col & 3) * kHeadDim + 16 * grp);
+    k.lo[x] = load16(b);
+    k.hi[x] = load16(b + 64);
+  }
+}
+__device__ __forceinline__ void issue_v(const Q8Pool& p, size_t tile0, size_t tile1, int grp, int col, VRegs& v) {
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const uint8_t* b = p.v + (x ? tile1 : tile0) * kTileBytes + (uint32_t)((2 * grp + (col >> 3)) * kHeadDim + 16 * (col & 7));
+    v.row[x][0] = load16(b);
+    v.row[x][1] = load16(b + 8 * kHeadDim);
+  }
+  // (32 bytes of scales for 4 KiB of codes: their offsets stay below 4 GiB on any card)
+  const uint32_t t = (uint32_t)((col & 4) ? tile1 : tile0);
+  v.scales = *reinterpret_cast<const uint16_t*>(p.scales + (t * kScaleBytes + (uint32_t)(8 * (col & 3) + 2 * grp)));
 }
 
 // The query of a segment, in the order of K's dims (padding columns repeat a head).
@@ -69,24 +88,76 @@ __device__ __forceinline__ void load_q(const void* q, size_t first_head, int grp
   for (int c = 0; c < 4; ++c) qf[c] = *reinterpret_cast<const v4u_t*>(p + 64 * (c >> 1) + 8 * (c & 1));
 }
 
-// Raw scores of a block: slots 4 grp + r of head col.
-__device__ __forceinline__ floatx4_t block_scores(const KRegs& k, const v4u_t (&qf)[4]) {
-  const float s = q8::scale_of(k.scale);
+// Products of a block's codes with the query: slots slot_of(grp, r) of head col, without K's scale.
+__device__ __forceinline__ floatx4_t block_products(const v4u_t& lo, const v4u_t& hi, const v4u_t (&qf)[4]) {
   floatx4_t sc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const v4u_t& w = c < 2 ? k.lo : k.hi;
+    const v4u_t& w = c < 2 ? lo : hi;
     const uint32_t w0 = w[2 * (c & 1)], w1 = w[2 * (c & 1) + 1];
-    const v4u_t kv = {q8::values2_bf16<false>(w0, s), q8::values2_bf16<true>(w0, s), q8::values2_bf16<false>(w1, s),
-                      q8::values2_bf16<true>(w1, s)};
+    const v4u_t kv = {q8::values2_bf16<false>(w0, 1.0f), q8::values2_bf16<true>(w0, 1.0f), q8::values2_bf16<false>(w1, 1.0f),
+                      q8::values2_bf16<true>(w1, 1.0f)};
     sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, qf[c]), sc, 0, 0, 0);
   }
   return sc;
 }
 
+// The scale bytes of a pair as words of four slots (slot_of), in every lane: block x's K
+// (w = 0) or V. From the two-byte pieces of lanes 4 x + 2 w and the next of each 16.
+struct PairScales {
+  uint32_t w[2][2];
+};
+template <int LANE>
+__device__ __forceinline__ uint32_t of_row(uint32_t w) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x150 + LANE, 0xf, 0xf, true);   // row_newbcast
+}
+__device__ __forceinline__ PairScales pair_scales(uint32_t two) {
+  const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)two, 0xb1, 0xf, 0xf, true);   // quad_perm: the neighbour's
+  const uint32_t four = two | (next << 16);   // (as wanted in the even lanes)
+  return PairScales{{{of_row<0>(four), of_row<2>(four)}, {of_row<4>(four), of_row<6>(four)}}};
+}
+__device__ __forceinline__ float byte_scale(uint32_t w, int j) { return q8::scale_of((w >> (8 * j)) & 0xffu); }
+
+// Scores of a pair in log2 units, slots slot_of(grp, r) of the first block, then of the second.
+__device__ __forceinline__ void pair_scores(const KRegs& k, const v4u_t (&qf)[4], const PairScales& ps, float scale_log2, float (&s)[8]) {
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const floatx4_t sc = block_products(k.lo[x], k.hi[x], qf);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[4 * x + r] = sc[r] * scale_log2 * byte_scale(ps.w[x][0], r);
+  }
+}
+
+// The V rows of a pair as the second product takes them: row slot_of(grp, j) of block x,
+// the lane's eight dims, and the rows' scale bytes.
+struct VRows {
+  v2u_t row[2][4];
+  uint32_t scales[2];
+};
+__device__ __forceinline__ VRows exchange(const VRegs& v, const PairScales& ps) {
+  constexpr int kShl8 = 0x108, kShr8 = 0x118;   // row_shl:8, row_shr:8: from lane + 8, from lane - 8 of 16
+  VRows o;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int low = (int)v.row[x][n][i], high = (int)v.row[x][n][2 + i];
+        // the even row: lanes 0..7 have it and keep its low half, lanes 8..15 get its high half
+        o.row[x][2 * n][i] = (uint32_t)__builtin_amdgcn_update_dpp(low, high, kShr8, 0xf, 0xc, false);
+        // the odd row: lanes 8..15 have it and keep its high half, lanes 0..7 get its low half
+        o.row[x][2 * n + 1][i] = (uint32_t)__builtin_amdgcn_update_dpp(high, low, kShl8, 0xf, 0x3, false);
+      }
+    }
+    o.scales[x] = ps.w[x][1];
+  }
+  return o;
+}
+
 // A wave's running result over its part of a segment, per head col.
 struct Running {
-  floatx4_t acc[8];   // acc[t][r]: dim 32 grp + 8 r + t
+  floatx4_t acc[8];   // acc[t][r]: dim run_dim(grp) + 16 r + t
   float m_ref, l_part;
 
   __device__ __forceinline__ void clear() {
@@ -96,9 +167,8 @@ struct Running {
     for (int t = 0; t < 8; ++t) acc[t] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // Folds a pair in: s its eight scores in log2 units (slots 4 grp + r of the first
-  // block, then of the second; -inf where masked), v its V rows.
-  __device__ __forceinline__ void fold(const float (&s)[8], const VRegs (&v)[2], bool head_lane) {
+  // Folds a pair in: s its scores (-inf where masked), v its V rows.
+  __device__ __forceinline__ void fold(const float (&s)[8], const VRows& v, bool head_lane) {
     float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     if (__builtin_amdgcn_ballot_w64(head_lane && mx > m_ref + kRescaleSlack) != 0) {
       // rare: move each head's reference max to the max over the pair's slots
@@ -119,7 +189,7 @@ struct Running {
     for (int i = 0; i < 8; ++i) p[i] = fast_exp2(s[i] - m_ref);
     l_part += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     // The weights as a bf16 and the bf16 of what it leaves: 8 bits more for eight
-    // products a pair, which the matrix cores have time for.
+    // products a pair, which cost nothing measurable.
     const v4u_t hi4 = {q8::pack2_bf16(p[0], p[1]), q8::pack2_bf16(p[2], p[3]), q8::pack2_bf16(p[4], p[5]), q8::pack2_bf16(p[6], p[7])};
     v4u_t lo4;
 #pragma unroll
@@ -129,7 +199,7 @@ struct Running {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sc[x][j] = q8::scale_of((v[x].scale >> (8 * j)) & 0xffu);
+      for (int j = 0; j < 4; ++j) sc[x][j] = byte_scale(v.scales[x], j);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {   // dims 2 u and 2 u + 1 of the lane's eight
@@ -138,7 +208,7 @@ struct Running {
       for (int x = 0; x < 2; ++x) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          w[x][j] = (u & 1) ? q8::values2_bf16<true>(v[x].row[j][u >> 1], sc[x][j]) : q8::values2_bf16<false>(v[x].row[j][u >> 1], sc[x][j]);
+          w[x][j] = (u & 1) ? q8::values2_bf16<true>(v.row[x][j][u >> 1], sc[x][j]) : q8::values2_bf16<false>(v.row[x][j][u >> 1], sc[x][j]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -160,13 +230,30 @@ struct Running {
     l += __shfl_xor(l, 32);
     return l;
   }
+
+  // The lane's dims of head col as fp32 / as bf16 times inv, at `o` (the head's dim 0).
+  __device__ __forceinline__ void store(float* o, int grp) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* d = o + run_dim(grp) + 16 * r;
+      *reinterpret_cast<floatx4_t*>(d) = floatx4_t{acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+      *reinterpret_cast<floatx4_t*>(d + 4) = floatx4_t{acc[4][r], acc[5][r], acc[6][r], acc[7][r]};
+    }
+  }
+  __device__ __forceinline__ void store_bf16(uint16_t* o, int grp, float inv) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *reinterpret_cast<v4u_t*>(o + run_dim(grp) + 16 * r) =
+          v4u_t{q8::pack2_bf16(acc[0][r] * inv, acc[1][r] * inv), q8::pack2_bf16(acc[2][r] * inv, acc[3][r] * inv),
+                q8::pack2_bf16(acc[4][r] * inv, acc[5][r] * inv), q8::pack2_bf16(acc[6][r] * inv, acc[7][r] * inv)};
+  }
 };
 
 // Removes what a pair's blocks do not hold of the context: block b0 + x is `ok`, or
 // an entry outside the pool (or a block past the context); slots from ctx on belong
 // to nobody or to a peer. By selection, so that no value there leaks.
 __device__ __forceinline__ void mask_pair(const DecodeArgs& a, int row, int ctx, int b0, const bool (&ok)[2], int grp,
-                                          float (&s)[8], VRegs (&v)[2]) {
+                                          float (&s)[8], VRows& v) {
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int b = b0 + x;
@@ -174,10 +261,10 @@ __device__ __forceinline__ void mask_pair(const DecodeArgs& a, int row, int ctx,
     const int dir = ok[x] ? entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, row, b) : 1;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      if (!ok[x] || b * kBlockSize + slot_of_offset(4 * grp + r, dir) >= ctx) {
+      if (!ok[x] || b * kBlockSize + slot_of_offset(slot_of(grp, r), dir) >= ctx) {
         s[4 * x + r] = -INFINITY;
-        v[x].row[r] = v2u_t{0u, 0u};
-        v[x].scale &= ~(0xffu << (8 * r));   // (0 times 2^-127)
+        v.row[x][r] = v2u_t{0u, 0u};
+        v.scales[x] &= ~(0xffu << (8 * r));   // (0 times 2^-127)
       }
     }
   }
