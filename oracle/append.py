@@ -57,10 +57,10 @@ def encode(x):
     e = row_exponents(x)
     z = x / 2.0 ** e[..., None].astype(np.float64)
     mag = np.abs(np.where(np.isfinite(z), z, 0.0))
-    # spacing 2^(x - 3) in [2^x, 2^(x + 1)), 2^-9 below 2^-6; the number of steps is rounded
+    # spacing 2^(b - 3) in [2^b, 2^(b + 1)), 2^-9 below 2^-6; the number of steps is rounded
     # half to even, and from the 8th on counts through the binades as the code does
-    x = np.where(mag > 0, np.maximum(np.frexp(mag)[1] - 1, -6), -6)
-    code = np.rint(np.ldexp(mag, 3 - x)).astype(np.int64) + 8 * (x + 6)
+    b = np.where(mag > 0, np.maximum(np.frexp(mag)[1] - 1, -6), -6)
+    code = np.rint(np.ldexp(mag, 3 - b)).astype(np.int64) + 8 * (b + 6)
     code = np.where(np.signbit(z), code + 128, code)
     code = np.where(np.isfinite(x), code, NAN_CODE)
     return code.astype(np.uint8), (e + 127).astype(np.uint8)

@@ -82,6 +82,11 @@ __device__ __forceinline__ void store_chunk(void* row, int chunk, const v4u_t (&
   for (int i = 0; i < (BF16 ? 1 : 2); ++i) p[i] = raw[i];
 }
 
+// The axis of a pair.
+__device__ __forceinline__ int axis_of(const AppendArgs& a, int pair) {
+  return (pair >= a.axis_end[0]) + (pair >= a.axis_end[1]) + (pair >= a.axis_end[2]);
+}
+
 // BF16: type of the rows (and of the pool unless Q8). ADJ: pairs (2 i, 2 i + 1)
 // instead of (i, i + R / 2).
 template <bool BF16, bool Q8, bool ADJ>
@@ -133,12 +138,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     load_chunk<BF16>(row, cb, rb);
   }
   const bool turned = (is_q || is_k) && lane8 * 2 * kPairs < a.rotary_dim;   // this lane's eight pairs are rotated
-  int at[4] = {0, 0, 0, 0};   // positions of the axes
-  if (live && turned && a.rope_pos != nullptr) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (x < a.axes) at[x] = a.rope_pos[(size_t)x * a.num_new_tokens + t0 + tok];
-  }
+  // Given positions: that of the axis of the lane's first pair (most lanes' pairs have one axis).
+  const int axis0 = axis_of(a, kPairs * lane8), axis7 = axis_of(a, kPairs * lane8 + kPairs - 1);
+  int given = 0;
+  if (live && turned && a.rope_pos != nullptr) given = a.rope_pos[(size_t)axis0 * a.num_new_tokens + t0 + tok];
 
   // The sequence and position of each token, as kv_write.hip finds them.
   if (tid < kRows) s_seq[tid] = -1;
@@ -160,28 +163,24 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   // Cosines and sines of this lane's pairs 8 lane8 .. 8 lane8 + 7. A position
   // outside the table: the token is not stored and its q rows are zeros.
   float c[kPairs], s[kPairs];
-  bool outside = false;
-  if (seq >= 0 && a.rope_table != nullptr) {
-    if (a.rope_pos == nullptr) {
-      outside = pos < 0 || pos >= a.table_rows;
-      if (turned && !outside) {
-        const float4* row = reinterpret_cast<const float4*>(a.rope_table + (size_t)pos * a.rotary_dim) + 2 * lane8;
-        const float4* row_s = row + a.rotary_dim / 8;
-        const float4 c0 = row[0], c1 = row[1], s0 = row_s[0], s1 = row_s[1];
-        c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
-        s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
-      }
-    } else if (turned) {
-      const int half = a.rotary_dim / 2;
+  if (seq >= 0 && turned && a.rope_table != nullptr) {
+    const int row = a.rope_pos == nullptr ? pos : given;
+    const bool outside = row < 0 || row >= a.table_rows;   // (dropped below)
+    const float4* r4 = reinterpret_cast<const float4*>(a.rope_table + (size_t)(outside ? 0 : row) * a.rotary_dim) + 2 * lane8;
+    const float4* s4 = r4 + a.rotary_dim / 8;
+    const float4 c0 = r4[0], c1 = r4[1], s0 = s4[0], s1 = s4[1];
+    c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+    s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
+    if (a.rope_pos != nullptr && axis0 != axis7) {   // an axis ends among the lane's pairs: those behind it
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        const int pair = kPairs * lane8 + i;
-        const int row = pair < a.axis_end[0] ? at[0] : pair < a.axis_end[1] ? at[1] : pair < a.axis_end[2] ? at[2] : at[3];
-        const bool bad = row < 0 || row >= a.table_rows;
-        outside |= bad;
-        const float* r = a.rope_table + (size_t)(bad ? 0 : row) * a.rotary_dim + pair;
+      for (int i = 1; i < kPairs; ++i) {
+        const int pair = kPairs * lane8 + i, x = axis_of(a, pair);
+        if (x == axis0) continue;
+        const int other = a.rope_pos[(size_t)x * a.num_new_tokens + t0 + tok];
+        const bool bad = other < 0 || other >= a.table_rows;
+        const float* r = a.rope_table + (size_t)(bad ? 0 : other) * a.rotary_dim + pair;
         c[i] = r[0];
-        s[i] = r[half];
+        s[i] = r[a.rotary_dim / 2];
       }
     }
   }
@@ -195,8 +194,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
       if (a.rope_pos == nullptr) {
         off = p < 0 || p >= a.table_rows;
       } else {
-        for (int x = 0; x < a.axes; ++x) {
-          const int r = a.rope_pos[(size_t)x * a.num_new_tokens + t0 + tid];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int r = a.rope_pos[(size_t)min(x, a.axes - 1) * a.num_new_tokens + t0 + tid];
           off |= r < 0 || r >= a.table_rows;
         }
       }
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
       for (int i = 0; i < kPairs; ++i) xb[i] = xb[i] * r * wa[i];
     }
   }
-  if (turned && seq >= 0 && a.rope_table != nullptr && !outside) {
+  if (turned && seq >= 0 && a.rope_table != nullptr) {   // (outside: the result is dropped)
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       // pair i: (xa[i], xb[i]); adjacent: values 2 i and 2 i + 1 of the lane's sixteen

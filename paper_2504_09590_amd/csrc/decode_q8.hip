@@ -1,11 +1,13 @@
 // bros_attn_decode_q8 on gfx950: one bf16 query row per sequence over the 8-bit
 // cache. decode_q8_device.h says what a step computes and how its operands lie.
 //
-// A workgroup takes a whole (row, KV head) segment, or split_blocks blocks of it;
-// wave w takes every fourth pair of blocks, and the waves' results are folded in LDS. Pieces
-// of one segment leave partials (max, sum, unnormalised output) that a second
-// kernel folds, the one of the 16-bit decode's pieces.
+// For short contexts and few rows a workgroup takes a whole (row, KV head) segment, or
+// split_blocks blocks of it; wave w takes every fourth pair of blocks, and the waves'
+// results are folded in LDS. Pieces of one segment leave partials (max, sum,
+// unnormalised output) that a second kernel folds, the one of the 16-bit decode's
+// pieces. Large batches run the even split below (plan.h says which calls).
 #include "decode_q8_device.h"
+#include "plan.h"
 
 #include <algorithm>
 
@@ -276,17 +278,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   even_worker<G, H>(a, pool, s_pre, chunk, nch, wid, hh, t0, t1 - t0, shares);
 }
 
-// The merge: workgroup w folds the run that worker w started and left unfinished (its
+// The merge: workgroups (w, y) fold the run that worker w started and left unfinished (its
 // entry of the cut list names the run and the worker of its last pair), o = sum_i
-// 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over the partials of the workers between. A thread takes
-// two dims of one head per pass. Workgroups behind the workers' write the zeros of
-// rows without context, one wave a row.
+// 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over the partials of the workers between, four heads
+// each, a thread two dims of one. Workgroups behind the workers' write the zeros of
+// rows without context, one wave a row. (One workgroup for all heads of a run, in
+// passes, took 7.2 us after 64 rows of 128 to 8192 tokens.)
 constexpr int kRound = 8;   // partials requested at once
 
 template <int HG>   // query heads of a run
 __global__ __launch_bounds__(kThreads) void decode_q8_merge_kernel(DecodeArgs a) {
   const int w = blockIdx.x;
   if (w >= a.num_workers) {
+    if (blockIdx.y > 0) return;
     const int row = (w - a.num_workers) * kWaves + wave_id_uniform();
     if (row >= a.num_rows) return;
     int s, ctx;
@@ -301,7 +305,8 @@ __global__ __launch_bounds__(kThreads) void decode_q8_merge_kernel(DecodeArgs a)
   const int w1 = load_uniform(a.ws_cut, 2 * (size_t)w + 1);
   const int n = w1 - w + 1;
   const size_t slot0 = ((size_t)run + w) * HG;
-  for (int i = threadIdx.x; i < HG * (kHeadDim / 2); i += kThreads) {
+  const int i = blockIdx.y * kThreads + threadIdx.x;
+  if (i < HG * (kHeadDim / 2)) {
     const int h = i / (kHeadDim / 2), d = 2 * (i % (kHeadDim / 2));
     const float2* ml = reinterpret_cast<const float2*>(a.ws_ml) + slot0 + h;
     const float* acc = a.ws_acc + (slot0 + h) * kHeadDim + d;
@@ -349,7 +354,7 @@ hipError_t launch_even(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot, 
   hipLaunchKernelGGL((decode_q8_even_kernel<G, H>), dim3(wgs), dim3(kThreads), 0, stream, a, pool);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(decode_q8_merge_kernel<G * H>, dim3(a.num_workers + (a.num_rows + kWaves - 1) / kWaves), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(decode_q8_merge_kernel<G * H>, dim3(a.num_workers + (a.num_rows + kWaves - 1) / kWaves, (G * H + 3) / 4), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -358,19 +363,15 @@ constexpr long long kMaxSegmentsPerLaunch = 1 << 23;   // (a launch's threads mu
 template <int G>
 hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot) {
   const int64_t segments = (int64_t)a.num_rows * a.num_kv_heads;
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(((int64_t)a.max_ctx + 15) / 16, a.max_blocks_per_seq));
+  const int32_t blocks = longest_blocks(a.max_ctx, a.max_blocks_per_seq);
+  // (partials: the workspace has a slot per query row and kDecodeGroupSlots groups more)
   const int64_t slots = (int64_t)a.num_rows * a.num_q_heads + (int64_t)kDecodeGroupSlots * std::min(a.num_q_heads, 8);
-  const int64_t cus = stream_compute_units(stream);
-  if (segments * ((blocks + 1) / 2) >= 64 * cus) {
-    if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot, (int)cus);
-    if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot, (int)cus);
-    return launch_even<G, 1>(a, pool, stream, slot, (int)cus);
+  const int cus = stream_compute_units(stream);
+  if (!plan_q8_decode(segments, G, blocks, cus, slots, &a.split_blocks, &a.n_split_max)) {
+    if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot, cus);
+    if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot, cus);
+    return launch_even<G, 1>(a, pool, stream, slot, cus);
   }
-  int64_t want = std::min<int64_t>((4 * cus + segments - 1) / segments, slots / (segments * G));
-  want = std::max<int64_t>(1, std::min<int64_t>(want, (blocks + 7) / 8));
-  const int64_t per = ((blocks + want - 1) / want + 7) / 8 * 8;
-  a.split_blocks = (int32_t)per;
-  a.n_split_max = (int32_t)((blocks + per - 1) / per);
   for (int64_t s0 = 0; s0 < segments; s0 += kMaxSegmentsPerLaunch) {
     const dim3 grid((unsigned)std::min<int64_t>(segments - s0, kMaxSegmentsPerLaunch), (unsigned)a.n_split_max);
     hipLaunchKernelGGL(decode_q8_kernel<G>, grid, dim3(kThreads), 0, stream, a, pool, (int)s0);

@@ -209,4 +209,46 @@ inline bool plan_short_decode(int64_t segments, int32_t group, int64_t blocks, i
   return false;
 }
 
+// Whether the decode over an 8-bit cache (decode_q8.hip) runs whole segments or pieces
+// of `split_blocks` blocks, or else its even split.
+//
+// A segment is half the bytes of a 16-bit one and a wave takes blocks in pairs, so
+// segments stay whole to longer contexts, and pieces pay further: an even split costs 4 us
+// of start-up and its merge, whatever the batch. Pieces take the shortest size whose count
+// per compute unit and per context stays within limits.
+//
+// Device time over 2965 calls of 1 to 512 rows of up to 32 to 16384 tokens (equal, uniform
+// and lognormal contexts; 64 / 8, 32 / 8, 16 / 8, 8 / 8 and 8 / 1 heads) on 256 compute units: 2.7 %
+// above the best of the even split and seven piece sizes for each call (in 113 by more
+// than 15 %), the even split alone 49 %. Calls in us, the even split / this (32 / 8 heads, contexts
+// uniform up to): four rows of 151 tokens 10.1 / 5.1, six of 2648 18.2 / 10.4, 64 of 434 20.6 /
+// 11.9, 64 of 1748 40.7 / 33.5.
+inline bool plan_q8_decode(int64_t segments, int32_t group, int64_t blocks, int32_t compute_units, int64_t slots,
+                           int32_t* split_blocks, int32_t* n_split) {
+  struct Pieces {
+    int32_t blocks, per_cu4, splits;   // size; pieces per four compute units and of a context, at most
+  };
+  constexpr Pieces kPieces[] = {{16, 5, 32}, {32, 32, 64}, {64, 48, 64}, {128, 32, 64}};
+  if (segments > 0x7fffffff) return false;
+  const int64_t cus = compute_units;
+  const int64_t whole = segments <= cus / 4 ? 36 : segments <= cus / 2 ? 56 : segments <= 4 * cus ? 112 : 256;
+  if (blocks <= whole) {
+    *split_blocks = (int32_t)blocks;
+    *n_split = 1;
+    return true;
+  }
+  // (beyond, pieces are level where contexts are alike, 66 rows of 8892 tokens 220 / 211 us, and
+  // slower where they are not, 64 of 128 to 8192 109 / 120)
+  if (segments * blocks > 448 * cus) return false;
+  for (const Pieces& p : kPieces) {
+    const int64_t splits = (blocks + p.blocks - 1) / p.blocks;
+    if (splits < 2 || splits > p.splits || 4 * segments * splits > p.per_cu4 * cus) continue;
+    if (segments * splits * group > slots) continue;   // (partials)
+    *split_blocks = p.blocks;
+    *n_split = (int32_t)splits;
+    return true;
+  }
+  return false;
+}
+
 }  // namespace bros

@@ -1,0 +1,69 @@
+"""The 8-bit decode's launch plan (csrc/plan.h), compiled alone on the CPU: pieces
+cover every context, partials fit the workspace, limits follow the compute units."""
+
+import ctypes
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2504_09590_amd", "csrc")
+
+WRAPPER = """
+#include "plan.h"
+extern "C" int q8(long long segments, int group, long long blocks, int cus, long long slots, int* out) {
+  return bros::plan_q8_decode(segments, group, blocks, cus, slots, out, out + 1);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no host compiler")
+    d = tmp_path_factory.mktemp("plan_q8")
+    src, so = d / "plan.cpp", d / "plan.so"
+    src.write_text(WRAPPER)
+    subprocess.run([gxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-ftrapv", "-shared", "-fPIC", "-I", CSRC, str(src),
+                    "-o", str(so)], check=True)
+    lib = ctypes.CDLL(str(so))
+    lib.q8.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_int)]
+
+    def call(segments, group, blocks, cus=256, slots=1 << 40):
+        out = (ctypes.c_int * 2)()
+        return tuple(out) if lib.q8(segments, group, blocks, cus, slots, out) else None
+
+    return call
+
+
+def test_pieces_cover_the_context_and_their_partials_fit(plan):
+    rng = random.Random(1)
+    for _ in range(4000):
+        hq, hkv = rng.choice([(32, 8), (64, 8), (8, 1), (16, 8), (8, 8), (3, 3)])
+        rows, cus = int(2 ** rng.uniform(0, 24)), rng.choice([32, 64, 96, 256, 304])
+        blocks = int(2 ** rng.uniform(0, 27))
+        slots = rows * hq + 4096 * min(hq, 8)
+        got = plan(rows * hkv, hq // hkv, blocks, cus, slots)
+        if got is None:
+            continue
+        size, n = got
+        assert n >= 1 and size * n >= blocks and size * (n - 1) < blocks
+        if n > 1:
+            assert size % 2 == 0 and rows * hkv * n * (hq // hkv) <= slots
+
+
+def test_which_calls(plan):
+    assert plan(8, 4, 10) == (10, 1)               # one short row: whole
+    assert plan(48, 4, 128) == (32, 4)
+    assert plan(8, 4, 500) == (16, 32)             # one long row: pieces
+    assert plan(16 * 8, 4, 512) == (64, 8)
+    assert plan(64 * 8, 4, 512) is None
+    assert plan(288 * 8, 8, 1024) is None          # a large batch: the even split
+    assert plan(1 << 32, 1, 1) is None
+    # on a part of the chip the limits scale
+    assert plan(64, 4, 100, cus=32) == (100, 1)
+    assert plan(64, 4, 100, cus=256)[1] > 1
