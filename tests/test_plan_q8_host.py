@@ -60,7 +60,7 @@ def test_which_calls(plan):
     assert plan(8, 4, 10) == (10, 1)               # one short row: whole
     assert plan(48, 4, 128) == (32, 4)
     assert plan(8, 4, 500) == (16, 32)             # one long row: pieces
-    assert plan(16 * 8, 4, 512) == (64, 8)
+    assert plan(16 * 8, 4, 512) == (32, 16)
     assert plan(64 * 8, 4, 512) is None
     assert plan(288 * 8, 8, 1024) is None          # a large batch: the even split
     assert plan(1 << 32, 1, 1) is None
