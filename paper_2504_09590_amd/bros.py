@@ -219,66 +219,96 @@ class QkNorm:
         self.ref = ctypes.byref(self._c)
 
 
-def _on_device(*tensors) -> None:
-    """Every tensor (None aside) lies on the current device, where the kernel runs."""
-    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+_I32, _I8, _U8 = torch.int32, torch.int8, torch.uint8
+
+
+def _addresses(*tensors, strided=()):
+    """Addresses of contiguous tensors (None: None), all on the current device, where the
+    kernel runs, like the `strided` ones."""
+    first = None
+    out = []
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != here):
+        if t is None:
+            out.append(None)
+            continue
+        at = t.get_device()   # (-1: host memory)
+        if at < 0 or (at != first and first is not None):
             raise ValueError(f"a tensor is on {t.device}, not on the current device")
+        if not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        first = at
+        out.append(t.data_ptr())
+    for t in strided:
+        if t is not None and t.get_device() != first:
+            raise ValueError(f"a tensor is on {t.device}, not on the current device")
+    if first != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{first}, not on the current device")
+    return out
 
 
-def _check_meta(rows: int, block_tables, dir, cls, *offsets) -> None:
-    """Metadata tensors of `rows` sequences: types and lengths."""
-    if block_tables.dtype != torch.int32 or block_tables.dim() != 2 or block_tables.shape[0] != rows:
+def _check_meta(rows: int, block_tables, dir, cls, *offsets) -> int:
+    """Checks types and lengths of `rows` sequences' metadata; gives the direction mode."""
+    if block_tables.dtype is not _I32 or block_tables.dim() != 2 or block_tables.size(0) != rows:
         raise ValueError(f"block_tables must be int32 [{rows}][max_blocks]")
-    if dir is not None and (dir.dtype != torch.int8 or dir.shape[0] != rows):
-        raise ValueError(f"dir must be int8 with {rows} rows")
-    _dir_mode(dir, block_tables)
-    if cls is not None and (cls.dtype != torch.uint8 or cls.shape[0] != rows):
+    per_entry = 0
+    if dir is not None:
+        if dir.dtype is not _I8 or dir.size(0) != rows:
+            raise ValueError(f"dir must be int8 with {rows} rows")
+        if dir.dim() != 1:
+            per_entry = _dir_mode(dir, block_tables)
+    if cls is not None and (cls.dtype is not _U8 or cls.numel() != rows):
         raise ValueError(f"cls must be uint8 [{rows}]")
     for t, n in offsets:
-        if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n:
+        if t.dtype is not _I32 or t.dim() != 1 or t.size(0) != n:
             raise ValueError(f"an offset or length array must be int32 [{n}]")
+    return per_entry
 
 
-def _token_rows(t, name: str, tokens: int, like):
-    """Address and elements between tokens of rows [tokens][heads][head_dim], contiguous within a token."""
-    if t.dim() != 3 or t.shape[0] != tokens or t.dtype != like.dtype or t.shape[2] != like.shape[2]:
-        raise ValueError(f"{name} must be [{tokens}][heads][{like.shape[2]}] {like.dtype}")
-    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+def _token_rows(t, name: str, tokens: int, d: int, dtype):
+    """Address, elements between tokens, and heads of rows [tokens][heads][d], contiguous within a token."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != tokens or t.dtype is not dtype or shape[2] != d:
+        raise ValueError(f"{name} must be [{tokens}][heads][{d}] {dtype}")
+    if stride[2] != 1 or stride[1] != d:
         raise ValueError(f"{name}'s heads must be contiguous within a token")
     # (one token's stride, or none's, is never used)
-    return t.data_ptr(), (t.stride(0) if tokens > 1 else t.shape[1] * t.shape[2])
+    return t.data_ptr(), (stride[0] if tokens > 1 else shape[1] * d), shape[1]
 
 
 def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm, pools):
-    nb, hkv, bs, _ = pools[0].shape
-    tn, d = int(k.shape[0]), int(k.shape[2])
-    kp, ks = _token_rows(k, "k", tn, k)
-    vp, vs = _token_rows(v, "v", tn, k)
-    if k.shape[1] != hkv or v.shape[1] != hkv:
+    nb, hkv, bs, d = pools[0].shape
+    dtype, tn = k.dtype, k.size(0)
+    kp, ks, kh = _token_rows(k, "k", tn, d, dtype)
+    vp, vs, vh = _token_rows(v, "v", tn, d, dtype)
+    if kh != hkv or vh != hkv:
         raise ValueError(f"k and v must have the pool's {hkv} heads")
     qp, qs, hq = None, 0, 0
-    if q is not None:
-        qp, qs = _token_rows(q, "q", tn, k)
-        hq = int(q.shape[1])
-        if q_out.shape != q.shape or q_out.dtype != q.dtype:
+    if q is None:
+        q_out = None
+    else:
+        qp, qs, hq = _token_rows(q, "q", tn, d, dtype)
+        if q_out.shape != q.shape or q_out.dtype is not dtype:
             raise ValueError("q_out must have q's shape and type")
-    if norm is not None and any(w.dtype != k.dtype or w.shape[0] != d for w in norm.weights):
-        raise ValueError(f"norm weights must be [{d}] {k.dtype}")
+    more = ()
+    if norm is not None:
+        if any(w.dtype is not dtype or w.size(0) != d for w in norm.weights):
+            raise ValueError(f"norm weights must be [{d}] {dtype}")
+        more = norm.weights
+        norm = norm.ref
     if rope_pos is not None:
         if rope is None:
             raise ValueError("rope_pos without a rotation")
-        if rope_pos.dtype != torch.int32 or rope_pos.numel() != rope.axes * tn:
+        if rope_pos.dtype is not _I32 or rope_pos.numel() != rope.axes * tn:
             raise ValueError(f"rope_pos must be int32 [{rope.axes}][{tn}]")
-    S = int(cu_new.shape[0]) - 1
-    _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
-    _on_device(*pools, q_out if q is not None else None, q, k, v, block_tables, dir, cls, pos0, cu_new, rope_pos,
-               None if rope is None else rope.table, *(() if norm is None else norm.weights))
-    head = (_ptr(q_out) if q is not None else None, qp, kp, vp, qs, ks, vs, tn, hq,
-            None if norm is None else norm.ref, None if rope is None else rope.ref, _ptr(rope_pos))
-    tail = (nb, _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls), _dir_mode(dir, block_tables),
-            _ptr(pos0), _ptr(cu_new), S, hkv, d, bs, _dtype_code(k))
+    S = cu_new.size(0) - 1
+    per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
+    table = None
+    if rope is not None:
+        table, rope = rope.table, rope.ref
+    op, bt, dr, cl, p0, cu, rp, *at = _addresses(q_out, block_tables, dir, cls, pos0, cu_new, rope_pos, *pools, table, *more,
+                                                 strided=(q, k, v))
+    head = (op, qp, kp, vp, qs, ks, vs, tn, hq, norm, rope, rp, *at[:len(pools)])
+    tail = (nb, bt, block_tables.size(1), dr, cl, per_entry, p0, cu, S, hkv, d, bs, _dtype_code(k))
     return head, tail
 
 
@@ -290,15 +320,16 @@ def bros_qkv_append(q_out, q, k, v, k_pool, v_pool, block_tables, dir, cls, pos0
     if k.dtype != k_pool.dtype or v_pool.dtype != k_pool.dtype or v_pool.shape != k_pool.shape:
         raise ValueError(f"rows are {k.dtype}, the pools {k_pool.dtype} and {v_pool.dtype}")
     head, tail = _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm, (k_pool, v_pool))
-    _check(LIB.bros_qkv_append(*head, _ptr(k_pool), _ptr(v_pool), *tail, _stream(stream)))
+    _check(LIB.bros_qkv_append(*head, *tail, _stream(stream)))
 
 
 def _eight_bit(k_pool, v_pool, kv_scales):
     """Checks an 8-bit pool: codes of one byte and [num_blocks][Hkv][2][16] scale bytes."""
-    nb, hkv, bs, d = k_pool.shape
-    if k_pool.element_size() != 1 or v_pool.element_size() != 1 or v_pool.shape != k_pool.shape:
+    shape = k_pool.shape
+    nb, hkv, bs, d = shape
+    if k_pool.element_size() != 1 or v_pool.element_size() != 1 or v_pool.shape != shape:
         raise ValueError("an 8-bit pool holds one byte per value, k and v alike")
-    if kv_scales.element_size() != 1 or tuple(kv_scales.shape) != (nb, hkv, 2, bs):
+    if kv_scales.element_size() != 1 or kv_scales.shape != (nb, hkv, 2, bs):
         raise ValueError(f"kv_scales must be uint8 [{nb}][{hkv}][2][{bs}]")
     return nb, hkv, bs, d
 
@@ -310,87 +341,86 @@ def bros_qkv_append_q8(q_out, q, k, v, k_pool, v_pool, kv_scales, block_tables, 
     _eight_bit(k_pool, v_pool, kv_scales)
     head, tail = _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm,
                               (k_pool, v_pool, kv_scales))
-    _check(LIB.bros_qkv_append_q8(*head, _ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), *tail, _stream(stream)))
+    _check(LIB.bros_qkv_append_q8(*head, *tail, _stream(stream)))
 
 
 def _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens, workspace, *offsets):
-    """Checks what the two attentions over an 8-bit pool share."""
+    """Checks what the two attentions over an 8-bit pool share; gives their common arguments."""
     nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
-    if q.dim() != 3 or q.shape[2] != d or out.shape != q.shape or out.dtype != q.dtype:
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != d or out.shape != shape or out.dtype is not q.dtype:
         raise ValueError(f"q and out must be [rows][Hq][{d}] of one type")
-    S = int(ctx_lens.shape[0])
-    _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *offsets)
-    _on_device(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens, workspace, *(t for t, _ in offsets))
-    return nb, hkv, bs, d, S, 0 if workspace is None else workspace.numel() * workspace.element_size()
+    S = ctx_lens.size(0)
+    per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *offsets)
+    op, qp, kp, vp, sp, bt, dr, cl, cx, ws, *more = _addresses(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens,
+                                                               workspace, *[t for t, _ in offsets])
+    pool = (kp, vp, sp, nb, bt, block_tables.size(1), dr, cl, per_entry, cx)
+    return shape, S, (op, qp, *more), pool, (shape[1], hkv, d, bs), (ws, 0 if ws is None else workspace.nbytes)
 
 
 def bros_attn_decode_q8(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens, max_ctx: int,
                         scale: float = 0.0, workspace=None, stream=None):
     """bros_attn_decode over an 8-bit pool (bfloat16 q and out, the bf16 decode's workspace)."""
-    nb, hkv, bs, d, S, ws_bytes = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens, workspace)
-    if q.shape[0] != S:
-        raise ValueError(f"{q.shape[0]} query rows for {S} sequences")
-    _check(LIB.bros_attn_decode_q8(_ptr(out), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb,
-                                   _ptr(block_tables), int(block_tables.shape[1]), _ptr(dir), _ptr(cls),
-                                   _dir_mode(dir, block_tables), _ptr(ctx_lens), int(max_ctx), S, int(q.shape[1]), hkv, d,
-                                   bs, float(scale), _dtype_code(q), _ptr(workspace), ws_bytes, _stream(stream)))
+    shape, S, rows, pool, heads, ws = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
+                                                    workspace)
+    if shape[0] != S:
+        raise ValueError(f"{shape[0]} query rows for {S} sequences")
+    _check(LIB.bros_attn_decode_q8(*rows, *pool, int(max_ctx), S, *heads, scale, _dtype_code(q), *ws,
+                                   _stream(stream)))
 
 
 def bros_attn_prefill_chunk_q8(out, q, cu_q, max_q_len: int, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens,
                                max_ctx: int, scale: float = 0.0, workspace=None, stream=None):
     """bros_attn_prefill_chunk over an 8-bit pool (bfloat16 q and out, the bf16 prefill's workspace)."""
-    nb, hkv, bs, d, S, ws_bytes = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
-                                                workspace, (cu_q, int(ctx_lens.shape[0]) + 1))
-    _check(LIB.bros_attn_prefill_chunk_q8(_ptr(out), _ptr(q), _ptr(cu_q), int(q.shape[0]), int(max_q_len), _ptr(k_pool),
-                                          _ptr(v_pool), _ptr(kv_scales), nb, _ptr(block_tables),
-                                          int(block_tables.shape[1]), _ptr(dir), _ptr(cls), _dir_mode(dir, block_tables),
-                                          _ptr(ctx_lens), int(max_ctx), S, int(q.shape[1]), hkv, d, bs, float(scale),
-                                          _dtype_code(q), _ptr(workspace), ws_bytes, _stream(stream)))
+    shape, S, rows, pool, heads, ws = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
+                                                    workspace, (cu_q, ctx_lens.size(0) + 1))
+    _check(LIB.bros_attn_prefill_chunk_q8(*rows, shape[0], int(max_q_len), *pool, int(max_ctx), S,
+                                          *heads, scale, _dtype_code(q), *ws, _stream(stream)))
 
 
-def _dense(n: int, pools, ids, rows, scales=None, one_byte=True) -> None:
-    """Dense sides of a move of n slots: [>= n][Hkv][D] each, scales [>= n][Hkv][2], on the
-    current device or in pinned host memory."""
-    hkv, d = pools[0].shape[1], pools[0].shape[3]
-    if n < 0 or (ids is not None and (ids.dtype != torch.int32 or ids.numel() < n)):
+def _move(pools, slot_ids, num_slots, rows, scales=None, one_byte=True):
+    """Checks of a move of n slots between an 8-bit pool and dense [>= n][Hkv][D] rows and
+    [>= n][Hkv][2] scales, on the current device or in pinned host memory. Gives n and
+    the addresses of pools, ids, rows and scales, then (blocks, heads, dims, block size)."""
+    nb, hkv, bs, d = _eight_bit(*pools)
+    n = int(num_slots) if num_slots is not None else 0 if slot_ids is None else slot_ids.size(0)
+    if n < 0 or (slot_ids is not None and (slot_ids.dtype is not _I32 or slot_ids.numel() < n)):
         raise ValueError(f"slot_ids must be int32 and hold {n} ids")
     for t in rows:
-        if t.shape[0] < n or tuple(t.shape[1:]) != (hkv, d) or (one_byte and t.element_size() != 1):
+        shape = t.shape
+        if shape[0] < n or shape[1:] != (hkv, d) or (one_byte and t.element_size() != 1):
             raise ValueError(f"a dense buffer must hold [{n}][{hkv}][{d}]" + (" bytes" if one_byte else ""))
-    if scales is not None and (scales.shape[0] < n or tuple(scales.shape[1:]) != (hkv, 2) or scales.element_size() != 1):
-        raise ValueError(f"the scales must hold [{n}][{hkv}][2] bytes")
-    _on_device(ids, *pools, *(t for t in (*rows, scales) if t is not None and (t.is_cuda or not t.is_pinned())))
+    if scales is not None:
+        shape = scales.shape
+        if shape[0] < n or shape[1:] != (hkv, 2) or scales.element_size() != 1:
+            raise ValueError(f"the scales must hold [{n}][{hkv}][2] bytes")
+        rows = (*rows, scales)
+    host = [not t.is_cuda and t.is_pinned() for t in rows]
+    at = _addresses(*pools, slot_ids, *(None if h else t for t, h in zip(rows, host)))
+    dense = [_ptr(t) if h else a for t, h, a in zip(rows, host, at[4:])]
+    return n, at[:3], at[3], dense, nb, (hkv, d, bs)
 
 
 def bros_kv_gather_q8(k_pool, v_pool, kv_scales, slot_ids, k_out, v_out, scales_out, num_slots: int | None = None,
                       stream=None):
     """Codes and scale bytes of an 8-bit pool's slots into dense [n][Hkv][D] and [n][Hkv][2] buffers."""
-    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
-    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
-    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_out, v_out), scales_out)
-    _check(LIB.bros_kv_gather_q8(_ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb, _ptr(slot_ids), n, _ptr(k_out),
-                                 _ptr(v_out), _ptr(scales_out), hkv, d, bs, _stream(stream)))
+    n, pools, ids, dense, nb, dims = _move((k_pool, v_pool, kv_scales), slot_ids, num_slots, (k_out, v_out), scales_out)
+    _check(LIB.bros_kv_gather_q8(*pools, nb, ids, n, *dense, *dims, _stream(stream)))
 
 
 def bros_kv_scatter_q8(k_in, v_in, scales_in, slot_ids, k_pool, v_pool, kv_scales, num_slots: int | None = None,
                        stream=None):
     """Dense codes and scale bytes back into an 8-bit pool's slots; ids outside the pool are skipped."""
-    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
-    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
-    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_in, v_in), scales_in)
-    _check(LIB.bros_kv_scatter_q8(_ptr(k_in), _ptr(v_in), _ptr(scales_in), _ptr(slot_ids), n, _ptr(k_pool),
-                                  _ptr(v_pool), _ptr(kv_scales), nb, hkv, d, bs, _stream(stream)))
+    n, pools, ids, dense, nb, dims = _move((k_pool, v_pool, kv_scales), slot_ids, num_slots, (k_in, v_in), scales_in)
+    _check(LIB.bros_kv_scatter_q8(*dense, ids, n, *pools, nb, *dims, _stream(stream)))
 
 
 def bros_kv_read_q8(k_pool, v_pool, kv_scales, slot_ids, k_out, v_out, num_slots: int | None = None, stream=None):
     """The values of an 8-bit pool's slots into dense [n][Hkv][D] tensors (bfloat16 or float32)."""
-    n = _numel0(slot_ids) if num_slots is None else int(num_slots)
-    nb, hkv, bs, d = _eight_bit(k_pool, v_pool, kv_scales)
-    if k_out.dtype != v_out.dtype:
+    if k_out.dtype is not v_out.dtype:
         raise ValueError("k_out and v_out must have one type")
-    _dense(n, (k_pool, v_pool, kv_scales), slot_ids, (k_out, v_out), one_byte=False)
-    _check(LIB.bros_kv_read_q8(_ptr(k_pool), _ptr(v_pool), _ptr(kv_scales), nb, _ptr(slot_ids), n, _ptr(k_out),
-                               _ptr(v_out), hkv, d, bs, _dtype_code(k_out), _stream(stream)))
+    n, pools, ids, dense, nb, dims = _move((k_pool, v_pool, kv_scales), slot_ids, num_slots, (k_out, v_out), one_byte=False)
+    _check(LIB.bros_kv_read_q8(*pools, nb, ids, n, *dense, *dims, _dtype_code(k_out), _stream(stream)))
 
 
 def bros_set_decode_kernel_events(before=None, after=None):
