@@ -94,6 +94,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(float)))) float float2_t;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 typedef unsigned v4u_t __attribute__((ext_vector_type(4)));
 typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef int v8i_t __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;                      // 4 waves: one per SIMD, two workgroups per CU
 constexpr int kRows = 128;                         // query rows per workgroup
@@ -113,6 +114,8 @@ constexpr int kMinSavedTiles = 12;                 // what splitting must take o
 constexpr int kPairTiles = 12;                     // what a second piece on every compute unit costs
 constexpr int kLongPieces = 96;                    // the shortest pieces of which two to a compute unit are the first choice
 constexpr int kLoadsPerStep = 4;                   // two K and two V loads per wave per step
+constexpr int kQ8TileBytes = kKeys * kHeadDim;     // one K tile of 8-bit rows in LDS
+constexpr int kGuardKeys = kRows + 2 * kKeys;      // keys of the tiles that not every row of a unit sees, at most
 constexpr int kXcds = 8;                           // accelerator dies of the chip; blockIdx % 8 picks the die
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(v4u_t v) { return __builtin_bit_cast(bf16x8_t, v); }
@@ -144,6 +147,11 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t lane_off,
   // LDS is the LDS address
   const uint32_t m0 = (uint32_t)(uintptr_t)dst;
   asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
+}
+// The same for 4 bytes per lane, at dst + 4 * lane.
+__device__ __forceinline__ void load_word_to_lds(const void* base, uint32_t lane_off, const void* dst) {
+  const uint32_t m0 = (uint32_t)(uintptr_t)dst;
+  asm volatile("global_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 // A load the compiler may issue as a scalar (uniform) load.
 typedef const int32_t __attribute__((address_space(4)))* scalar_i32_ptr;
@@ -587,17 +595,33 @@ __device__ __forceinline__ int paired_id(const PrefillArgs& a, int b, int grid) 
 // (contexts up to kPrefillWholeTableCtx); the step loop then carries one more
 // scalar test per four tiles, which is why short contexts keep their own variant.
 //
-// kQ8: the pools hold 8-bit codes and `scales` their scales (q8_device.h). Each wave
-// reads its eight rows of a K and a V tile into registers, 16 codes a lane, two steps
-// before it turns them into bf16 values and writes them to the rings, a step before
-// they are used: 16 conversions and four LDS writes a wave and step, where the 16-bit
-// rows go to LDS by themselves. From there on a step is the same.
+// kQ8: the pools hold 8-bit codes and `scales` their scales (q8_device.h).
+//
+// K stays in 8 bits: its rows go to LDS as they are, and S^T = K Q^T runs on the scaled
+// 8-bit products, which take each row's scale byte. Q is given to them as two e4m3 terms,
+// the second what the first leaves, four binades lower: a bf16 value has 8 significant
+// bits, each term holds 4, so the terms add up to it exactly (below 2^-14 of the row's
+// largest value to 2^-22 of that). Twice the products at twice the rate, half of
+// K's LDS traffic and no conversion. V has a scale per key, along the products' inner
+// dimension, where they take one for 32, so its rows become bf16 values: they go to LDS as they are
+// too, and a step before a tile is used each wave reads its own eight rows back and writes
+// their values to the V ring. (Rows of K and V read into registers and written to the rings as
+// values: 512 rows on 16000 tokens 157 us. Loads into registers that stay in flight over
+// several steps of the loop are waited for at its joins.)
+//
+// A value of V that is not a number must reach no row that does not see its key, though the
+// products add 0 times it: in tiles that not every row of the unit sees such values are
+// stored as zeros and noted in LDS, and rows that see one are set to NaN at the end. (Looked
+// for in the operands of every such tile instead, a prompt of 301 rows took 15.7 us, not 13.6.)
 template <int G, bool kOff32, bool kRing, bool kQ8 = false>
 __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8_t* s_kring, uint8_t* s_vring,
                                              int* s_first_bad_p, int* s_tbl, int8_t* s_dir,
-                                             const uint8_t* scales = nullptr) {
+                                             const uint8_t* scales = nullptr, uint16_t* s_nan = nullptr,
+                                             int* s_any_nan = nullptr,
+                                             uint8_t* s_raw = nullptr, uint32_t* s_scale = nullptr) {
   constexpr int QT = kRows / G;   // positions per unit
   constexpr int kSlotBytes = kTileBytes;
+  constexpr int kKSlotBytes = kQ8 ? kQ8TileBytes : kTileBytes;   // a K tile in LDS
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int wv = wave_id_uniform();
@@ -655,7 +679,17 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   // Q^T operand: for d-step c, lane holds Q[row][16c + 8*half .. +8). Issued
   // before every load into LDS, so waiting for the first tiles covers it.
   bf16x8_t qf[8];
-  {
+  [[maybe_unused]] v8i_t qt[2][2];      // 8-bit: [term][dims 64 c + 32 half .. + 31]
+  [[maybe_unused]] int q_scale[2];      // their scale bytes
+  [[maybe_unused]] v4u_t q_raw[8];
+  if constexpr (kQ8) {
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + row_off + 32 * half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      q_raw[i] = v4u_t{0u, 0u, 0u, 0u};
+      if (row_valid) q_raw[i] = *reinterpret_cast<const v4u_t*>(qp + 64 * (i >> 2) + 8 * (i & 3));
+    }
+  } else {
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) + row_off;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -664,6 +698,40 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
       qf[c] = as_bf16x8(v);
     }
   }
+
+  // The terms, once the first tiles are on their way. (A q that is not finite gives NaN rows
+  // whatever its terms are.)
+  [[maybe_unused]] auto split_q = [&]() __attribute__((always_inline)) {
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(q_raw[i][k])), fabsf(bf16_hi(q_raw[i][k]))));
+    }
+    const int e = q8::row_exponent(pair_max(amax));
+    const float mul = q8::exp2_int(-e);
+    q_scale[0] = e + 127;
+    q_scale[1] = e + 127 - 4;
+    auto codes = [](const float (&x)[4]) __attribute__((always_inline)) -> int {
+      return __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {   // four values
+        const uint32_t w0 = q_raw[i][2 * k], w1 = q_raw[i][2 * k + 1];
+        float x[4] = {bf16_lo(w0) * mul, bf16_hi(w0) * mul, bf16_lo(w1) * mul, bf16_hi(w1) * mul};
+        const int c = codes(x);
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+        x[0] = (x[0] - lo[0]) * 16.0f;
+        x[1] = (x[1] - lo[1]) * 16.0f;
+        x[2] = (x[2] - hi[0]) * 16.0f;
+        x[3] = (x[3] - hi[1]) * 16.0f;
+        qt[0][i >> 2][2 * (i & 3) + k] = c;
+        qt[1][i >> 2][2 * (i & 3) + k] = codes(x);
+      }
+    }
+  };
 
   // Table entries. The first few come in as scalar loads; the piece's
   // entries are then staged in LDS as (block, KV head) row indices,
@@ -727,30 +795,73 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     }
   };
 
-  // 8-bit rows: lane l holds codes 16 (l % 8) .. + 15 of the wave's row l / 8, the two
-  // 16-byte chunks 2 (l % 8), + 1 of the bf16 row. Batch b (K of tile b + 1, V of tile b)
-  // sits in set b % 2 from step b - 3 to step b - 1.
-  struct Staged {
-    v4u_t k, v;
-    uint32_t ks, vs;
-  };
-  [[maybe_unused]] Staged sets[2];
+  // 8-bit rows: tile j's sit in slot j % 4 of the K ring, of the raw V ring and of the
+  // wave's scales. One load covers the wave's eight rows, lane l writing physical chunk l % 8
+  // of row l / 8. In K that holds logical chunk (l % 8) ^ (row / 2 % 8), so that 16 rows of an
+  // operand read meet 16 different groups of banks; V's rows are only read back by the wave itself.
+  // Scales: the 16 words of the tile's two blocks (K's and V's), in every 16 lanes again.
   [[maybe_unused]] const int q8_row = lane >> 3, q8_c = lane & 7;
-  [[maybe_unused]] const uint32_t q8_off = (uint32_t)((my_slot0 + q8_row) * kHeadDim + 16 * q8_c);
-  auto fetch_q8 = [&](int idx, const void* pool, int which, v4u_t& codes, uint32_t& scale) __attribute__((always_inline)) {
-    const uint8_t* p = static_cast<const uint8_t*>(pool);
-    const uint32_t so = (uint32_t)(kBlockSize * which + my_slot0 + q8_row);
+  [[maybe_unused]] const uint32_t q8_v_off = (uint32_t)((my_slot0 + q8_row) * kHeadDim + 16 * q8_c);
+  [[maybe_unused]] const uint32_t q8_k_off =
+      (uint32_t)((my_slot0 + q8_row) * kHeadDim + 16 * (q8_c ^ (((8 * rg + q8_row) >> 1) & 7)));
+  // idx: row of the wave's block; sidx: of the lane's block (l / 8 % 2) of scales.
+  auto issue_q8 = [&](int idx, int sidx, int slot) __attribute__((always_inline)) {
+    uint8_t* kd = s_kring + slot * kKSlotBytes + 8 * rg * kHeadDim;
+    uint8_t* vd = s_raw + slot * kKSlotBytes + 8 * rg * kHeadDim;
     if constexpr (kOff32) {
-      codes = *reinterpret_cast<const v4u_t*>(p + (((uint32_t)idx << 11) + q8_off));
-      scale = scales[((uint32_t)idx << 5) + so];
+      load_to_lds(a.k_pool, ((uint32_t)idx << 11) + q8_k_off, kd);
+      load_to_lds(a.v_pool, ((uint32_t)idx << 11) + q8_v_off, vd);
     } else {
-      const size_t r = (size_t)__builtin_amdgcn_readfirstlane(idx);
-      codes = *reinterpret_cast<const v4u_t*>(p + r * (kBlockSize * kHeadDim) + q8_off);
-      scale = (scales + r * (2 * kBlockSize))[so];
+      const size_t r = (size_t)__builtin_amdgcn_readfirstlane(idx) * (kBlockSize * kHeadDim);
+      load_to_lds(static_cast<const uint8_t*>(a.k_pool) + r, q8_k_off, kd);
+      load_to_lds(static_cast<const uint8_t*>(a.v_pool) + r, q8_v_off, vd);
     }
+    // (32 bytes of scales for 4 KiB of codes: their offsets stay below 4 GiB on any card)
+    load_word_to_lds(scales, ((uint32_t)sidx << 5) + 4u * (uint32_t)(lane & 7), s_scale + (slot * 4 + rg) * kWave);
   };
-  auto put_q8 = [&](const v4u_t& codes, uint32_t scale, uint8_t* ring, bool keep) __attribute__((always_inline)) {
+  // Scale byte at `at_byte` of the wave's scales of tile j.
+  auto scale_q8 = [&](int j, int at_byte) __attribute__((always_inline)) -> uint32_t {
+    return reinterpret_cast<const uint8_t*>(s_scale + ((j & 3) * 4 + rg) * kWave)[at_byte];
+  };
+  auto k_scale_q8 = [&](int j) __attribute__((always_inline)) -> uint32_t {   // of the lane's key
+    return scale_q8(j, 2 * kBlockSize * (mrow >> 4) + (mrow & 15));
+  };
+  auto sidx_q8 = [&](int j) __attribute__((always_inline)) -> int { return s_tbl[at(2 * (kb + j) + ((lane >> 3) & 1))]; };
+  const int guard0 = full_below / kKeys;   // tiles from here on are not seen by every row
+  // V of tile j to the V ring (two slots); FIX: rows that are not context become zeros, and
+  // values that are not numbers, in tiles from guard0 on, zeros and notes.
+  auto put_v_q8 = [&](int j, auto fixc) __attribute__((always_inline)) {
+    uint8_t* ring = s_vring + (j & 1) * kSlotBytes;
     const int row = 8 * rg + q8_row;   // tile row
+    v4u_t codes = *reinterpret_cast<const v4u_t*>(s_raw + (j & 3) * kKSlotBytes + row * kHeadDim + 16 * q8_c);
+    uint32_t scale = scale_q8(j, 2 * kBlockSize * my_bt + kBlockSize + my_slot0 + q8_row);
+    bool keep = true;
+    if constexpr (decltype(fixc)::value) {
+      const int b = 2 * (kb + j) + my_bt;
+      const int dirv = s_dir[at(b)];
+      keep = dirv != 0 && b * kBlockSize + slot_of_offset(my_slot0 + q8_row, dirv) < ctx;
+      uint32_t bad[4], any = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bad[i] = ((codes[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // bytes that are the NaN code
+        if (scale == 255u) bad[i] = 0x80808080u;
+        any |= bad[i];
+      }
+      if (__builtin_amdgcn_ballot_w64(keep && any != 0u) != 0 && kb + j >= guard0) {
+        if (keep && any != 0u) {
+          uint32_t note = 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t m = bad[i] >> 7;   // a bit in the lowest place of each byte
+            note |= ((m & 1u) | ((m >> 7) & 2u) | ((m >> 14) & 4u) | ((m >> 21) & 8u)) << (4 * i);
+            codes[i] &= ~(m * 255u);
+          }
+          if (scale == 255u) scale = 127u;
+          s_nan[((kb + j - guard0) * kKeys + row) * 8 + q8_c] = (uint16_t)note;
+          *s_any_nan = 1;
+        }
+      }
+    }
     const float f = q8::scale_of(scale);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -760,24 +871,20 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
       *reinterpret_cast<v4u_t*>(ring + row * kRowBytes + (((2 * q8_c + h) ^ swz(row)) << 4)) = w;
     }
   };
-  // Whether this lane's row of tile j is context (by what LDS holds of the table).
-  auto context_q8 = [&](int j) __attribute__((always_inline)) -> bool {
-    const int b = 2 * (kb + j) + my_bt;
-    const int dirv = s_dir[at(b)];
-    return dirv != 0 && b * kBlockSize + slot_of_offset(my_slot0 + q8_row, dirv) < ctx;
+  // At the start of step ii: V of tile ii + 1 goes to the V ring (its slot was last read in step
+  // ii - 1), and tile ii + 4 is requested into the slots of tile ii, whose K and scales step
+  // ii - 1 read last: three loads a step. Gives the lane's K scale of tile ii + 1.
+  auto turn_q8 = [&](int ii, auto fixc) __attribute__((always_inline)) -> uint32_t {
+    put_v_q8(ii + 1, fixc);
+    const uint32_t ks = k_scale_q8(ii + 1);
+    issue_q8(own(ii + 4), sidx_q8(ii + 4), ii & 3);
+    return ks;
   };
-  auto fetch_batch = [&](int b, Staged& st) __attribute__((always_inline)) {
-    fetch_q8(own(b + 1), a.k_pool, 0, st.k, st.ks);
-    fetch_q8(own(b), a.v_pool, 1, st.v, st.vs);
-  };
-  // At the start of step ii: batch ii + 1 goes to the rings, and batch ii + 3 is
-  // requested into its set. (The slots written were last read two steps ago.)
-  auto turn_q8 = [&](int ii, Staged& st, auto fixc) __attribute__((always_inline)) {
-    bool keep = true;
-    if constexpr (decltype(fixc)::value) keep = context_q8(ii + 1);
-    put_q8(st.k, st.ks, s_kring + ((ii + 2) & (kSlots - 1)) * kSlotBytes, true);
-    put_q8(st.v, st.vs, s_vring + ((ii + 1) & (kSlots - 1)) * kSlotBytes, keep);
-    fetch_batch(ii + 3, st);
+  // At its end: tile ii + 2, requested in step ii - 2, is in LDS (the six loads of steps ii - 1
+  // and ii may be outstanding).
+  auto publish_q8 = [&]() __attribute__((always_inline)) {
+    wait_vmem<6>();
+    lds_barrier();
   };
 
   // K operand (S^T = K Q^T, d-step c): tile row mrow, logical chunk 2c + half.
@@ -815,12 +922,31 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
 
   // K operands of the tile in K ring `sk`, all eight d-steps, issued
   // together.
+  [[maybe_unused]] const int k8_lane = mrow * kHeadDim, k8_sw = (mrow >> 1) & 7;
   auto k_operands = [&](const uint8_t* sk, v4u_t (&kv)[8]) __attribute__((always_inline)) {
+    if constexpr (kQ8) {   // kv[2 c + h]: dims 64 c + 32 half + 16 h ..
+#pragma unroll
+      for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const v4u_t*>(sk + k8_lane + (((4 * (c >> 1) + 2 * half + (c & 1)) ^ k8_sw) << 4));
+      return;
+    }
 #pragma unroll
     for (int c = 0; c < 8; ++c) kv[c] = *reinterpret_cast<const v4u_t*>(sk + k_lane + (((2 * c) ^ (k_sw & 14)) << 4));
   };
   // S^T = K Q^T (one dependent chain; back-to-back accumulation needs no gap).
-  auto scores = [&](const v4u_t (&kv)[8], floatx16& acc) __attribute__((always_inline)) {
+  // (8-bit: ks is the scale byte of the lane's key row)
+  auto scores = [&](const v4u_t (&kv)[8], floatx16& acc, uint32_t ks) __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const v4u_t x = kv[2 * c], y = kv[2 * c + 1];
+        const v8i_t k8 = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, qt[t][c], c + t == 0 ? floatx16{} : acc, 0, 0, 0, (int)ks, 0,
+                                                                q_scale[t]);
+      }
+      return;
+    }
 #pragma unroll
     for (int c = 0; c < 8; ++c)
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kv[c]), qf[c], c == 0 ? floatx16{} : acc, 0, 0, 0);
@@ -888,53 +1014,6 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     for (int dt = 0; dt < 4; ++dt)
       o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[dt]), pf[c2], o[dt], 0, 0, 0);
   };
-  // PV of a tile with keys that not every row sees, 8-bit cache: a row that does not
-  // see a key must not meet a NaN there (0 * NaN), and the chunk's own rows of a
-  // 16-bit cache cannot be told apart either, but here a NaN is what an infinity was
-  // stored as. Values that are not finite are taken out of V, and the rows that see
-  // one get their NaN from a product of ones: marks of such values, marks of seen keys.
-  [[maybe_unused]] auto pv_guarded = [&](v4u_t (&v0)[4], v4u_t (&v1)[4], const bf16x8_t (&pf)[2], const floatx16& cur)
-      __attribute__((always_inline)) {
-    constexpr uint32_t kLo = 0x7f80u, kHi = 0x7f800000u;
-    bool bad = false;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bad |= (v0[dt][i] & kLo) == kLo || (v0[dt][i] & kHi) == kHi;
-        bad |= (v1[dt][i] & kLo) == kLo || (v1[dt][i] & kHi) == kHi;
-      }
-    }
-    if (__builtin_amdgcn_ballot_w64(bad) != 0) {
-      v4u_t seen[2];
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          seen[c2][i] = (cur[8 * c2 + 2 * i] == -INFINITY ? 0u : 0x3f80u) | (cur[8 * c2 + 2 * i + 1] == -INFINITY ? 0u : 0x3f800000u);
-      }
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt) {
-        floatx16 hit = {};
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) {
-          v4u_t& w = c2 ? v1[dt] : v0[dt];
-          v4u_t mark;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = (w[i] & kLo) == kLo ? 0xffffu : 0u, hi = (w[i] & kHi) == kHi ? 0xffff0000u : 0u;
-            mark[i] = (lo | hi) & 0x3f803f80u;
-            w[i] &= ~(lo | hi);
-          }
-          hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(mark), as_bf16x8(seen[c2]), hit, 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[dt][j] = hit[j] > 0.0f ? __uint_as_float(0x7fc00000u) : o[dt][j];
-      }
-    }
-    pv(v0, pf, 0);
-    pv(v1, pf, 1);
-  };
   // Rare (lazy max).
   auto rescale_o = [&]() __attribute__((always_inline)) {
     if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
@@ -956,24 +1035,18 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   // wave on the SIMD fills the gaps.
   // `in` holds the current tile's scores, `out` receives the next tile's.
   auto step = [&](const uint8_t* sk, const uint8_t* sv, int next_tile, auto has_next, auto mask_next,
-                  const floatx16& in, floatx16& out) __attribute__((always_inline)) {
+                  const floatx16& in, floatx16& out, uint32_t ks) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(has_next)::value;
-    // (the current tile may have keys that not every row sees, but for the main loop's)
-    constexpr bool GUARD = kQ8 && (!NEXT || decltype(mask_next)::value);
     v4u_t kv[8];
     v4u_t vv0[4], vv1[4];
     if constexpr (NEXT) k_operands(sk, kv);
     v_operands(sv, 0, vv0);
     bf16x8_t pf[2];
-    if constexpr (NEXT) scores(kv, out);
+    if constexpr (NEXT) scores(kv, out, ks);
     probs(pf, in);
     v_operands(sv, 1, vv1);
-    if constexpr (GUARD) {
-      pv_guarded(vv0, vv1, pf, in);
-    } else {
-      pv(vv0, pf, 0);
-      pv(vv1, pf, 1);
-    }
+    pv(vv0, pf, 0);
+    pv(vv1, pf, 1);
     if constexpr (NEXT) mask_max(out, mask_next, next_tile);
   };
   // After step ii: wait for batch ii + 1 (K of step ii + 2, V of step ii + 1),
@@ -1000,12 +1073,17 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   auto own0 = [&](int j) -> int { return entry(2 * (kb + j) + my_bt); };
   const int e0 = own0(0);
   const int w0 = own0(1), w1 = own0(2), w2 = own0(3), w3 = own0(4);
-  [[maybe_unused]] v4u_t k0_codes;
-  [[maybe_unused]] uint32_t k0_scale;
   if constexpr (kQ8) {
-    fetch_q8(e0, a.k_pool, 0, k0_codes, k0_scale);
-    fetch_q8(w0, a.k_pool, 0, sets[0].k, sets[0].ks);
-    fetch_q8(e0, a.v_pool, 1, sets[0].v, sets[0].vs);
+    auto sidx0 = [&](int j) -> int {   // (entries as scalar loads; the LDS copy is not there yet)
+      const int x = entry(2 * (kb + j)), y = entry(2 * (kb + j) + 1);
+      return (lane >> 3) & 1 ? y : x;
+    };
+    issue_q8(e0, sidx0(0), 0);
+    issue_q8(w0, sidx0(1), 1);
+    issue_q8(w1, sidx0(2), 2);
+    issue_q8(w2, sidx0(3), 3);
+    for (int i = tid; i < kGuardKeys * 8 / 2; i += kThreads) reinterpret_cast<uint32_t*>(s_nan)[i] = 0u;
+    if (tid == 0) *s_any_nan = 0;
   } else {
     issue(e0, kpool, s_kring);
     issue(w0, kpool, s_kring + 1 * kSlotBytes);
@@ -1049,11 +1127,9 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   const int first_bad = __builtin_amdgcn_readfirstlane((*s_first_bad_p));
   const int plain_tiles = min(full_below / kKeys, first_bad / 2);
   if constexpr (kQ8) {
-    put_q8(k0_codes, k0_scale, s_kring, true);
-    put_q8(sets[0].k, sets[0].ks, s_kring + kSlotBytes, true);
-    put_q8(sets[0].v, sets[0].vs, s_vring, context_q8(0));
-    fetch_batch(1, sets[1]);
-    fetch_batch(2, sets[0]);
+    split_q();
+    wait_vmem<0>();   // tiles 0 .. 3 of this wave's rows
+    put_v_q8(0, std::true_type{});
   } else {
     // Everything so far, Q included: a wait the compiler sees, so it knows the
     // Q registers are ready and adds no wait of its own later.
@@ -1064,12 +1140,14 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   {
     v4u_t kv[8];
     k_operands(kr, kv);
-    scores(kv, sa);
+    uint32_t ks = 0;
+    if constexpr (kQ8) ks = k_scale_q8(0);
+    scores(kv, sa, ks);
     if (kb >= plain_tiles) mask_max(sa, std::true_type{}, kb);
     else mask_max(sa, std::false_type{}, kb);
   }
+  lds_barrier();   // K slot 0 is free again
   if constexpr (!kQ8) {
-    lds_barrier();   // K slot 0 is free again
     issue(w1, kpool, s_kring + 2 * kSlotBytes);
     issue(w0, vpool, s_vring + 1 * kSlotBytes);
     issue(w2, kpool, s_kring + 3 * kSlotBytes);
@@ -1108,15 +1186,18 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     if (ii + 1 >= n_plain) return false;
     if constexpr (u == 0) refill();   // (u and ii agree mod 4)
     int ik = 0;
-    if constexpr (kQ8) turn_q8(ii, sets[(u + 1) % 2], std::false_type{});
+    uint32_t ks = 0;
+    if constexpr (kQ8) ks = turn_q8(ii, std::false_type{});
     else ik = own(ii + 5);
+    const uint8_t* sk = kr + ((u + 1) % kSlots) * kKSlotBytes;
+    const uint8_t* sv = vr + (kQ8 ? u & 1 : u) * kSlotBytes;
     // step ii reads buffer ii % 2 and fills the other (u and ii agree mod 4)
     if constexpr (u % 2 == 0)
-      step(kr + ((u + 1) % kSlots) * kSlotBytes, vr + u * kSlotBytes, 0, std::true_type{}, std::false_type{}, sa, sb);
+      step(sk, sv, 0, std::true_type{}, std::false_type{}, sa, sb, ks);
     else
-      step(kr + ((u + 1) % kSlots) * kSlotBytes, vr + u * kSlotBytes, 0, std::true_type{}, std::false_type{}, sb, sa);
+      step(sk, sv, 0, std::true_type{}, std::false_type{}, sb, sa, ks);
     rescale_o();
-    if constexpr (kQ8) lds_barrier();
+    if constexpr (kQ8) publish_q8();
     else advance(ii, u, ik, iv, std::false_type{});
     iv = ik;
     ++ii;
@@ -1131,16 +1212,13 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     const int sl1 = (sl + 1) & (kSlots - 1);
     refill();
     int ik = 0;
-    if constexpr (kQ8) {
-      if (ii & 1) turn_q8(ii, sets[0], std::true_type{});
-      else turn_q8(ii, sets[1], std::true_type{});
-    } else {
-      ik = own(ii + 5);
-    }
-    step(kr + sl1 * kSlotBytes, vr + sl * kSlotBytes, kb + ii + 1, std::true_type{}, std::true_type{}, sa, sb);
+    uint32_t ks = 0;
+    if constexpr (kQ8) ks = turn_q8(ii, std::true_type{});
+    else ik = own(ii + 5);
+    step(kr + sl1 * kKSlotBytes, vr + (kQ8 ? sl & 1 : sl) * kSlotBytes, kb + ii + 1, std::true_type{}, std::true_type{}, sa, sb, ks);
     sa = sb;
     rescale_o();
-    if constexpr (kQ8) lds_barrier();
+    if constexpr (kQ8) publish_q8();
     else advance(ii, sl, ik, iv, std::true_type{});
     iv = ik;
   }
@@ -1148,16 +1226,36 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   if (ii < n_kt) {
     const int sl = ii & (kSlots - 1);
     if constexpr (kQ8) {
-      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb);
+      step(kr, vr + (sl & 1) * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u);
     } else {
       const int ik = own(ii + 5);
-      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb);
+      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u);
       advance(ii, sl, ik, iv, std::true_type{});
       iv = ik;
     }
     ++ii;
   }
   wait_vmem<0>();
+  if constexpr (kQ8) {
+    // Rows that see a key whose value is not a number (noted a barrier or more ago; rare).
+    if (*s_any_nan != 0) {
+      for (int t2 = max(guard0, kb); t2 < kb + n_kt; ++t2) {
+        for (int r = 0; r < kKeys; ++r) {
+          const int b = 2 * t2 + (r >> 4);
+          const int dirv = s_dir[at(b)];
+          const bool sees = dirv != 0 && b * kBlockSize + slot_of_offset(r & 15, dirv) <= qpos;
+          const v4u_t note = *reinterpret_cast<const v4u_t*>(s_nan + ((t2 - guard0) * kKeys + r) * 8);   // 128 bits, one a dim
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) {
+            const uint32_t bits = sees ? note[dt] >> (4 * half) : 0u;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              o[dt][j] = (bits >> (8 * (j >> 2) + (j & 3))) & 1u ? __uint_as_float(0x7fc00000u) : o[dt][j];
+          }
+        }
+      }
+    }
+  }
   const float l_run = pair_sum(l0 + l1);
   if (parts > 1) {
     // ---- A piece of a split unit: unnormalised rows plus their max and sum.

@@ -7,9 +7,16 @@ namespace pf {
 
 template <int G, bool kOff32, bool kRing>
 __global__ __launch_bounds__(kThreads, 2) void prefill_q8_kernel(PrefillArgs a, const uint8_t* scales) {
-  BROS_PREFILL_UNIT_LDS
+  __shared__ __attribute__((aligned(1024))) uint8_t s_kring[kSlots * kQ8TileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_raw[kSlots * kQ8TileBytes];   // V as it is in the pool
+  __shared__ __attribute__((aligned(1024))) uint8_t s_vring[2 * kTileBytes];
+  __shared__ __attribute__((aligned(256))) uint32_t s_scale[kSlots * kThreads];      // per slot and wave
+  __shared__ __attribute__((aligned(16))) uint16_t s_nan[kGuardKeys * 8];   // per key and 16 dims: values that are not numbers
+  __shared__ int s_tbl[kMaxTableLds + kTablePad];
+  __shared__ int8_t s_dir[kMaxTableLds + kTablePad];
+  __shared__ int s_first_bad, s_any_nan;
   prefill_unit<G, kOff32, kRing, true>(a, paired_id(a, blockIdx.x, gridDim.x), s_kring, s_vring, &s_first_bad, s_tbl, s_dir,
-                                       scales);
+                                       scales, s_nan, &s_any_nan, s_raw, s_scale);
 }
 
 template <int G>
