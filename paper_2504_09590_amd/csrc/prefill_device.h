@@ -830,11 +830,19 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   const int guard0 = full_below / kKeys;   // tiles from here on are not seen by every row
   // V of tile j to the V ring (two slots); FIX: rows that are not context become zeros, and
   // values that are not numbers, in tiles from guard0 on, zeros and notes.
-  auto put_v_q8 = [&](int j, auto fixc) __attribute__((always_inline)) {
+  struct RawV {
+    v4u_t codes;
+    uint32_t scale;
+  };
+  auto raw_v_q8 = [&](int j) __attribute__((always_inline)) -> RawV {
+    return RawV{*reinterpret_cast<const v4u_t*>(s_raw + (j & 3) * kKSlotBytes + (8 * rg + q8_row) * kHeadDim + 16 * q8_c),
+                scale_q8(j, 2 * kBlockSize * my_bt + kBlockSize + my_slot0 + q8_row)};
+  };
+  auto put_v_q8 = [&](int j, RawV raw, auto fixc) __attribute__((always_inline)) {
     uint8_t* ring = s_vring + (j & 1) * kSlotBytes;
     const int row = 8 * rg + q8_row;   // tile row
-    v4u_t codes = *reinterpret_cast<const v4u_t*>(s_raw + (j & 3) * kKSlotBytes + row * kHeadDim + 16 * q8_c);
-    uint32_t scale = scale_q8(j, 2 * kBlockSize * my_bt + kBlockSize + my_slot0 + q8_row);
+    v4u_t codes = raw.codes;
+    uint32_t scale = raw.scale;
     bool keep = true;
     if constexpr (decltype(fixc)::value) {
       const int b = 2 * (kb + j) + my_bt;
@@ -871,11 +879,9 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
       *reinterpret_cast<v4u_t*>(ring + row * kRowBytes + (((2 * q8_c + h) ^ swz(row)) << 4)) = w;
     }
   };
-  // At the start of step ii: V of tile ii + 1 goes to the V ring (its slot was last read in step
-  // ii - 1), and tile ii + 4 is requested into the slots of tile ii, whose K and scales step
-  // ii - 1 read last: three loads a step. Gives the lane's K scale of tile ii + 1.
-  auto turn_q8 = [&](int ii, auto fixc) __attribute__((always_inline)) -> uint32_t {
-    put_v_q8(ii + 1, fixc);
+  // At the start of step ii: tile ii + 4 is requested into the slots of tile ii, whose K, raw V
+  // and scales step ii - 1 read last: three loads a step. Gives the lane's K scale of tile ii + 1.
+  auto turn_q8 = [&](int ii) __attribute__((always_inline)) -> uint32_t {
     const uint32_t ks = k_scale_q8(ii + 1);
     issue_q8(own(ii + 4), sidx_q8(ii + 4), ii & 3);
     return ks;
@@ -1035,14 +1041,20 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   // wave on the SIMD fills the gaps.
   // `in` holds the current tile's scores, `out` receives the next tile's.
   auto step = [&](const uint8_t* sk, const uint8_t* sv, int next_tile, auto has_next, auto mask_next,
-                  const floatx16& in, floatx16& out, uint32_t ks) __attribute__((always_inline)) {
+                  const floatx16& in, floatx16& out, uint32_t ks, int ii) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(has_next)::value;
     v4u_t kv[8];
     v4u_t vv0[4], vv1[4];
+    [[maybe_unused]] RawV raw;
+    if constexpr (kQ8 && NEXT) raw = raw_v_q8(ii + 1);
     if constexpr (NEXT) k_operands(sk, kv);
     v_operands(sv, 0, vv0);
     bf16x8_t pf[2];
     if constexpr (NEXT) scores(kv, out, ks);
+    // 8-bit: V of the next tile to the V ring (its slot was last read in step ii - 1), beside
+    // the score products (a workgroup alone takes 0.57 us a step; 0.64 with this at the end, before
+    // the barrier; the 16-bit prefill 0.47)
+    if constexpr (kQ8 && NEXT) put_v_q8(ii + 1, raw, mask_next);
     probs(pf, in);
     v_operands(sv, 1, vv1);
     pv(vv0, pf, 0);
@@ -1129,7 +1141,7 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   if constexpr (kQ8) {
     split_q();
     wait_vmem<0>();   // tiles 0 .. 3 of this wave's rows
-    put_v_q8(0, std::true_type{});
+    put_v_q8(0, raw_v_q8(0), std::true_type{});
   } else {
     // Everything so far, Q included: a wait the compiler sees, so it knows the
     // Q registers are ready and adds no wait of its own later.
@@ -1187,15 +1199,15 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     if constexpr (u == 0) refill();   // (u and ii agree mod 4)
     int ik = 0;
     uint32_t ks = 0;
-    if constexpr (kQ8) ks = turn_q8(ii, std::false_type{});
+    if constexpr (kQ8) ks = turn_q8(ii);
     else ik = own(ii + 5);
     const uint8_t* sk = kr + ((u + 1) % kSlots) * kKSlotBytes;
     const uint8_t* sv = vr + (kQ8 ? u & 1 : u) * kSlotBytes;
     // step ii reads buffer ii % 2 and fills the other (u and ii agree mod 4)
     if constexpr (u % 2 == 0)
-      step(sk, sv, 0, std::true_type{}, std::false_type{}, sa, sb, ks);
+      step(sk, sv, 0, std::true_type{}, std::false_type{}, sa, sb, ks, ii);
     else
-      step(sk, sv, 0, std::true_type{}, std::false_type{}, sb, sa, ks);
+      step(sk, sv, 0, std::true_type{}, std::false_type{}, sb, sa, ks, ii);
     rescale_o();
     if constexpr (kQ8) publish_q8();
     else advance(ii, u, ik, iv, std::false_type{});
@@ -1213,9 +1225,9 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     refill();
     int ik = 0;
     uint32_t ks = 0;
-    if constexpr (kQ8) ks = turn_q8(ii, std::true_type{});
+    if constexpr (kQ8) ks = turn_q8(ii);
     else ik = own(ii + 5);
-    step(kr + sl1 * kKSlotBytes, vr + (kQ8 ? sl & 1 : sl) * kSlotBytes, kb + ii + 1, std::true_type{}, std::true_type{}, sa, sb, ks);
+    step(kr + sl1 * kKSlotBytes, vr + (kQ8 ? sl & 1 : sl) * kSlotBytes, kb + ii + 1, std::true_type{}, std::true_type{}, sa, sb, ks, ii);
     sa = sb;
     rescale_o();
     if constexpr (kQ8) publish_q8();
@@ -1226,10 +1238,10 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   if (ii < n_kt) {
     const int sl = ii & (kSlots - 1);
     if constexpr (kQ8) {
-      step(kr, vr + (sl & 1) * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u);
+      step(kr, vr + (sl & 1) * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u, ii);
     } else {
       const int ik = own(ii + 5);
-      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u);
+      step(kr, vr + sl * kSlotBytes, 0, std::false_type{}, std::false_type{}, sa, sb, 0u, ii);
       advance(ii, sl, ik, iv, std::true_type{});
       iv = ik;
     }
