@@ -29,6 +29,9 @@ slots are early positions of decode sequences, which no write of the step
 touches, and the restore puts back the bytes they hold, so the step's outputs
 do not change; the step then waits for the copies, so its time is about
 max(t_exec, t_swap).
+
+QkvStep is the step one operator earlier: it takes the projection's rows, and
+the append's norms, rotation and writes stand in place of bros_kv_write.
 """
 
 from __future__ import annotations
@@ -207,3 +210,63 @@ class MixedStep:
             self._ev_leave.record(main)
             cur.wait_event(self._ev_leave)
         return self.out_prefill, self.out_decode
+
+
+class QkvStep:
+    """One step from the projection's rows: append, then the attention of both halves.
+
+    batch and dev are those of MixedStep (its tensors of q and of new k and v rows are not
+    used); sequences [0, P) are prefill chunks and [P, S) decode rows of one token each.
+    The pools of dev are 16- or 32-bit ones, or with kv_scales an 8-bit cache (bf16
+    rows). rope and norm are bros.Rope and bros.QkNorm or None, kept for every run.
+
+    Order of one run:  bros_qkv_append (norms, rotation, k and v to their slots, q kept)
+                       -> bros_attn_prefill_chunk (rows of sequences [0, P))
+                       -> bros_attn_decode (sequences [P, S))
+    or the _q8 calls of the same names, all on the current stream.
+    """
+
+    def __init__(self, batch, dev: bros.DeviceBatch, rope=None, norm=None, kv_scales=None):
+        P, S = batch.num_prefill, batch.num_seqs
+        self.rows_prefill = int(batch.cu_new[P])
+        if int(batch.cu_new[-1]) - self.rows_prefill != S - P or (np.diff(batch.cu_new[P:]) != 1).any():
+            raise ValueError("every sequence behind the prefill chunks must have one new token")
+        if not np.array_equal(batch.cu_q, batch.cu_new[:P + 1]):
+            raise ValueError("the prefill rows must be the chunks' new tokens")
+        self.batch, self.dev, self.rope, self.norm, self.kv_scales = batch, dev, rope, norm, kv_scales
+        self.P, self.S = P, S
+        hq, d = batch.num_q_heads, batch.head_dim
+        dtype = torch.float32 if batch.dtype == "f32" else torch.bfloat16
+        code = bros.BROS_F32 if batch.dtype == "f32" else bros.BROS_BF16
+        self.max_ctx_pre = int(batch.ctx_lens[:P].max()) if P else 0
+        self.max_ctx_dec = int(batch.ctx_lens[P:].max()) if S > P else 0
+        self.max_q_len = int(np.diff(batch.cu_q).max()) if P else 0
+        device = dev.k_pool.device
+        # q rows as the append leaves them, and the outputs: prefill rows, then decode rows
+        self.q = torch.empty((int(batch.cu_new[-1]), hq, d), dtype=dtype, device=device)
+        self.out = torch.empty_like(self.q)
+        ws_dec = bros.bros_attn_workspace_size(bros.BROS_WS_DECODE, code, S - P, hq, d, self.max_ctx_dec)
+        ws_pre = bros.bros_attn_workspace_size(bros.BROS_WS_PREFILL, code, self.rows_prefill, hq, d, self.max_ctx_pre)
+        size = max(ws_dec, ws_pre)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+    def run(self, q, k, v, rope_pos=None):
+        """q, k, v: the new tokens' rows [Tn][heads][D], contiguous within a token. Enqueues
+        the step on the current stream; returns (prefill output, decode output), which the
+        next run overwrites. Runs of one step must not overlap in time."""
+        d, P, n = self.dev, self.P, self.rows_prefill
+        pools = (d.k_pool, d.v_pool) if self.kv_scales is None else (d.k_pool, d.v_pool, self.kv_scales)
+        eight = self.kv_scales is not None
+        append = bros.bros_qkv_append_q8 if eight else bros.bros_qkv_append
+        append(self.q, q, k, v, *pools, d.block_tables, d.dir, d.cls, d.pos0, d.cu_new, rope=self.rope, rope_pos=rope_pos,
+               norm=self.norm)
+        pre, dec = self.out[:n], self.out[n:]
+        if P:
+            prefill = bros.bros_attn_prefill_chunk_q8 if eight else bros.bros_attn_prefill_chunk
+            prefill(pre, self.q[:n], d.cu_q, self.max_q_len, *pools, d.block_tables[:P], d.dir[:P], d.cls[:P],
+                    d.ctx_lens[:P], self.max_ctx_pre, workspace=self.workspace)
+        if self.S > P:
+            decode = bros.bros_attn_decode_q8 if eight else bros.bros_attn_decode
+            decode(dec, self.q[n:], *pools, d.block_tables[P:], d.dir[P:], d.cls[P:], d.ctx_lens[P:], self.max_ctx_dec,
+                   workspace=self.workspace)
+        return pre, dec

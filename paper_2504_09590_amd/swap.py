@@ -182,56 +182,50 @@ class PlanExecutor:
     gathered and copied to pinned host memory, relocated entries are moved
     (gather into staging, scatter to their new slots), and checkpointed rows
     come back (host to staging, scatter). The step's kv_write follows. Rows
-    are kept on the host per (request, position) until restored."""
+    are kept on the host per (request, position) until restored. With kv_scales
+    the pools are an 8-bit cache, and a row's scale bytes go with its codes."""
 
-    def __init__(self, k_pool, v_pool, max_rows: int):
-        import torch
+    def __init__(self, k_pool, v_pool, max_rows: int, kv_scales=None):
         hkv, d = k_pool.shape[1], k_pool.shape[3]
-        self.k_pool, self.v_pool = k_pool, v_pool
+        self.pools = (k_pool, v_pool) if kv_scales is None else (k_pool, v_pool, kv_scales)
+        self._gather = bros.bros_kv_gather if kv_scales is None else bros.bros_kv_gather_q8
+        self._scatter = bros.bros_kv_scatter if kv_scales is None else bros.bros_kv_scatter_q8
         self.max_rows = int(max_rows)
-        shape = (self.max_rows, hkv, d)
-        self.sk = torch.empty(shape, dtype=k_pool.dtype, device=k_pool.device)
-        self.sv = torch.empty(shape, dtype=k_pool.dtype, device=k_pool.device)
-        self.hk = torch.empty(shape, dtype=k_pool.dtype, pin_memory=True)
-        self.hv = torch.empty(shape, dtype=k_pool.dtype, pin_memory=True)
-        self.store = {}        # (request, position) -> (K row, V row) on the host
-        self._row = self.sk[0].numel() * self.sk.element_size()
+        # staging on the device and in pinned host memory: K rows, V rows and, in 8 bits, scales
+        shapes = [(self.max_rows, hkv, d)] * 2 + ([] if kv_scales is None else [(self.max_rows, hkv, 2)])
+        self.staging = [torch.empty(s, dtype=p.dtype, device=p.device) for s, p in zip(shapes, self.pools)]
+        self.host = [torch.empty(s, dtype=p.dtype, pin_memory=True) for s, p in zip(shapes, self.pools)]
+        self.store = {}        # (request, position) -> the row of each staging buffer, on the host
 
     def _ids(self, ids):
-        import torch
-        return torch.from_numpy(np.ascontiguousarray(ids, dtype=np.int32)).to(self.k_pool.device)
+        return torch.from_numpy(np.ascontiguousarray(ids, dtype=np.int32)).to(self.pools[0].device)
+
+    def _copy(self, dst, src, n: int, stream) -> None:
+        for a, b in zip(dst, src):
+            bros.bros_copy_dma(a, b, n * b[0].numel() * b.element_size(), stream=stream)
 
     def execute(self, req: int, plan, stream=None) -> None:
-        import torch
         stream = stream if stream is not None else torch.cuda.current_stream()
         for lo in range(0, len(plan.victims), self.max_rows):
             part = plan.victims[lo:lo + self.max_rows]
             n = len(part)
-            ids = self._ids(part[:, 2] * 16 + part[:, 3])
-            bros.bros_kv_gather(self.k_pool, self.v_pool, ids, self.sk, self.sv, num_slots=n, stream=stream)
-            bros.bros_copy_dma(self.hk, self.sk, n * self._row, stream=stream)
-            bros.bros_copy_dma(self.hv, self.sv, n * self._row, stream=stream)
+            self._gather(*self.pools, self._ids(part[:, 2] * 16 + part[:, 3]), *self.staging, num_slots=n, stream=stream)
+            self._copy(self.host, self.staging, n, stream)
             stream.synchronize()
             for i, (r, p, _, _) in enumerate(part):
-                self.store[(int(r), int(p))] = (self.hk[i].clone(), self.hv[i].clone())
+                self.store[(int(r), int(p))] = tuple(h[i].clone() for h in self.host)
         for lo in range(0, len(plan.move_src), self.max_rows):
             src, dst = plan.move_src[lo:lo + self.max_rows], plan.move_dst[lo:lo + self.max_rows]
-            bros.bros_kv_gather(self.k_pool, self.v_pool, self._ids(src), self.sk, self.sv, num_slots=len(src),
-                                stream=stream)
-            bros.bros_kv_scatter(self.sk, self.sv, self._ids(dst), self.k_pool, self.v_pool, num_slots=len(dst),
-                                 stream=stream)
+            self._gather(*self.pools, self._ids(src), *self.staging, num_slots=len(src), stream=stream)
+            self._scatter(*self.staging, self._ids(dst), *self.pools, num_slots=len(dst), stream=stream)
         for lo in range(0, len(plan.restore_pos), self.max_rows):
             pos, dst = plan.restore_pos[lo:lo + self.max_rows], plan.restore_dst[lo:lo + self.max_rows]
             stream.synchronize()                      # the host rows are reused below
             for i, p in enumerate(pos):
-                k, v = self.store.pop((int(req), int(p)))
-                self.hk[i].copy_(k)
-                self.hv[i].copy_(v)
-            n = len(pos)
-            bros.bros_copy_dma(self.sk, self.hk, n * self._row, stream=stream)
-            bros.bros_copy_dma(self.sv, self.hv, n * self._row, stream=stream)
-            bros.bros_kv_scatter(self.sk, self.sv, self._ids(dst), self.k_pool, self.v_pool, num_slots=n,
-                                 stream=stream)
+                for h, row in zip(self.host, self.store.pop((int(req), int(p)))):
+                    h[i].copy_(row)
+            self._copy(self.staging, self.host, len(pos), stream)
+            self._scatter(*self.staging, self._ids(dst), *self.pools, num_slots=len(pos), stream=stream)
 
     def drop(self, req: int) -> None:
         for key in [k for k in self.store if k[0] == req]:

@@ -51,11 +51,12 @@ def poison(q8, mask):
     return q8
 
 
-def check(got_bits, want, q, batch, seq_of_row, w, what, kmax=None, vmax=None):
-    """got [rows][Hq][D] bf16 bits against fp64 `want`; q as stored, seq_of_row: each row's sequence."""
-    got = oracle.widen(got_bits, "bf16")
+def check(got_bits, want, q, batch, seq_of_row, w, what, kmax=None, vmax=None, dtype="bf16"):
+    """got [rows][Hq][D] as stored against fp64 `want`; q as stored, seq_of_row: each row's sequence.
+    dtype "f32": the same tolerance with a rounding of 2^-24 at the end."""
+    got = oracle.widen(got_bits, dtype)
     assert np.isfinite(got).all(), f"{what}: not finite"
-    qn = np.linalg.norm(oracle.widen(q, "bf16"), axis=-1)                     # [rows][Hq]
+    qn = np.linalg.norm(oracle.widen(q, dtype), axis=-1)                      # [rows][Hq]
     hq, hkv = qn.shape[1], batch.num_kv_heads
     if kmax is None:
         kmax, vmax = np.zeros((batch.num_seqs, hkv)), np.zeros((batch.num_seqs, hkv))
@@ -63,12 +64,12 @@ def check(got_bits, want, q, batch, seq_of_row, w, what, kmax=None, vmax=None):
             n = min(int(batch.ctx_lens[s]), batch.block_tables.shape[1] * 16)
             tab = np.where((batch.block_tables >= 0) & (batch.block_tables < batch.num_blocks), batch.block_tables, 0)
             if n > 0:
-                kmax[s] = np.linalg.norm(oracle.widen(oracle.gather_kv(batch.k_pool, tab, batch.dir, s, n), "bf16"), axis=-1).max(0)
-                vmax[s] = np.abs(oracle.widen(oracle.gather_kv(batch.v_pool, tab, batch.dir, s, n), "bf16")).max((0, 2))
+                kmax[s] = np.linalg.norm(oracle.widen(oracle.gather_kv(batch.k_pool, tab, batch.dir, s, n), dtype), axis=-1).max(0)
+                vmax[s] = np.abs(oracle.widen(oracle.gather_kv(batch.v_pool, tab, batch.dir, s, n), dtype)).max((0, 2))
     group = np.arange(hq) // (hq // hkv)
     k_row, v_row = kmax[seq_of_row][:, group], vmax[seq_of_row][:, group]
     n = np.maximum(batch.ctx_lens[seq_of_row], 0)[:, None]
     d = 132 * 2.0 ** -24 * qn * k_row / np.sqrt(batch.head_dim)
-    tol = 2.0 ** -8 * np.abs(want) + (v_row * (2 * d + w + 2.0 ** -20 + n * 2.0 ** -27))[..., None]
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + (v_row * (2 * d + w + 2.0 ** -20 + n * 2.0 ** -27))[..., None]
     bad = ~(np.abs(got - want) <= tol)
     assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.abs(got - want)[bad].max():.3g}"
