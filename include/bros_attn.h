@@ -168,8 +168,8 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  * token without a valid table entry gets its q rows and is not stored.
  *
  * Errors as bros_kv_write; also BROS_E_SHAPE for a stride below a token's rows or
- * one that is not a multiple of 16 bytes, q without q_out, more than 2^31 - 1 head
- * rows, a rotary_dim outside 16 .. head_dim or not a multiple of 16, axes outside
+ * one that is not a multiple of 16 bytes, q without q_out, more than 2^29 - 32
+ * head rows, a rotary_dim outside 16 .. head_dim or not a multiple of 16, axes outside
  * 1 .. 4, axes without rope_pos, or sections that do not add up to rotary_dim / 2.
  */
 enum bros_rope_pairs { BROS_ROPE_HALF = 0,       /* pair i: dims i and i + rotary_dim / 2 */

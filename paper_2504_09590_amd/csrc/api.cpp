@@ -106,8 +106,8 @@ int qkv_append(const char* fn, bool eight, void* q_out, const void* q, const voi
   if ((q == nullptr) != (q_out == nullptr)) return fail(BROS_E_NULL, "%s: give both q and q_out, or neither", fn);
   if (q != nullptr && num_q_heads == 0) return fail(BROS_E_SHAPE, "%s: q rows but num_q_heads is 0", fn);
   const int32_t hq = q == nullptr ? 0 : num_q_heads;
-  if ((int64_t)num_new_tokens * (hq + 2 * (int64_t)num_kv_heads) > 0x7fffffffLL)
-    return fail(BROS_E_SHAPE, "%s: more than 2^31 - 1 head rows", fn);
+  if ((int64_t)num_new_tokens * (hq + 2 * (int64_t)num_kv_heads) > (1LL << 29) - 32)
+    return fail(BROS_E_SHAPE, "%s: more than 2^29 - 32 head rows", fn);   // (a launch's threads must stay below 2^32)
   if (num_new_tokens == 0) return ok();
   if (num_seqs == 0) return fail(BROS_E_SHAPE, "%s: %d new tokens but no sequences", fn, num_new_tokens);
   if (!k || !v || !k_pool || !v_pool || !pos0 || !cu_new || (eight && !kv_scales))

@@ -290,7 +290,7 @@ int stream_compute_units(hipStream_t stream) {
 
 int workgroups_per_cu(const void* kernel, int threads, int slot) {
   constexpr int kMaxDevices = 64;
-  constexpr int kSlots = 12;
+  constexpr int kSlots = 20;
   static int per_cu_cache[kMaxDevices][kSlots];
   static std::mutex mu;
   int dev = 0;

@@ -368,8 +368,8 @@ hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot)
   const int64_t slots = (int64_t)a.num_rows * a.num_q_heads + (int64_t)kDecodeGroupSlots * std::min(a.num_q_heads, 8);
   const int cus = stream_compute_units(stream);
   if (!plan_q8_decode(segments, G, blocks, cus, slots, &a.split_blocks, &a.n_split_max)) {
-    if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot, cus);
-    if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot, cus);
+    if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot + 2, cus);
+    if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot + 1, cus);
     return launch_even<G, 1>(a, pool, stream, slot, cus);
   }
   for (int64_t s0 = 0; s0 < segments; s0 += kMaxSegmentsPerLaunch) {
@@ -386,9 +386,9 @@ hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot)
 hipError_t launch_decode_q8(DecodeArgs a, Q8Pool pool, int group, hipStream_t stream) {
   switch (group) {
     case 1: return dq::launch_group<1>(a, pool, stream, 8);
-    case 2: return dq::launch_group<2>(a, pool, stream, 9);
-    case 4: return dq::launch_group<4>(a, pool, stream, 10);
-    case 8: return dq::launch_group<8>(a, pool, stream, 11);
+    case 2: return dq::launch_group<2>(a, pool, stream, 11);
+    case 4: return dq::launch_group<4>(a, pool, stream, 14);
+    case 8: return dq::launch_group<8>(a, pool, stream, 17);
     default: return hipErrorInvalidValue;
   }
 }

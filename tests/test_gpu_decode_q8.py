@@ -90,6 +90,16 @@ def test_many_rows(rows, lo, hi, hq, hkv):
     check(q8, run(q8), f"{rows} rows")
 
 
+def test_more_rows_than_the_prefix_holds():
+    rng = np.random.default_rng(12)
+    ctx = rng.integers(1, 40, 5001)
+    ctx[[7, 2500, 5000]] = 6000, 4100, 900
+    b = W.custom(ctx, (rng.random(5001) < 0.5).astype(np.uint8), 4, 1, seed=12, spare_blocks=5)
+    q8 = Q.poison(Q.held(b, 12), owned_mask(b))
+    announce("decode_q8 5001 rows, three of them long")
+    check(q8, run(q8), "5001 rows")
+
+
 def test_one_long_context_among_short_ones():
     ctx = [50] * 40 + [60000] + [17] * 23
     b = W.custom(ctx, [W.BE] * 64, 8, 2, seed=11, share_tails=False)

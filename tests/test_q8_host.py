@@ -46,7 +46,7 @@ NULL, SHAPE, DTYPE, UNSUPPORTED = -1, -2, -3, -4
     (dict(pos0=None), NULL), (dict(cu=None), NULL), (dict(nb=0), SHAPE), (dict(maxb=0), SHAPE), (dict(dpe=2), SHAPE),
     (dict(qs=1023), SHAPE), (dict(qs=1028), SHAPE), (dict(ks=255), SHAPE), (dict(ks=0), SHAPE), (dict(vs=-256), SHAPE),
     (dict(vs=2 ** 62), SHAPE), (dict(q=FAKE + 4), SHAPE), (dict(q_out=FAKE + 8), SHAPE), (dict(kp=FAKE + 2), SHAPE),
-    (dict(tn=2 ** 31 - 1), SHAPE),
+    (dict(tn=2 ** 31 - 1), SHAPE), (dict(tn=(2 ** 29 - 32) // 12 + 1), SHAPE),   # 12 head rows a token
     (dict(rope=rope(dim=0)), SHAPE), (dict(rope=rope(dim=144)), SHAPE), (dict(rope=rope(dim=24)), SHAPE),
     (dict(rope=rope(pairs=2)), SHAPE), (dict(rope=rope(axes=0)), SHAPE), (dict(rope=rope(axes=5)), SHAPE),
     (dict(rope=rope(rows=0)), SHAPE), (dict(rope=rope(table=None)), NULL), (dict(rope=rope(table=FAKE + 4)), SHAPE),
