@@ -200,6 +200,7 @@ class Rope:
         if len(sections) > 4:
             raise ValueError(f"{len(sections)} sections; at most 4")
         self.table = table
+        self.device = table.get_device()
         self.axes = max(len(sections), 1)
         self._c = _Rope(_ptr(table), int(table.shape[0]), int(table.shape[1]), int(pairs), self.axes,
                         (ctypes.c_int32 * 4)(*sections))
@@ -213,8 +214,10 @@ class QkNorm:
 
     def __init__(self, q_weight, k_weight, eps: float = 1e-6):
         self.weights = [w for w in (q_weight, k_weight) if w is not None]
-        if any(w.dim() != 1 or w.dtype != self.weights[0].dtype for w in self.weights):
-            raise ValueError("weights must be vectors of one type")
+        kinds = {(w.dtype, w.size(0), w.get_device()) for w in self.weights if w.dim() == 1}
+        if len(kinds) > 1 or any(w.dim() != 1 for w in self.weights):
+            raise ValueError("weights must be vectors of one type and length, on one device")
+        self.kind = kinds.pop() if kinds else None
         self._c = _QkNorm(_ptr(q_weight), _ptr(k_weight), float(eps))
         self.ref = ctypes.byref(self._c)
 
@@ -222,27 +225,28 @@ class QkNorm:
 _I32, _I8, _U8 = torch.int32, torch.int8, torch.uint8
 
 
+def _refuse(t, device: int):
+    if t.get_device() == device and not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    raise ValueError(f"a tensor is on {t.device}, not on the current device")
+
+
 def _addresses(*tensors, strided=()):
     """Addresses of contiguous tensors (None: None), all on the current device, where the
-    kernel runs, like the `strided` ones."""
-    first = None
+    kernel runs, like the `strided` ones. (This runs before every call: a tenth of a
+    microsecond a tensor counts where the kernel takes five.)"""
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
     out = []
     for t in tensors:
         if t is None:
             out.append(None)
-            continue
-        at = t.get_device()   # (-1: host memory)
-        if at < 0 or (at != first and first is not None):
-            raise ValueError(f"a tensor is on {t.device}, not on the current device")
-        if not t.is_contiguous():
-            raise ValueError("tensor must be contiguous")
-        first = at
-        out.append(t.data_ptr())
+        elif t.get_device() == device and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            _refuse(t, device)
     for t in strided:
-        if t is not None and t.get_device() != first:
-            raise ValueError(f"a tensor is on {t.device}, not on the current device")
-    if first != torch._C._cuda_getDevice():
-        raise ValueError(f"the tensors are on cuda:{first}, not on the current device")
+        if t is not None and t.get_device() != device:
+            _refuse(t, device)
     return out
 
 
@@ -289,25 +293,24 @@ def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rop
         qp, qs, hq = _token_rows(q, "q", tn, d, dtype)
         if q_out.shape != q.shape or q_out.dtype is not dtype:
             raise ValueError("q_out must have q's shape and type")
-    more = ()
+    device = k.get_device()
     if norm is not None:
-        if any(w.dtype is not dtype or w.size(0) != d for w in norm.weights):
-            raise ValueError(f"norm weights must be [{d}] {dtype}")
-        more = norm.weights
+        if norm.kind is not None and norm.kind != (dtype, d, device):
+            raise ValueError(f"norm weights must be [{d}] {dtype}, on the rows' device")
         norm = norm.ref
     if rope_pos is not None:
         if rope is None:
             raise ValueError("rope_pos without a rotation")
-        if rope_pos.dtype is not _I32 or rope_pos.numel() != rope.axes * tn:
+        if rope_pos.dtype is not _I32 or rope_pos.size(-1) != tn or rope_pos.numel() != rope.axes * tn:
             raise ValueError(f"rope_pos must be int32 [{rope.axes}][{tn}]")
     S = cu_new.size(0) - 1
     per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
-    table = None
     if rope is not None:
-        table, rope = rope.table, rope.ref
-    op, bt, dr, cl, p0, cu, rp, *at = _addresses(q_out, block_tables, dir, cls, pos0, cu_new, rope_pos, *pools, table, *more,
-                                                 strided=(q, k, v))
-    head = (op, qp, kp, vp, qs, ks, vs, tn, hq, norm, rope, rp, *at[:len(pools)])
+        if rope.device != device:
+            raise ValueError("the rotation's table must be on the rows' device")
+        rope = rope.ref
+    op, bt, dr, cl, p0, cu, rp, *at = _addresses(q_out, block_tables, dir, cls, pos0, cu_new, rope_pos, *pools, strided=(q, k, v))
+    head = (op, qp, kp, vp, qs, ks, vs, tn, hq, norm, rope, rp, *at)
     tail = (nb, bt, block_tables.size(1), dr, cl, per_entry, p0, cu, S, hkv, d, bs, _dtype_code(k))
     return head, tail
 
@@ -388,16 +391,19 @@ def _move(pools, slot_ids, num_slots, rows, scales=None, one_byte=True):
         raise ValueError(f"slot_ids must be int32 and hold {n} ids")
     for t in rows:
         shape = t.shape
-        if shape[0] < n or shape[1:] != (hkv, d) or (one_byte and t.element_size() != 1):
+        if len(shape) != 3 or shape[0] < n or shape[1] != hkv or shape[2] != d or (one_byte and t.element_size() != 1):
             raise ValueError(f"a dense buffer must hold [{n}][{hkv}][{d}]" + (" bytes" if one_byte else ""))
     if scales is not None:
         shape = scales.shape
-        if shape[0] < n or shape[1:] != (hkv, 2) or scales.element_size() != 1:
+        if len(shape) != 3 or shape[0] < n or shape[1] != hkv or shape[2] != 2 or scales.element_size() != 1:
             raise ValueError(f"the scales must hold [{n}][{hkv}][2] bytes")
         rows = (*rows, scales)
-    host = [not t.is_cuda and t.is_pinned() for t in rows]
-    at = _addresses(*pools, slot_ids, *(None if h else t for t, h in zip(rows, host)))
-    dense = [_ptr(t) if h else a for t, h, a in zip(rows, host, at[4:])]
+    if all(t.is_cuda for t in rows):
+        at = _addresses(*pools, slot_ids, *rows)
+        dense = at[4:]
+    else:   # (some in pinned host memory)
+        at = _addresses(*pools, slot_ids, *(t for t in rows if t.is_cuda or not t.is_pinned()))
+        dense = [_ptr(t) for t in rows]
     return n, at[:3], at[3], dense, nb, (hkv, d, bs)
 
 

@@ -125,6 +125,7 @@ def py_call(**kw):
     (dict(pos0=torch.zeros(3, dtype=torch.int32)), "offset"),
     (dict(rope_pos=torch.zeros((1, 5), dtype=torch.int32)), "without a rotation"),
     (dict(rope=bros.Rope(torch.zeros((9, 128))), rope_pos=torch.zeros((2, 5), dtype=torch.int32)), "rope_pos"),
+    (dict(rope=bros.Rope(torch.zeros((9, 128)), sections=(16, 24, 24)), rope_pos=torch.zeros((5, 3), dtype=torch.int32)), "rope_pos"),
     (dict(norm=bros.QkNorm(torch.ones(64, dtype=torch.bfloat16), None)), "norm weights"),
     (dict(norm=bros.QkNorm(torch.ones(128), None)), "norm weights"),
 ])
