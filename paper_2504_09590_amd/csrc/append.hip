@@ -15,6 +15,12 @@
 // nothing (the rows themselves, the sequences' offsets, given positions) are
 // requested first; the cosines are requested as soon as the position is known,
 // beside the table entry.
+//
+// Device time, and bytes that must move by it: four prompts of 2000 rows (64 / 8 heads,
+// bf16, three position axes) 63.0 us, 4.9 TB/s, what a large copy reaches here; 2176 rows
+// (32 / 8 heads) 12.4 us, 4.4 TB/s; four rows 3.2 us. (The eight pairs of a lane's cosines
+// loaded one by one, each from its own axis, where most lanes' pairs have one: 106 us for the
+// four prompts.)
 #include "bros_kernels.h"
 #include "q8_device.h"
 

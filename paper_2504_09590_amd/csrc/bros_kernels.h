@@ -219,8 +219,8 @@ constexpr int32_t kPrefillWholeTableCtx = 32768;
 // count is queried once per device, the stream's CU mask read on every call.
 int stream_compute_units(hipStream_t stream);
 // Workgroups of `kernel` (launched with `threads` threads) that a compute unit
-// holds at once, queried once per device and cache slot (0..11: bf16 decode 0..3,
-// fp32 decode 4..7, 8-bit decode 8..11), and that those enabled for `stream` do.
+// holds at once, queried once per device and cache slot (0..19: bf16 decode 0..3,
+// fp32 decode 4..7, 8-bit decode 8..19), and that those enabled for `stream` do.
 int workgroups_per_cu(const void* kernel, int threads, int slot);
 int resident_workgroups(const void* kernel, int threads, int slot, hipStream_t stream);
 

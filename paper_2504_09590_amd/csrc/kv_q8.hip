@@ -9,6 +9,9 @@
 // whole ids of K (blockIdx.y = 0) or V, as many as one pass of its threads holds,
 // so that a chunk's place takes 32-bit arithmetic. The thread that moves a row's
 // first chunk moves its scale byte.
+//
+// Device time at 8 KV heads: 4096 slots out or in 5.1 us (17 MB each way, 3.3 TB/s: two
+// thirds of it start and end, 24 slots take 2.7 us); 12000 slots read as bf16 14.0 us.
 #include "bros_kernels.h"
 #include "q8_device.h"
 

@@ -212,6 +212,24 @@ def test_scale_and_large_scores():
         Q.check(got, ref, b.q_decode, grown, np.arange(2), WEIGHTS, f"scale={scale}", kmax * scale * np.sqrt(128), vmax)
 
 
+@pytest.mark.parametrize("rows", [3, 200])
+def test_a_query_that_is_not_finite_stays_alone(rows):
+    # infinite scores have no softmax (inf - inf), NaNs neither: NaN in their own heads, nothing elsewhere
+    rng = np.random.default_rng(rows)
+    b = W.custom(rng.integers(700, 900, rows), rng.integers(0, 2, rows).astype(np.uint8), 16, 4, seed=29)
+    q8 = Q.held(b, 29)
+    odd = dataclasses.replace(q8, batch=dataclasses.replace(q8.batch, q_decode=q8.batch.q_decode.copy()))
+    bad = [(0, 2, 0x7F80), (1, 15, 0x7FC0), (rows - 1, 0, 0xFF80)]        # +inf, NaN, -inf
+    for r, h, bits in bad:
+        odd.batch.q_decode[r, h, 17] = bits
+    announce(f"decode_q8 {rows} rows, queries that are not finite")
+    got, plain = run(odd), run(q8)
+    for r, h, _ in bad:
+        assert np.isnan(oracle.widen(got[r, h], "bf16")).all()
+        got[r, h] = plain[r, h]
+    check(q8, got, "the other rows")
+
+
 def test_repeatable_and_a_stream_share():
     torch = require_gpu()
     from paper_2504_09590_amd import bros

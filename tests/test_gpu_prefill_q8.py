@@ -155,6 +155,23 @@ def test_a_nan_reaches_only_rows_that_see_it():
         assert np.array_equal(nan, want)
 
 
+def test_a_query_that_is_not_finite_stays_alone():
+    # infinite scores have no softmax (inf - inf), NaNs neither: NaN in their own rows, nothing elsewhere
+    b = chunks([20, 0], [70, 40], 4, 2, seed=19, cls=[W.RT] * 2)
+    q8 = Q.held(b, 19)
+    odd = dataclasses.replace(q8, batch=dataclasses.replace(q8.batch, q_prefill=q8.batch.q_prefill.copy()))
+    rows = [(3, 2, 0x7F80), (69, 7, 0x7FC0), (70 + 39, 0, 0xFF80)]        # +inf, NaN, -inf
+    for r, h, bits in rows:
+        odd.batch.q_prefill[r, h, 17] = bits
+    announce("prefill_q8 queries that are not finite")
+    for ws in (True, False):
+        got, plain = run(odd, with_ws=ws), run(q8, with_ws=ws)
+        for r, h, _ in rows:
+            assert np.isnan(oracle.widen(got[r, h], "bf16")).all()
+            got[r, h] = plain[r, h]
+        check(q8, got, "the other rows")
+
+
 def test_on_a_share_and_captured():
     torch = require_gpu()
     from paper_2504_09590_amd import bros
