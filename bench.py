@@ -66,10 +66,10 @@ DECODE_SOURCES = ("paper_2504_09590_amd/csrc/decode.hip", "paper_2504_09590_amd/
                   "paper_2504_09590_amd/csrc/bros_kernels.h")
 DECODE_COUNTERS = {
     # workload: (sha256 of DECODE_SOURCES when the counters were read, FETCH_SIZE KiB, WRITE_SIZE KiB)
-    "llama3-70b-decode": ("3f0a6e6c9dc0d7b3338c2c29967d32070a5cf5719a666aa6f4a141e9b9f2f710", 4992080.9, 16515.1),
-    "llama3-8b-decode": ("3f0a6e6c9dc0d7b3338c2c29967d32070a5cf5719a666aa6f4a141e9b9f2f710", 454830.1, 5197.7),
-    "llama3-8b-mixed-step": ("3f0a6e6c9dc0d7b3338c2c29967d32070a5cf5719a666aa6f4a141e9b9f2f710", 1129323.4, 6173.3),
-    "llama3-8b-pressure": ("3f0a6e6c9dc0d7b3338c2c29967d32070a5cf5719a666aa6f4a141e9b9f2f710", 601660.5, 10116.1),
+    "llama3-70b-decode": ("96c84c64cd10d4b69cfab451cbc2ec2f803c9042431cf727b2fe349de88757c6", 4991904.6, 16515.0),
+    "llama3-8b-decode": ("96c84c64cd10d4b69cfab451cbc2ec2f803c9042431cf727b2fe349de88757c6", 454816.2, 5197.5),
+    "llama3-8b-mixed-step": ("96c84c64cd10d4b69cfab451cbc2ec2f803c9042431cf727b2fe349de88757c6", 1129290.9, 6173.3),
+    "llama3-8b-pressure": ("96c84c64cd10d4b69cfab451cbc2ec2f803c9042431cf727b2fe349de88757c6", 601655.2, 10115.4),
 }
 
 
