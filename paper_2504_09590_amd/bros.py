@@ -250,22 +250,23 @@ def _addresses(*tensors, strided=()):
     return out
 
 
-def _check_meta(rows: int, block_tables, dir, cls, *offsets) -> int:
-    """Checks types and lengths of `rows` sequences' metadata; gives the direction mode."""
-    if block_tables.dtype is not _I32 or block_tables.dim() != 2 or block_tables.size(0) != rows:
+def _check_meta(rows: int, block_tables, dir, cls, *offsets):
+    """Checks types and lengths of `rows` sequences' metadata; gives the table's width and the direction mode."""
+    shape = block_tables.shape
+    if block_tables.dtype is not _I32 or len(shape) != 2 or shape[0] != rows:
         raise ValueError(f"block_tables must be int32 [{rows}][max_blocks]")
     per_entry = 0
     if dir is not None:
-        if dir.dtype is not _I8 or dir.size(0) != rows:
-            raise ValueError(f"dir must be int8 with {rows} rows")
         if dir.dim() != 1:
             per_entry = _dir_mode(dir, block_tables)
+        if dir.dtype is not _I8 or (not per_entry and dir.numel() != rows):
+            raise ValueError(f"dir must be int8 with {rows} rows")
     if cls is not None and (cls.dtype is not _U8 or cls.numel() != rows):
         raise ValueError(f"cls must be uint8 [{rows}]")
     for t, n in offsets:
-        if t.dtype is not _I32 or t.dim() != 1 or t.size(0) != n:
+        if t.dtype is not _I32 or t.numel() != n:
             raise ValueError(f"an offset or length array must be int32 [{n}]")
-    return per_entry
+    return shape[1], per_entry
 
 
 def _token_rows(t, name: str, tokens: int, d: int, dtype):
@@ -281,7 +282,7 @@ def _token_rows(t, name: str, tokens: int, d: int, dtype):
 
 def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rope_pos, norm, pools):
     nb, hkv, bs, d = pools[0].shape
-    dtype, tn = k.dtype, k.size(0)
+    dtype, tn = k.dtype, k.shape[0]
     kp, ks, kh = _token_rows(k, "k", tn, d, dtype)
     vp, vs, vh = _token_rows(v, "v", tn, d, dtype)
     if kh != hkv or vh != hkv:
@@ -303,15 +304,15 @@ def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rop
             raise ValueError("rope_pos without a rotation")
         if rope_pos.dtype is not _I32 or rope_pos.size(-1) != tn or rope_pos.numel() != rope.axes * tn:
             raise ValueError(f"rope_pos must be int32 [{rope.axes}][{tn}]")
-    S = cu_new.size(0) - 1
-    per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
+    S = cu_new.numel() - 1
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
     if rope is not None:
         if rope.device != device:
             raise ValueError("the rotation's table must be on the rows' device")
         rope = rope.ref
     op, bt, dr, cl, p0, cu, rp, *at = _addresses(q_out, block_tables, dir, cls, pos0, cu_new, rope_pos, *pools, strided=(q, k, v))
     head = (op, qp, kp, vp, qs, ks, vs, tn, hq, norm, rope, rp, *at)
-    tail = (nb, bt, block_tables.size(1), dr, cl, per_entry, p0, cu, S, hkv, d, bs, _dtype_code(k))
+    tail = (nb, bt, width, dr, cl, per_entry, p0, cu, S, hkv, d, bs, _dtype_code(k))
     return head, tail
 
 
@@ -353,11 +354,11 @@ def _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx
     shape = q.shape
     if len(shape) != 3 or shape[2] != d or out.shape != shape or out.dtype is not q.dtype:
         raise ValueError(f"q and out must be [rows][Hq][{d}] of one type")
-    S = ctx_lens.size(0)
-    per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *offsets)
+    S = ctx_lens.numel()
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *offsets)
     op, qp, kp, vp, sp, bt, dr, cl, cx, ws, *more = _addresses(out, q, k_pool, v_pool, kv_scales, block_tables, dir, cls, ctx_lens,
                                                                workspace, *[t for t, _ in offsets])
-    pool = (kp, vp, sp, nb, bt, block_tables.size(1), dr, cl, per_entry, cx)
+    pool = (kp, vp, sp, nb, bt, width, dr, cl, per_entry, cx)
     return shape, S, (op, qp, *more), pool, (shape[1], hkv, d, bs), (ws, 0 if ws is None else workspace.nbytes)
 
 
@@ -376,7 +377,7 @@ def bros_attn_prefill_chunk_q8(out, q, cu_q, max_q_len: int, k_pool, v_pool, kv_
                                max_ctx: int, scale: float = 0.0, workspace=None, stream=None):
     """bros_attn_prefill_chunk over an 8-bit pool (bfloat16 q and out, the bf16 prefill's workspace)."""
     shape, S, rows, pool, heads, ws = _q8_attention(out, q, kv_scales, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
-                                                    workspace, (cu_q, ctx_lens.size(0) + 1))
+                                                    workspace, (cu_q, ctx_lens.numel() + 1))
     _check(LIB.bros_attn_prefill_chunk_q8(*rows, shape[0], int(max_q_len), *pool, int(max_ctx), S,
                                           *heads, scale, _dtype_code(q), *ws, _stream(stream)))
 
@@ -386,7 +387,7 @@ def _move(pools, slot_ids, num_slots, rows, scales=None, one_byte=True):
     [>= n][Hkv][2] scales, on the current device or in pinned host memory. Gives n and
     the addresses of pools, ids, rows and scales, then (blocks, heads, dims, block size)."""
     nb, hkv, bs, d = _eight_bit(*pools)
-    n = int(num_slots) if num_slots is not None else 0 if slot_ids is None else slot_ids.size(0)
+    n = int(num_slots) if num_slots is not None else 0 if slot_ids is None else slot_ids.numel()
     if n < 0 or (slot_ids is not None and (slot_ids.dtype is not _I32 or slot_ids.numel() < n)):
         raise ValueError(f"slot_ids must be int32 and hold {n} ids")
     for t in rows:

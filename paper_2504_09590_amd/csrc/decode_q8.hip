@@ -153,11 +153,91 @@ __device__ __forceinline__ void even_worker(const DecodeArgs& a, const Q8Pool& p
   }
 }
 
+// Folds pairs first, first + STRIDE, ... of blocks below b1 of a (row, KV head) segment into `run`.
+template <int G, int STRIDE>
+__device__ __forceinline__ void fold_pairs(const DecodeArgs& a, const Q8Pool& pool, int row, int g, int ctx, int first, int b1,
+                                           Running& run) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int grp = lane >> 4;
+  const int col = lane & 15;
+  const int nkv = a.num_kv_heads;
+  const int n = b1 > first ? (b1 - first + STRIDE - 1) / STRIDE : 0;
+  if (n == 0) return;
+  v4u_t qf[4];
+  KRegs k;
+  VRegs v;
+
+  // Pool tile of the x-th block of the wave's i-th pair: tile 0 of the head in place
+  // of an entry outside the pool or past the piece (masked whole), so that the loads
+  // need no branch. (The table is not read past the piece.)
+  auto entry = [&](int i, int x, bool& ok) -> size_t {
+    const int b = first + STRIDE * i + x;
+    const int e = load_uniform(a.block_tables, (size_t)row * a.max_blocks_per_seq + min(b, b1 - 1));
+    ok = b < b1 && e >= 0 && e < a.num_blocks;
+    return (size_t)(ok ? e : 0) * nkv + g;
+  };
+
+  bool ok[2];
+  size_t tile[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) tile[x] = entry(0, x, ok[x]);
+  issue_k(pool, tile[0], tile[1], grp, col, k);
+  load_q<G>(a.q, (size_t)row * a.num_q_heads + g * G, grp, col, qf);
+  issue_v(pool, tile[0], tile[1], grp, col, v);
+#pragma clang loop unroll(disable)
+  for (int i = 0; i < n; ++i) {
+    const int b = first + STRIDE * i;
+    bool next_ok[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) tile[x] = entry(i + 1, x, next_ok[x]);
+    float s[8];
+    const PairScales ps = pair_scales(v.scales);
+    pair_scores(k, qf, ps, a.scale_log2, s);
+    issue_k(pool, tile[0], tile[1], grp, col, k);   // the K registers are free
+    VRows rows = exchange(v, ps);
+    issue_v(pool, tile[0], tile[1], grp, col, v);   // and V's
+    if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > ctx) mask_pair(a, row, ctx, b, ok, grp, s, rows);
+    run.fold(s, rows, col < G);
+    ok[0] = next_ok[0];
+    ok[1] = next_ok[1];
+  }
+}
+
+__device__ __forceinline__ int row_context(const DecodeArgs& a, int row) {
+  return max(0, min(load_uniform(a.ctx_lens, row), min(a.max_ctx, a.max_blocks_per_seq * kBlockSize)));
+}
+
+// Many short contexts (plan.h: q8_decode_by_waves): a wave takes whole segments, x, x + W, ... of
+// W waves, four neighbours to a workgroup. Nothing to fold, no barrier, a quarter of the
+// workgroups: 512 rows of 10 to 100 tokens, 64 / 8 heads, 32.6 us with a workgroup per segment, 23.1
+// here; 128 of 6 to 60, 32 / 8 heads, 10.2 and 7.1. (A workgroup of four waves for every four
+// segments, none taking a second: 26.7 and 6.9. The next segment's loads requested before a
+// segment ends: 22.1 and 7.0, and slower from 200 tokens on.)
+constexpr int kWavesPerSimd = 3;
+template <int G>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void decode_q8_wave_kernel(DecodeArgs a, Q8Pool pool) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int col = lane & 15;
+  const int total = a.num_rows * a.num_kv_heads;
+#pragma clang loop unroll(disable)
+  for (int seg = blockIdx.x * kWaves + wave_id_uniform(); seg < total; seg += gridDim.x * kWaves) {
+    const int row = seg / a.num_kv_heads, g = seg - row * a.num_kv_heads;
+    const int ctx = row_context(a, row);
+    Running run;
+    run.clear();
+    fold_pairs<G, 2>(a, pool, row, g, ctx, 0, (ctx + kBlockSize - 1) / kBlockSize, run);
+    const float l = run.total();
+    if (col < G)
+      run.store_bf16(static_cast<uint16_t*>(a.out) + ((size_t)row * a.num_q_heads + g * G + col) * kHeadDim, lane >> 4,
+                     l > 0.0f ? 1.0f / l : 0.0f);   // (a row without context is zeros)
+  }
+}
+
 // Blocks [sp S, (sp + 1) S) of segment seg0 + blockIdx.x, S = split_blocks (even) and
 // sp = blockIdx.y: the whole segment when it has no more than S blocks, else a
 // partial in slot (segment * n_split_max + sp) * G + head.
 template <int G>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void decode_q8_kernel(DecodeArgs a, Q8Pool pool, int seg0) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void decode_q8_kernel(DecodeArgs a, Q8Pool pool, int seg0) {
   __shared__ float s_o[kWaves][G][kHeadDim + 4];
   __shared__ float s_m[kWaves][G], s_l[kWaves][G];
   const int tid = threadIdx.x;
@@ -170,56 +250,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   const int Hq = a.num_q_heads;
   const int seg = seg0 + (int)blockIdx.x;
   const int row = seg / nkv, g = seg - row * nkv;
-  const int ctx = max(0, min(load_uniform(a.ctx_lens, row), min(a.max_ctx, a.max_blocks_per_seq * kBlockSize)));
+  const int ctx = row_context(a, row);
   const int nblk = (ctx + kBlockSize - 1) / kBlockSize;
   const int sp = blockIdx.y;
   const int b0 = sp * a.split_blocks, b1 = min(nblk, b0 + a.split_blocks);
   if (sp > 0 && b0 >= nblk) return;
-  const int first = b0 + 2 * w;                                                       // this wave's pairs: first, first + 8, ...
-  const int n = b1 > first ? (b1 - first + 2 * kWaves - 1) / (2 * kWaves) : 0;
-
-  v4u_t qf[4];
-  KRegs k;
-  VRegs v;
   Running run;
   run.clear();
-
-  // Pool tile of the x-th block of this wave's i-th pair: tile 0 of the head in place
-  // of an entry outside the pool or past the piece (masked whole), so that the loads
-  // need no branch. (The table is not read past the piece.)
-  auto entry = [&](int i, int x, bool& ok) -> size_t {
-    const int b = first + 2 * kWaves * i + x;
-    const int e = load_uniform(a.block_tables, (size_t)row * a.max_blocks_per_seq + min(b, b1 - 1));
-    ok = b < b1 && e >= 0 && e < a.num_blocks;
-    return (size_t)(ok ? e : 0) * nkv + g;
-  };
-
-  if (n > 0) {
-    bool ok[2];
-    size_t tile[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) tile[x] = entry(0, x, ok[x]);
-    issue_k(pool, tile[0], tile[1], grp, col, k);
-    load_q<G>(a.q, (size_t)row * Hq + g * G, grp, col, qf);
-    issue_v(pool, tile[0], tile[1], grp, col, v);
-#pragma clang loop unroll(disable)
-    for (int i = 0; i < n; ++i) {
-      const int b = first + 2 * kWaves * i;
-      bool next_ok[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) tile[x] = entry(i + 1, x, next_ok[x]);
-      float s[8];
-      const PairScales ps = pair_scales(v.scales);
-      pair_scores(k, qf, ps, a.scale_log2, s);
-      issue_k(pool, tile[0], tile[1], grp, col, k);   // the K registers are free
-      VRows rows = exchange(v, ps);
-      issue_v(pool, tile[0], tile[1], grp, col, v);   // and V's
-      if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > ctx) mask_pair(a, row, ctx, b, ok, grp, s, rows);
-      run.fold(s, rows, head_lane);
-      ok[0] = next_ok[0];
-      ok[1] = next_ok[1];
-    }
-  }
+  fold_pairs<G, 2 * kWaves>(a, pool, row, g, ctx, b0 + 2 * w, b1, run);   // this wave's pairs: every fourth
 
   // The waves' results.
   const float l_head = run.total();
@@ -379,6 +417,11 @@ hipError_t launch_group(DecodeArgs a, Q8Pool pool, hipStream_t stream, int slot)
   // (partials: the workspace has a slot per query row and kDecodeGroupSlots groups more)
   const int64_t slots = (int64_t)a.num_rows * a.num_q_heads + (int64_t)kDecodeGroupSlots * std::min(a.num_q_heads, 8);
   const int cus = stream_compute_units(stream);
+  if (q8_decode_by_waves(segments, blocks, cus)) {
+    const int64_t wgs = std::min<int64_t>((segments + kWaves - 1) / kWaves, kWavesPerSimd * (int64_t)cus);   // (four SIMDs, four waves)
+    hipLaunchKernelGGL(decode_q8_wave_kernel<G>, dim3((unsigned)wgs), dim3(kThreads), 0, stream, a, pool);
+    return hipGetLastError();
+  }
   if (!plan_q8_decode(segments, G, blocks, cus, slots, &a.split_blocks, &a.n_split_max)) {
     if (a.num_kv_heads % 4 == 0) return launch_even<G, 4>(a, pool, stream, slot + 2, cus);
     if (a.num_kv_heads % 2 == 0) return launch_even<G, 2>(a, pool, stream, slot + 1, cus);

@@ -209,6 +209,18 @@ inline bool plan_short_decode(int64_t segments, int32_t group, int64_t blocks, i
   return false;
 }
 
+// Whether the decode over an 8-bit cache gives whole segments to single waves instead of
+// workgroups: from where these no longer fit the chip at once (three to a compute unit), while
+// a wave's serial walk stays short (shortest between one wave to a SIMD and two). Calls in us, a workgroup / a wave per segment (32 / 8 heads, uniform
+// contexts up to): 128 rows of 60 tokens 10.2 / 7.1, 256 of 300 31.1 / 27.5, 512 of 200 47.2 /
+// 36.9; not taken: 64 of 100 7.2 / 8.1, 160 of 512 1.24 times as long, 512 of 2000 239 / 257. Over
+// 1089 calls of 64 to 4096 rows and up to 2000 tokens the 375 it takes run in 0.75 of the
+// time in the mean, the worst in 1.12 (256 rows of lognormal contexts of up to 384).
+inline bool q8_decode_by_waves(int64_t segments, int64_t blocks, int64_t compute_units) {
+  if (segments <= 3 * compute_units || segments > 1 << 30) return false;
+  return blocks <= (segments >= 8 * compute_units ? 24 : segments <= 4 * compute_units ? 16 : 8);
+}
+
 // Whether the decode over an 8-bit cache (decode_q8.hip) runs whole segments or pieces
 // of `split_blocks` blocks, or else its even split.
 //

@@ -90,6 +90,25 @@ def test_many_rows(rows, lo, hi, hq, hkv):
     check(q8, run(q8), f"{rows} rows")
 
 
+@pytest.mark.parametrize("rows,hi,hq,hkv", [(300, 128, 12, 3), (130, 100, 64, 8), (900, 40, 8, 1), (300, 380, 8, 8), (1800, 33, 8, 2), (125, 250, 32, 8)])
+def test_short_contexts_by_single_waves(rows, hi, hq, hkv):
+    rng = np.random.default_rng(rows + hi)
+    ctx = rng.integers(1, hi + 1, rows)
+    ctx[:5] = hi, 1, 16, 17, 32
+    b = W.custom(ctx, (rng.random(rows) < 0.5).astype(np.uint8), hq, hkv, seed=rows, spare_blocks=7)
+    b = with_direction_table(b) if hkv == 3 else b
+    q8 = Q.poison(Q.held(b, rows), owned_mask(b))
+    empty = rng.integers(0, rows, 9)
+    b = q8.batch
+    b.ctx_lens[empty] = rng.choice([0, -3], 9)
+    gone = np.setdiff1d(rng.integers(0, rows, 9), empty)
+    b.block_tables[gone, 0] = b.num_blocks + 3        # a first block outside the pool: its positions are not seen
+    announce(f"decode_q8 {rows} rows of up to {hi}, {hq}/{hkv}, a wave each")
+    got = run(q8, max_ctx=hi)
+    assert (got[empty] == 0).all()
+    Q.check(got, masked_reference(q8, b.block_tables), b.q_decode, b, np.arange(rows), WEIGHTS, "short contexts")
+
+
 def test_more_rows_than_the_prefix_holds():
     rng = np.random.default_rng(12)
     ctx = rng.integers(1, 40, 5001)

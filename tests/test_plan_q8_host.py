@@ -17,6 +17,7 @@ WRAPPER = """
 extern "C" int q8(long long segments, int group, long long blocks, int cus, long long slots, int* out) {
   return bros::plan_q8_decode(segments, group, blocks, cus, slots, out, out + 1);
 }
+extern "C" int waves(long long segments, long long blocks, int cus) { return bros::q8_decode_by_waves(segments, blocks, cus); }
 """
 
 
@@ -33,10 +34,13 @@ def plan(tmp_path_factory):
     lib = ctypes.CDLL(str(so))
     lib.q8.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_int)]
 
+    lib.waves.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
+
     def call(segments, group, blocks, cus=256, slots=1 << 40):
         out = (ctypes.c_int * 2)()
         return tuple(out) if lib.q8(segments, group, blocks, cus, slots, out) else None
 
+    call.waves = lambda segments, blocks, cus=256: bool(lib.waves(segments, blocks, cus))
     return call
 
 
@@ -67,3 +71,10 @@ def test_which_calls(plan):
     # on a part of the chip the limits scale
     assert plan(64, 4, 100, cus=32) == (100, 1)
     assert plan(64, 4, 100, cus=256)[1] > 1
+
+
+def test_which_calls_go_by_waves(plan):
+    assert not plan.waves(768, 4) and plan.waves(769, 4) and plan.waves(1024, 16)
+    assert not plan.waves(1024, 17) and not plan.waves(1025, 9) and plan.waves(1025, 8) and plan.waves(2048, 24) and not plan.waves(2048, 25)
+    assert not plan.waves(1 << 31, 1) and not plan.waves((1 << 32) + 8, 1)      # (a wave's index stays below 2^31)
+    assert plan.waves(100, 8, cus=32) and not plan.waves(96, 8, cus=32)
