@@ -399,7 +399,7 @@ def _move(pools, slot_ids, num_slots, rows, scales=None, one_byte=True):
         if len(shape) != 3 or shape[0] < n or shape[1] != hkv or shape[2] != 2 or scales.element_size() != 1:
             raise ValueError(f"the scales must hold [{n}][{hkv}][2] bytes")
         rows = (*rows, scales)
-    if all(t.is_cuda for t in rows):
+    if rows[0].is_cuda and rows[1].is_cuda and (scales is None or scales.is_cuda):
         at = _addresses(*pools, slot_ids, *rows)
         dense = at[4:]
     else:   # (some in pinned host memory)
