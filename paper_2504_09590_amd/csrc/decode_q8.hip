@@ -115,7 +115,7 @@ __device__ __forceinline__ void even_worker(const DecodeArgs& a, const Q8Pool& p
     if (i + 1 < n && seg_end) load_q<G>(a.q, first_head(cur[1]), grp, col, qf);
     VRows rows = exchange(v, ps);
     if (!p.ok[0] || !p.ok[1] || last) mask_pair(a, p.c.row, p.c.ctx, 2 * p.c.b, p.ok, grp, s, rows);
-    run.fold(s, rows, head_lane);
+    run.fold<true>(s, rows, head_lane);
     // (V's registers are free before the fold, but requested there they come no sooner
     // and everything takes longer: 848 us against 832 in the case above)
     asm volatile("" ::: "memory");
@@ -153,58 +153,20 @@ __device__ __forceinline__ void even_worker(const DecodeArgs& a, const Q8Pool& p
   }
 }
 
+__device__ __forceinline__ int row_context(const DecodeArgs& a, int row) {
+  return max(0, min(load_uniform(a.ctx_lens, row), min(a.max_ctx, a.max_blocks_per_seq * kBlockSize)));
+}
+
 // Folds pairs first, first + STRIDE, ... of blocks below b1 of a (row, KV head) segment into `run`.
 template <int G, int STRIDE>
-__device__ __forceinline__ void fold_pairs(const DecodeArgs& a, const Q8Pool& pool, int row, int g, int ctx, int first, int b1,
-                                           Running& run) {
+__device__ __forceinline__ void fold_segment(const DecodeArgs& a, const Q8Pool& pool, int row, int g, int ctx, int first, int b1,
+                                             Running& run) {
   const int lane = threadIdx.x & (kWave - 1);
   const int grp = lane >> 4;
   const int col = lane & 15;
-  const int nkv = a.num_kv_heads;
-  const int n = b1 > first ? (b1 - first + STRIDE - 1) / STRIDE : 0;
-  if (n == 0) return;
-  v4u_t qf[4];
-  KRegs k;
-  VRegs v;
-
-  // Pool tile of the x-th block of the wave's i-th pair: tile 0 of the head in place
-  // of an entry outside the pool or past the piece (masked whole), so that the loads
-  // need no branch. (The table is not read past the piece.)
-  auto entry = [&](int i, int x, bool& ok) -> size_t {
-    const int b = first + STRIDE * i + x;
-    const int e = load_uniform(a.block_tables, (size_t)row * a.max_blocks_per_seq + min(b, b1 - 1));
-    ok = b < b1 && e >= 0 && e < a.num_blocks;
-    return (size_t)(ok ? e : 0) * nkv + g;
-  };
-
-  bool ok[2];
-  size_t tile[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) tile[x] = entry(0, x, ok[x]);
-  issue_k(pool, tile[0], tile[1], grp, col, k);
-  load_q<G>(a.q, (size_t)row * a.num_q_heads + g * G, grp, col, qf);
-  issue_v(pool, tile[0], tile[1], grp, col, v);
-#pragma clang loop unroll(disable)
-  for (int i = 0; i < n; ++i) {
-    const int b = first + STRIDE * i;
-    bool next_ok[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) tile[x] = entry(i + 1, x, next_ok[x]);
-    float s[8];
-    const PairScales ps = pair_scales(v.scales);
-    pair_scores(k, qf, ps, a.scale_log2, s);
-    issue_k(pool, tile[0], tile[1], grp, col, k);   // the K registers are free
-    VRows rows = exchange(v, ps);
-    issue_v(pool, tile[0], tile[1], grp, col, v);   // and V's
-    if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > ctx) mask_pair(a, row, ctx, b, ok, grp, s, rows);
-    run.fold(s, rows, col < G);
-    ok[0] = next_ok[0];
-    ok[1] = next_ok[1];
-  }
-}
-
-__device__ __forceinline__ int row_context(const DecodeArgs& a, int row) {
-  return max(0, min(load_uniform(a.ctx_lens, row), min(a.max_ctx, a.max_blocks_per_seq * kBlockSize)));
+  const size_t head = (size_t)row * a.num_q_heads + g * G + min(col, G - 1);
+  fold_pairs<STRIDE, true>(a, pool, row, g, head, first, b1, ctx, col < G, run,
+                     [&](int b, const bool (&ok)[2], float (&s)[8], VRows& v) { mask_pair(a, row, ctx, b, ok, grp, s, v); });
 }
 
 // Many short contexts (plan.h: q8_decode_by_waves): a wave takes whole segments, x, x + W, ... of
@@ -225,7 +187,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWaves
     const int ctx = row_context(a, row);
     Running run;
     run.clear();
-    fold_pairs<G, 2>(a, pool, row, g, ctx, 0, (ctx + kBlockSize - 1) / kBlockSize, run);
+    fold_segment<G, 2>(a, pool, row, g, ctx, 0, (ctx + kBlockSize - 1) / kBlockSize, run);
     const float l = run.total();
     if (col < G)
       run.store_bf16(static_cast<uint16_t*>(a.out) + ((size_t)row * a.num_q_heads + g * G + col) * kHeadDim, lane >> 4,
@@ -257,7 +219,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWaves
   if (sp > 0 && b0 >= nblk) return;
   Running run;
   run.clear();
-  fold_pairs<G, 2 * kWaves>(a, pool, row, g, ctx, b0 + 2 * w, b1, run);   // this wave's pairs: every fourth
+  fold_segment<G, 2 * kWaves>(a, pool, row, g, ctx, b0 + 2 * w, b1, run);   // this wave's pairs: every fourth
 
   // The waves' results.
   const float l_head = run.total();

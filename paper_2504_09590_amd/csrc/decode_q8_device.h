@@ -81,12 +81,16 @@ __device__ __forceinline__ void issue_v(const Q8Pool& p, size_t tile0, size_t ti
   v.scales = *reinterpret_cast<const uint16_t*>(p.scales + (t * kScaleBytes + (uint32_t)(8 * (col & 3) + 2 * grp)));
 }
 
-// The query of a segment, in the order of K's dims (padding columns repeat a head).
-template <int G>
-__device__ __forceinline__ void load_q(const void* q, size_t first_head, int grp, int col, v4u_t (&qf)[4]) {
-  const uint16_t* p = static_cast<const uint16_t*>(q) + (first_head + min(col, G - 1)) * kHeadDim + 16 * grp;
+// The lane's column of the query, in the order of K's dims: row `head` of q.
+__device__ __forceinline__ void load_q_row(const void* q, size_t head, int grp, v4u_t (&qf)[4]) {
+  const uint16_t* p = static_cast<const uint16_t*>(q) + head * kHeadDim + 16 * grp;
 #pragma unroll
   for (int c = 0; c < 4; ++c) qf[c] = *reinterpret_cast<const v4u_t*>(p + 64 * (c >> 1) + 8 * (c & 1));
+}
+// A segment's (padding columns repeat a head).
+template <int G>
+__device__ __forceinline__ void load_q(const void* q, size_t first_head, int grp, int col, v4u_t (&qf)[4]) {
+  load_q_row(q, first_head + min(col, G - 1), grp, qf);
 }
 
 // Products of a block's codes with the query: slots slot_of(grp, r) of head col, without K's scale.
@@ -168,7 +172,9 @@ struct Running {
     for (int t = 0; t < 8; ++t) acc[t] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // Folds a pair in: s its scores (-inf where masked), v its V rows.
+  // Folds a pair in: s its scores (-inf where masked), v its V rows. kTwoParts: the weights as
+  // two bf16 values instead of one.
+  template <bool kTwoParts>
   __device__ __forceinline__ void fold(const float (&s)[8], const VRows& v, bool head_lane) {
     float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     if (__builtin_amdgcn_ballot_w64(head_lane && mx > m_ref + kRescaleSlack) != 0) {
@@ -190,11 +196,11 @@ struct Running {
     for (int i = 0; i < 8; ++i) p[i] = fast_exp2(s[i] - m_ref);
     l_part += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     // The weights as a bf16 and the bf16 of what it leaves: 8 bits more for eight
-    // products a pair, which cost nothing measurable.
+    // products a pair, which cost the decode nothing measurable.
     const v4u_t hi4 = {q8::pack2_bf16(p[0], p[1]), q8::pack2_bf16(p[2], p[3]), q8::pack2_bf16(p[4], p[5]), q8::pack2_bf16(p[6], p[7])};
-    v4u_t lo4;
+    v4u_t lo4 = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lo4[i] = q8::pack2_bf16(p[2 * i] - bf16_lo(hi4[i]), p[2 * i + 1] - bf16_hi(hi4[i]));
+    for (int i = 0; kTwoParts && i < 4; ++i) lo4[i] = q8::pack2_bf16(p[2 * i] - bf16_lo(hi4[i]), p[2 * i + 1] - bf16_hi(hi4[i]));
     const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, hi4), pl = __builtin_bit_cast(bf16x8_t, lo4);
     float sc[2][4];
 #pragma unroll
@@ -219,8 +225,27 @@ struct Running {
         const bf16x8_t va = __builtin_bit_cast(bf16x8_t, vt);
         const int t = 2 * u + h;
         acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, acc[t], 0, 0, 0);
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, acc[t], 0, 0, 0);
+        if constexpr (kTwoParts) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, acc[t], 0, 0, 0);
       }
+    }
+  }
+
+  // NaN where the lane's column sees a marked value: `marks` holds a byte that is not zero
+  // in its place, `seen` a bf16 one for each slot that the column sees.
+  __device__ __forceinline__ void spoil(const VRows& marks, const uint32_t (&seen)[4]) {
+    const bf16x8_t p = __builtin_bit_cast(bf16x8_t, v4u_t{seen[0], seen[1], seen[2], seen[3]});
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      uint32_t w[2][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[x][j] = (marks.row[x][j][t >> 2] >> (8 * (t & 3))) & 0xffu ? 0x3f80u : 0u;
+      }
+      const v4u_t vt = {w[0][0] | w[0][1] << 16, w[0][2] | w[0][3] << 16, w[1][0] | w[1][1] << 16, w[1][2] | w[1][3] << 16};
+      const floatx4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vt), p, floatx4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][r] = hit[r] > 0.0f ? __uint_as_float(0x7fc00000u) : acc[t][r];
     }
   }
 
@@ -268,6 +293,58 @@ __device__ __forceinline__ void mask_pair(const DecodeArgs& a, int row, int ctx,
         v.scales[x] &= ~(0xffu << (8 * r));   // (0 times 2^-127)
       }
     }
+  }
+}
+
+// Folds pairs first, first + STRIDE, ... of blocks below b1 of sequence `seq`, KV head g, into
+// `run`. `head` is the lane's row of q; pairs that end above position `plain`, or have a block
+// outside the pool, go through mask(first block, ok, scores, V rows).
+template <int STRIDE, bool kTwoParts, class Args, class Mask>
+__device__ __forceinline__ void fold_pairs(const Args& a, const Q8Pool& pool, int seq, int g, size_t head, int first, int b1,
+                                           int plain, bool head_lane, Running& run, Mask mask) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int grp = lane >> 4;
+  const int col = lane & 15;
+  const int nkv = a.num_kv_heads;
+  const int n = b1 > first ? (b1 - first + STRIDE - 1) / STRIDE : 0;
+  if (n == 0) return;
+  v4u_t qf[4];
+  KRegs k;
+  VRegs v;
+
+  // Pool tile of the x-th block of the wave's i-th pair: tile 0 of the head in place
+  // of an entry outside the pool or past the piece (masked whole), so that the loads
+  // need no branch. (The table is not read past the piece.)
+  auto entry = [&](int i, int x, bool& ok) -> size_t {
+    const int b = first + STRIDE * i + x;
+    const int e = load_uniform(a.block_tables, (size_t)seq * a.max_blocks_per_seq + min(b, b1 - 1));
+    ok = b < b1 && e >= 0 && e < a.num_blocks;
+    return (size_t)(ok ? e : 0) * nkv + g;
+  };
+
+  bool ok[2];
+  size_t tile[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) tile[x] = entry(0, x, ok[x]);
+  issue_k(pool, tile[0], tile[1], grp, col, k);
+  load_q_row(a.q, head, grp, qf);
+  issue_v(pool, tile[0], tile[1], grp, col, v);
+#pragma clang loop unroll(disable)
+  for (int i = 0; i < n; ++i) {
+    const int b = first + STRIDE * i;
+    bool next_ok[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) tile[x] = entry(i + 1, x, next_ok[x]);
+    float s[8];
+    const PairScales ps = pair_scales(v.scales);
+    pair_scores(k, qf, ps, a.scale_log2, s);
+    issue_k(pool, tile[0], tile[1], grp, col, k);   // the K registers are free
+    VRows rows = exchange(v, ps);
+    issue_v(pool, tile[0], tile[1], grp, col, v);   // and V's
+    if (!ok[0] || !ok[1] || (b + 2) * kBlockSize > plain) mask(b, ok, s, rows);
+    run.fold<kTwoParts>(s, rows, head_lane);
+    ok[0] = next_ok[0];
+    ok[1] = next_ok[1];
   }
 }
 

@@ -48,14 +48,19 @@ def check(q8, got, what):
     Q.check(got, want, b.q_prefill, b, seq, WEIGHTS, what)
 
 
+# A bound of 3000 tokens takes the call to units of 128 rows, the exact one to groups of 16 columns.
+BOUNDS = [None, 3000]
+
+
+@pytest.mark.parametrize("bound", BOUNDS)
 @pytest.mark.parametrize("group", [1, 2, 4, 8])
-def test_edge_lengths_and_groups(group):
+def test_edge_lengths_and_groups(group, bound):
     c0s = [0, 0, 0, 0, 5, 16, 31, 100, 3, 64, 0, 250]
     ns = [1, 16, 17, 130, 40, 1, 33, 64, 1, 16, 300, 7]
     b = chunks(c0s, ns, group, 2, seed=group)
     q8 = Q.poison(Q.held(b, group), owned_mask(b))
-    announce(f"prefill_q8 edges G={group}")
-    check(q8, run(q8), f"edges G={group}")
+    announce(f"prefill_q8 edges G={group} bound={bound}")
+    check(q8, run(q8, max_ctx=bound), f"edges G={group}")
 
 
 @pytest.mark.parametrize("group,hkv", [(4, 2), (1, 8), (8, 1)])
@@ -78,6 +83,46 @@ def test_beyond_the_whole_table():
     check(q8, run(q8), "40000 tokens")
 
 
+@pytest.mark.parametrize("group,hkv", [(1, 1), (2, 3), (4, 8), (8, 2)])
+def test_groups_of_columns(group, hkv):
+    # many sequences (more than a wave looks at at once), empty ones among them, deep contexts
+    rng = np.random.default_rng(group)
+    ns = rng.integers(0, 4, 90)
+    ns[[3, 70, 88]] = 33, 17, 5
+    c0s = rng.integers(0, 60, 90)
+    c0s[[3, 70]] = 1300, 700
+    m = 90 if hkv < 8 else 50
+    b = chunks(c0s[:m].tolist(), ns[:m].tolist(), group, hkv, seed=50 + group)
+    q8 = Q.poison(Q.held(b, group), owned_mask(b))
+    announce(f"prefill_q8 groups of columns, G={group} Hkv={hkv}")
+    n = int(b.cu_q[-1])
+    got = run(q8, pad=5)
+    assert (oracle.widen(got[n:], "bf16") == 7.0).all()
+    check(q8, got[:n], "groups of columns")
+
+
+def test_nans_in_groups_of_columns():
+    # every value of a row of V, one of V, an unset scale: each reaches the rows from its position on
+    b = chunks([90], [40], 2, 3, seed=61, cls=[W.RT])
+    q8 = Q.held(b, 61)
+    for p, h, what in ((95, 0, "row"), (128, 1, "one"), (100, 2, "scale"), (3, 1, "one")):
+        blk, slot = oracle.physical_location(b.block_tables, b.dir, 0, np.array([p]))
+        if what == "row":
+            q8.v[blk, h, slot] = 0xFF
+        elif what == "one":
+            q8.v[blk, h, slot, 77 + p % 5] = 0x7F
+        else:
+            q8.scales[blk, h, 1, slot] = 255
+    announce("prefill_q8 NaNs in groups of columns")
+    nan = ~np.isfinite(oracle.widen(run(q8), "bf16"))
+    want = np.zeros_like(nan)
+    want[5:, :2] = True
+    want[38:, 2:4, 77 + 128 % 5] = True
+    want[:, 2:4, 77 + 3] = True
+    want[10:, 4:] = True
+    assert np.array_equal(nan, want)
+
+
 def test_many_units():
     rng = np.random.default_rng(4)
     b = chunks(rng.integers(0, 40, 300).tolist(), rng.integers(1, 40, 300).tolist(), 4, 2, seed=4)
@@ -92,24 +137,30 @@ def test_directions_and_loose_bounds():
     announce("prefill_q8 explicit directions")
     got = run(q8)
     check(q8, got, "explicit directions")
-    assert np.array_equal(run(q8, max_ctx=5000, max_q=4000, with_ws=False), run(q8, with_ws=False))
+    assert np.array_equal(got, run(q8, with_ws=False))                  # groups of columns: no workspace
+    loose = run(q8, max_ctx=5000, max_q=4000, with_ws=False)
+    check(q8, loose, "loose bounds")
+    assert np.array_equal(loose, run(q8, max_ctx=2500, with_ws=False))  # units, whatever the bounds
     t = with_direction_table(chunks([20, 0, 77, 300], [50, 90, 16, 33], 4, 4, seed=6))
     q8 = Q.poison(Q.held(t, 6), owned_mask(t))
     announce("prefill_q8 direction table")
-    check(q8, run(q8), "direction table")
+    for bound in BOUNDS:
+        check(q8, run(q8, max_ctx=bound), "direction table")
 
 
-def test_empty_chunks_and_rows_behind_the_last():
+@pytest.mark.parametrize("bound", BOUNDS)
+def test_empty_chunks_and_rows_behind_the_last(bound):
     b = chunks([20, 40, 77, 0], [50, 0, 16, 33], 4, 2, seed=7, cls=[W.RT] * 4)
     q8 = Q.held(b, 7)
     announce("prefill_q8 an empty chunk, rows behind the last")
-    got = run(q8, pad=29)
+    got = run(q8, pad=29, max_ctx=bound)
     n = int(b.cu_q[-1])
     assert (oracle.widen(got[n:], "bf16") == 7.0).all()
     check(q8, got[:n], "empty chunk")
 
 
-def test_invalid_entries():
+@pytest.mark.parametrize("bound", BOUNDS)
+def test_invalid_entries(bound):
     b = chunks([200, 0], [60, 90], 4, 2, seed=8, cls=[W.RT] * 2)
     tables = b.block_tables.copy()
     tables[0, [1, 9, 14]] = [-1, b.num_blocks, 2 ** 31 - 1]
@@ -117,7 +168,7 @@ def test_invalid_entries():
     b = dataclasses.replace(b, block_tables=tables)
     q8 = Q.held(b, 8)
     announce("prefill_q8 invalid entries")
-    got = run(q8)
+    got = run(q8, max_ctx=bound)
     want = np.zeros(b.q_prefill.shape)
     for s in range(2):
         lo, hi = int(b.cu_q[s]), int(b.cu_q[s + 1])
@@ -146,8 +197,8 @@ def test_a_nan_reaches_only_rows_that_see_it():
     blk, slot = oracle.physical_location(b.block_tables, b.dir, 1, np.array([30]))
     q8.k[blk, 0, slot, 9] = 0xFF
     announce("prefill_q8 NaN codes")
-    for ws in (True, False):
-        got = oracle.widen(run(q8, with_ws=ws), "bf16")
+    for ws, bound in ((True, None), (True, 3000), (False, 3000)):
+        got = oracle.widen(run(q8, with_ws=ws, max_ctx=bound), "bf16")
         nan = np.isnan(got)
         want = np.zeros_like(nan)
         want[57 - 20:70, 4:, 5] = True          # heads of KV head 1, dim 5, rows at positions 57 and later
@@ -164,8 +215,8 @@ def test_a_query_that_is_not_finite_stays_alone():
     for r, h, bits in rows:
         odd.batch.q_prefill[r, h, 17] = bits
     announce("prefill_q8 queries that are not finite")
-    for ws in (True, False):
-        got, plain = run(odd, with_ws=ws), run(q8, with_ws=ws)
+    for ws, bound in ((True, None), (True, 3000), (False, 3000)):
+        got, plain = run(odd, with_ws=ws, max_ctx=bound), run(q8, with_ws=ws, max_ctx=bound)
         for r, h, _ in rows:
             assert np.isnan(oracle.widen(got[r, h], "bf16")).all()
             got[r, h] = plain[r, h]
@@ -225,6 +276,8 @@ def test_far_blocks():
     q = bros._tensor(b.q_prefill, "bf16", "cuda")
     out = torch.empty_like(q)
     announce("prefill_q8 in blocks beyond 4 GiB")
-    bros.bros_attn_prefill_chunk_q8(out, q, up(b.cu_q), 200, *far, up(tables), up(b.dir), None, up(b.ctx_lens), 220)
-    torch.cuda.synchronize()
-    check(q8, bros.to_host_bits(out), "far blocks")
+    for bound in (220, 3000):
+        out.fill_(7.0)
+        bros.bros_attn_prefill_chunk_q8(out, q, up(b.cu_q), 200, *far, up(tables), up(b.dir), None, up(b.ctx_lens), bound)
+        torch.cuda.synchronize()
+        check(q8, bros.to_host_bits(out), f"far blocks, bound {bound}")

@@ -17,6 +17,7 @@ WRAPPER = """
 extern "C" int q8(long long segments, int group, long long blocks, int cus, long long slots, int* out) {
   return bros::plan_q8_decode(segments, group, blocks, cus, slots, out, out + 1);
 }
+extern "C" int by_rows(long long groups, long long blocks, int cus) { return bros::q8_prefill_by_rows(groups, blocks, cus); }
 extern "C" int waves(long long segments, long long blocks, int cus) { return bros::q8_decode_by_waves(segments, blocks, cus); }
 """
 
@@ -41,6 +42,8 @@ def plan(tmp_path_factory):
         return tuple(out) if lib.q8(segments, group, blocks, cus, slots, out) else None
 
     call.waves = lambda segments, blocks, cus=256: bool(lib.waves(segments, blocks, cus))
+    lib.by_rows.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
+    call.by_rows = lambda groups, blocks, cus=256: bool(lib.by_rows(groups, blocks, cus))
     return call
 
 
@@ -78,3 +81,9 @@ def test_which_calls_go_by_waves(plan):
     assert not plan.waves(1024, 17) and not plan.waves(1025, 9) and plan.waves(1025, 8) and plan.waves(2048, 24) and not plan.waves(2048, 25)
     assert not plan.waves(1 << 31, 1) and not plan.waves((1 << 32) + 8, 1)      # (a wave's index stays below 2^31)
     assert plan.waves(100, 8, cus=32) and not plan.waves(96, 8, cus=32)
+
+
+def test_which_chunks_go_by_rows(plan):
+    assert plan.by_rows(8, 1) and plan.by_rows(512, 128) and not plan.by_rows(512, 129)
+    assert plan.by_rows(768, 96) and not plan.by_rows(513, 97) and not plan.by_rows(769, 1)
+    assert plan.by_rows(96, 96, cus=32) and not plan.by_rows(97, 1, cus=32)
