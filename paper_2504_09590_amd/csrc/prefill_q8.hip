@@ -50,14 +50,15 @@ hipError_t launch_q8_group(PrefillArgs a, const uint8_t* scales, int num_units, 
 
 namespace dq {
 
-// Few rows (plan.h: q8_prefill_by_rows): the decode's steps (decode_q8_device.h), their 16 columns
-// filled with 16 / G positions of G heads. A workgroup takes 16 columns; wave w folds every fourth
-// pair of blocks into a running result of its own, and the four meet in LDS.
+// Few rows (plan.h: plan_q8_prefill_rows): the decode's steps (decode_q8_device.h), their 16 columns
+// filled with 16 / G positions of G heads. A workgroup takes 16 columns, or a piece of the blocks they
+// see; wave w folds every fourth pair of blocks into a running result of its own, and the four
+// meet in LDS. Pieces leave partials (max, sum, unnormalised output) that a second kernel folds.
 //
 // In the other kernel a prompt of 301 rows is 80 chains of up to ten steps, one after another, behind a
 // start of 9 us (Q's terms, the first tiles, their conversion); here it is 600 workgroups of at most three
-// steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there). K and V are read
-// once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
+// steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there), 13.0 for 16 rows on
+// 4000 cached tokens in pieces (25.1 there). K and V are read once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
 // the marks of values that are not numbers made inside the step spill or take 0.4 us more.)
 
 // The bytes of w that are the NaN code as ones, all of them where the row's scale is none.
@@ -109,19 +110,18 @@ __device__ __forceinline__ void mask_causal(const PrefillArgs& a, int seq, int l
 // sees once more, and NaN where a column sees one, by a product of their places and what the
 // columns see.
 __device__ __forceinline__ void spoil_pairs(const PrefillArgs& a, const Q8Pool& pool, int seq, int g, int limit, int last, int first,
-                                            int stride, int plain, Running& run) {
+                                            int b1, int plain, Running& run) {
   const int lane = threadIdx.x & (kWave - 1);
   const int grp = lane >> 4;
   const int col = lane & 15;
-  const int nblk = (last + kBlockSize - 1) / kBlockSize;
-  for (int b0 = first; b0 < nblk; b0 += stride) {
+  for (int b0 = first; b0 < b1; b0 += 2 * kWaves) {
     if ((b0 + 2) * kBlockSize <= plain) continue;
     bool ok[2];
     size_t tile[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int e = load_uniform(a.block_tables, (size_t)seq * a.max_blocks_per_seq + min(b0 + x, nblk - 1));
-      ok[x] = b0 + x < nblk && e >= 0 && e < a.num_blocks;
+      const int e = load_uniform(a.block_tables, (size_t)seq * a.max_blocks_per_seq + min(b0 + x, b1 - 1));
+      ok[x] = b0 + x < b1 && e >= 0 && e < a.num_blocks;
       tile[x] = (size_t)(ok[x] ? e : 0) * a.num_kv_heads + g;
     }
     VRegs raw;
@@ -145,9 +145,45 @@ __device__ __forceinline__ void spoil_pairs(const PrefillArgs& a, const Q8Pool& 
   }
 }
 
+// Rows [j0, j0 + 16 / G) of sequence s, KV head g.
+struct Group {
+  int s, g, j0, q_begin, n, c0, ctx;
+};
 template <int G>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void prefill_q8_rows_kernel(PrefillArgs a, Q8Pool pool) {
-  constexpr int P = 16 / G;   // positions of a workgroup
+__device__ __forceinline__ bool find_group(const PrefillArgs& a, Group& u) {
+  constexpr int P = 16 / G;
+  const int lane = threadIdx.x & (kWave - 1);
+  u.g = blockIdx.x % a.num_kv_heads;
+  const int x = gridDim.x / a.num_kv_heads - 1 - blockIdx.x / a.num_kv_heads;   // (the longest rows of a chunk first)
+  // Sequence s has the groups cu_q[s] / P + s and on: the last one that starts at or below x.
+  u.s = -1;
+  for (int s0 = 0; s0 < a.num_seqs; s0 += kWave) {
+    const int i = s0 + lane;
+    const bool below = i < a.num_seqs && a.cu_q[min(i, a.num_seqs - 1)] / P + i <= x;
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
+    if (c > 0) u.s = s0 + c - 1;
+    if (c < kWave) break;
+  }
+  if (u.s < 0) return false;
+  u.q_begin = load_uniform(a.cu_q, u.s);
+  u.n = load_uniform(a.cu_q, u.s + 1) - u.q_begin;
+  const int ctx_s = load_uniform(a.ctx_lens, u.s);
+  u.j0 = (x - (u.q_begin / P + u.s)) * P;
+  u.c0 = ctx_s - u.n;
+  u.ctx = min(ctx_s, min(a.max_ctx, a.max_blocks_per_seq * kBlockSize));
+  return u.q_begin >= 0 && u.n > 0 && u.q_begin + u.n <= a.num_q_tokens && u.j0 >= 0 && u.j0 < u.n && ctx_s >= u.n;
+}
+// Output row of the group's column c.
+template <int G>
+__device__ __forceinline__ size_t out_row(const PrefillArgs& a, const Group& u, int c) {
+  return (size_t)(u.q_begin + u.j0 + c / G) * a.num_q_heads + u.g * G + c % G;
+}
+
+// Blocks [sp S, (sp + 1) S) of what group blockIdx.x sees, S = split_blocks (even) and sp = blockIdx.y:
+// all of it where it has no more than S blocks, else a partial in slot (group * pieces + sp) * 16 + column.
+template <int G>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void prefill_q8_rows_kernel(PrefillArgs a, Q8Pool pool, int split_blocks) {
+  constexpr int P = 16 / G;   // positions of a group
   __shared__ float s_o[kWaves][16][kHeadDim + 4];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int tid = threadIdx.x;
@@ -155,37 +191,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   const int w = wave_id_uniform();
   const int grp = lane >> 4;
   const int col = lane & 15;
-  const int nkv = a.num_kv_heads;
-  const int g = blockIdx.x % nkv;
-  const int x = gridDim.x / nkv - 1 - blockIdx.x / nkv;   // (the longest rows of a chunk first)
-  // Sequence s has the groups of rows cu_q[s] / P + s and on: the last one that starts at or below x.
-  int s = -1;
-  for (int s0 = 0; s0 < a.num_seqs; s0 += kWave) {
-    const int i = s0 + lane;
-    const bool below = i < a.num_seqs && a.cu_q[min(i, a.num_seqs - 1)] / P + i <= x;
-    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
-    if (c > 0) s = s0 + c - 1;
-    if (c < kWave) break;
-  }
-  if (s < 0) return;
-  const int q_begin = load_uniform(a.cu_q, s);
-  const int n = load_uniform(a.cu_q, s + 1) - q_begin;
-  const int ctx_s = load_uniform(a.ctx_lens, s);
-  const int j0 = (x - (q_begin / P + s)) * P;
-  if (q_begin < 0 || n <= 0 || q_begin + n > a.num_q_tokens || j0 < 0 || j0 >= n || ctx_s < n) return;
-  const int ctx = min(ctx_s, min(a.max_ctx, a.max_blocks_per_seq * kBlockSize));
-  const int c0 = ctx_s - n;
-  const int j = min(j0 + col / G, n - 1);                          // the lane's row (behind the chunk: its last)
-  const int limit = min(ctx, c0 + j + 1);                          // positions its column sees
-  const int last = min(ctx, c0 + min(j0 + P, n));                  // and any
-  const size_t head = (size_t)(q_begin + j) * a.num_q_heads + g * G + col % G;
+  Group u;
+  if (!find_group<G>(a, u)) return;
+  const int j = min(u.j0 + col / G, u.n - 1);                      // the lane's row (behind the chunk: its last)
+  const int limit = min(u.ctx, u.c0 + j + 1);                      // positions its column sees,
+  const int last = min(u.ctx, u.c0 + min(u.j0 + P, u.n));          // any column,
+  const int plain = min(u.ctx, u.c0 + u.j0 + 1);                   // and every one
+  const int nblk = (last + kBlockSize - 1) / kBlockSize;
+  const int b0 = blockIdx.y * split_blocks, b1 = min(nblk, b0 + split_blocks);
+  if (b0 > 0 && b0 >= nblk) return;
+  const size_t head = (size_t)(u.q_begin + j) * a.num_q_heads + u.g * G + col % G;
   Running run;
   run.clear();
-  const int plain = min(ctx, c0 + j0 + 1);                         // positions that every column sees
   bool found = false;
-  fold_pairs<2 * kWaves, false>(a, pool, s, g, head, 2 * w, (last + kBlockSize - 1) / kBlockSize, plain, true, run,
-                         [&](int b, const bool (&ok)[2], float (&sc)[8], VRows& v) { mask_causal(a, s, limit, last, b, ok, grp, sc, v, found); });
-  if (__builtin_amdgcn_ballot_w64(found) != 0) spoil_pairs(a, pool, s, g, limit, last, 2 * w, 2 * kWaves, plain, run);
+  fold_pairs<2 * kWaves, false>(a, pool, u.s, u.g, head, b0 + 2 * w, b1, plain, true, run,
+                                [&](int b, const bool (&ok)[2], float (&sc)[8], VRows& v) { mask_causal(a, u.s, limit, last, b, ok, grp, sc, v, found); });
+  if (__builtin_amdgcn_ballot_w64(found) != 0) spoil_pairs(a, pool, u.s, u.g, limit, last, b0 + 2 * w, b1, plain, run);
 
   const float l = run.total();
   run.store(s_o[w][col], grp);
@@ -196,7 +217,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   __syncthreads();
   for (int i = tid; i < 16 * (kHeadDim / 2); i += kThreads) {
     const int c = i / (kHeadDim / 2), d = 2 * (i % (kHeadDim / 2));
-    if (j0 + c / G >= n) break;   // (a later c is a later row)
+    if (u.j0 + c / G >= u.n) break;   // (a later c is a later row)
     float M = kNoMax;
 #pragma unroll
     for (int y = 0; y < kWaves; ++y) M = fmaxf(M, s_m[y][c]);
@@ -209,10 +230,61 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
       A0 = fmaf(o.x, wt, A0);
       A1 = fmaf(o.y, wt, A1);
     }
+    if (nblk > split_blocks) {
+      const size_t slot = ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * 16 + c;
+      *reinterpret_cast<float2*>(a.ws_o + slot * kHeadDim + d) = make_float2(A0, A1);
+      if (d == 0) {
+        a.ws_ml[2 * slot] = M;
+        a.ws_ml[2 * slot + 1] = L;
+      }
+      continue;
+    }
     const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-    const size_t row = (size_t)(q_begin + j0 + c / G) * a.num_q_heads + g * G + c % G;
-    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + row * kHeadDim + d) = q8::pack2_bf16(A0 * inv, A1 * inv);
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + out_row<G>(a, u, c) * kHeadDim + d) = q8::pack2_bf16(A0 * inv, A1 * inv);
   }
+}
+
+// Folds the pieces of a group, o = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i: four columns a
+// workgroup (blockIdx.y), a thread two dims of one.
+template <int G>
+__global__ __launch_bounds__(kThreads) void prefill_q8_rows_merge_kernel(PrefillArgs a, int split_blocks, int pieces) {
+  constexpr int kRound = 8;   // partials requested at once
+  Group u;
+  if (!find_group<G>(a, u)) return;
+  const int nblk = (min(u.ctx, u.c0 + min(u.j0 + 16 / G, u.n)) + kBlockSize - 1) / kBlockSize;
+  if (nblk <= split_blocks) return;   // (written whole)
+  const int n = (nblk + split_blocks - 1) / split_blocks;
+  const int c = 4 * blockIdx.y + threadIdx.x / (kHeadDim / 2), d = 2 * (threadIdx.x % (kHeadDim / 2));
+  if (u.j0 + c / G >= u.n) return;
+  const size_t slot0 = (size_t)blockIdx.x * pieces * 16 + c;
+  float M = kNoMax, L = 0.0f, A0 = 0.0f, A1 = 0.0f;
+  for (int i = 0; i < n; i += kRound) {   // indices clamped in range
+    float2 x[kRound], v[kRound];
+#pragma unroll
+    for (int y = 0; y < kRound; ++y) {
+      const size_t slot = slot0 + 16 * (size_t)min(i + y, n - 1);
+      x[y] = *reinterpret_cast<const float2*>(a.ws_ml + 2 * slot);
+      v[y] = *reinterpret_cast<const float2*>(a.ws_o + slot * kHeadDim + d);
+    }
+    float Mn = M;
+#pragma unroll
+    for (int y = 0; y < kRound; ++y) Mn = fmaxf(Mn, x[y].x);
+    const float alpha = fast_exp2(M - Mn);
+    L *= alpha;
+    A0 *= alpha;
+    A1 *= alpha;
+    M = Mn;
+#pragma unroll
+    for (int y = 0; y < kRound; ++y) {
+      const bool use = i + y < n;   // (the rest of a round repeats a partial)
+      const float wt = use ? fast_exp2(x[y].x - M) : 0.0f;
+      L = fmaf(use ? x[y].y : 0.0f, wt, L);
+      A0 = fmaf(use ? v[y].x : 0.0f, wt, A0);
+      A1 = fmaf(use ? v[y].y : 0.0f, wt, A1);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + out_row<G>(a, u, c) * kHeadDim + d) = q8::pack2_bf16(A0 * inv, A1 * inv);
 }
 
 // Launches the groups where they are the better arrangement; false: not taken.
@@ -220,9 +292,13 @@ template <int G>
 bool launch_rows(const PrefillArgs& a, const uint8_t* scales, hipStream_t stream, hipError_t* e) {
   const int64_t groups = ((int64_t)(a.num_q_tokens / (16 / G)) + a.num_seqs) * a.num_kv_heads;
   const int64_t blocks = std::min<int64_t>((a.max_ctx + kBlockSize - 1LL) / kBlockSize, a.max_blocks_per_seq);
-  if (!q8_prefill_by_rows(groups, blocks, stream_compute_units(stream))) return false;
+  int32_t split = 0, pieces = 0;
+  if (!plan_q8_prefill_rows(groups, blocks, stream_compute_units(stream), (int64_t)a.ws_slots * pf::kRows, &split, &pieces)) return false;
   const Q8Pool pool{static_cast<const uint8_t*>(a.k_pool), static_cast<const uint8_t*>(a.v_pool), scales};
-  hipLaunchKernelGGL(prefill_q8_rows_kernel<G>, dim3((unsigned)groups), dim3(kThreads), 0, stream, a, pool);
+  hipLaunchKernelGGL(prefill_q8_rows_kernel<G>, dim3((unsigned)groups, (unsigned)pieces), dim3(kThreads), 0, stream, a, pool, split);
+  *e = hipGetLastError();
+  if (*e != hipSuccess || pieces == 1) return true;
+  hipLaunchKernelGGL(prefill_q8_rows_merge_kernel<G>, dim3((unsigned)groups, 4), dim3(kThreads), 0, stream, a, split, pieces);
   *e = hipGetLastError();
   return true;
 }

@@ -48,8 +48,9 @@ def check(q8, got, what):
     Q.check(got, want, b.q_prefill, b, seq, WEIGHTS, what)
 
 
-# A bound of 3000 tokens takes the call to units of 128 rows, the exact one to groups of 16 columns.
-BOUNDS = [None, 3000]
+# A bound of 30000 tokens takes the call to units of 128 rows, the exact one to groups of 16 columns.
+UNITS = 30000
+BOUNDS = [None, UNITS]
 
 
 @pytest.mark.parametrize("bound", BOUNDS)
@@ -101,6 +102,27 @@ def test_groups_of_columns(group, hkv):
     check(q8, got[:n], "groups of columns")
 
 
+@pytest.mark.parametrize("group,hkv,c0s,ns", [(4, 2, [4000, 30, 900], [20, 3, 9]), (8, 1, [9000], [9]), (1, 8, [1500, 0], [16, 7]),
+                                               (2, 3, [20000, 5], [4, 33])])
+def test_groups_of_columns_in_pieces(group, hkv, c0s, ns):
+    b = chunks(c0s, ns, group, hkv, seed=70 + group, cls=[W.RT, W.BE, W.RT][:len(ns)])
+    q8 = Q.poison(Q.held(b, group), owned_mask(b))
+    announce(f"prefill_q8 groups of columns in pieces, {ns} rows on {c0s}, G={group} Hkv={hkv}")
+    n = int(b.cu_q[-1])
+    got = run(q8, pad=3)
+    assert (oracle.widen(got[n:], "bf16") == 7.0).all()
+    check(q8, got[:n], "pieces")
+    assert np.array_equal(got, run(q8, pad=3))
+    # a NaN in a row of V that the first new row does not see, and one that all see
+    for at, first in ((c0s[0] + 2, 2), (1, 0)):
+        blk, slot = oracle.physical_location(b.block_tables, b.dir, 0, np.array([at]))
+        q8.v[blk, hkv - 1, slot, 3] = 0x7F
+        nan = np.isnan(oracle.widen(run(q8), "bf16"))
+        want = np.zeros_like(nan)
+        want[first:ns[0], (hkv - 1) * group:, 3] = True
+        assert np.array_equal(nan, want)
+
+
 def test_nans_in_groups_of_columns():
     # every value of a row of V, one of V, an unset scale: each reaches the rows from its position on
     b = chunks([90], [40], 2, 3, seed=61, cls=[W.RT])
@@ -138,9 +160,9 @@ def test_directions_and_loose_bounds():
     got = run(q8)
     check(q8, got, "explicit directions")
     assert np.array_equal(got, run(q8, with_ws=False))                  # groups of columns: no workspace
-    loose = run(q8, max_ctx=5000, max_q=4000, with_ws=False)
+    loose = run(q8, max_ctx=UNITS, max_q=4000, with_ws=False)
     check(q8, loose, "loose bounds")
-    assert np.array_equal(loose, run(q8, max_ctx=2500, with_ws=False))  # units, whatever the bounds
+    assert np.array_equal(loose, run(q8, max_ctx=20000, with_ws=False))  # units, whatever the bounds
     t = with_direction_table(chunks([20, 0, 77, 300], [50, 90, 16, 33], 4, 4, seed=6))
     q8 = Q.poison(Q.held(t, 6), owned_mask(t))
     announce("prefill_q8 direction table")
@@ -197,7 +219,7 @@ def test_a_nan_reaches_only_rows_that_see_it():
     blk, slot = oracle.physical_location(b.block_tables, b.dir, 1, np.array([30]))
     q8.k[blk, 0, slot, 9] = 0xFF
     announce("prefill_q8 NaN codes")
-    for ws, bound in ((True, None), (True, 3000), (False, 3000)):
+    for ws, bound in ((True, None), (True, UNITS), (False, UNITS)):
         got = oracle.widen(run(q8, with_ws=ws, max_ctx=bound), "bf16")
         nan = np.isnan(got)
         want = np.zeros_like(nan)
@@ -215,7 +237,7 @@ def test_a_query_that_is_not_finite_stays_alone():
     for r, h, bits in rows:
         odd.batch.q_prefill[r, h, 17] = bits
     announce("prefill_q8 queries that are not finite")
-    for ws, bound in ((True, None), (True, 3000), (False, 3000)):
+    for ws, bound in ((True, None), (True, UNITS), (False, UNITS)):
         got, plain = run(odd, with_ws=ws, max_ctx=bound), run(q8, with_ws=ws, max_ctx=bound)
         for r, h, _ in rows:
             assert np.isnan(oracle.widen(got[r, h], "bf16")).all()
@@ -276,7 +298,7 @@ def test_far_blocks():
     q = bros._tensor(b.q_prefill, "bf16", "cuda")
     out = torch.empty_like(q)
     announce("prefill_q8 in blocks beyond 4 GiB")
-    for bound in (220, 3000):
+    for bound in (220, UNITS):
         out.fill_(7.0)
         bros.bros_attn_prefill_chunk_q8(out, q, up(b.cu_q), 200, *far, up(tables), up(b.dir), None, up(b.ctx_lens), bound)
         torch.cuda.synchronize()

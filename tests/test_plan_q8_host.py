@@ -17,7 +17,9 @@ WRAPPER = """
 extern "C" int q8(long long segments, int group, long long blocks, int cus, long long slots, int* out) {
   return bros::plan_q8_decode(segments, group, blocks, cus, slots, out, out + 1);
 }
-extern "C" int by_rows(long long groups, long long blocks, int cus) { return bros::q8_prefill_by_rows(groups, blocks, cus); }
+extern "C" int by_rows(long long groups, long long blocks, int cus, long long slots, int* out) {
+  return bros::plan_q8_prefill_rows(groups, blocks, cus, slots, out, out + 1);
+}
 extern "C" int waves(long long segments, long long blocks, int cus) { return bros::q8_decode_by_waves(segments, blocks, cus); }
 """
 
@@ -42,8 +44,13 @@ def plan(tmp_path_factory):
         return tuple(out) if lib.q8(segments, group, blocks, cus, slots, out) else None
 
     call.waves = lambda segments, blocks, cus=256: bool(lib.waves(segments, blocks, cus))
-    lib.by_rows.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
-    call.by_rows = lambda groups, blocks, cus=256: bool(lib.by_rows(groups, blocks, cus))
+    lib.by_rows.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_int)]
+
+    def by_rows(groups, blocks, cus=256, slots=65536):
+        out = (ctypes.c_int * 2)()
+        return tuple(out) if lib.by_rows(groups, blocks, cus, slots, out) else None
+
+    call.by_rows = by_rows
     return call
 
 
@@ -84,6 +91,22 @@ def test_which_calls_go_by_waves(plan):
 
 
 def test_which_chunks_go_by_rows(plan):
-    assert plan.by_rows(8, 1) and plan.by_rows(512, 128) and not plan.by_rows(512, 129)
-    assert plan.by_rows(768, 96) and not plan.by_rows(513, 97) and not plan.by_rows(769, 1)
-    assert plan.by_rows(96, 96, cus=32) and not plan.by_rows(97, 1, cus=32)
+    assert plan.by_rows(8, 1) == (1, 1) and plan.by_rows(8, 0) == (1, 1)
+    assert plan.by_rows(512, 128) == (128, 1) and plan.by_rows(512, 129) is None
+    assert plan.by_rows(768, 96) == (96, 1) and plan.by_rows(513, 97) is None and plan.by_rows(769, 1) is None
+    assert plan.by_rows(96, 96, cus=32) == (96, 1) and plan.by_rows(97, 1, cus=32) is None
+    # few groups on long contexts: pieces, where the workspace holds their partials
+    assert plan.by_rows(24, 250) == (24, 11)
+    assert plan.by_rows(24, 250, slots=24 * 11 * 16 - 1) is None
+    assert plan.by_rows(24, 120, slots=0) == (120, 1)
+    assert plan.by_rows(24, 2049) is None
+    rng = random.Random(2)
+    for _ in range(4000):
+        groups, blocks, cus = int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 27)), rng.choice([32, 96, 256, 304])
+        slots = rng.choice([0, 1000, 65536])
+        got = plan.by_rows(groups, blocks, cus, slots)
+        if got is None:
+            continue
+        size, n = got
+        assert size * n >= blocks and size * (n - 1) < blocks
+        assert n == 1 or (size % 8 == 0 and groups * n * 16 <= slots)
