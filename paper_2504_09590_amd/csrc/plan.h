@@ -224,23 +224,20 @@ inline bool q8_decode_by_waves(int64_t segments, int64_t blocks, int64_t compute
 // Whether the chunks over an 8-bit cache run in groups of 16 (position, head) columns, a workgroup each
 // (prefill_q8_rows_kernel), instead of units of 128 rows, and in how many pieces of `split_blocks` blocks:
 // while the groups fit the chip at once (three to a compute unit) and their steps, groups times blocks,
-// stay few. Pieces (partials and a merge, 4 us) pay while groups leave compute units idle. Calls in us, units
+// stay few. Pieces (partials and a merge, 4 us) are as many as give every compute unit one. Calls in us, units
 // / groups (32 / 8 heads): 128 rows of a prompt 11.4 / 6.3, 301 14.6 / 10.6, 64 rows on 500 cached tokens 19.9 /
-// 9.1, 16 on 4000 25.1 / 13.0 (28.1 in one piece); not taken: 301 (64 / 8 heads) 15.7 / 17.5. Of 645 calls of up to
-// 1500 rows on up to 40000 tokens the 444 it takes run in 0.60 of the time in the mean, the worst in 1.10, and
-// all calls 3 % above the best of both and ten numbers of pieces. `slots`: partial rows that the workspace holds.
+// 8.9, 16 on 4000 25.1 / 12.2 (28.1 in one piece); not taken: 301 (64 / 8 heads) 15.7 / 17.5. Of 645 calls of up to
+// 1500 rows on up to 40000 tokens the 435 it takes run in 0.59 of the time in the mean, the worst in 1.06, and
+// all calls 2 % above the best of both and ten numbers of pieces. `slots`: partial rows that the workspace holds.
 inline bool plan_q8_prefill_rows(int64_t groups, int64_t blocks, int64_t compute_units, int64_t slots, int32_t* split_blocks,
                                  int32_t* pieces) {
   if (groups <= 0 || groups > 3 * compute_units) return false;
-  const bool whole = blocks <= (groups <= 2 * compute_units ? 128 : 96);
-  if (!whole && blocks * groups > 192 * compute_units) return false;
   int64_t n = 1;
-  if (blocks > 40 && (2 * groups <= compute_units || blocks > 192))
-    n = std::max<int64_t>(1, std::min<int64_t>({2 * compute_units / groups, blocks / 16, 32}));
+  if (blocks > 40) n = std::max<int64_t>(1, std::min<int64_t>({compute_units / groups, blocks / 12, 32}));
   if (n > 1) {
     const int64_t each = ((blocks + n - 1) / n + 7) / 8 * 8;   // (a pair for each of four waves)
     n = (blocks + each - 1) / each;
-    if (n > 1 && groups * n * 16 <= slots) {
+    if (n > 1 && groups * blocks <= 192 * compute_units && groups * n * 16 <= slots) {
       *split_blocks = (int32_t)each;
       *pieces = (int32_t)n;
       return true;
@@ -248,7 +245,8 @@ inline bool plan_q8_prefill_rows(int64_t groups, int64_t blocks, int64_t compute
   }
   *split_blocks = (int32_t)std::max<int64_t>(blocks, 1);
   *pieces = 1;
-  return whole || n <= 1;
+  // (n > 1: pieces would be better, and are not to be had)
+  return blocks <= (groups > 2 * compute_units ? 96 : groups > compute_units || n > 1 ? 128 : 192);
 }
 
 // Whether the decode over an 8-bit cache (decode_q8.hip) runs whole segments or pieces

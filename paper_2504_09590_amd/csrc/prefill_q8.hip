@@ -57,7 +57,7 @@ namespace dq {
 //
 // In the other kernel a prompt of 301 rows is 80 chains of up to ten steps, one after another, behind a
 // start of 9 us (Q's terms, the first tiles, their conversion); here it is 600 workgroups of at most three
-// steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there), 13.0 for 16 rows on
+// steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there), 12.2 for 16 rows on
 // 4000 cached tokens in pieces (25.1 there). K and V are read once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
 // the marks of values that are not numbers made inside the step spill or take 0.4 us more.)
 

@@ -96,9 +96,10 @@ def test_which_chunks_go_by_rows(plan):
     assert plan.by_rows(768, 96) == (96, 1) and plan.by_rows(513, 97) is None and plan.by_rows(769, 1) is None
     assert plan.by_rows(96, 96, cus=32) == (96, 1) and plan.by_rows(97, 1, cus=32) is None
     # few groups on long contexts: pieces, where the workspace holds their partials
-    assert plan.by_rows(24, 250) == (24, 11)
-    assert plan.by_rows(24, 250, slots=24 * 11 * 16 - 1) is None
+    assert plan.by_rows(24, 250) == (32, 8)
+    assert plan.by_rows(24, 250, slots=24 * 8 * 16 - 1) is None
     assert plan.by_rows(24, 120, slots=0) == (120, 1)
+    assert plan.by_rows(129, 192) == (192, 1) and plan.by_rows(129, 193) is None and plan.by_rows(128, 200) == (104, 2)
     assert plan.by_rows(24, 2049) is None
     rng = random.Random(2)
     for _ in range(4000):
