@@ -106,16 +106,15 @@ __device__ __forceinline__ void mask_causal(const PrefillArgs& a, int seq, int l
   }
 }
 
-// After the last pair, where a wave found such values (rare): its pairs that not every column
-// sees once more, and NaN where a column sees one, by a product of their places and what the
-// columns see.
+// After the last pair, where a wave found such values (rare): the pairs that mask_causal cleaned once
+// more (fold_pairs: those that not every column sees whole, or with a block outside the pool), and
+// NaN where a column sees one, by a product of their places and what the columns see.
 __device__ __forceinline__ void spoil_pairs(const PrefillArgs& a, const Q8Pool& pool, int seq, int g, int limit, int last, int first,
                                             int b1, int plain, Running& run) {
   const int lane = threadIdx.x & (kWave - 1);
   const int grp = lane >> 4;
   const int col = lane & 15;
   for (int b0 = first; b0 < b1; b0 += 2 * kWaves) {
-    if ((b0 + 2) * kBlockSize <= plain) continue;
     bool ok[2];
     size_t tile[2];
 #pragma unroll
@@ -124,6 +123,7 @@ __device__ __forceinline__ void spoil_pairs(const PrefillArgs& a, const Q8Pool& 
       ok[x] = b0 + x < b1 && e >= 0 && e < a.num_blocks;
       tile[x] = (size_t)(ok[x] ? e : 0) * a.num_kv_heads + g;
     }
+    if (ok[0] && ok[1] && (b0 + 2) * kBlockSize <= plain) continue;
     VRegs raw;
     issue_v(pool, tile[0], tile[1], grp, col, raw);
     VRows v = exchange(raw, pair_scales(raw.scales));

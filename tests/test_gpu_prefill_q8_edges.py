@@ -1,0 +1,78 @@
+"""bros_attn_prefill_chunk_q8 where values that are not finite meet invalid table
+entries, long tables and keys of the future: they reach the rows that see them and no
+others, in every arrangement of the work."""
+
+import dataclasses
+
+import numpy as np
+import pytest
+
+import oracle
+from paper_2504_09590_amd import workload as W
+from tests import q8_helpers as Q
+from tests.gpu_helpers import announce
+from tests.test_gpu_prefill_q8 import chunks, run
+
+pytestmark = pytest.mark.gpu
+
+# Groups of 16 columns, which the rule takes for the calls here, and units of 128 rows, which it takes
+# where the longest context may have many blocks: by the table's width and the bound, and no workspace for pieces.
+ARRANGEMENTS = ["groups", "units"]
+
+
+def wide(b, width=1900):
+    """The batch with tables of `width` entries, what is behind the contexts' invalid."""
+    more = width - b.block_tables.shape[1]
+    tables = np.pad(b.block_tables, ((0, 0), (0, more)), constant_values=-1)
+    dirs = np.pad(b.dir, ((0, 0), (0, more)), constant_values=-1) if b.dir.ndim == 2 else b.dir
+    return dataclasses.replace(b, block_tables=np.ascontiguousarray(tables), dir=np.ascontiguousarray(dirs))
+
+
+def arranged(q8, how, **kw):
+    if how == "groups":
+        return run(q8, **kw)
+    return run(dataclasses.replace(q8, batch=wide(q8.batch)), with_ws=False, max_ctx=30000, **kw)
+
+
+def place(b, s, pos):
+    """Block and slot of a position of sequence s."""
+    blk, slot = oracle.physical_location(b.block_tables, b.dir, s, np.array([pos]))
+    return int(blk[0]), int(slot[0])
+
+
+def spoilt(q8):
+    """A copy that values may be planted in."""
+    return dataclasses.replace(q8, k=q8.k.copy(), v=q8.v.copy(), scales=q8.scales.copy())
+
+
+def check_spoilt(got_bits, clean_bits, want, what):
+    """Not finite exactly where `want` says, every other output as without the planted values, bit for bit."""
+    odd = ~np.isfinite(oracle.widen(got_bits, "bf16"))
+    assert (odd == want).all(), f"{what}: {(odd & ~want).sum()} outputs too many, {(want & ~odd).sum()} missing"
+    same = want | (got_bits == clean_bits)
+    assert same.all(), f"{what}: {(~same).sum()} other outputs changed"
+
+
+@pytest.mark.parametrize("how", ARRANGEMENTS)
+@pytest.mark.parametrize("c0", [200, 4000])
+def test_a_nan_beside_an_invalid_entry(c0, how):
+    # pairs of blocks whose other block is invalid: far below every row's position, and around it
+    n = 60
+    b = chunks([c0], [n], 4, 2, seed=c0, cls=[W.RT])
+    first = c0 // 16                     # block of the first new row
+    tables = b.block_tables.copy()
+    tables[0, [1, 8, first + 2]] = [-1, b.num_blocks, -7]
+    b = dataclasses.replace(b, block_tables=tables)
+    q8 = Q.held(b, 18)
+    odd = spoilt(q8)
+    want = np.zeros((n, 8, 128), dtype=bool)
+    for pos, head, dim in ((5, 1, 7), (9 * 16 + 3, 0, 120), ((first + 3) * 16 + 2, 1, 64)):
+        blk, slot = place(b, 0, pos)
+        odd.v[blk, head, slot, dim] = 0x7F
+        want[max(0, pos - c0):, 4 * head:4 * head + 4, dim] = True
+    blk, slot = place(b, 0, 9 * 16 + 7)
+    odd.scales[blk, 1, 1, slot] = 255    # a scale that is none: every dim
+    odd.v[blk, 1, slot] = 0x38
+    want[:, 4:] = True
+    announce(f"prefill_q8 NaNs beside invalid entries, {n} rows on {c0}, {how}")
+    check_spoilt(arranged(odd, how), arranged(q8, how), want, how)
