@@ -1182,9 +1182,10 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   int iv = w3;
   // Ring variant, before step ii (a multiple of kRefillTiles): the entries of
   // the kRefillTiles tiles before it give way to those kRefillTiles ahead of
-  // it. Every wave is past the barrier that ended step ii - 1, so nobody
-  // reads the former any more (step ii reads entries of tiles ii .. ii + 5),
-  // and many barriers lie before the first read of the latter.
+  // it. Every wave is past the barrier that ended step ii - 1, so no step
+  // reads the former any more (step ii reads entries of tiles ii .. ii + 5; what
+  // follows the last step reads none), and many barriers lie before the first
+  // read of the latter.
   auto refill = [&]() __attribute__((always_inline)) {
     if constexpr (kRing) {
       if (ii != 0 && (ii & (kRefillTiles - 1)) == 0) {
@@ -1251,13 +1252,15 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   }
   wait_vmem<0>();
   if constexpr (kQ8) {
-    // Rows that see a key whose value is not a number (noted a barrier or more ago; rare).
+    // Rows that see a key whose value is not a number (noted a barrier or more ago; rare). Only
+    // keys of the context have notes. Their directions come from memory: the ring of entries may have
+    // gone on (step ii refills the entries of the tiles before it, the guarded ones among them).
     if (*s_any_nan != 0) {
       for (int t2 = max(guard0, kb); t2 < kb + n_kt; ++t2) {
         for (int r = 0; r < kKeys; ++r) {
           const int b = 2 * t2 + (r >> 4);
-          const int dirv = s_dir[at(b)];
-          const bool sees = dirv != 0 && b * kBlockSize + slot_of_offset(r & 15, dirv) <= qpos;
+          const int dirv = entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(b, nblk - 1));
+          const bool sees = b * kBlockSize + slot_of_offset(r & 15, dirv) <= qpos;
           const v4u_t note = *reinterpret_cast<const v4u_t*>(s_nan + ((t2 - guard0) * kKeys + r) * 8);   // 128 bits, one a dim
 #pragma unroll
           for (int dt = 0; dt < 4; ++dt) {

@@ -76,3 +76,20 @@ def test_a_nan_beside_an_invalid_entry(c0, how):
     want[:, 4:] = True
     announce(f"prefill_q8 NaNs beside invalid entries, {n} rows on {c0}, {how}")
     check_spoilt(arranged(odd, how), arranged(q8, how), want, how)
+
+
+@pytest.mark.parametrize("group,c0,n", [(1, 16320, 128), (2, 16370, 64)])
+def test_a_nan_where_the_table_ring_has_gone_on(group, c0, n):
+    # contexts beyond the table's copy in LDS: 514 tiles of 32 keys, of which the last but one step
+    # takes in entries for those behind tile 512, in the places of tiles up to 511. With 600
+    # empty chunks more there are units enough for the chip, and none is split.
+    b = chunks([c0] + [1] * 600, [n] + [0] * 600, group, 1, seed=group, cls=[W.RT] * 601)
+    q8 = Q.held(dataclasses.replace(b, block_tables=wide(b, 2600).block_tables), 5)
+    odd = spoilt(q8)
+    want = np.zeros((n, group, 128), dtype=bool)
+    for j, dim in ((3, 9), (13, 70), (40, 101), (n - 2, 33)):
+        blk, slot = place(q8.batch, 0, c0 + j)
+        odd.v[blk, 0, slot, dim] = 0xFF
+        want[j:, :, dim] = True
+    announce(f"prefill_q8 NaNs in the new rows, {n} rows on {c0}, G={group}")
+    check_spoilt(run(odd, max_ctx=41000), run(q8, max_ctx=41000), want, f"G={group}")
