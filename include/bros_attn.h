@@ -159,7 +159,9 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  * [2][16], the scales of the K rows and of the V rows, one byte e + 127 per slot for
  * the scale 2^e. A row's e is the least integer, within -100 .. 120, with
  * max |x| <= 448 * 2^e over its finite values; a code is x * 2^-e rounded to the
- * nearest e4m3 value, ties to even; infinities and NaNs are stored as NaN. The
+ * nearest e4m3 value, ties to even; infinities and NaNs are stored as NaN. (A finite
+ * value above 1.9375 * 2^127 is nearest to 2^128, which no bf16 and no fp32 value holds:
+ * it is stored as that, and infinite when read.) The
  * scale belongs to the slot, as the row does: two requests may share a block.
  *
  * A token in no sequence's range is left alone: its q_out row keeps what it held,
@@ -439,7 +441,9 @@ int bros_attn_decode_q8(void* out, const void* q,
  * bros_attn_prefill_chunk: rows, causal limits, max_q_len, max_ctx, and the
  * workspace (optional up to max_ctx 32768, required beyond; sizes by
  * bros_attn_workspace_size(BROS_WS_PREFILL, BROS_BF16, ...)). Rows behind
- * cu_q[num_seqs] keep what out held. bf16 q and out only.
+ * cu_q[num_seqs] keep what out held. bf16 q and out only. Keys and values that are
+ * not finite (NaN codes, values from 2^128 on) reach the rows that see them, whose outputs
+ * are then not finite either, and no others.
  */
 int bros_attn_prefill_chunk_q8(void* out, const void* q, const int32_t* cu_q,
                                int32_t num_q_tokens, int32_t max_q_len,

@@ -609,7 +609,7 @@ __device__ __forceinline__ int paired_id(const PrefillArgs& a, int b, int grid) 
 // values: 512 rows on 16000 tokens 157 us. Loads into registers that stay in flight over
 // several steps of the loop are waited for at its joins.)
 //
-// A value of V that is not a number must reach no row that does not see its key, though the
+// A value of V that is not finite must reach no row that does not see its key, though the
 // products add 0 times it: in tiles that not every row of the unit sees such values are
 // stored as zeros and noted in LDS, and rows that see one are set to NaN at the end. (Looked
 // for in the operands of every such tile instead, a prompt of 301 rows took 15.7 us, not 13.6.)
@@ -831,7 +831,7 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   // (A row's eight lanes write every other chunk, twice to the same banks: 32 cycles a step. With
   // the halves swapped in four of the lanes there are none, and the selects cost as much: 0 to 2 % slower.)
   // V of tile j to the V ring (two slots); FIX: rows that are not context become zeros, and
-  // values that are not numbers, in tiles from guard0 on, zeros and notes.
+  // values that are not finite, in tiles from guard0 on, zeros and notes.
   struct RawV {
     v4u_t codes;
     uint32_t scale;
@@ -853,8 +853,7 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
       uint32_t bad[4], any = 0u;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        bad[i] = ((codes[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // bytes that are the NaN code
-        if (scale == 255u) bad[i] = 0x80808080u;
+        bad[i] = q8::not_finite(codes[i], scale);
         any |= bad[i];
       }
       if (__builtin_amdgcn_ballot_w64(keep && any != 0u) != 0 && kb + j >= guard0) {
@@ -1252,7 +1251,7 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
   }
   wait_vmem<0>();
   if constexpr (kQ8) {
-    // Rows that see a key whose value is not a number (noted a barrier or more ago; rare). Only
+    // Rows that see a key whose value is not finite (noted a barrier or more ago; rare). Only
     // keys of the context have notes. Their directions come from memory: the ring of entries may have
     // gone on (step ii refills the entries of the tiles before it, the guarded ones among them).
     if (*s_any_nan != 0) {

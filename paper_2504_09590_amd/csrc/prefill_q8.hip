@@ -19,7 +19,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_q8_kernel(PrefillArgs a, 
   __shared__ __attribute__((aligned(1024))) uint8_t s_raw[kSlots * kQ8TileBytes];   // V as it is in the pool
   __shared__ __attribute__((aligned(1024))) uint8_t s_vring[2 * kTileBytes];
   __shared__ __attribute__((aligned(256))) uint32_t s_scale[kSlots * kThreads];      // per slot and wave
-  __shared__ __attribute__((aligned(16))) uint16_t s_nan[kGuardKeys * 8];   // per key and 16 dims: values that are not numbers
+  __shared__ __attribute__((aligned(16))) uint16_t s_nan[kGuardKeys * 8];   // per key and 16 dims: values that are not finite
   __shared__ int s_tbl[kMaxTableLds + kTablePad];
   __shared__ int8_t s_dir[kMaxTableLds + kTablePad];
   __shared__ int s_first_bad, s_any_nan;
@@ -59,16 +59,14 @@ namespace dq {
 // start of 9 us (Q's terms, the first tiles, their conversion); here it is 600 workgroups of at most three
 // steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there), 12.2 for 16 rows on
 // 4000 cached tokens in pieces (25.1 there). K and V are read once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
-// the marks of values that are not numbers made inside the step spill or take 0.4 us more.)
+// the marks of values that are not finite made inside the step spill or take 0.4 us more.)
 
-// The bytes of w that are the NaN code as ones, all of them where the row's scale is none.
-__device__ __forceinline__ uint32_t not_numbers(uint32_t w, uint32_t scale) {
-  return scale == 255u ? 0x01010101u : (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-}
+// The bytes of w whose values are not finite, as ones.
+__device__ __forceinline__ uint32_t odd_ones(uint32_t w, uint32_t scale) { return q8::not_finite(w, scale) >> 7; }
 
 // Removes what the lane's column does not see of a pair (slots from `limit` on) and, by selection, V
 // rows that no column does (from `last` on). A row that only some columns see must not reach the
-// others through 0 * NaN: its values that are not numbers become zeros, and `found` is set.
+// others through 0 times infinity or NaN: its values that are not finite become zeros, and `found` is set.
 __device__ __forceinline__ void mask_causal(const PrefillArgs& a, int seq, int limit, int last, int b0, const bool (&ok)[2], int grp,
                                             float (&s)[8], VRows& v, bool& found) {
   uint32_t odd = 0u;
@@ -87,7 +85,7 @@ __device__ __forceinline__ void mask_causal(const PrefillArgs& a, int seq, int l
 #pragma unroll
       for (int i = 0; i < 2; ++i) odd |= (v.row[x][r][i] & 0x7f7f7f7fu) + 0x01010101u;
     }
-    odd |= ((v.scales[x] & 0x7f7f7f7fu) + 0x01010101u) & v.scales[x];
+    odd |= ((v.scales[x] & 0x7f7f7f7fu) + 0x09090909u) & v.scales[x];   // scale bytes from 247 on
   }
   if (__builtin_amdgcn_ballot_w64((odd & 0x80808080u) != 0u) == 0) return;
 #pragma unroll
@@ -97,7 +95,7 @@ __device__ __forceinline__ void mask_causal(const PrefillArgs& a, int seq, int l
       const uint32_t scale = (v.scales[x] >> (8 * r)) & 0xffu;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t m = not_numbers(v.row[x][r][i], scale);
+        const uint32_t m = odd_ones(v.row[x][r][i], scale);
         found |= m != 0u;
         v.row[x][r][i] &= ~(m * 255u);
       }
@@ -137,7 +135,7 @@ __device__ __forceinline__ void spoil_pairs(const PrefillArgs& a, const Q8Pool& 
         const int at = b * kBlockSize + slot_of_offset(slot_of(grp, r), dir);
         const uint32_t scale = (v.scales[x] >> (8 * r)) & 0xffu;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v.row[x][r][i] = ok[x] && at < last ? not_numbers(v.row[x][r][i], scale) : 0u;
+        for (int i = 0; i < 2; ++i) v.row[x][r][i] = ok[x] && at < last ? odd_ones(v.row[x][r][i], scale) : 0u;
         if (ok[x] && at < limit) seen[2 * x + r / 2] |= r % 2 ? 0x3f800000u : 0x3f80u;
       }
     }

@@ -50,6 +50,18 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
 
 // The values of a scale byte and of codes.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// A byte that marks, added to the magnitude of a row's code (below 128), the sum's top bit where
+// the value is not finite in bf16 and fp32: the NaN code, a scale of 255 (none), and values from
+// 2^128 on. These are codes 2^(x - 7) (1 + m / 8), x their exponent field, with x >= 262 - byte: of the
+// scales that an append writes only the largest, 247, has any (256 and up, where a
+// row's largest value lies above 1.9375 * 2^127).
+__device__ __forceinline__ uint32_t not_finite_mark(uint32_t byte) {
+  return byte < 247u ? 1u : byte < 255u ? 8u * (byte - 246u) : 128u;
+}
+// The bytes of w whose values are not finite, as their top bits.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w, uint32_t byte) {
+  return ((w & 0x7f7f7f7fu) + not_finite_mark(byte) * 0x01010101u) & 0x80808080u;
+}
 // Two codes (the low or the high half of w) times the scale, as bf16 (exact).
 template <bool HI>
 __device__ __forceinline__ uint32_t values2_bf16(uint32_t w, float scale) {

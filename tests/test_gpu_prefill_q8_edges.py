@@ -93,3 +93,33 @@ def test_a_nan_where_the_table_ring_has_gone_on(group, c0, n):
         want[j:, :, dim] = True
     announce(f"prefill_q8 NaNs in the new rows, {n} rows on {c0}, G={group}")
     check_spoilt(run(odd, max_ctx=41000), run(q8, max_ctx=41000), want, f"G={group}")
+
+
+@pytest.mark.parametrize("how", ARRANGEMENTS)
+def test_infinite_values_reach_only_rows_that_see_them(how):
+    # codes and scales of 2^128 and more, as the append writes them for finite values above 1.9375 * 2^127
+    # (scale byte 247, code 256) and as larger scale bytes have them, in keys that some rows do not see
+    c0, n = 90, 75
+    b = chunks([c0], [n], 4, 2, seed=44, cls=[W.BE])
+    q8 = Q.held(b, 44)
+    odd = spoilt(q8)
+    row = np.zeros(128)
+    row[7], row[30] = 3.38e38, -3.38e38
+    codes, byte = oracle.encode(row[None])
+    assert byte[0] == 247 and codes[0, 7] == 0x78 and codes[0, 30] == 0xF8
+    want = np.zeros((n, 8, 128), dtype=bool)
+    blk, slot = place(b, 0, c0 + 6)
+    odd.v[blk, 0, slot], odd.scales[blk, 0, 1, slot] = codes[0], 247
+    want[6:, :4, [7, 30]] = True
+    for j, code, by in ((18, 0x70, 248), (41, 0xC0, 254), (70, 0x7E, 250)):
+        blk, slot = place(b, 0, c0 + j)
+        odd.v[blk, 1, slot] = 0
+        odd.v[blk, 1, slot, j] = code
+        odd.scales[blk, 1, 1, slot] = by
+        want[j:, 4:, j] = True
+    announce(f"prefill_q8 infinite values, {how}")
+    got, clean = arranged(odd, how), arranged(q8, how)
+    # (rows that see a planted key have other values too: only those that see none are compared bit for bit)
+    odd_at = ~np.isfinite(oracle.widen(got, "bf16"))
+    assert (odd_at == want).all(), f"{(odd_at & ~want).sum()} outputs too many, {(want & ~odd_at).sum()} missing"
+    assert (got[:6, :4] == clean[:6, :4]).all() and (got[:18, 4:] == clean[:18, 4:]).all()
