@@ -194,13 +194,23 @@ struct Running {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = fast_exp2(s[i] - m_ref);
-    l_part += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     // The weights as a bf16 and the bf16 of what it leaves: 8 bits more for eight
-    // products a pair, which cost the decode nothing measurable.
+    // products a pair, which cost the decode nothing measurable. The total is that of the weights
+    // which the products apply: what many alike keys lose in rounding it loses too. (Of two parts
+    // it takes the fp32 weights: they differ by 2^-16 of them.)
     const v4u_t hi4 = {q8::pack2_bf16(p[0], p[1]), q8::pack2_bf16(p[2], p[3]), q8::pack2_bf16(p[4], p[5]), q8::pack2_bf16(p[6], p[7])};
     v4u_t lo4 = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; kTwoParts && i < 4; ++i) lo4[i] = q8::pack2_bf16(p[2 * i] - bf16_lo(hi4[i]), p[2 * i + 1] - bf16_hi(hi4[i]));
+    if constexpr (kTwoParts) {
+      l_part += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = hi4[i];   // (a bit cast of the vector's element itself reads its first)
+        l_part = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q8::bf16x2_t, two), q8::bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, l_part, false);
+      }
+    }
     const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, hi4), pl = __builtin_bit_cast(bf16x8_t, lo4);
     float sc[2][4];
 #pragma unroll

@@ -123,3 +123,31 @@ def test_infinite_values_reach_only_rows_that_see_them(how):
     odd_at = ~np.isfinite(oracle.widen(got, "bf16"))
     assert (odd_at == want).all(), f"{(odd_at & ~want).sum()} outputs too many, {(want & ~odd_at).sum()} missing"
     assert (got[:6, :4] == clean[:6, :4]).all() and (got[:18, 4:] == clean[:18, 4:]).all()
+
+
+@pytest.mark.parametrize("how", ARRANGEMENTS)
+def test_equal_weights_sum_to_one(how):
+    # Four keys ahead of all others, one in each of the first four pairs of blocks (where a wave's
+    # reference maximum comes from), the others equally far behind them, and V one constant: whatever the
+    # common weight is rounded to, the output is the constant. The others' weight is 2^-3 (1 + 0.0038),
+    # which bf16 rounds down to 2^-3: with some 200 of them, 25 beside 4 in all, numerators of rounded
+    # weights over the sum of those that are not are 0.0032 short, 0.0061 at 1.875, more than half a
+    # bf16 step there (2^-8).
+    # Tolerance: sums in fp32 of at most 209 terms are off by 2 * 209 * 2^-24 = 2.5e-5 of the quotient, far below
+    # half a step, so the constant comes out exactly.
+    c0, n = 200, 9
+    b = chunks([c0], [n], 4, 2, seed=3, cls=[W.RT])
+    k, v = np.zeros(b.k_pool.shape), np.full(b.v_pool.shape, 1.875)
+    for pos in (2, 34, 66, 98):
+        blk, slot = place(b, 0, pos)
+        k[blk, :, slot, :2] = 1.0
+    (kc, ks), (vc, vs) = oracle.encode(k), oracle.encode(v)
+    q = np.zeros(b.q_prefill.shape)
+    q[..., 0], q[..., 1] = 23.5, -0.0166
+    ahead = (23.5 - 0.0166) / np.sqrt(128) / np.log(2)             # in powers of two
+    assert 0.0036 < 2.0 ** (3 - ahead) - 1 < 2.0 ** -8             # the others' weight: a little above 2^-3, less than half a step
+    b = dataclasses.replace(b, q_prefill=W._to_bf16_bits(q.astype(np.float32)))
+    q8 = Q.Q8Batch(b, kc, vc, np.ascontiguousarray(np.stack([ks, vs], axis=2)))
+    announce(f"prefill_q8 equal weights, {how}")
+    got = oracle.widen(arranged(q8, how), "bf16")
+    assert (got == 1.875).all(), f"off by up to {np.abs(got - 1.875).max()}"
