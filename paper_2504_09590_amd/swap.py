@@ -205,7 +205,14 @@ class PlanExecutor:
             bros.bros_copy_dma(a, b, n * b[0].numel() * b.element_size(), stream=stream)
 
     def execute(self, req: int, plan, stream=None) -> None:
+        """Carries the plan out for request `req`, on `stream` (default: the current one)."""
         stream = stream if stream is not None else torch.cuda.current_stream()
+        # (`stream` made the current one: the ids are uploaded in its order, and their memory is free
+        # for other tensors of that stream only, behind the kernels that read them)
+        with torch.cuda.stream(stream):
+            self._carry_out(req, plan, stream)
+
+    def _carry_out(self, req: int, plan, stream) -> None:
         for lo in range(0, len(plan.victims), self.max_rows):
             part = plan.victims[lo:lo + self.max_rows]
             n = len(part)
