@@ -196,6 +196,7 @@ class PlanExecutor:
         self.staging = [torch.empty(s, dtype=p.dtype, device=p.device) for s, p in zip(shapes, self.pools)]
         self.host = [torch.empty(s, dtype=p.dtype, pin_memory=True) for s, p in zip(shapes, self.pools)]
         self.store = {}        # (request, position) -> the row of each staging buffer, on the host
+        self._done = None      # the end of the last plan, on its stream
 
     def _ids(self, ids):
         return torch.from_numpy(np.ascontiguousarray(ids, dtype=np.int32)).to(self.pools[0].device)
@@ -210,7 +211,10 @@ class PlanExecutor:
         # (`stream` made the current one: the ids are uploaded in its order, and their memory is free
         # for other tensors of that stream only, behind the kernels that read them)
         with torch.cuda.stream(stream):
+            if self._done is not None:
+                stream.wait_event(self._done)     # (a plan on another stream may still use the staging)
             self._carry_out(req, plan, stream)
+            self._done = stream.record_event()
 
     def _carry_out(self, req: int, plan, stream) -> None:
         for lo in range(0, len(plan.victims), self.max_rows):

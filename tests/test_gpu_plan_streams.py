@@ -1,4 +1,4 @@
-"""PlanExecutor on a stream that is not the current one and is held back by earlier work."""
+"""PlanExecutor on streams that are not the current one and are held back by earlier work."""
 
 import types
 
@@ -76,3 +76,25 @@ def test_on_a_held_stream(eight):
         put(h, back, was)
     assert all(np.array_equal(a, b) for a, b in zip(bits(ps), host))
     assert all(int((t != 5).sum()) == 0 for t in other) and not ex.store
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_plans_on_two_streams(eight):
+    # the first waits behind earlier work; the second, on a free stream, takes the same staging buffers
+    torch = require_gpu()
+    ps = pools(eight)
+    ex = executor(ps)
+    ids = np.random.default_rng(2).permutation(NB * 16)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    announce(f"plans on two streams, eight={eight}")
+    torch.cuda.synchronize()
+    host = bits(ps)
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(HELD)
+    ex.execute(1, plan(move=(ids[:8], ids[8:16])), stream=a)
+    ex.execute(2, plan(move=(ids[16:24], ids[24:32])), stream=b)
+    torch.cuda.synchronize()
+    for h in host:
+        put(h, ids[8:16], rows(h, ids[:8]).copy())
+        put(h, ids[24:32], rows(h, ids[16:24]).copy())
+    assert all(np.array_equal(x, y) for x, y in zip(bits(ps), host))

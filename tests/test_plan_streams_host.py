@@ -1,5 +1,6 @@
-"""PlanExecutor makes its id lists on the stream that it is given (no GPU): their memory is then
-handed out again in that stream's order only, behind the kernels that read them."""
+"""PlanExecutor's plans on streams of the caller's (no GPU). It makes a plan's id lists on the plan's
+stream: their memory is then handed out again in that stream's order only, behind the
+kernels that read them. And a plan waits for the one before it: they share the staging."""
 
 import contextlib
 import types
@@ -13,8 +14,24 @@ pytest.importorskip("paper_2504_09590_amd.bros", reason="libbros_attn.so not bui
 from paper_2504_09590_amd import swap  # noqa: E402
 
 
-def test_ids_are_made_on_the_given_stream(monkeypatch):
-    current, seen = ["the current stream"], []
+class Stream:
+    def __init__(self, name, log):
+        self.name, self.log = name, log
+
+    def synchronize(self):
+        pass
+
+    def record_event(self):
+        self.log.append(("end", self.name))
+        return f"end of {self.name}'s plan"
+
+    def wait_event(self, e):
+        self.log.append(("wait", self.name, e))
+
+
+def executor(monkeypatch, log):
+    """An executor without a device; what it does goes to `log`."""
+    current = ["the current stream"]
 
     @contextlib.contextmanager
     def stream(s):
@@ -31,14 +48,30 @@ def test_ids_are_made_on_the_given_stream(monkeypatch):
             self._gather = self._scatter = lambda *a, **kw: None
             self.max_rows, self.store = 2, {(3, 0): (torch.zeros(2),) * 2, (3, 1): (torch.zeros(2),) * 2}
             self.staging = self.host = [torch.zeros((2, 2))] * 2
-            self.at = types.SimpleNamespace(synchronize=lambda: None)
+            self._done = None
 
         def _ids(self, ids):
-            seen.append(current[-1])
+            log.append(("ids", current[-1]))
             return super()._ids(ids)
 
-    ex = Watched()
+    return Watched()
+
+
+def test_ids_are_made_on_the_given_stream(monkeypatch):
+    log = []
+    ex, at = executor(monkeypatch, log), Stream("side", log)
     plan = types.SimpleNamespace(victims=np.array([[4, 0, 1, 2]]), move_src=np.array([1, 2, 3]), move_dst=np.array([5, 6, 7]),
                                  restore_pos=np.array([0, 1]), restore_dst=np.array([8, 9]))
-    ex.execute(3, plan, stream=ex.at)
-    assert len(seen) == 6 and all(s is ex.at for s in seen)
+    ex.execute(3, plan, stream=at)
+    assert [x[1] for x in log if x[0] == "ids"] == [at] * 6
+
+
+def test_a_plan_waits_for_the_one_before(monkeypatch):
+    log = []
+    ex = executor(monkeypatch, log)
+    plan = types.SimpleNamespace(victims=np.zeros((0, 4), dtype=int), move_src=np.array([1]), move_dst=np.array([5]),
+                                 restore_pos=np.array([]), restore_dst=np.array([]))
+    a, b = Stream("a", log), Stream("b", log)
+    ex.execute(3, plan, stream=a)
+    ex.execute(3, plan, stream=b)
+    assert log == [("ids", a), ("ids", a), ("end", "a"), ("wait", "b", "end of a's plan"), ("ids", b), ("ids", b), ("end", "b")]
