@@ -147,7 +147,8 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  *              (three views of one projection's output, or three tensors). dtype
  *              is theirs, that of the norm's weights and of q_out.
  *   q_out    : [num_new_tokens][num_q_heads][head_dim]; may be q itself where q's
- *              tokens are contiguous. q and q_out NULL: no q rows (num_q_heads 0).
+ *              tokens are contiguous, and must not overlap the rows of q, k and v
+ *              otherwise. q and q_out NULL: no q rows (num_q_heads 0).
  *   norm     : NULL: none. A weight that is NULL leaves its rows without a norm.
  *   rope     : NULL: no rotation.
  *   rope_pos : int32 [axes][num_new_tokens], device; NULL (one axis only): the
@@ -170,8 +171,8 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  * token without a valid table entry gets its q rows and is not stored.
  *
  * Errors as bros_kv_write; also BROS_E_SHAPE for a stride below a token's rows or
- * one that is not a multiple of 16 bytes, q without q_out, more than 2^29 - 32
- * head rows, a rotary_dim outside 16 .. head_dim or not a multiple of 16, axes outside
+ * one that is not a multiple of 16 bytes, a q_out that overlaps rows of q, k or v,
+ * q without q_out, more than 2^29 - 32 head rows, a rotary_dim outside 16 .. head_dim or not a multiple of 16, axes outside
  * 1 .. 4, axes without rope_pos, or sections that do not add up to rotary_dim / 2.
  */
 enum bros_rope_pairs { BROS_ROPE_HALF = 0,       /* pair i: dims i and i + rotary_dim / 2 */

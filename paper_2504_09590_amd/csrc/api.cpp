@@ -124,6 +124,17 @@ int qkv_append(const char* fn, bool eight, void* q_out, const void* q, const voi
   if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
       !aligned(kv_scales, 16) || (norm && (!aligned(norm->q_weight, 16) || !aligned(norm->k_weight, 16))))
     return fail(BROS_E_SHAPE, "%s: tensors must be 16-byte aligned", fn);
+  // Workgroups read rows while others write theirs: q_out must not meet rows still to be read, but for q
+  // where every row lies in its place.
+  const auto meets = [&](const void* rows, int64_t stride, int32_t heads) {
+    const uint64_t elem = 16 / per16, len = (uint64_t)heads * head_dim * elem, step = (uint64_t)stride * elem;
+    const uint64_t out = reinterpret_cast<uintptr_t>(q_out), first = reinterpret_cast<uintptr_t>(rows);
+    const uint64_t i = out < first + len ? 0 : (out - first - len) / step + 1;   // the first token that ends behind out
+    return i < (uint64_t)num_new_tokens && first + i * step < out + (uint64_t)num_new_tokens * hq * head_dim * elem;
+  };
+  const bool in_place = q_out == q && (num_new_tokens == 1 || q_stride == (int64_t)hq * head_dim);
+  if (q && ((!in_place && meets(q, q_stride, hq)) || meets(k, k_stride, num_kv_heads) || meets(v, v_stride, num_kv_heads)))
+    return fail(BROS_E_SHAPE, "%s: q_out overlaps rows of q, k or v (only q itself, with contiguous tokens, may be q_out)", fn);
   a.q = q;
   a.k = k;
   a.v = v;
