@@ -199,6 +199,8 @@ class Rope:
         sections = () if sections is None else tuple(int(x) for x in sections)
         if len(sections) > 4:
             raise ValueError(f"{len(sections)} sections; at most 4")
+        if sections and (min(sections) < 0 or 2 * sum(sections) != table.shape[1]):
+            raise ValueError(f"sections {sections} must add up to the {table.shape[1] // 2} pairs of the table")
         self.table = table
         self.device = table.get_device()
         self.axes = max(len(sections), 1)

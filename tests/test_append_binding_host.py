@@ -1,0 +1,19 @@
+"""What the binding of the append takes and turns down (no GPU: what passes its checks of
+shapes fails the device check, never a launch)."""
+
+import pytest
+import torch
+
+from tests.test_q8_host import bros
+
+
+@pytest.mark.parametrize("sections", [(63,), (65,), (128,), (0,), (16, 24, 23), (70, -6), (16, 24, 24, 1)])
+def test_sections_that_do_not_fit_the_table(sections):
+    with pytest.raises(ValueError, match="sections"):
+        bros.Rope(torch.zeros((9, 128)), sections=sections)
+
+
+def test_sections_that_fit():
+    assert bros.Rope(torch.zeros((9, 128)), sections=(64,)).axes == 1
+    assert bros.Rope(torch.zeros((9, 96)), sections=(0, 24, 24)).axes == 3
+    assert bros.Rope(torch.zeros((9, 96))).axes == 1
