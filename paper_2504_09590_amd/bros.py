@@ -290,9 +290,9 @@ def _append_args(q_out, q, k, v, block_tables, dir, cls, pos0, cu_new, rope, rop
     if kh != hkv or vh != hkv:
         raise ValueError(f"k and v must have the pool's {hkv} heads")
     qp, qs, hq = None, 0, 0
-    if q is None:
-        q_out = None
-    else:
+    if (q is None) != (q_out is None):
+        raise ValueError("give both q and q_out, or neither")
+    if q is not None:
         qp, qs, hq = _token_rows(q, "q", tn, d, dtype)
         if q_out.shape != q.shape or q_out.dtype is not dtype:
             raise ValueError("q_out must have q's shape and type")

@@ -4,7 +4,7 @@ shapes fails the device check, never a launch)."""
 import pytest
 import torch
 
-from tests.test_q8_host import bros
+from tests.test_q8_host import bros, py_call
 
 
 @pytest.mark.parametrize("sections", [(63,), (65,), (128,), (0,), (16, 24, 23), (70, -6), (16, 24, 24, 1)])
@@ -17,3 +17,11 @@ def test_sections_that_fit():
     assert bros.Rope(torch.zeros((9, 128)), sections=(64,)).axes == 1
     assert bros.Rope(torch.zeros((9, 96)), sections=(0, 24, 24)).axes == 3
     assert bros.Rope(torch.zeros((9, 96))).axes == 1
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(q_out=None)])
+def test_q_and_q_out_come_together(kw):
+    with pytest.raises(ValueError, match="both q and q_out"):
+        py_call(**kw)
+    with pytest.raises(ValueError, match="current device"):
+        py_call(q=None, q_out=None)
