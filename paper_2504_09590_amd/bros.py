@@ -276,7 +276,7 @@ def _token_rows(t, name: str, tokens: int, d: int, dtype):
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[0] != tokens or t.dtype is not dtype or shape[2] != d:
         raise ValueError(f"{name} must be [{tokens}][heads][{d}] {dtype}")
-    if stride[2] != 1 or stride[1] != d:
+    if stride[2] != 1 or (stride[1] != d and shape[1] != 1):   # (one head's stride is never used)
         raise ValueError(f"{name}'s heads must be contiguous within a token")
     # (one token's stride, or none's, is never used)
     return t.data_ptr(), (stride[0] if tokens > 1 else shape[1] * d), shape[1]

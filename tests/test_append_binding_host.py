@@ -4,7 +4,7 @@ shapes fails the device check, never a launch)."""
 import pytest
 import torch
 
-from tests.test_q8_host import bros, py_call
+from tests.test_q8_host import bros, py_call, rows
 
 
 @pytest.mark.parametrize("sections", [(63,), (65,), (128,), (0,), (16, 24, 23), (70, -6), (16, 24, 24, 1)])
@@ -25,3 +25,12 @@ def test_q_and_q_out_come_together(kw):
         py_call(**kw)
     with pytest.raises(ValueError, match="current device"):
         py_call(q=None, q_out=None)
+
+
+def test_one_head_of_many():
+    # one KV head as every fourth of a wider tensor: contiguous within a token, whatever the heads' stride says
+    pool = torch.zeros((4, 1, 16, 128), dtype=torch.bfloat16)
+    k = rows(5, 4)[:, ::4]
+    assert k.shape == (5, 1, 128) and k.stride(1) != 128
+    with pytest.raises(ValueError, match="current device"):
+        py_call(k=k, v=k, k_pool=pool, v_pool=pool)
