@@ -442,7 +442,9 @@ int bros_attn_decode_q8(void* out, const void* q,
  * bros_attn_prefill_chunk: rows, causal limits, max_q_len, max_ctx, and the
  * workspace (optional up to max_ctx 32768, required beyond; sizes by
  * bros_attn_workspace_size(BROS_WS_PREFILL, BROS_BF16, ...)). Rows behind
- * cu_q[num_seqs] keep what out held. bf16 q and out only. Keys and values that are
+ * cu_q[num_seqs] keep what out held. bf16 q and out only. A q row may be taken in two
+ * e4m3 terms: its values down to 2^-13 of the row's largest are exact, smaller ones off by up to
+ * 2^-21 of that; softmax weights are rounded to bf16, as in the 16-bit prefill. Keys and values that are
  * not finite (NaN codes, values from 2^128 on) reach the rows that see them, whose outputs
  * are then not finite either, and no others.
  */

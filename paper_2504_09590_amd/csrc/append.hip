@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   // This lane's part of the workgroup's head row tid / 8: token t0 + tok, head h of q, k or v.
   const int lane8 = tid % kLanes;
   int tok = 0, h = head0 + tid / kLanes;
-  while (h >= heads) {   // (at most kRows / 3 rounds, for one q, one k and one v row per token)
+  while (h >= heads) {   // (at most kRows / 2 rounds: without q rows a token may have one k and one v row)
     h -= heads;
     ++tok;
   }

@@ -225,9 +225,9 @@ inline bool q8_decode_by_waves(int64_t segments, int64_t blocks, int64_t compute
 // (prefill_q8_rows_kernel), instead of units of 128 rows, and in how many pieces of `split_blocks` blocks:
 // while the groups fit the chip at once (three to a compute unit) and their steps, groups times blocks,
 // stay few. Pieces (partials and a merge, 4 us) are as many as give every compute unit one. Calls in us, units
-// / groups (32 / 8 heads): 128 rows of a prompt 11.4 / 6.3, 301 14.6 / 10.6, 64 rows on 500 cached tokens 19.9 /
-// 8.9, 16 on 4000 25.1 / 12.2 (28.1 in one piece); not taken: 301 (64 / 8 heads) 15.7 / 17.5. Of 645 calls of up to
-// 1500 rows on up to 40000 tokens the 435 it takes run in 0.59 of the time in the mean, the worst in 1.06, and
+// / groups (32 / 8 heads, calls of one graph): 128 rows of a prompt 11.8 / 6.9, 301 15.1 / 11.3, 64 rows on 500 cached
+// tokens 20.3 / 9.5, 16 on 4000 25.3 / 13.1; not taken: 301 (64 / 8 heads) 16.0 / 18.0. Of 645 calls of up to
+// 1480 rows on 150 to 40000 tokens the 435 it takes run in 0.59 of the time in the mean, the worst in 1.06, and
 // all calls 2 % above the best of both and ten numbers of pieces. `slots`: partial rows that the workspace holds.
 inline bool plan_q8_prefill_rows(int64_t groups, int64_t blocks, int64_t compute_units, int64_t slots, int32_t* split_blocks,
                                  int32_t* pieces) {

@@ -600,8 +600,8 @@ __device__ __forceinline__ int paired_id(const PrefillArgs& a, int b, int grid) 
 // K stays in 8 bits: its rows go to LDS as they are, and S^T = K Q^T runs on the scaled
 // 8-bit products, which take each row's scale byte. Q is given to them as two e4m3 terms,
 // the second what the first leaves, four binades lower: a bf16 value has 8 significant
-// bits, each term holds 4, so the terms add up to it exactly (below 2^-14 of the row's
-// largest value to 2^-22 of that). Twice the products at twice the rate, half of
+// bits, each term holds 4, so the terms add up to it exactly (below 2^-13 of the row's
+// largest value to 2^-21 of that). Twice the products at twice the rate, half of
 // K's LDS traffic and no conversion. V has a scale per key, along the products' inner
 // dimension, where they take one for 32, so its rows become bf16 values: they go to LDS as they are
 // too, and a step before a tile is used each wave reads its own eight rows back and writes
@@ -612,7 +612,7 @@ __device__ __forceinline__ int paired_id(const PrefillArgs& a, int b, int grid) 
 // A value of V that is not finite must reach no row that does not see its key, though the
 // products add 0 times it: in tiles that not every row of the unit sees such values are
 // stored as zeros and noted in LDS, and rows that see one are set to NaN at the end. (Looked
-// for in the operands of every such tile instead, a prompt of 301 rows took 15.7 us, not 13.6.)
+// for in the operands of every such tile instead, a prompt of 301 rows took 2.1 us longer.)
 template <int G, bool kOff32, bool kRing, bool kQ8 = false>
 __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8_t* s_kring, uint8_t* s_vring,
                                              int* s_first_bad_p, int* s_tbl, int8_t* s_dir,
@@ -986,7 +986,8 @@ __device__ __forceinline__ void prefill_unit(const PrefillArgs& a, int id, uint8
     m_prev = m_run;
     m_run = mx > m_run + kRescaleSlack ? mx : m_run;
   };
-  // P = exp2(S * scale - m) rounded to bf16 (the P^T operands); the row sums
+  // P = exp2(S * scale - m) rounded to bf16 (the P^T operands): one part, as a second
+  // would double the PV products, half of a step's; the row sums
   // add exactly these rounded weights, the ones the PV product applies. Operand c2 (16 keys) holds accumulators 8*c2 .. 8*c2 + 7.
   auto probs = [&](bf16x8_t (&pf)[2], const floatx16& cur) __attribute__((always_inline)) {
 #pragma unroll

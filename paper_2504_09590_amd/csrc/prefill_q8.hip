@@ -2,8 +2,8 @@
 // 8-bit pool. Units, pieces and their merge are the 16-bit prefill's.
 //
 // The matrix cores bound it from a few dozen rows on: 512 rows on 16000 cached tokens,
-// 32 / 8 heads, 144 us, 946 TFLOP/s of the formula's products (the 16-bit prefill 143 us; a
-// large library product 1208 TFLOP/s). Few rows on short contexts run in smaller groups (below).
+// 32 / 8 heads, 142 us, 960 TFLOP/s of the formula's products (the 16-bit prefill over the same values
+// 135 us; a large library product 1208 TFLOP/s). Few rows on short contexts run in smaller groups (below).
 #include "decode_q8_device.h"
 #include "plan.h"
 #include "prefill_device.h"
@@ -57,8 +57,8 @@ namespace dq {
 //
 // In the other kernel a prompt of 301 rows is 80 chains of up to ten steps, one after another, behind a
 // start of 9 us (Q's terms, the first tiles, their conversion); here it is 600 workgroups of at most three
-// steps a wave. Latency bounds it: 5.2 us for 16 rows, 10.6 for the 301 (14.6 there), 12.2 for 16 rows on
-// 4000 cached tokens in pieces (25.1 there). K and V are read once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
+// steps a wave. Latency bounds it: 5.7 us for 16 rows, 11.3 for the 301 (15.1 there; calls of one graph), 13.1 for 16
+// rows on 4000 cached tokens in pieces (25.3 there). K and V are read once per 16 columns, from L2. (Two bf16 parts for the weights, as in the decode, take 2 to 8 % longer;
 // the marks of values that are not finite made inside the step spill or take 0.4 us more.)
 
 // The bytes of w whose values are not finite, as ones.

@@ -21,8 +21,8 @@ typedef unsigned v4u_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2_t;
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float float2_t;
 
-// Exponents a row may take. Below, 2^e times the smallest code would leave the
-// normal range of bf16; above, no finite fp32 row reaches.
+// Exponents a row may take. The smallest code, 2^-9, times 2^e stays a normal bf16 value down to
+// e = -117; -100 is that with a margin. Above 120 no finite fp32 row reaches.
 constexpr int kMinExp = -100, kMaxExp = 120;
 constexpr uint32_t kNaNBits = 0x7fc00000u;
 
