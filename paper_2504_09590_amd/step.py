@@ -233,7 +233,7 @@ class QkvStep:
             raise ValueError("every sequence behind the prefill chunks must have one new token")
         if not np.array_equal(batch.cu_q, batch.cu_new[:P + 1]):
             raise ValueError("the prefill rows must be the chunks' new tokens")
-        if kv_scales is not None and batch.dtype != "bf16":
+        if kv_scales is not None and batch.dtype == "f32":
             raise ValueError(f"an 8-bit cache takes bf16 rows, not {batch.dtype}")   # (its attentions do)
         self.batch, self.dev, self.rope, self.norm, self.kv_scales = batch, dev, rope, norm, kv_scales
         self.P, self.S = P, S
