@@ -162,7 +162,8 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  * max |x| <= 448 * 2^e over its finite values; a code is x * 2^-e rounded to the
  * nearest e4m3 value, ties to even; infinities and NaNs are stored as NaN. (A finite
  * value above 1.9375 * 2^127 is nearest to 2^128, which no bf16 and no fp32 value holds:
- * it is stored as that, and infinite when read.) The
+ * it is stored as that, and infinite when read.) Appends write the bytes 27 .. 247; 255 is the
+ * scale of no number: every value of such a row is NaN, so a cache may be filled with it. The
  * scale belongs to the slot, as the row does: two requests may share a block.
  *
  * A token in no sequence's range is left alone: its q_out row keeps what it held,
@@ -445,7 +446,7 @@ int bros_attn_decode_q8(void* out, const void* q,
  * cu_q[num_seqs] keep what out held. bf16 q and out only. A q row may be taken in two
  * e4m3 terms: its values down to 2^-13 of the row's largest are exact, smaller ones off by up to
  * 2^-21 of that; softmax weights are rounded to bf16, as in the 16-bit prefill. Keys and values that are
- * not finite (NaN codes, values from 2^128 on) reach the rows that see them, whose outputs
+ * not finite (NaN codes, a scale byte of 255, values from 2^128 on) reach the rows that see them, whose outputs
  * are then not finite either, and no others.
  */
 int bros_attn_prefill_chunk_q8(void* out, const void* q, const int32_t* cu_q,

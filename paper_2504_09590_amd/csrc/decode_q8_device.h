@@ -129,7 +129,12 @@ __device__ __forceinline__ void pair_scores(const KRegs& k, const v4u_t (&qf)[4]
   for (int x = 0; x < 2; ++x) {
     const floatx4_t sc = block_products(k.lo[x], k.hi[x], qf);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s[4 * x + r] = sc[r] * scale_log2 * byte_scale(ps.w[x][0], r);
+    for (int r = 0; r < 4; ++r) {
+      // (byte 255, the scale of no number, is infinite here: added to the score it makes NaN of what would else be
+      // an infinity, and a key without weight where it is negative)
+      const float f = byte_scale(ps.w[x][0], r);
+      s[4 * x + r] = fmaf(sc[r] * scale_log2, f, f - f);
+    }
   }
 }
 

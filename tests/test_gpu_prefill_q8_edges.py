@@ -151,3 +151,20 @@ def test_equal_weights_sum_to_one(how):
     announce(f"prefill_q8 equal weights, {how}")
     got = oracle.widen(arranged(q8, how), "bf16")
     assert (got == 1.875).all(), f"off by up to {np.abs(got - 1.875).max()}"
+
+
+@pytest.mark.parametrize("how", ARRANGEMENTS)
+def test_rows_without_a_scale(how):
+    # scale byte 255, K's and V's, in a key that all rows see and in keys that some do; codes of one sign, of zero
+    c0, n = 100, 50
+    b = chunks([c0], [n], 4, 6, seed=45, cls=[W.RT])
+    q8 = Q.held(b, 45)
+    odd = spoilt(q8)
+    want = np.zeros((n, 24, 128), dtype=bool)
+    for h, (pos, codes, which) in enumerate(((20, odd.k, 0), (120, odd.k, 0), (21, odd.v, 1), (123, odd.v, 1), (22, odd.v, 1), (130, odd.v, 1))):
+        blk, slot = place(b, 0, pos)
+        codes[blk, h, slot] = 0x30 if h < 4 else 0
+        odd.scales[blk, h, which, slot] = 255
+        want[max(0, pos - c0):, 4 * h:4 * h + 4] = True
+    announce(f"prefill_q8 rows without a scale, {how}")
+    check_spoilt(arranged(odd, how), arranged(q8, how), want, how)
