@@ -152,22 +152,36 @@ def test_a_query_that_is_not_finite_stays_alone():
     check(q8, got, "the other rows")
 
 
-def test_far_blocks():
-    # rows beyond 32-bit byte offsets: the variant with 64-bit ones
+@pytest.mark.parametrize("group,hkv,ring", [(1, 8, False), (2, 8, False), (4, 8, False), (8, 8, False), (1, 8, True), (2, 8, True), (4, 8, True),
+                                            (8, 8, True)])
+def test_far_blocks(group, hkv, ring):
+    # rows beyond 32-bit byte offsets: the variants with 64-bit ones, tables whole in LDS and through its ring
     torch = require_gpu()
     from paper_2504_09590_amd import bros
-    nb, hkv = 300000, 8
-    b = chunks([150, 0], [70, 200], 2, hkv, seed=17, cls=[W.RT] * 2)
+    nb = 300000
+    b = chunks([150, 0], [70, 200], group, hkv, seed=17, cls=[W.RT] * 2)
     q8 = Q.held(b, 17)
     up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()  # noqa: E731
     far = [torch.full((nb,) + x.shape[1:], 0x7F, dtype=torch.uint8, device="cuda") for x in (q8.k, q8.v, q8.scales)]
     for x, y in zip(far, (q8.k, q8.v, q8.scales)):
         x[nb - b.num_blocks:] = up(y)
-    tables = wide(b).block_tables
+    tables = wide(b, 2600 if ring else 1900).block_tables
     tables = np.where(tables >= 0, tables + (nb - b.num_blocks), tables).astype(np.int32)
     q = bros._tensor(b.q_prefill, "bf16", "cuda")
     out = torch.full_like(q, 7.0)
-    announce("prefill_q8 units in blocks beyond 4 GiB")
-    bros.bros_attn_prefill_chunk_q8(out, q, up(b.cu_q), 200, *far, up(tables), up(b.dir), None, up(b.ctx_lens), 30000)
+    bound = 41000 if ring else 30000
+    ws = None
+    if ring:
+        size = bros.bros_attn_workspace_size(bros.BROS_WS_PREFILL, bros.BROS_BF16, q.shape[0], hkv * group, 128, bound)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    announce(f"prefill_q8 units in blocks beyond 4 GiB, G={group}, ring={ring}")
+    bros.bros_attn_prefill_chunk_q8(out, q, up(b.cu_q), 200, *far, up(tables), up(b.dir), None, up(b.ctx_lens), bound, workspace=ws)
     torch.cuda.synchronize()
-    check(q8, bros.to_host_bits(out), "far blocks")
+    check(q8, bros.to_host_bits(out), f"far blocks, G={group}")
+
+
+def test_eight_heads_through_the_ring():
+    b = chunks([150, 0], [70, 200], 8, 2, seed=18, cls=[W.BE] * 2)
+    q8 = Q.poison(Q.held(b, 18), owned_mask(b))
+    announce("prefill_q8 units, a ring of table entries, G=8")
+    check(q8, run(dataclasses.replace(q8, batch=wide(q8.batch, 2600)), max_ctx=41000), "G=8")
