@@ -213,8 +213,10 @@ class PlanExecutor:
         with torch.cuda.stream(stream):
             if self._done is not None:
                 stream.wait_event(self._done)     # (a plan on another stream may still use the staging)
-            self._carry_out(req, plan, stream)
-            self._done = stream.record_event()
+            try:
+                self._carry_out(req, plan, stream)
+            finally:   # (also behind the part of a plan that failed)
+                self._done = stream.record_event()
 
     def _carry_out(self, req: int, plan, stream) -> None:
         for lo in range(0, len(plan.victims), self.max_rows):

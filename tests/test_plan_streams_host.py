@@ -75,3 +75,16 @@ def test_a_plan_waits_for_the_one_before(monkeypatch):
     ex.execute(3, plan, stream=a)
     ex.execute(3, plan, stream=b)
     assert log == [("ids", a), ("ids", a), ("end", "a"), ("wait", "b", "end of a's plan"), ("ids", b), ("ids", b), ("end", "b")]
+
+
+def test_a_plan_waits_for_one_that_failed(monkeypatch):
+    log = []
+    ex = executor(monkeypatch, log)
+    nothing = np.zeros((0, 4), dtype=int)
+    lost = types.SimpleNamespace(victims=nothing, move_src=np.array([1]), move_dst=np.array([5]), restore_pos=np.array([77]),
+                                 restore_dst=np.array([8]))
+    with pytest.raises(KeyError):      # (a row that was never saved; its moves are on the way)
+        ex.execute(3, lost, stream=Stream("a", log))
+    ex.execute(3, types.SimpleNamespace(victims=nothing, move_src=np.array([1]), move_dst=np.array([5]), restore_pos=np.array([]),
+                                        restore_dst=np.array([])), stream=Stream("b", log))
+    assert [x for x in log if x[0] != "ids"] == [("end", "a"), ("wait", "b", "end of a's plan"), ("end", "b")]
