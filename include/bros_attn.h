@@ -161,7 +161,7 @@ int bros_kv_write(const void* k_new, const void* v_new, int32_t num_new_tokens,
  * the scale 2^e. A row's e is the least integer, within -100 .. 120, with
  * max |x| <= 448 * 2^e over its finite values; a code is x * 2^-e rounded to the
  * nearest e4m3 value, ties to even; infinities and NaNs are stored as NaN. (A finite
- * value above 1.9375 * 2^127 is nearest to 2^128, which no bf16 and no fp32 value holds:
+ * value of 1.9375 * 2^127 or more is nearest to 2^128, which no bf16 and no fp32 value holds:
  * it is stored as that, and infinite when read.) Appends write the bytes 27 .. 247; 255 is the
  * scale of no number: every value of such a row is NaN, so a cache may be filled with it. The
  * scale belongs to the slot, as the row does: two requests may share a block.

@@ -53,8 +53,8 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 // A byte that marks, added to the magnitude of a row's code (below 128), the sum's top bit where
 // the value is not finite in bf16 and fp32: the NaN code, a scale of 255 (none), and values from
 // 2^128 on. These are codes 2^(x - 7) (1 + m / 8), x their exponent field, with x >= 262 - byte: of the
-// scales that an append writes only the largest, 247, has any (256 and up, where a
-// row's largest value lies above 1.9375 * 2^127).
+// scales that an append writes only the largest, 247, has any (256, for a
+// finite value of 1.9375 * 2^127 or more).
 __device__ __forceinline__ uint32_t not_finite_mark(uint32_t byte) {
   return byte < 247u ? 1u : byte < 255u ? 8u * (byte - 246u) : 128u;
 }
