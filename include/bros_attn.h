@@ -86,7 +86,7 @@ enum bros_status {
   BROS_E_TABLE = -7,       /* bros_check_batch found an inconsistent batch               */
   BROS_E_NOMEM = -8        /* the block manager found no block for a request            */
 };
-enum bros_workspace_kind { BROS_WS_DECODE = 0, BROS_WS_PREFILL = 1 };
+enum bros_workspace_kind { BROS_WS_DECODE = 0, BROS_WS_PREFILL = 1, BROS_WS_TREE = 2, BROS_WS_LATENT = 3 };
 
 /* Static string naming a status code. */
 const char* bros_status_str(int status);
@@ -336,7 +336,9 @@ int bros_attn_mixed(void* out_prefill, const void* q_prefill, const int32_t* cu_
  * (num_seqs for decode, num_q_tokens for prefill). Pure host arithmetic; it
  * does not know num_kv_heads and sizes bf16 decode for groups of up to 8
  * query heads. For the bf16 prefill with max_ctx <= 32768 it returns the size
- * of the optional split workspace, the same for every call. Returns 0 for
+ * of the optional split workspace, the same for every call. BROS_WS_TREE and
+ * BROS_WS_LATENT are the workspaces of bros_attn_tree (head_dim 128) and of
+ * bros_attn_latent (head_dim 576), one size for every call. Returns 0 for
  * unsupported arguments.
  */
 size_t bros_attn_workspace_size(int32_t kind, int32_t dtype, int32_t num_rows,
@@ -484,6 +486,142 @@ int bros_kv_read_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_sc
                     const int32_t* slot_ids, int32_t num_slots,
                     void* k_out, void* v_out,
                     int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype, void* stream);
+
+/*
+ * bros_attn_tree -- drafted tokens over the pool: several new rows of each sequence, each
+ * seeing what its mask names.
+ *
+ * For speculative decoding: a step's drafts are written to the positions behind the cached
+ * tokens (bros_kv_write or bros_qkv_append; a draft's rotation position is its depth, not its
+ * place: rope_pos), and one call scores all of them. Rows of sequence s are q[cu_q[s] .. cu_q[s+1]);
+ * with n of them and c0 = ctx_lens[s] - n, row j is the draft at position c0 + j and attends to
+ * the positions below c0 and to position c0 + i for every i < n with bit i of its mask set
+ * (bit i % 64 of word i / 64), in any order: itself only if its own bit is set. Without a mask
+ * row j sees positions 0 .. c0 + j (a chain of drafts). A row that sees nothing gets zeros.
+ *
+ *   q, out     : [num_q_tokens][num_q_heads][head_dim]
+ *   cu_q       : int32 [num_seqs + 1]; NULL: one row per sequence (num_q_tokens == num_seqs)
+ *   max_q_len  : host-side upper bound of every n (a bound beyond num_q_tokens counts as that)
+ *   mask       : uint64 [num_q_tokens][mask_words], device, 8-byte aligned, or NULL; 64 mask_words
+ *                at least max_q_len, at most BROS_TREE_MAX_DRAFTS. Bits from n on are ignored.
+ *   max_ctx    : host-side upper bound of every ctx_lens[s]; contexts above it are truncated
+ *   workspace  : bros_attn_workspace_size(BROS_WS_TREE, BROS_BF16, ...) bytes, 16-byte aligned,
+ *                required; contents undefined after the call. Two calls that share it
+ *                must not overlap in time (two captured graphs neither).
+ * bf16 only (BROS_E_UNSUPPORTED otherwise). Softmax weights are rounded to bf16 before the
+ * value product, as in the prefill; sums and statistics are fp32. Keys and values that are
+ * not finite reach the rows that see them and no others. Rows behind cu_q[num_seqs], and those of a
+ * sequence whose range is not within num_q_tokens, keep what out held; the rows of a
+ * sequence with more rows than ctx_lens see nothing.
+ */
+#define BROS_TREE_MAX_DRAFTS 256
+int bros_attn_tree(void* out, const void* q, const int32_t* cu_q, int32_t num_q_tokens, int32_t max_q_len,
+                   const uint64_t* mask, int32_t mask_words,
+                   const void* k_pool, const void* v_pool, int32_t num_blocks,
+                   const int32_t* block_tables, int32_t max_blocks_per_seq,
+                   const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                   int32_t max_ctx, int32_t num_seqs, int32_t num_q_heads,
+                   int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                   float scale, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bros_tree_commit -- the accepted drafts' rows to the positions they now have.
+ *
+ * After bros_attn_tree: of sequence s (n drafts, c0 = ctx_lens[s] - n, both as in that call) the
+ * drafts path[s][0 .. path_lens[s]) are kept, in this order. For i < min(path_lens[s], n):
+ *     row at position c0 + i  <-  row at position c0 + path[s][i]
+ * for every KV head, keys and values, as if all were read before any is written. The caller's
+ * next ctx_lens[s] is c0 + path_lens[s]. An index outside [0, n) leaves its position as it
+ * is, and so does a position without a valid table entry on either side. Bytes move unchanged;
+ * nothing else changes.
+ *
+ *   k_pool, v_pool : a pool of BROS_F32 or BROS_BF16 rows, row_dim 128; or a latent pool
+ *                    (below): row_dim 576, num_kv_heads 1, BROS_BF16 and v_pool NULL
+ *   path           : int32 [num_seqs][max_path], device; max_path at most BROS_TREE_MAX_DRAFTS
+ *   path_lens      : int32 [num_seqs], device
+ */
+int bros_tree_commit(void* k_pool, void* v_pool, int32_t num_blocks,
+                     const int32_t* block_tables, int32_t max_blocks_per_seq,
+                     const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                     const int32_t* ctx_lens, const int32_t* cu_q,
+                     const int32_t* path, const int32_t* path_lens, int32_t max_path,
+                     int32_t num_seqs, int32_t num_kv_heads, int32_t row_dim, int32_t block_size,
+                     int32_t dtype, void* stream);
+
+/*
+ * A CACHE OF ONE LATENT VECTOR PER TOKEN
+ *
+ * Models whose keys and values are all made from one latent vector a token cache that vector
+ * alone: pool [num_blocks][16][576] bf16, a slot's row being 512 values of the latent c and 64 of a
+ * key k_r that carries the position's rotation; all heads share both. Blocks, tables, directions
+ * and contexts are those of the other pools (bros_kv_gather and its like do not take this one).
+ * Head h has weights W_h [256][512]: its key for a token is (W_h[0:128] c | k_r), its value
+ * W_h[128:256] c; a query is (q_n | q_r), 128 and 64 values; scale <= 0 selects 1 / sqrt(192).
+ *
+ * bros_latent_append writes a step's new rows and turns its queries: for token t of sequence s at
+ * position p (cu_new, pos0 as in bros_kv_write), with x = kv[t],
+ *     c = x[0:512] * rsqrt(mean(x[0:512]^2) + eps) * norm_weight   (norm_weight NULL: as it is),
+ *     k_r = x[512:576] turned as bros_qkv_append turns a row of 64 (rope NULL: as it is),
+ *     pool[slot of p] = c | k_r,    q_out[t][h] = q[t][h] turned, 64 values each.
+ * Arithmetic is fp32, rounded once. q is a view of the queries' last 64 dims; q_out may be q itself,
+ * or a view of the absorbed form's queries.
+ *   kv           : [num_new_tokens][576], kv_stride elements from a token to the next
+ *   q, q_out     : [num_new_tokens][num_q_heads][64], with a token's and a head's stride each; both
+ *                  NULL: no q rows. q_out must not overlap rows of q (unless it is q, with its
+ *                  strides) or kv; where strides differ, ranges that interleave count as overlapping.
+ *   rope         : rotary_dim 64; rope_pos and axes as in bros_qkv_append
+ * Strides are multiples of 8 elements, pointers 16-byte aligned. Tokens in no sequence's range,
+ * positions outside the rotation's table and tokens without a valid table entry: as in bros_qkv_append.
+ */
+int bros_latent_append(void* q_out, const void* q, int64_t q_out_stride, int64_t q_out_head_stride,
+                       int64_t q_stride, int64_t q_head_stride, const void* kv, int64_t kv_stride,
+                       int32_t num_new_tokens, int32_t num_q_heads, const void* norm_weight, float eps,
+                       const bros_rope* rope, const int32_t* rope_pos, void* pool, int32_t num_blocks,
+                       const int32_t* block_tables, int32_t max_blocks_per_seq,
+                       const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry,
+                       const int32_t* pos0, const int32_t* cu_new, int32_t num_seqs, int32_t row_dim,
+                       int32_t block_size, int32_t dtype, void* stream);
+
+/*
+ * bros_attn_latent -- the absorbed form: queries in the latent space over a latent pool.
+ *
+ * q[t][h] = (W_h[0:128]^T q_n | q_r), 576 values, and out[t][h] = sum_p softmax_p(scale q . row_p)
+ * c_p, 512 values, of which the head's output is W_h[128:256] out. Rows, masks, cu_q (NULL for a
+ * decode step of one row per sequence), bounds, directions and what is not finite are as in
+ * bros_attn_tree (a row of the pool that is not finite may make the whole of an output that sees it
+ * NaN). Any number of rows per sequence without a mask; from about 170 on the expanded form
+ * is less work.
+ *   q          : [num_q_tokens][num_q_heads][576]      out : [num_q_tokens][num_q_heads][512]
+ *   num_q_heads: 1 .. 1024, any number
+ *   workspace  : bros_attn_workspace_size(BROS_WS_LATENT, BROS_BF16, ..., head_dim 576, ...) bytes
+ */
+int bros_attn_latent(void* out, const void* q, const int32_t* cu_q, int32_t num_q_tokens, int32_t max_q_len,
+                     const uint64_t* mask, int32_t mask_words, const void* pool, int32_t num_blocks,
+                     const int32_t* block_tables, int32_t max_blocks_per_seq,
+                     const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                     int32_t max_ctx, int32_t num_seqs, int32_t num_q_heads, int32_t row_dim, int32_t block_size,
+                     float scale, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bros_attn_latent_prefill -- the expanded form: causal chunks over a latent pool.
+ *
+ * Keys and values of every head are made from the latents in the workspace (rounded to bf16), then
+ * row j of sequence s attends to positions 0 .. c0 + j, as in bros_attn_prefill_chunk.
+ *   q         : [num_q_tokens][num_q_heads][192]       out : [num_q_tokens][num_q_heads][128]
+ *   w_kv      : [num_q_heads][256][512], 16-byte aligned
+ *   total_ctx : host-side upper bound of the sum of the contexts; a sequence whose context does not
+ *               fit into it behind those before it gets zero rows
+ *   workspace : bros_latent_prefill_workspace_size(num_seqs, total_ctx, heads) bytes, 16-byte aligned,
+ *               for num_heads heads, or for fewer, one at least: then the heads go in several passes.
+ */
+size_t bros_latent_prefill_workspace_size(int32_t num_seqs, int32_t total_ctx, int32_t num_heads);
+int bros_attn_latent_prefill(void* out, const void* q, const int32_t* cu_q, int32_t num_q_tokens, int32_t max_q_len,
+                             const void* w_kv, const void* pool, int32_t num_blocks,
+                             const int32_t* block_tables, int32_t max_blocks_per_seq,
+                             const int8_t* dir, const uint8_t* cls, int32_t dir_per_entry, const int32_t* ctx_lens,
+                             int32_t max_ctx, int32_t total_ctx, int32_t num_seqs, int32_t num_q_heads, int32_t row_dim,
+                             int32_t block_size, float scale, int32_t dtype, void* workspace, size_t workspace_bytes,
+                             void* stream);
 
 /*
  * bros_copy_dma -- an asynchronous copy of `bytes` bytes on a copy (SDMA)

@@ -22,7 +22,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbros_att
 
 BROS_F32, BROS_BF16 = 0, 1
 BROS_RT, BROS_BE = 0, 1
-BROS_WS_DECODE, BROS_WS_PREFILL = 0, 1
+BROS_WS_DECODE, BROS_WS_PREFILL, BROS_WS_TREE, BROS_WS_LATENT = 0, 1, 2, 3
+BROS_TREE_MAX_DRAFTS = 256
 BROS_ROPE_HALF, BROS_ROPE_ADJACENT = 0, 1
 STATUS = {0: "BROS_OK", -1: "BROS_E_NULL", -2: "BROS_E_SHAPE", -3: "BROS_E_DTYPE",
           -4: "BROS_E_UNSUPPORTED", -5: "BROS_E_WORKSPACE", -6: "BROS_E_HIP", -7: "BROS_E_TABLE",
@@ -37,7 +38,8 @@ EXPORTED = ["bros_status_str", "bros_last_error", "bros_abi_version", "bros_kv_w
             "bros_mgr_entries_needed", "bros_mgr_preemption_table", "bros_schedule", "bros_next_batch_size",
             "bros_mgr_grow_batch", "bros_mgr_plan_bound", "bros_schedule_pulled", "bros_set_decode_kernel_events",
             "bros_qkv_append", "bros_qkv_append_q8", "bros_kv_gather_q8", "bros_kv_scatter_q8", "bros_kv_read_q8",
-            "bros_attn_decode_q8", "bros_attn_prefill_chunk_q8"]
+            "bros_attn_decode_q8", "bros_attn_prefill_chunk_q8", "bros_attn_tree", "bros_tree_commit", "bros_latent_append",
+            "bros_attn_latent", "bros_attn_latent_prefill", "bros_latent_prefill_workspace_size"]
 
 
 class BrosError(RuntimeError):
@@ -113,6 +115,19 @@ def _load() -> ctypes.CDLL:
     lib.bros_kv_scatter_q8.restype = ctypes.c_int
     lib.bros_kv_read_q8.argtypes = [P, P, P, I, P, I, P, P, I, I, I, I, P]
     lib.bros_kv_read_q8.restype = ctypes.c_int
+    tables = [P, I, P, P, I]
+    lib.bros_attn_tree.argtypes = [P, P, P, I, I, P, I, P, P, I, *tables, P, I, I, I, I, I, I, F, I, P, Z, P]
+    lib.bros_attn_tree.restype = ctypes.c_int
+    lib.bros_tree_commit.argtypes = [P, P, I, *tables, P, P, P, P, I, I, I, I, I, I, P]
+    lib.bros_tree_commit.restype = ctypes.c_int
+    lib.bros_latent_append.argtypes = [P, P, L, L, L, L, P, L, I, I, P, F, ctypes.POINTER(_Rope), P, P, I, *tables, P, P, I, I, I, I, P]
+    lib.bros_latent_append.restype = ctypes.c_int
+    lib.bros_attn_latent.argtypes = [P, P, P, I, I, P, I, P, I, *tables, P, I, I, I, I, I, F, I, P, Z, P]
+    lib.bros_attn_latent.restype = ctypes.c_int
+    lib.bros_attn_latent_prefill.argtypes = [P, P, P, I, I, P, P, I, *tables, P, I, I, I, I, I, I, F, I, P, Z, P]
+    lib.bros_attn_latent_prefill.restype = ctypes.c_int
+    lib.bros_latent_prefill_workspace_size.argtypes = [I, I, I]
+    lib.bros_latent_prefill_workspace_size.restype = Z
     from . import manager as _m   # host block manager and scheduler signatures
     _m.declare(lib)
     return lib
@@ -430,6 +445,162 @@ def bros_kv_read_q8(k_pool, v_pool, kv_scales, slot_ids, k_out, v_out, num_slots
         raise ValueError("k_out and v_out must have one type")
     n, pools, ids, dense, nb, dims = _move((k_pool, v_pool, kv_scales), slot_ids, num_slots, (k_out, v_out), one_byte=False)
     _check(LIB.bros_kv_read_q8(*pools, nb, ids, n, *dense, *dims, _dtype_code(k_out), _stream(stream)))
+
+
+_I64, _BF16 = torch.int64, torch.bfloat16
+
+
+def _rows_offsets(q, cu_q, S: int):
+    """The offsets to check of rows [rows][Hq][..] of S sequences (cu_q None: one row each)."""
+    if cu_q is None:
+        if q.shape[0] != S:
+            raise ValueError(f"without cu_q, {S} sequences have {S} rows, not {q.shape[0]}")
+        return ()
+    return ((cu_q, S + 1),)
+
+
+def _draft_mask(mask, rows: int) -> int:
+    """Words of a row of a mask of drafts."""
+    if mask is None:
+        return 0
+    if mask.dtype not in (_I64, torch.uint64) or mask.dim() != 2 or mask.shape[0] != rows:
+        raise ValueError(f"mask must be int64 or uint64 [{rows}][words]")
+    return mask.shape[1]
+
+
+def _bf16_rows(name: str, t, shape) -> None:
+    if t.dtype is not _BF16 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be bfloat16 {list(shape)}, not {t.dtype} {list(t.shape)}")
+
+
+def _latent_pool(pool):
+    shape = pool.shape
+    if pool.dtype is not _BF16 or len(shape) != 3:
+        raise ValueError("a latent pool is bfloat16 [num_blocks][16][576]")
+    return shape
+
+
+def bros_attn_tree(out, q, cu_q, max_q_len: int, k_pool, v_pool, block_tables, dir, cls, ctx_lens, max_ctx: int, mask=None,
+                   scale: float = 0.0, workspace=None, stream=None):
+    """Drafted tokens' rows over a bfloat16 K/V pool: row j of a sequence sees the tokens before the
+    drafts and the drafts whose bits its row of `mask` (int64 [rows][words]) sets; mask None: a
+    chain (causal). cu_q None: one row per sequence."""
+    nb, hkv, bs, d = k_pool.shape
+    shape, S = q.shape, ctx_lens.numel()
+    if len(shape) != 3 or shape[2] != d or k_pool.dtype is not q.dtype or v_pool.dtype is not q.dtype or v_pool.shape != k_pool.shape:
+        raise ValueError(f"q must be [rows][Hq][{d}] of the pools' type")
+    if out.shape != shape or out.dtype is not q.dtype:
+        raise ValueError("out must have q's shape and type")
+    words = _draft_mask(mask, shape[0])
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *_rows_offsets(q, cu_q, S))
+    op, qp, cu, mp, kp, vp, bt, dr, cl, cx, ws = _addresses(out, q, cu_q, mask, k_pool, v_pool, block_tables, dir, cls, ctx_lens,
+                                                            workspace)
+    _check(LIB.bros_attn_tree(op, qp, cu, shape[0], int(max_q_len), mp, words, kp, vp, nb, bt, width, dr, cl, per_entry, cx,
+                              int(max_ctx), S, shape[1], hkv, d, bs, scale, _dtype_code(q), ws,
+                              0 if ws is None else workspace.nbytes, _stream(stream)))
+
+
+def bros_tree_commit(k_pool, v_pool, block_tables, dir, cls, ctx_lens, cu_q, path, path_lens, stream=None):
+    """Moves accepted drafts' rows: of sequence s, with its drafts at positions c0 .. ctx_lens[s] - 1, the
+    row at c0 + path[s][i] to c0 + i for i < path_lens[s]. path: int32 [S][most]. A latent
+    pool is given as k_pool, with v_pool None."""
+    S = ctx_lens.numel()
+    if v_pool is None:
+        nb, bs, d = _latent_pool(k_pool)
+        hkv = 1
+    else:
+        nb, hkv, bs, d = k_pool.shape
+        if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype:
+            raise ValueError("k_pool and v_pool must have one shape and type")
+    if path.dtype is not _I32 or path.dim() != 2 or path.shape[0] != S:
+        raise ValueError(f"path must be int32 [{S}][most]")
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), (cu_q, S + 1), (path_lens, S))
+    kp, vp, bt, dr, cl, cx, cu, pa, pl = _addresses(k_pool, v_pool, block_tables, dir, cls, ctx_lens, cu_q, path, path_lens)
+    _check(LIB.bros_tree_commit(kp, vp, nb, bt, width, dr, cl, per_entry, cx, cu, pa, pl, path.shape[1], S, hkv, d, bs,
+                                _dtype_code(k_pool), _stream(stream)))
+
+
+def _turned_rows(t, name: str, tokens: int):
+    """Address, token stride, head stride and heads of rows [tokens][heads][64] of bfloat16."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != 64 or t.dtype is not _BF16 or stride[2] != 1:
+        raise ValueError(f"{name} must be bfloat16 [{tokens}][heads][64], each head's values contiguous")
+    heads = stride[1] if shape[1] > 1 else 64
+    # (strides of one head or one token are never used)
+    return t.data_ptr(), (stride[0] if tokens > 1 else shape[1] * heads), heads, shape[1]
+
+
+def bros_latent_append(q_out, q, kv, pool, block_tables, dir, cls, pos0, cu_new, rope=None, rope_pos=None, norm=None,
+                       eps: float = 1e-6, stream=None):
+    """New tokens' latent rows kv [Tn][576] (512 normed by `norm`, a vector, and 64 turned) to their slots
+    of a latent pool; the queries' last 64 dims, q [Tn][Hq][64] (a view will do), turned into q_out (q itself,
+    or a view of other queries; both None: no queries)."""
+    nb, bs, d = _latent_pool(pool)
+    tn = kv.shape[0]
+    if kv.dtype is not _BF16 or kv.dim() != 2 or kv.shape[1] != d or kv.stride(1) != 1:
+        raise ValueError(f"kv must be bfloat16 [tokens][{d}], a token's values contiguous")
+    if (q is None) != (q_out is None):
+        raise ValueError("give both q and q_out, or neither")
+    qp = qs = qh = op = os_ = oh = hq = 0
+    if q is not None:
+        qp, qs, qh, hq = _turned_rows(q, "q", tn)
+        op, os_, oh, _ = _turned_rows(q_out, "q_out", tn)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+    device = kv.get_device()
+    if norm is not None and (norm.dtype is not _BF16 or norm.numel() != d - 64):
+        raise ValueError(f"norm must be bfloat16 [{d - 64}]")
+    if rope is not None and rope.device != device:
+        raise ValueError("the rotation's table must be on the rows' device")
+    if rope_pos is not None:
+        if rope is None:
+            raise ValueError("rope_pos without a rotation")
+        if rope_pos.dtype is not _I32 or rope_pos.size(-1) != tn or rope_pos.numel() != rope.axes * tn:
+            raise ValueError(f"rope_pos must be int32 [{rope.axes}][{tn}]")
+    S = cu_new.numel() - 1
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
+    pl, nm, bt, dr, cl, p0, cu, rp = _addresses(pool, norm, block_tables, dir, cls, pos0, cu_new, rope_pos, strided=(q, q_out, kv))
+    _check(LIB.bros_latent_append(op or None, qp or None, os_, oh, qs, qh, kv.data_ptr(), kv.stride(0) if tn > 1 else d, tn, hq, nm,
+                                  eps, None if rope is None else rope.ref, rp, pl, nb, bt, width, dr, cl, per_entry, p0, cu, S,
+                                  d, bs, BROS_BF16, _stream(stream)))
+
+
+def bros_attn_latent(out, q, cu_q, max_q_len: int, pool, block_tables, dir, cls, ctx_lens, max_ctx: int, mask=None,
+                     scale: float = 0.0, workspace=None, stream=None):
+    """Absorbed form over a latent pool: q [rows][Hq][576], out [rows][Hq][512]. Rows and mask as in
+    bros_attn_tree; cu_q None: one row per sequence (a decode step)."""
+    nb, bs, d = _latent_pool(pool)
+    shape, S = q.shape, ctx_lens.numel()
+    if len(shape) != 3 or shape[2] != d or q.dtype is not _BF16:
+        raise ValueError(f"q must be bfloat16 [rows][Hq][{d}]")
+    _bf16_rows("out", out, (shape[0], shape[1], d - 64))
+    words = _draft_mask(mask, shape[0])
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), *_rows_offsets(q, cu_q, S))
+    op, qp, cu, mp, pl, bt, dr, cl, cx, ws = _addresses(out, q, cu_q, mask, pool, block_tables, dir, cls, ctx_lens, workspace)
+    _check(LIB.bros_attn_latent(op, qp, cu, shape[0], int(max_q_len), mp, words, pl, nb, bt, width, dr, cl, per_entry, cx,
+                                int(max_ctx), S, shape[1], d, bs, scale, BROS_BF16, ws, 0 if ws is None else workspace.nbytes,
+                                _stream(stream)))
+
+
+def bros_latent_prefill_workspace_size(num_seqs: int, total_ctx: int, num_heads: int) -> int:
+    return int(LIB.bros_latent_prefill_workspace_size(num_seqs, total_ctx, num_heads))
+
+
+def bros_attn_latent_prefill(out, q, cu_q, max_q_len: int, w_kv, pool, block_tables, dir, cls, ctx_lens, max_ctx: int,
+                             total_ctx: int, scale: float = 0.0, workspace=None, stream=None):
+    """Expanded form over a latent pool: causal chunks q [rows][Hq][192], out [rows][Hq][128], keys and
+    values made with w_kv [Hq][256][512]. total_ctx: a bound of the sum of ctx_lens."""
+    nb, bs, d = _latent_pool(pool)
+    shape, S = q.shape, ctx_lens.numel()
+    if len(shape) != 3 or shape[2] != 192 or q.dtype is not _BF16:
+        raise ValueError("q must be bfloat16 [rows][Hq][192]")
+    _bf16_rows("out", out, (shape[0], shape[1], 128))
+    _bf16_rows("w_kv", w_kv, (shape[1], 256, 512))
+    width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), (cu_q, S + 1))
+    op, qp, cu, wp, pl, bt, dr, cl, cx, ws = _addresses(out, q, cu_q, w_kv, pool, block_tables, dir, cls, ctx_lens, workspace)
+    _check(LIB.bros_attn_latent_prefill(op, qp, cu, shape[0], int(max_q_len), wp, pl, nb, bt, width, dr, cl, per_entry, cx,
+                                        int(max_ctx), int(total_ctx), S, shape[1], d, bs, scale, BROS_BF16, ws,
+                                        0 if ws is None else workspace.nbytes, _stream(stream)))
 
 
 def bros_set_decode_kernel_events(before=None, after=None):

@@ -143,6 +143,111 @@ struct PrefillArgs {
   int32_t* ws_list;
 };
 
+// Attention of a few new rows of each sequence (rows_device.h): drafts over a K/V pool, latent
+// queries over a pool of latent rows, causal chunks over expanded keys and values.
+struct RowsArgs {
+  void* out;
+  const void* q;
+  const int32_t* cu_q;        // null: one row per sequence
+  const uint64_t* mask;       // [num_q_tokens][mask_words], or null: causal
+  int32_t mask_words;
+  const void* k_pool;         // latent: the only pool; expanded: keys [heads][dense_rows][128]
+  const void* v_pool;
+  const void* rot_rows;       // expanded: [dense_rows][64]
+  int64_t dense_rows;
+  const int32_t* block_tables;
+  const int8_t* dir;
+  const uint8_t* cls;
+  const int32_t* ctx_lens;
+  int32_t dir_per_entry;      // dir is [S][max_blocks_per_seq] (else [S])
+  int32_t num_q_tokens;
+  int32_t max_q_len;          // host bound of a sequence's rows
+  int32_t num_seqs;
+  int32_t num_blocks;
+  int32_t max_blocks_per_seq;
+  int32_t max_ctx;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;       // expanded: heads of this pass
+  int32_t head0;              // expanded: the first of them (else 0)
+  float scale_log2;
+  int32_t workers;            // shares the work is cut into, at most (set by the launch)
+  int32_t min_steps;          // the least steps of a share (set by the launch)
+  float* ws_o;                // [2 workers] x (columns of a unit x value dims) partial sums
+  float* ws_ml;               // [2 workers][columns of a unit][2] maximum (log2 units) and total
+};
+
+// Accepted drafts moved to their final positions (tree.hip).
+struct CommitArgs {
+  void* k_pool;
+  void* v_pool;               // null: one pool
+  const int32_t* block_tables;
+  const int8_t* dir;
+  const uint8_t* cls;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* path;        // [num_seqs][max_path] drafts
+  const int32_t* path_lens;
+  int32_t dir_per_entry;
+  int32_t max_path;
+  int32_t num_seqs;
+  int32_t num_blocks;
+  int32_t max_blocks_per_seq;
+  int32_t num_heads;
+  int32_t row_bytes;          // of a (slot, head): a multiple of 16
+};
+
+// New latent rows with their norm and rotation, and the rotation of the queries' rows of 64 (latent.hip).
+struct LatentAppendArgs {
+  const void* q;              // null: no q rows (num_q_heads 0)
+  void* q_out;
+  int64_t q_stride, q_head_stride, out_stride, out_head_stride;   // elements
+  const void* kv;
+  int64_t kv_stride;
+  const void* norm;           // [512], or null
+  float eps;
+  const float* rope_table;    // [table_rows][64], or null
+  const int32_t* rope_pos;    // [axes][num_new_tokens], or null: the logical position
+  int32_t table_rows;
+  int32_t adjacent;
+  int32_t axes;
+  int32_t axis_end[3];
+  void* pool;
+  const int32_t* block_tables;
+  const int8_t* dir;
+  const uint8_t* cls;
+  const int32_t* pos0;
+  const int32_t* cu_new;
+  int32_t dir_per_entry;
+  int32_t num_new_tokens;
+  int32_t num_seqs;
+  int32_t num_blocks;
+  int32_t max_blocks_per_seq;
+  int32_t num_q_heads;
+};
+
+// Keys and values of a group of heads from the latents of every sequence (latent.hip).
+struct ExpandArgs {
+  const void* pool;
+  const void* w;              // [heads][256][512] of this group
+  void* latents;              // [dense_rows][512]
+  void* rot_rows;             // [dense_rows][64]
+  void* k_rows;               // [heads][dense_rows][128]
+  void* v_rows;
+  int64_t dense_rows;
+  const int32_t* block_tables;
+  const int8_t* dir;
+  const uint8_t* cls;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  int32_t dir_per_entry;
+  int32_t num_q_tokens;
+  int32_t num_seqs;
+  int32_t num_blocks;
+  int32_t max_blocks_per_seq;
+  int32_t max_ctx;
+  int32_t heads;
+};
+
 // Rows of a list of slots moved between the pool and a dense [n][Hkv][D]
 // buffer (gather: pool -> dense, scatter: dense -> pool).
 struct KvMoveArgs {
@@ -184,6 +289,15 @@ size_t decode_workspace_bytes(int32_t num_rows, int32_t num_q_heads, int32_t max
 void set_decode_workspace(DecodeArgs& a, void* ws, bool bf16);
 
 hipError_t launch_kv_write(const KvWriteArgs& a, bool bf16, hipStream_t stream);
+// Rows attention. The partials' workspace (one size for every call) and the three launches.
+size_t rows_workspace_bytes(bool latent);
+hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream);
+hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream);
+hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream);
+hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream);
+hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream);
+hipError_t launch_latent_gather(const ExpandArgs& a, hipStream_t stream);
+hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream);
 hipError_t launch_kv_move(const KvMoveArgs& a, bool gather, hipStream_t stream);
 // bf16 rows over an 8-bit pool (a.k_pool and a.v_pool unused), with the bf16 decode's workspace.
 hipError_t launch_decode_q8(DecodeArgs a, Q8Pool pool, int group, hipStream_t stream);

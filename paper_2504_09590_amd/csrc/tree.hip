@@ -1,0 +1,90 @@
+// bros_attn_tree and bros_tree_commit on gfx950.
+//
+// The attention is rows_device.h's over a K/V pool. With M columns (rows times heads of a KV
+// head) a key of 512 bytes takes 512 M operations: few columns are bound by memory, from about
+// 150 on by the matrix cores. The columns a unit holds follow the longest tree: 32 with four
+// waves along the keys, 64 with two, 128 with none.
+#include "rows_launch.h"
+
+namespace bros {
+
+namespace {
+
+constexpr int kCommitThreads = 256;
+constexpr int kCommitRows = kCommitThreads / 16;   // rows a workgroup moves at once, 16 lanes each
+constexpr int kCommitRounds = 16;                  // so many times at most
+
+// Sequence blockIdx.x, 256 bytes (16 chunks) blockIdx.y of its slots' rows. Every row is in
+// registers before the first is written, so a path may go any way.
+__global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitArgs a) {
+  const int s = blockIdx.x;
+  const int n = a.cu_q[s + 1] - a.cu_q[s];
+  const int c0 = a.ctx_lens[s] - n;
+  if (n <= 0 || c0 < 0) return;
+  const int len = min(a.path_lens[s], min(n, a.max_path));
+  // 256-byte pieces of a (slot, head) row, K's heads then V's
+  const int pieces = (a.row_bytes + 255) / 256;
+  int y = blockIdx.y;
+  const int piece = y % pieces;
+  y /= pieces;
+  const int head = y % a.num_heads;
+  uint8_t* pool = static_cast<uint8_t*>(y / a.num_heads == 0 ? a.k_pool : a.v_pool);
+  const int at = 256 * piece + 16 * (threadIdx.x & 15);
+  const int r0 = threadIdx.x >> 4;
+  if (len <= 0) return;
+
+  const auto place = [&](int pos) -> uint8_t* {
+    const int e = pos >> 4;
+    if (e >= a.max_blocks_per_seq) return nullptr;
+    const int b = a.block_tables[(size_t)s * a.max_blocks_per_seq + e];
+    if (b < 0 || b >= a.num_blocks) return nullptr;
+    const int slot = slot_of_offset(pos & 15, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, e));
+    return pool + (((size_t)b * a.num_heads + head) * kBlockSize + slot) * a.row_bytes + at;
+  };
+  // (constant indices: the rows stay in registers)
+  uint4 v[kCommitRounds];
+  uint8_t* to[kCommitRounds];
+#pragma unroll
+  for (int i = 0; i < kCommitRounds; ++i) {
+    const int r = kCommitRows * i + r0;
+    v[i] = make_uint4(0, 0, 0, 0);
+    to[i] = nullptr;
+    if (kCommitRows * i < len && r < len && at < a.row_bytes) {
+      const int from = a.path[(size_t)s * a.max_path + r];
+      if (from >= 0 && from < n && from != r) {
+        const uint8_t* src = place(c0 + from);
+        uint8_t* dst = place(c0 + r);
+        if (src != nullptr && dst != nullptr) {
+          v[i] = *reinterpret_cast<const uint4*>(src);
+          to[i] = dst;
+        }
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kCommitRounds; ++i)
+    if (to[i] != nullptr) *reinterpret_cast<uint4*>(to[i]) = v[i];
+}
+
+}  // namespace
+
+size_t rows_workspace_bytes(bool latent) {
+  return latent ? ra::partial_bytes(ra::kMaxCus, 128, 512) : ra::partial_bytes(2 * ra::kMaxCus, 128, 128);
+}
+
+hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
+  const int64_t columns = (int64_t)a.max_q_len * (a.num_q_heads / a.num_kv_heads);
+  if (columns <= 32) return ra::launch_rows<ra::KvPool, 1, 4, 1, 2, 1, 2>(a, workspace, stream);
+  if (columns <= 64) return ra::launch_rows<ra::KvPool, 2, 2, 1, 4, 1, 2>(a, workspace, stream);
+  return ra::launch_rows<ra::KvPool, 4, 1, 1, 4, 2, 4>(a, workspace, stream);
+}
+
+hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream) {
+  const int64_t pieces = (int64_t)((a.row_bytes + 255) / 256) * a.num_heads * (a.v_pool != nullptr ? 2 : 1);
+  if (pieces > 65535) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(commit_kernel, dim3(a.num_seqs, (unsigned)pieces), dim3(kCommitThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace bros
