@@ -339,9 +339,9 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
 
 hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * a.num_q_heads;
-  if (columns <= 32) return ra::launch_rows<ra::LatentPool, 1, 1, 4, 3, 1, 2>(a, workspace, stream);
-  if (columns <= 64) return ra::launch_rows<ra::LatentPool, 2, 1, 2, 3, 1, 2>(a, workspace, stream);
-  return ra::launch_rows<ra::LatentPool, 4, 1, 2, 3, 1, 4>(a, workspace, stream);
+  if (columns <= 32) return ra::launch_latent_rows<1, 4, 2>(a, workspace, stream);
+  if (columns <= 64) return ra::launch_latent_rows<2, 4, 2>(a, workspace, stream);
+  return ra::launch_latent_rows<4, 2, 4>(a, workspace, stream);
 }
 
 hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {

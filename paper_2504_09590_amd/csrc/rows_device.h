@@ -61,6 +61,19 @@ constexpr float kRescaleSlack = 8.0f;    // log2 units: weights stay <= 2^8
 constexpr float kNoMax = -1.0e30f;       // finite "no score yet" reference
 constexpr int kTable = 128;              // staged table entries of a wave: two windows of 64
 
+typedef const v4u_t __attribute__((address_space(3)))* lds_v4u_ptr;
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef v4s_t __attribute__((address_space(3)))* lds_v4s_ptr;
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)p; }   // (the aperture is 4 GiB aligned)
+__device__ __forceinline__ v4u_t lds_read(uint32_t at) { return *(lds_v4u_ptr)(uintptr_t)at; }
+__device__ __forceinline__ uint2 lds_read_turned(uint32_t at) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)at));
+}
+// A word that a load into LDS may have written. (As LDS memory: a generic read would also wait for every load in flight.)
+__device__ __forceinline__ int32_t lds_word(const int32_t* p) {
+  return *(const volatile int32_t __attribute__((address_space(3)))*)(uintptr_t)lds_address(p);
+}
+
 // What is read. kMain: bytes of a key row's first part, kRot: of its second (0: none);
 // kVal: bytes of a value row, or 0 where the first part is the value.
 struct KvPool {          // 128 dims each, [blocks][Hkv][16][128]
@@ -130,6 +143,26 @@ struct TileBlocks {
 };
 // Bits 15 and 31: the halves that are infinite or NaN, as bf16.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// Bits of the positions pos0 .. + 31 that row j of a sequence sees, of a context of ctx.
+__device__ __forceinline__ uint32_t row_window(const RowsArgs& a, const Seq& q, int ctx, int j, bool valid, int pos0) {
+  const auto below = [](int k) -> uint32_t { return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u; };
+  uint32_t win;
+  if (a.mask != nullptr) {
+    const int i0 = pos0 - q.c0;   // draft of position pos0 (negative: before the drafts)
+    win = below(-i0);
+    const uint64_t* bits = a.mask + (size_t)(q.q0 + min(j, q.n - 1)) * a.mask_words;
+    // the 64 bits from draft max(i0, 0) on
+    const int f = max(i0, 0), wd = f >> 6, sh = f & 63;
+    uint64_t b = wd < a.mask_words ? bits[wd] >> sh : 0;
+    if (sh != 0 && wd + 1 < a.mask_words) b |= bits[wd + 1] << (64 - sh);
+    if (q.n - f < 64) b &= q.n - f <= 0 ? 0 : (1ull << (q.n - f)) - 1;
+    if (i0 > -32) win |= i0 < 0 ? (uint32_t)b << -i0 : (uint32_t)b;
+  } else {
+    win = below(q.c0 + j + 1 - pos0);
+  }
+  return valid ? win & below(ctx - pos0) : 0u;
+}
 
 // Where a workgroup's share begins.
 struct Place {
@@ -360,7 +393,7 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
       load_word_to_lds(tbl, 4u * (uint32_t)e, tab + (e0 & (kTable - 1)));
     };
     auto entry = [&](int e) __attribute__((always_inline)) -> int {   // -1: none
-      const int v = __builtin_amdgcn_readfirstlane(*const_cast<volatile int32_t*>(tab + (e & (kTable - 1))));
+      const int v = __builtin_amdgcn_readfirstlane(lds_word(tab + (e & (kTable - 1))));
       return (e < nblk && v >= 0 && v < a.num_blocks) ? v : -1;
     };
     // Requests the wave's part of the rows of step `step`; whether a block of them is missing.
@@ -431,25 +464,6 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
     uint32_t odd = 0;   // a value that is not finite was left out of a product
 
-    // Positions pos0 .. + 31 that the lane's row sees.
-    auto window = [&](int pos0) -> uint32_t {
-      const auto below = [](int k) -> uint32_t { return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u; };
-      uint32_t win;
-      if (a.mask != nullptr) {
-        const int i0 = pos0 - q.c0;   // draft of position pos0 (negative: before the drafts)
-        win = below(-i0);
-        const uint64_t* bits = a.mask + (size_t)(q.q0 + min(j, n - 1)) * a.mask_words;
-        // the 64 bits from draft max(i0, 0) on
-        const int f = max(i0, 0), wd = f >> 6, sh = f & 63;
-        uint64_t b = wd < a.mask_words ? bits[wd] >> sh : 0;
-        if (sh != 0 && wd + 1 < a.mask_words) b |= bits[wd + 1] << (64 - sh);
-        if (n - f < 64) b &= n - f <= 0 ? 0 : (1ull << (n - f)) - 1;
-        if (i0 > -32) win |= i0 < 0 ? (uint32_t)b << -i0 : (uint32_t)b;
-      } else {
-        win = below(q.c0 + j + 1 - pos0);
-      }
-      return valid ? win & below(ctx - pos0) : 0u;
-    };
     // The two blocks of the tile at pos0: whether they are there, and their directions.
     auto blocks_of = [&](int pos0) -> TileBlocks {
       const int e = pos0 / kBlockSize, em = max(nblk - 1, 0);
@@ -497,7 +511,7 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
       uint32_t win = 0xffffffffu;
       TileBlocks tb{true, true, 1, 1};
       if (masked) {
-        win = window(pos0);
+        win = row_window(a, q, ctx, j, valid, pos0);
         tb = blocks_of(pos0);
       }
       // The wave's rows of values: zeros where no context is, and for values that are not finite.
@@ -699,7 +713,7 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
           }
         }
         if (pos0 + kKeys <= full_below && !hole) continue;
-        const uint32_t win = window(pos0);
+        const uint32_t win = row_window(a, q, ctx, j, valid, pos0);
         // value row of tile row r, or null where no context is
         const auto value_row = [&](int r) -> const uint8_t* {
           if constexpr (P::kPaged) {

@@ -2,7 +2,7 @@
 // workspace, the merge.
 #pragma once
 
-#include "rows_device.h"
+#include "latent_device.h"
 
 #include <algorithm>
 
@@ -27,6 +27,20 @@ hipError_t launch_rows(RowsArgs a, void* workspace, hipStream_t stream) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((rows_merge_kernel<P, NCW, NKW, H, SLOTS>), dim3(std::max(1, a.workers - 1), NCW), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int NCW, int H, int MIN>
+hipError_t launch_latent_rows(RowsArgs a, void* workspace, hipStream_t stream) {
+  using S = LatentShape<NCW, H>;
+  a.workers = std::min(stream_compute_units(stream), kMaxCus);
+  a.min_steps = MIN;
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = a.ws_o + 2 * (size_t)a.workers * S::kSlotFloats;
+  hipLaunchKernelGGL((latent_kernel<NCW, H, S::kWaves / 4>), dim3(a.workers), dim3(S::kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((rows_merge_kernel<LatentPool, NCW, 1, H, 3>), dim3(std::max(1, a.workers - 1), NCW), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
