@@ -339,13 +339,14 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
 
 hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * a.num_q_heads;
-  if (columns <= 32) return ra::launch_latent_rows<1, 4, 2>(a, workspace, stream);
-  if (columns <= 64) return ra::launch_latent_rows<2, 4, 2>(a, workspace, stream);
-  return ra::launch_latent_rows<4, 2, 4>(a, workspace, stream);
+  if (columns <= 16) return ra::launch_latent_rows<1, 4>(a, 4, 6, workspace, stream);
+  if (columns <= 32) return ra::launch_latent_rows<2, 2>(a, 4, 6, workspace, stream);
+  if (columns <= 64) return ra::launch_latent_rows<4, 2>(a, 4, 6, workspace, stream);
+  return ra::launch_latent_rows<8, 1>(a, 6, 6, workspace, stream);
 }
 
 hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {
-  return ra::launch_rows<ra::Expanded, 4, 1, 1, 3, 2, 4>(a, workspace, stream);
+  return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, workspace, stream);
 }
 
 }  // namespace bros

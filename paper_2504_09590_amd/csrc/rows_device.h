@@ -4,22 +4,23 @@
 //
 // Columns. The G query heads that read one key make a column each of every new row, so a
 // sequence has n G columns per KV head (a latent row is the key of all heads: n Hq
-// columns). A unit is a (sequence, KV head, tile of 32 NCW columns); its keys come in steps of
-// 32 NKW. A workgroup of NCW NKW H waves takes a step: wave (cw, kg, h) the columns 32 cw ..
-// + 31 against the keys 32 kg .. + 31, and part h of H of the dims: of the score products, whose
-// partial sums the H waves exchange in LDS, and of the values. (Long rows only: 576 dims of a query
-// and 512 of sums in fp32 for 32 columns are 400 registers of a wave.)
+// columns). A unit is a (sequence, KV head, tile of columns); its keys come in steps of
+// 32 NKW. A workgroup of NCW NKW waves takes a step: wave (cw, kg) the columns 32 cw .. + 31
+// against the keys 32 kg .. + 31.
 //
 // Products, transposed: S^T[key][column] = K Q^T and O^T[dim][column] += V^T P^T, both with
 // 32x32x16 matrix instructions, so that a lane owns one column (lane % 32), the softmax needs
 // one exchange between the two half-waves, and P goes from the score accumulators straight
 // into the second product's operand (keys are permuted alike in P and V^T). K^T operands are
 // 16-byte reads of LDS rows, V^T operands transposing reads; the chunks of a row are permuted
-// (swz) so that neither meets a bank conflict. Rows reach LDS without registers.
+// (swz) so that neither meets a bank conflict. Rows reach LDS without registers; each wave waits
+// for those it requested itself, and puts in order what it finds there, before the barrier
+// that publishes them.
 //
 // Work. The steps of all units are laid end to end and cut into equal shares, one per
 // workgroup, whatever the sequences' lengths; a unit cut between workgroups leaves partial
-// sums (fp32, with their maximum and total) that a merge folds.
+// sums (fp32, with their maximum and total) that a merge folds. Where no unit is long,
+// whole units are shared out instead, and nothing is merged.
 //
 // Masks. A row sees the keys before the drafts, and of those the ones its bits name (or the
 // causal ones). Only steps that reach the drafts, the context's end or an invalid table
@@ -69,6 +70,12 @@ __device__ __forceinline__ v4u_t lds_read(uint32_t at) { return *(lds_v4u_ptr)(u
 __device__ __forceinline__ uint2 lds_read_turned(uint32_t at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)at));
 }
+// Lane id that is computed where it is used (values made of it are not held in registers over a loop).
+__device__ __forceinline__ int lane_here() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
 // A word that a load into LDS may have written. (As LDS memory: a generic read would also wait for every load in flight.)
 __device__ __forceinline__ int32_t lds_word(const int32_t* p) {
   return *(const volatile int32_t __attribute__((address_space(3)))*)(uintptr_t)lds_address(p);
@@ -112,24 +119,25 @@ template <class P, int CT, int KS>
 struct Steps {
   int tiles, each;   // units per KV head; steps of one (causal units: of the last)
   int before;        // causal units: steps of the keys before the new rows
+  bool whole;        // shares are of whole units
   __device__ __forceinline__ Steps(const RowsArgs& a, const Seq& q, int group) {
     tiles = (int)(((int64_t)q.n * group + CT - 1) / CT);
     each = max(1, (q.ctx + KS - 1) / KS);
     before = (max(q.c0, 0) + KS - 1) / KS;
+    whole = a.whole_units != 0;
   }
   // Steps of unit t. Causal units (one column a row): those of its last row's keys.
   __device__ __forceinline__ int of(int t) const {
     if constexpr (P::kCausalUnits) return t + 1 < tiles ? min(before + (CT / KS) * (t + 1), each) : each;
     return each;
   }
-  // Steps of units 0 .. t - 1 (t <= tiles).
+  // What units 0 .. t - 1 (t <= tiles) count, in what is shared out.
   __device__ __forceinline__ int64_t first(int t) const {
+    if (whole) return t;
     if constexpr (P::kCausalUnits) {
-      int64_t sum = 0;
       // (the context may be cut short by max_ctx: units beyond it have `each` steps)
       const int free = min(t, min(tiles - 1, max(0, (each - before) / (CT / KS))));   // units whose `of` is not cut
-      sum = (int64_t)free * before + (int64_t)(CT / KS) * free * (free + 1) / 2;
-      return sum + (int64_t)(t - free) * each;
+      return (int64_t)free * before + (int64_t)(CT / KS) * free * (free + 1) / 2 + (int64_t)(t - free) * each;
     }
     return (int64_t)t * each;
   }
@@ -141,6 +149,14 @@ struct TileBlocks {
   bool ok0, ok1;
   int dir0, dir1;
 };
+__device__ __forceinline__ TileBlocks tile_blocks(const RowsArgs& a, const int32_t* tbl, int nblk, int s, int pos0, bool paged) {
+  const int e = pos0 / kBlockSize, em = max(nblk - 1, 0);
+  const int v0 = tbl[min(e, em)], v1 = tbl[min(e + 1, em)];
+  const bool ok0 = e < nblk && v0 >= 0 && v0 < a.num_blocks, ok1 = e + 1 < nblk && v1 >= 0 && v1 < a.num_blocks;
+  if (!paged) return TileBlocks{ok0, ok1, 1, 1};   // (dense rows lie in the order of their positions)
+  return TileBlocks{ok0, ok1, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e, em)),
+                    entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e + 1, em))};
+}
 // Bits 15 and 31: the halves that are infinite or NaN, as bf16.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
@@ -254,13 +270,30 @@ __device__ __forceinline__ Place find_place(const RowsArgs& a, int group, At at,
   return p;
 }
 
-// Workgroups that get a share of `total` steps, and where share w begins.
-__device__ __forceinline__ int sharers(const RowsArgs& a, int64_t total) {
-  return (int)max((int64_t)1, min((int64_t)a.workers, (total + a.min_steps - 1) / a.min_steps));
-}
-__device__ __forceinline__ int64_t share_begin(int64_t total, int w, int n) { return total * w / n; }
-// The share that step x lies in.
-__device__ __forceinline__ int share_of(int64_t total, int64_t x, int n) { return (int)(((x + 1) * n - 1) / total); }
+// How `total` steps are shared out: n shares, the first `more` of them one step longer than `per`.
+struct Shares {
+  int n;
+  int64_t per, more;
+  __device__ __forceinline__ Shares(const RowsArgs& a, int64_t total) {
+    // (32-bit division is a tenth of the other, and nearly every call's steps fit)
+    if (total < (1 << 30)) {
+      const uint32_t x = (uint32_t)total;
+      n = max(1u, min((uint32_t)a.workers, (x + a.min_steps - 1) / a.min_steps));
+      per = x / (uint32_t)n;
+    } else {
+      n = a.workers;
+      per = total / n;
+    }
+    more = total - per * n;
+  }
+  __device__ __forceinline__ int64_t begin(int w) const { return per * w + min((int64_t)w, more); }
+  // The share that step x lies in.
+  __device__ __forceinline__ int of(int64_t x) const {
+    const int64_t longer = more * (per + 1);
+    if (x < longer) return (int)(x / (per + 1));
+    return (int)(more + (x - longer) / per);
+  }
+};
 
 // Writes a wave's normalised columns: lane l holds column l % 32, accumulators 4 jq .. + 3 of o[i] are dims
 // 32 (dt0 + i) + 8 jq + 4 (l / 32) .. + 3.
@@ -278,37 +311,69 @@ __device__ __forceinline__ void write_columns(uint16_t* row, int dt0, const floa
   }
 }
 
-template <class P, int NCW, int NKW, int H, int SLOTS>
+// N products, product(i, operand(i)), with the operands of the next DEPTH on their way: the order stands
+// as written. (Left alone the compiler reads an operand, waits and multiplies, in turn.)
+template <int N, int DEPTH, class Operand, class Product>
+__device__ __forceinline__ void pipelined(Operand operand, Product product) {
+  v4u_t x[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i) x[i] = operand(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    product(i, as_bf16x8(x[i % DEPTH]));
+    if (i + DEPTH < N) x[i % DEPTH] = operand(i + DEPTH);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The table entries of a sequence as a wave keeps them: two windows of 64 in LDS, the next requested when the
+// loads enter the one before it.
+struct Table {
+  const int32_t* tbl;
+  int32_t* lds;      // [kTable]
+  int nblk, num_blocks;
+  __device__ __forceinline__ void load(int e0) const {   // entries e0 .. + 63
+    load_word_to_lds(tbl, 4u * (uint32_t)max(0, min(e0 + lane_here(), nblk - 1)), lds + (e0 & (kTable - 1)));
+  }
+  __device__ __forceinline__ int operator()(int e) const {   // -1: none
+    const int v = __builtin_amdgcn_readfirstlane(lds_word(lds + (e & (kTable - 1))));
+    return (e < nblk && v >= 0 && v < num_blocks) ? v : -1;
+  }
+};
+
+// A unit cut between shares, as its first share notes it for the merge: its last share (-1: none).
+struct Cut {
+  int32_t s, g, t, last;
+};
+
+template <class P, int NCW, int NKW, int SLOTS_>
 struct Shape {
-  static constexpr int kWaves = NCW * NKW * H, kThreads = kWaves * kWave;
-  static constexpr int kSharers = NCW * H;                          // waves that share a tile
+  static constexpr int SLOTS = SLOTS_;
+  static constexpr int kWaves = NCW * NKW, kThreads = kWaves * kWave;
   static constexpr int CT = 32 * NCW, KS = kKeys * NKW;
-  static constexpr int kDt = (P::kVal ? P::kVal : P::kMain) / 64;   // 32-dim pieces of a value
-  static constexpr int kDims = 32 * kDt;
+  static constexpr int kLaneCols = 32;                              // columns of a wave
+  static constexpr int kDims = P::kVal / 2, kDt = kDims / 32;       // 32-dim pieces of a value
   static constexpr int kQDims = (P::kMain + P::kRot) / 2;
   static constexpr int kRotAt = kKeys * P::kMain;                   // LDS of a tile: first parts, second parts, values
   static constexpr int kValAt = kRotAt + kKeys * P::kRot;
   static constexpr int kTile = kValAt + kKeys * P::kVal;
   static constexpr int kRing = NKW * SLOTS * kTile;
-  static constexpr int kRows = kKeys / kSharers;                    // rows of a tile that a wave loads
-  // loads of a wave per step, 1 KiB each (second parts: eight rows, or fewer lanes)
-  static constexpr int kLoads = (P::kVal ? 2 * kRows / 4 : kRows * P::kMain / 1024) + (P::kRot ? (kRows + 7) / 8 : 0);
-  static constexpr int kExchange = H > 1 ? kWaves * 4096 : 16;      // score sums of a step
+  static constexpr int kRows = kKeys / NCW;                         // rows of a tile that a wave requests
+  static constexpr int kLoads = 2 * kRows / 4 + (P::kRot ? (kRows + 7) / 8 : 0);   // of 1 KiB
   static constexpr int kSlotFloats = CT * kDims;                    // a partial's sums
+  static constexpr int kChunks = kDims / 8;                         // of a wave's partial, 1 KiB each
+  // first of the four dims that a lane has in chunk i
+  static __device__ __forceinline__ int dim_of(int i, int lane) { return 8 * i + 4 * (lane >> 5); }
   static_assert(kRows % 4 == 0, "a load takes four rows of 256 bytes");
-  static_assert(H == 1 || NKW == 1, "");
-  static_assert(H > 1 || P::kVal != 0, "a shared row is cleaned behind the exchange's barrier");
-  static_assert(kDt % H == 0 && (P::kMain / 32) % H == 0 && (P::kRot / 32) % H == 0, "");
-  static_assert(H == 1 || (kDt / H) % 4 == 0, "a part starts at a multiple of 16 chunks");
   static_assert((NKW - 1) * NCW * 32 * kDims * 4 <= kRing, "the key groups' sums meet in the ring");
 };
 
-template <class P, int NCW, int NKW, int H, int SLOTS, int OCC>
-__global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs a) {
-  using S = Shape<P, NCW, NKW, H, SLOTS>;
-  // of this wave: 32-dim pieces of its values, 16-dim steps of its score products
-  constexpr int kDt = S::kDt / H, kMainSteps = P::kMain / 32 / H, kQSteps = kMainSteps + P::kRot / 32 / H;
-  __shared__ __attribute__((aligned(16))) uint8_t s_x[S::kExchange];
+template <class P, int NCW, int NKW, int SLOTS, int OCC>
+__global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
+  using S = Shape<P, NCW, NKW, SLOTS>;
+  constexpr int kDt = S::kDt, kMainSteps = P::kMain / 32, kQSteps = S::kQDims / 16, kR = S::kRows;
+  constexpr int kAhead = 4;   // operands read before the first product
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[S::kRing];
   __shared__ int32_t s_tab[S::kWaves][kTable];
   __shared__ int64_t s_scan[2 * S::kWaves];
@@ -316,147 +381,99 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
   __shared__ int s_odd;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
-  const int cw = wave % NCW, kg = H > 1 ? 0 : wave / NCW, hp = H > 1 ? wave / NCW : 0;
-  const int sharer = H > 1 ? wave : cw;   // among the waves of its tile
+  const int cw = wave % NCW, kg = wave / NCW;
   const int half = lane >> 5, col = lane & 31;
   const int Hkv = a.num_kv_heads, G = P::kPaged ? a.num_q_heads / Hkv : 1;   // (expanded: heads of their own)
   // neighbouring shares to one die
   const int nb = gridDim.x;
   const int me = nb % pf::kXcds == 0 ? (blockIdx.x % pf::kXcds) * (nb / pf::kXcds) + blockIdx.x / pf::kXcds : blockIdx.x;
+  Cut* cut = reinterpret_cast<Cut*>(a.ws_cut) + me;
+  if (tid == 0) cut->last = -1;
 
   Place at = find_place<P, S::CT, S::KS, S::kThreads>(
       a, G, [&](int64_t total) -> int64_t {
-        const int n = sharers(a, total);
-        return me < n ? share_begin(total, me, n) : -1;
+        const Shares sh(a, total);
+        return me < sh.n ? sh.begin(me) : -1;
       }, s_scan, &s_place);
   if (at.s < 0) return;   // (uniform: no step left for this workgroup)
-  const int nshare = sharers(a, at.total);
-  int64_t x = share_begin(at.total, me, nshare);
-  const int64_t x_end = share_begin(at.total, me + 1, nshare);
+  const Shares shares(a, at.total);
+  int64_t x = shares.begin(me);
+  const int64_t x_end = shares.begin(me + 1);
 
-  constexpr int kR = S::kRows;
-  uint8_t* ring = s_ring + kg * SLOTS * S::kTile;
-  int32_t* tab = s_tab[wave];
   const float sl2 = a.scale_log2;
   const bf16x2_t one2 = {(__bf16)1.0f, (__bf16)1.0f};
-
-  // operand reads (see the top)
-  const int k_sw = swz(col);
-  const int k_lane = col * P::kMain + (((half ^ k_sw) & 1) << 4) + hp * (P::kMain / H);
-  const int r_lane = (col >> 1) * 256 + ((col & 1) << 7), r_sw = ((col >> 1) & 7) ^ (hp * (P::kRot / 16 / H));
-  constexpr int kVRow = P::kVal ? P::kVal : P::kMain, kVAt = P::kVal ? S::kValAt : 0;
-  int v_off[2], v_sw[2];
-#pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    const int key = 8 * part + 4 * half + ((lane >> 2) & 3);
-    v_sw[part] = swz(key);
-    v_off[part] = key * kVRow + ((((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_sw[part]) & 3) << 4) + (lane & 1) * 8 + hp * (kDt * 64);
-  }
+  // Operand reads: lane addresses of a tile at 0. A chunk's low four bits are those of the
+  // row's permutation, so that other chunks are a xor and a constant away.
+  const uint32_t k_lane = col * P::kMain + ((half ^ swz(col)) << 4);
+  const uint32_t r_lane = S::kRotAt + (col >> 1) * 256 + ((col & 1) << 7) + ((half ^ ((col >> 1) & 7)) << 4);
+  const int v_key = 4 * half + ((lane >> 2) & 3);
+  const uint32_t v_lane = S::kValAt + v_key * P::kVal + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz(v_key)) << 4) + (lane & 1) * 8;
+  uint8_t* const ring = s_ring + kg * SLOTS * S::kTile;
+  const uint32_t ring0 = lds_address(ring);
 
   while (x < x_end) {
-    // ---- The segment: steps [first, first + cnt) of unit (s, g, t).
+    // ---- The segment: steps [first, last) of unit (s, g, t).
     const int s = at.s, g = at.g, t = at.t;
     const Seq q = seq_of(a, s);
     const Steps<P, S::CT, S::KS> st(a, q, G);
     const int usteps = __builtin_amdgcn_readfirstlane(st.of(t));
-    const int first = at.step;
-    const int cnt = (int)min((int64_t)(usteps - first), x_end - x);
+    const int first = st.whole ? 0 : at.step;
+    const int cnt = st.whole ? usteps : (int)min((int64_t)(usteps - first), x_end - x);
+    const int last = first + cnt;
     const bool whole = cnt == usteps;
     // (dense keys that do not fit their buffer: the sequence's rows see nothing)
     const bool fits = P::kPaged || at.row0 + dense_rows(q.ctx) <= a.dense_rows;
     const int ctx = fits ? q.ctx : 0, n = q.n;
-    const int nblk = (ctx + kBlockSize - 1) / kBlockSize;
     const int c = t * S::CT + 32 * cw + col;        // the lane's column
     const int j = c / G;                            // its row
     const bool valid = j < n;
     const size_t orow = (size_t)(q.q0 + min(j, n - 1)) * a.num_q_heads + a.head0 + g * G + (c - j * G);
     // keys below this position are seen by every row of the unit
     const int full_below = a.mask != nullptr ? min(ctx, q.c0) : min(ctx, q.c0 + t * S::CT / G + 1);
+    const Table table{a.block_tables + (size_t)s * a.max_blocks_per_seq, s_tab[wave], (ctx + kBlockSize - 1) / kBlockSize, a.num_blocks};
 
     bf16x8_t qf[kQSteps];
     {
+      // (columns behind the last row take that row's values: nothing is made of them)
       const uint16_t* qp = static_cast<const uint16_t*>(a.q) + orow * S::kQDims + 8 * half;
 #pragma unroll
-      for (int i = 0; i < kQSteps; ++i) {
-        v4u_t v = {0, 0, 0, 0};
-        const int d = i < kMainSteps ? 16 * (hp * kMainSteps + i) : P::kMain / 2 + 16 * (hp * (kQSteps - kMainSteps) + i - kMainSteps);
-        if (valid) v = *reinterpret_cast<const v4u_t*>(qp + d);
-        qf[i] = as_bf16x8(v);
-      }
+      for (int i = 0; i < kQSteps; ++i) qf[i] = as_bf16x8(*reinterpret_cast<const v4u_t*>(qp + 16 * i));
     }
 
-    // Table entries: a wave keeps two windows of 64 in LDS; the next is requested when the loads
-    // enter the one before it.
-    const int32_t* tbl = a.block_tables + (size_t)s * a.max_blocks_per_seq;
-    auto load_window = [&](int e0) __attribute__((always_inline)) {   // e0: a multiple of 64
-      const int e = max(0, min(e0 + lane, nblk - 1));
-      load_word_to_lds(tbl, 4u * (uint32_t)e, tab + (e0 & (kTable - 1)));
-    };
-    auto entry = [&](int e) __attribute__((always_inline)) -> int {   // -1: none
-      const int v = __builtin_amdgcn_readfirstlane(lds_word(tab + (e & (kTable - 1))));
-      return (e < nblk && v >= 0 && v < a.num_blocks) ? v : -1;
-    };
-    // Requests the wave's part of the rows of step `step`; whether a block of them is missing.
-    auto issue = [&](int step) __attribute__((always_inline)) -> bool {
+    uint32_t holes = 0;   // bit step % 32: a block of that step's tile is missing
+    // Requests the wave's part of the rows of a step.
+    auto request = [&](int step) __attribute__((always_inline)) {
       const int e = 2 * (step * NKW + kg);
+      if ((e & 63) < 2 * NKW && step > first) table.load((e & ~63) + 64);
+      const int b0 = table(e), b1 = table(e + 1);
+      holes = (holes & ~(1u << (step & 31))) | ((b0 < 0 || b1 < 0 ? 1u : 0u) << (step & 31));
       uint8_t* dst = ring + (step % SLOTS) * S::kTile;
-      if ((e & 63) < 2 * NKW && step > first) load_window((e & ~63) + 64);
-      const int b0 = entry(e), b1 = entry(e + 1);
-      bool gone = b0 < 0 || b1 < 0;
-      if constexpr (P::kPaged) {
-        if constexpr (NCW > 1 && NKW > 1) {   // (the workgroup's waves meet at the step's barriers: all look at all its entries)
+      const int ln = lane_here();
+      // (dense rows: of the tile, whose place is known)
+      const size_t row0 = P::kPaged || !fits ? 0 : (size_t)(at.row0 + (int64_t)step * S::KS + kKeys * kg);
 #pragma unroll
-          for (int i = 2; i < 2 * NKW; ++i) gone |= entry((e - 2 * kg) + (2 * kg + i) % (2 * NKW)) < 0;
-        }
-        if constexpr (P::kVal != 0) {
-#pragma unroll
-          for (int i = 0; i < kR / 4; ++i) {
-            const int row = kR * sharer + 4 * i;   // its first of four
-            const size_t at_row = ((size_t)max((row >> 4) ? b1 : b0, 0) * Hkv + g) * (kBlockSize * P::kMain) + (row & 15) * P::kMain;
-            const int r = row + (lane >> 4);
-            const uint32_t off = (uint32_t)((lane >> 4) * P::kMain + (((lane & 15) ^ swz(r)) << 4));
-            load_to_lds(static_cast<const uint8_t*>(a.k_pool) + at_row, off, dst + row * P::kMain);
-            load_to_lds(static_cast<const uint8_t*>(a.v_pool) + at_row, off, dst + S::kValAt + row * P::kVal);
-          }
-        } else {
-          constexpr int kRow = P::kMain + P::kRot;
-#pragma unroll
-          for (int i = 0; i < kR; ++i) {
-            const int row = kR * sharer + i;
-            const uint8_t* src = static_cast<const uint8_t*>(a.k_pool) +
-                                 ((size_t)max((row >> 4) ? b1 : b0, 0) * kBlockSize + (row & 15)) * kRow;
-            load_to_lds(src, (uint32_t)((lane ^ swz(row)) << 4), dst + row * P::kMain);
-          }
-#pragma unroll
-          for (int i = 0; i < (kR + 7) / 8; ++i) {   // second parts, eight rows at once
-            const int row = kR * sharer + 8 * i;
-            const uint8_t* src = static_cast<const uint8_t*>(a.k_pool) +
-                                 ((size_t)max((row >> 4) ? b1 : b0, 0) * kBlockSize + (row & 15)) * kRow + P::kMain;
-            const int r = row + (lane >> 3);
-            if (kR >= 8 || lane < 8 * kR)
-              load_to_lds(src, (uint32_t)((lane >> 3) * kRow + (((lane & 7) ^ ((r >> 1) & 7)) << 4)),
-                          dst + S::kRotAt + row * P::kRot);
-          }
-        }
-      } else {
-        const size_t row0 = fits ? (size_t)(at.row0 + (int64_t)step * S::KS + kKeys * kg) : 0;
-        const size_t head = ((size_t)g * a.dense_rows + row0) * P::kMain;
-#pragma unroll
-        for (int i = 0; i < kR / 4; ++i) {
-          const int row = kR * sharer + 4 * i, r = row + (lane >> 4);
-          const uint32_t off = (uint32_t)((lane >> 4) * P::kMain + (((lane & 15) ^ swz(r)) << 4));
-          load_to_lds(static_cast<const uint8_t*>(a.k_pool) + head + row * P::kMain, off, dst + row * P::kMain);
-          load_to_lds(static_cast<const uint8_t*>(a.v_pool) + head + row * P::kMain, off, dst + S::kValAt + row * P::kVal);
-        }
+      for (int i = 0; i < kR / 4; ++i) {
+        const int row = kR * cw + 4 * i;   // the first of four
+        size_t src;
+        if constexpr (P::kPaged) src = ((size_t)max((row >> 4) ? b1 : b0, 0) * Hkv + g) * (kBlockSize * P::kMain) + (row & 15) * P::kMain;
+        else src = ((size_t)g * a.dense_rows + row0 + row) * P::kMain;
+        const uint32_t off = (uint32_t)((ln >> 4) * P::kMain + (((ln & 15) ^ swz(row + (ln >> 4))) << 4));
+        load_to_lds(static_cast<const uint8_t*>(a.k_pool) + src, off, dst + row * P::kMain);
+        load_to_lds(static_cast<const uint8_t*>(a.v_pool) + src, off, dst + S::kValAt + row * P::kVal);
+      }
+      if constexpr (P::kRot != 0) {
 #pragma unroll
         for (int i = 0; i < kR / 8; ++i) {
-          const int row = kR * sharer + 8 * i, r = row + (lane >> 3);
+          const int row = kR * cw + 8 * i, r = row + (ln >> 3);
           load_to_lds(static_cast<const uint8_t*>(a.rot_rows) + (row0 + row) * P::kRot,
-                      (uint32_t)((lane >> 3) * P::kRot + (((lane & 7) ^ ((r >> 1) & 7)) << 4)), dst + S::kRotAt + row * P::kRot);
+                      (uint32_t)((ln >> 3) * P::kRot + (((ln & 7) ^ ((r >> 1) & 7)) << 4)), dst + S::kRotAt + row * P::kRot);
         }
       }
-      return gone;
     };
+    // The first position of the wave's tile in a step; whether the step needs masks there.
+    auto pos_of = [&](int step) -> int { return step * S::KS + kKeys * kg; };
+    auto masked = [&](int step) -> bool { return ((holes >> (step & 31)) & 1) || pos_of(step) + kKeys > full_below; };
+    auto blocks_of = [&](int pos0) -> TileBlocks { return tile_blocks(a, table.tbl, table.nblk, s, pos0, P::kPaged); };
 
     floatx16 o[kDt];
 #pragma unroll
@@ -464,116 +481,74 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
     uint32_t odd = 0;   // a value that is not finite was left out of a product
 
-    // The two blocks of the tile at pos0: whether they are there, and their directions.
-    auto blocks_of = [&](int pos0) -> TileBlocks {
-      const int e = pos0 / kBlockSize, em = max(nblk - 1, 0);
-      const int v0 = tbl[min(e, em)], v1 = tbl[min(e + 1, em)];
-      const bool ok0 = e < nblk && v0 >= 0 && v0 < a.num_blocks, ok1 = e + 1 < nblk && v1 >= 0 && v1 < a.num_blocks;
-      if constexpr (!P::kPaged) return TileBlocks{ok0, ok1, 1, 1};   // (dense rows lie in the order of their positions)
-      return TileBlocks{ok0, ok1, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e, em)),
-                        entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e + 1, em))};
+    // Waits for the wave's rows of a step (those of the next SLOTS - 2 may be in flight) and, where the step is
+    // masked, puts its values in order: zeros where no context is, and for values that are not finite. Then
+    // the waves that share a tile meet.
+    auto publish = [&](int step) __attribute__((always_inline)) {
+      if (step < last) {
+        const int later = min(SLOTS - 2, last - 1 - step);
+        if (later >= 2) wait_vmem<2 * S::kLoads>();
+        else if (later == 1) wait_vmem<S::kLoads>();
+        else wait_vmem<0>();
+        if (masked(step)) {
+          const int pos0 = pos_of(step);
+          const TileBlocks tb = blocks_of(pos0);
+          uint8_t* vt = ring + (step % SLOTS) * S::kTile + S::kValAt;
+          for (int i = lane; i < kR * (P::kVal / 16); i += kWave) {
+            const int r = kR * cw + i / (P::kVal / 16);
+            const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
+            const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;
+            v4u_t* at_v = reinterpret_cast<v4u_t*>(vt + r * P::kVal) + i % (P::kVal / 16);
+            v4u_t w = there ? *at_v : v4u_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t bad = not_finite(w[e]);
+              odd |= bad;
+              w[e] &= ~((bad >> 15) * 0xffffu);
+            }
+            *at_v = w;
+          }
+        }
+      }
+      if constexpr (NCW > 1) lds_barrier();
+      else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (a wave's own rows: what was read is read, what was written is there)
     };
 
-    // ---- Start: the first windows of the table, then the first SLOTS - 1 steps' rows.
+    // ---- Start: the first windows of the table, the first SLOTS - 1 steps' rows.
     __syncthreads();   // (the ring's last use: the segment before this one)
     if (tid == 0) s_odd = 0;
-    __syncthreads();
     {
       const int e = 2 * (first * NKW + kg) & ~63;
-      load_window(e);
-      load_window(e + 64);
+      table.load(e);
+      table.load(e + 64);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): a wait the compiler sees, q's included
     asm volatile("" ::: "memory");
-    uint32_t missing = 0;   // bit step % 32: a block of that step is missing
-    const int last = first + cnt;
-    auto request = [&](int step) __attribute__((always_inline)) {
-      const bool gone = issue(step);
-      missing = (missing & ~(1u << (step & 31))) | ((gone ? 1u : 0u) << (step & 31));
-    };
 #pragma unroll
     for (int i = 0; i < SLOTS - 1; ++i)
       if (first + i < last) request(first + i);
+    publish(first);
 
+#pragma unroll 1
     for (int step = first; step < last; ++step) {
-      // ---- This step's rows are in LDS (all waves'), and every wave is past the step before.
-      const int ahead = min(SLOTS - 2, last - 1 - step);   // later steps still in flight
-      if (ahead >= 2) wait_vmem<(2 * S::kLoads < 63 ? 2 * S::kLoads : 63)>();
-      else if (ahead == 1) wait_vmem<S::kLoads>();
-      else wait_vmem<0>();
-      if constexpr (S::kSharers > 1) lds_barrier();
-      else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (a wave's own rows: the step before is read out)
+      // (every wave is past the step before: its slot is free)
       if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
-      uint8_t* tile = ring + (step % SLOTS) * S::kTile;
-      const int pos0 = step * S::KS + kKeys * kg;            // first position of this wave's tile
-      const bool hole = (missing >> (step & 31)) & 1;
-      const bool masked = hole || pos0 + kKeys > full_below;
-      uint32_t win = 0xffffffffu;
-      TileBlocks tb{true, true, 1, 1};
-      if (masked) {
-        win = row_window(a, q, ctx, j, valid, pos0);
-        tb = blocks_of(pos0);
-      }
-      // The wave's rows of values: zeros where no context is, and for values that are not finite.
-      // Then the waves that share the tile meet (the condition is the same for all of the workgroup).
-      const auto clean = [&]() __attribute__((always_inline)) {
-        if (masked) {
-          constexpr int kChunks = kVRow / 16;
-          for (int i = lane; i < kR * kChunks; i += kWave) {
-            const int r = kR * sharer + i / kChunks;
-            const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
-            v4u_t* at_v = reinterpret_cast<v4u_t*>(tile + kVAt + r * kVRow) + i % kChunks;
-            if (!((r < 16 ? tb.ok0 : tb.ok1) && pos < ctx)) {
-              *at_v = v4u_t{0, 0, 0, 0};
-              continue;
-            }
-            v4u_t w = *at_v;
-            uint32_t any = 0;
-  #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t bad = not_finite(w[e]);
-              any |= bad;
-              w[e] &= ~((bad >> 15) * 0xffffu);
-            }
-            if (any != 0) *at_v = w;
-            odd |= any;
-          }
-        }
-        if (S::kSharers > 1 && (hole || (step + 1) * S::KS > full_below)) lds_barrier();
-      };
-      if constexpr (P::kVal != 0) clean();
+      const uint32_t tile = ring0 + (step % SLOTS) * S::kTile;
 
       // ---- Scores.
       floatx16 cur;
-#pragma unroll
-      for (int i = 0; i < kQSteps; ++i) {
-        const uint8_t* src = i < kMainSteps ? tile + k_lane + (((2 * i) ^ (k_sw & 14)) << 4)
-                                            : tile + S::kRotAt + r_lane + (((2 * (i - kMainSteps) + half) ^ r_sw) << 4);
-        const v4u_t kv = *reinterpret_cast<const v4u_t*>(src);
-        cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kv), qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
+      {
+        const uint32_t k = tile + k_lane, r = tile + r_lane;
+        pipelined<kQSteps, kAhead>(
+            [&](int i) __attribute__((always_inline)) { return i < kMainSteps ? lds_read(k ^ (i << 5)) : lds_read(r ^ ((i - kMainSteps) << 5)); },
+            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
+              cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
+            });
       }
-      if constexpr (H > 1) {   // the other parts' sums
-        float4* mine = reinterpret_cast<float4*>(s_x) + wave * 4 * kWave + lane;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mine[i * kWave] = make_float4(cur[4 * i], cur[4 * i + 1], cur[4 * i + 2], cur[4 * i + 3]);
-        lds_barrier();
-        // ((0 + 1) + (2 + 3), whichever part adds: the waves of a column must hold the same scores)
-        const auto part = [&](int k, int i) { return (reinterpret_cast<const float4*>(s_x) + ((hp ^ k) * NCW + cw) * 4 * kWave + lane)[i * kWave]; };
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float4 y = part(1, i), z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if constexpr (H == 4) {
-            const float4 u = part(2, i), v = part(3, i);
-            z = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w);
-          }
-          cur[4 * i] = (cur[4 * i] + y.x) + z.x;
-          cur[4 * i + 1] = (cur[4 * i + 1] + y.y) + z.y;
-          cur[4 * i + 2] = (cur[4 * i + 2] + y.z) + z.z;
-          cur[4 * i + 3] = (cur[4 * i + 3] + y.w) + z.w;
-        }
-      }
-      if constexpr (P::kVal == 0) clean();   // (the scores have been taken from the rows as they are)
-      if (masked) {
+      if (masked(step)) {
+        const int pos0 = pos_of(step);
+        const TileBlocks tb = blocks_of(pos0);
+        const uint32_t win = row_window(a, q, ctx, j, valid, pos0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int k = 8 * (i >> 2) + 4 * half + (i & 3);
@@ -612,20 +587,21 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
                           __builtin_bit_cast(uint32_t, pw[2]), __builtin_bit_cast(uint32_t, pw[3])};
         pfr[c2] = as_bf16x8(pk);
       }
-
       // ---- Values.
-      const uint8_t* vt = tile + kVAt;
-      const auto values = [&](int c2, int dt) __attribute__((always_inline)) -> v4u_t {
-        const uint2 x0 = lds_read_tr(vt + 16 * c2 * kVRow + v_off[0] + (((4 * dt) ^ (v_sw[0] & 12)) << 4));
-        const uint2 x1 = lds_read_tr(vt + 16 * c2 * kVRow + v_off[1] + (((4 * dt) ^ (v_sw[1] & 12)) << 4));
-        return v4u_t{x0.x, x0.y, x1.x, x1.y};
-      };
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(values(c2, dt)), pfr[c2], o[dt], 0, 0, 0);
+      {
+        const uint32_t v = tile + v_lane;
+        pipelined<2 * kDt, kAhead>(
+            [&](int i) __attribute__((always_inline)) {
+              const uint32_t at_v = (v ^ ((i % kDt) << 6)) + 16 * (i / kDt) * P::kVal;
+              // (keys 8 on: another bit of the row's permutation)
+              const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned((at_v ^ 16) + 8 * P::kVal);
+              return v4u_t{x0.x, x0.y, x1.x, x1.y};
+            },
+            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
+              o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pfr[i / kDt], o[i % kDt], 0, 0, 0);
+            });
       }
+      publish(step + 1);
     }
 
     // ---- The end of the segment.
@@ -674,28 +650,28 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
         }
       }
     }
+    const size_t ws = 2 * (size_t)me + (first == 0 ? 1 : 0);   // the partial's slot
     if (kg == 0) {
       if (whole) {
-        const float inv = l > 0.0f ? 1.0f / l : l < 0.0f ? 0.0f : l == 0.0f ? 0.0f : l;   // (NaN stays)
-        if (valid) write_columns<kDt>(static_cast<uint16_t*>(a.out) + orow * S::kDims, hp * kDt, o, inv, half);
+        const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // (NaN stays)
+        if (valid) write_columns<kDt>(static_cast<uint16_t*>(a.out) + orow * S::kDims, 0, o, inv, half);
       } else {
         // the accumulators as they lie: every store of the wave is 1 KiB contiguous
-        const size_t slot = 2 * (size_t)me + (first == 0 ? 1 : 0);
-        float4* po = reinterpret_cast<float4*>(a.ws_o + slot * S::kSlotFloats) + (cw * S::kDt + hp * kDt) * 4 * kWave + lane;
+        float4* po = reinterpret_cast<float4*>(a.ws_o + ws * S::kSlotFloats) + cw * kDt * 4 * kWave + lane;
 #pragma unroll
         for (int i = 0; i < kDt; ++i) {
 #pragma unroll
           for (int jq = 0; jq < 4; ++jq)
             po[(4 * i + jq) * kWave] = make_float4(o[i][4 * jq], o[i][4 * jq + 1], o[i][4 * jq + 2], o[i][4 * jq + 3]);
         }
-        if (half == 0 && hp == 0) {
-          float* ml = a.ws_ml + (slot * S::CT + 32 * cw + col) * 2;
+        if (half == 0) {
+          float* ml = a.ws_ml + (ws * S::CT + 32 * cw + col) * 2;
           ml[0] = m_run;
           ml[1] = l;
         }
+        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x + usteps - 1)};
       }
     }
-
     // ---- Values that were left out and are seen: added to the rows that see them, where
     // those now lie. (Every key of the segment's masked tiles is looked at again, in memory.)
     if (kg == 0 && s_odd != 0) {
@@ -703,34 +679,22 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
 #pragma unroll 1
       for (int ti = 0; ti < tiles; ++ti) {
         const int pos0 = first * S::KS + kKeys * ti;
-        TileBlocks tb{true, true, 1, 1};
-        tb = blocks_of(pos0);
-        bool hole = !tb.ok0 || !tb.ok1;
-        if constexpr (NCW > 1 && NKW > 1) {
-          for (int k = 0; k < NKW; ++k) {
-            const TileBlocks other = blocks_of((pos0 / S::KS) * S::KS + kKeys * k);
-            hole |= !other.ok0 || !other.ok1;
-          }
-        }
-        if (pos0 + kKeys <= full_below && !hole) continue;
+        const TileBlocks tb = blocks_of(pos0);
+        if (pos0 + kKeys <= full_below && tb.ok0 && tb.ok1) continue;
         const uint32_t win = row_window(a, q, ctx, j, valid, pos0);
         // value row of tile row r, or null where no context is
         const auto value_row = [&](int r) -> const uint8_t* {
-          if constexpr (P::kPaged) {
-            const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
-            if (!(r < 16 ? tb.ok0 : tb.ok1) || pos >= ctx) return nullptr;
-            const size_t slot = ((size_t)tbl[pos / kBlockSize] * Hkv + g) * kBlockSize + (r & 15);
-            if constexpr (P::kVal != 0) return static_cast<const uint8_t*>(a.v_pool) + slot * P::kVal;
-            return static_cast<const uint8_t*>(a.k_pool) + slot * (P::kMain + P::kRot);
-          }
-          if (!(r < 16 ? tb.ok0 : tb.ok1) || pos0 + r >= ctx) return nullptr;
-          return static_cast<const uint8_t*>(a.v_pool) + ((size_t)g * a.dense_rows + at.row0 + pos0 + r) * P::kMain;
+          const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
+          if (!(r < 16 ? tb.ok0 : tb.ok1) || pos >= ctx) return nullptr;
+          if constexpr (P::kPaged)
+            return static_cast<const uint8_t*>(a.v_pool) + (((size_t)table.tbl[pos / kBlockSize] * Hkv + g) * kBlockSize + (r & 15)) * P::kVal;
+          return static_cast<const uint8_t*>(a.v_pool) + ((size_t)g * a.dense_rows + at.row0 + pos0 + r) * P::kVal;
         };
         uint32_t any = 0;
-        for (int i = lane; i < kKeys * (kVRow / 16); i += kWave) {
-          const uint8_t* row = value_row(i / (kVRow / 16));
+        for (int i = lane; i < kKeys * (P::kVal / 16); i += kWave) {
+          const uint8_t* row = value_row(i / (P::kVal / 16));
           if (row == nullptr) continue;
-          const v4u_t w = *reinterpret_cast<const v4u_t*>(row + 16 * (i % (kVRow / 16)));
+          const v4u_t w = *reinterpret_cast<const v4u_t*>(row + 16 * (i % (P::kVal / 16)));
           any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
         }
         if (__builtin_amdgcn_ballot_w64(any != 0) == 0) continue;
@@ -738,24 +702,23 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
         for (int r = 0; r < kKeys; ++r) {
           const uint8_t* row = value_row(r);
           if (row == nullptr) continue;
-          const int off = P::kPaged ? (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1) : r;
+          const int off = (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
           if (!((win >> off) & 1u)) continue;
 #pragma unroll 1
           for (int i = 0; i < 4 * kDt; ++i) {
-            const int d = 32 * hp * kDt + 8 * i + 4 * half;   // four dims
+            const int d = 8 * i + 4 * half;   // four dims
             const uint2 w = *reinterpret_cast<const uint2*>(row + 2 * d);
             if ((not_finite(w.x) | not_finite(w.y)) == 0) continue;
             const float v[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
             if (whole) {
               uint2* at_out = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + orow * S::kDims + d);
-              uint2 y = *at_out;
-              float x[4] = {bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
+              const uint2 y = *at_out;
+              float z[4] = {bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = fabsf(v[e]) < INFINITY ? x[e] : x[e] + v[e];
-              *at_out = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
+              for (int e = 0; e < 4; ++e) z[e] = fabsf(v[e]) < INFINITY ? z[e] : z[e] + v[e];
+              *at_out = make_uint2(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]));
             } else {
-              float* at_ws = a.ws_o + (2 * (size_t)me + (first == 0 ? 1 : 0)) * S::kSlotFloats +
-                             ((cw * S::kDt + hp * kDt) * 4 + i) * (4 * kWave) + 4 * lane;
+              float* at_ws = a.ws_o + ws * S::kSlotFloats + (cw * kDt * 4 + i) * (4 * kWave) + 4 * lane;
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (!(fabsf(v[e]) < INFINITY)) at_ws[e] += v[e];
@@ -766,7 +729,7 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
     }
 
     // ---- The next unit.
-    x += cnt;
+    x += st.whole ? 1 : cnt;
     at.step = 0;
     if (x < x_end) {
       if (++at.t >= st.tiles) {
@@ -783,59 +746,74 @@ __global__ __launch_bounds__(64 * NCW * NKW * H, OCC) void rows_kernel(RowsArgs 
   }
 }
 
-// Folds the partials of the units cut between shares: workgroup (w, cw) those of the unit in
-// which share w's end is the first cut. Four waves, each a quarter of the value's dims.
-template <class P, int NCW, int NKW, int H, int SLOTS>
-__global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) {
-  using S = Shape<P, NCW, NKW, H, SLOTS>;
-  constexpr int kPer = S::kDt / 4;   // 32-dim pieces of a wave
-  __shared__ int64_t s_scan[2 * 4];
-  __shared__ Place s_place;
-  const int G = P::kPaged ? a.num_q_heads / a.num_kv_heads : 1;
-  const int w0 = blockIdx.x, cw = blockIdx.y;
-  const int lane = threadIdx.x & (kWave - 1), wave = wave_id_uniform(), half = lane >> 5, col = lane & 31;
-  const Place at = find_place<P, S::CT, S::KS, 256>(
-      a, G, [&](int64_t total) -> int64_t {
-        const int n = sharers(a, total);
-        return w0 + 1 < n ? share_begin(total, w0 + 1, n) : -1;
-      }, s_scan, &s_place);
-  if (at.s < 0 || at.step == 0) return;
-  const int n = sharers(a, at.total);
-  const int64_t x = share_begin(at.total, w0 + 1, n), begin = x - at.step;
-  if (share_begin(at.total, w0, n) > begin) return;   // an earlier share's end cuts this unit too
-  const Seq q = seq_of(a, at.s);
-  const Steps<P, S::CT, S::KS> st(a, q, G);
-  const int w1 = share_of(at.total, begin + st.of(at.t) - 1, n);
+// Folds the partials of the units cut between shares: workgroup (w, y) the chunks kWaves kEach y .. of the unit
+// that share w noted. A chunk is 1 KiB of a partial: a wave's columns, four dims to a lane.
+constexpr int kMergeWaves = 4, kMergeEach = 2;   // waves of a workgroup, chunks of a wave
+template <class S, bool DENSE>
+__global__ __launch_bounds__(kMergeWaves * kWave) void rows_merge_kernel(RowsArgs a) {
+  constexpr int kGroups = S::CT / S::kLaneCols;            // column waves of a partial
+  constexpr int kParts = S::kChunks / kMergeEach;          // waves to one of them
+  static_assert(S::kChunks % kMergeEach == 0 && kGroups * kParts % kMergeWaves == 0, "");
+  const int w0 = blockIdx.x, lane = threadIdx.x & (kWave - 1);
+  const Cut cut = reinterpret_cast<const Cut*>(a.ws_cut)[w0];
+  if (cut.last < 0) return;
+  const int item = blockIdx.y * kMergeWaves + wave_id_uniform();
+  const int cw = item / kParts, i0 = (item % kParts) * kMergeEach;
+  const int col = S::kLaneCols * cw + lane % S::kLaneCols;
+  const int pieces = cut.last - w0 + 1;
+  const auto slot = [&](int p) -> size_t { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };
+  const auto ml = [&](int p) -> float2 { return reinterpret_cast<const float2*>(a.ws_ml)[slot(p) * S::CT + col]; };
 
-  const int c = at.t * S::CT + 32 * cw + col, j = c / G;
-  floatx16 o[kPer];
+  float m = kNoMax;
+  for (int p = 0; p < pieces; p += 4) {   // (past the end: the last again)
+    float2 y[4];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) o[i] = floatx16{};
-  float m = kNoMax, l = 0.0f;
-  for (int w = w0; w <= w1; ++w) {
-    const size_t slot = 2 * (size_t)w + (w == w0 ? 1 : 0);
-    const float4* po = reinterpret_cast<const float4*>(a.ws_o + slot * S::kSlotFloats) + (cw * S::kDt + wave * kPer) * 4 * kWave + lane;
-    const float* ml = a.ws_ml + (slot * S::CT + 32 * cw + col) * 2;
-    const float m2 = ml[0], l2 = ml[1];
-    const float mn = fmaxf(m, m2), f1 = fast_exp2(m - mn), f2 = fast_exp2(m2 - mn);
-    m = mn;
-    l = l * f1 + l2 * f2;
+    for (int u = 0; u < 4; ++u) y[u] = ml(min(p + u, pieces - 1));
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int u = 0; u < 4; ++u) m = fmaxf(m, y[u].x);
+  }
+  float l = 0.0f;
+  float4 o[kMergeEach];
 #pragma unroll
-      for (int jq = 0; jq < 4; ++jq) {
-        const float4 y = po[(4 * i + jq) * kWave];
-        o[i][4 * jq] = o[i][4 * jq] * f1 + y.x * f2;
-        o[i][4 * jq + 1] = o[i][4 * jq + 1] * f1 + y.y * f2;
-        o[i][4 * jq + 2] = o[i][4 * jq + 2] * f1 + y.z * f2;
-        o[i][4 * jq + 3] = o[i][4 * jq + 3] * f1 + y.w * f2;
+  for (int i = 0; i < kMergeEach; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int p = 0; p < pieces; p += 4) {
+    float2 y[4];
+    float4 z[4][kMergeEach];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int pu = min(p + u, pieces - 1);
+      y[u] = ml(pu);
+      const float4* po = reinterpret_cast<const float4*>(a.ws_o + slot(pu) * S::kSlotFloats) + (cw * S::kChunks + i0) * kWave + lane;
+#pragma unroll
+      for (int i = 0; i < kMergeEach; ++i) z[u][i] = po[i * kWave];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (p + u >= pieces) break;
+      const float f = fast_exp2(y[u].x - m);
+      l = fmaf(y[u].y, f, l);
+#pragma unroll
+      for (int i = 0; i < kMergeEach; ++i) {
+        o[i].x = fmaf(z[u][i].x, f, o[i].x);
+        o[i].y = fmaf(z[u][i].y, f, o[i].y);
+        o[i].z = fmaf(z[u][i].z, f, o[i].z);
+        o[i].w = fmaf(z[u][i].w, f, o[i].w);
       }
     }
   }
+  const int G = DENSE ? 1 : a.num_q_heads / a.num_kv_heads;
+  const Seq q = seq_of(a, cut.s);
+  const int c = cut.t * S::CT + col, j = c / G;
   if (j >= q.n) return;
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  const size_t orow = (size_t)(q.q0 + j) * a.num_q_heads + a.head0 + at.g * G + (c - j * G);
-  write_columns<kPer>(static_cast<uint16_t*>(a.out) + orow * S::kDims, wave * kPer, o, inv, half);
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // (NaN stays)
+  const size_t orow = (size_t)(q.q0 + j) * a.num_q_heads + a.head0 + cut.g * G + (c - j * G);
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) {
+    uint2 w;
+    w.x = pack2_bf16(o[i].x * inv, o[i].y * inv);
+    w.y = pack2_bf16(o[i].z * inv, o[i].w * inv);
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + orow * S::kDims + S::dim_of(i0 + i, lane)) = w;
+  }
 }
 
 }  // namespace ra

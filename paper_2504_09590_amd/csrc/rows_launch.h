@@ -1,5 +1,5 @@
-// Launching the kernels of rows_device.h: shares for a stream's compute units, the partials'
-// workspace, the merge.
+// Launching the kernels of rows_device.h and latent_device.h: shares for a stream's compute units,
+// the partials' workspace, the merge.
 #pragma once
 
 #include "latent_device.h"
@@ -11,37 +11,42 @@ namespace ra {
 
 constexpr int kMaxCus = 256;   // compute units whose shares' partials the workspace holds
 
-// Bytes of the partials of `workers` shares of units of CT columns and `dims` dims.
-constexpr size_t partial_bytes(size_t workers, size_t ct, size_t dims) { return 2 * workers * ct * (dims + 2) * sizeof(float); }
+// Bytes of the notes and partials of `workers` shares of units of CT columns and `dims` dims.
+constexpr size_t partial_bytes(size_t workers, size_t ct, size_t dims) {
+  return workers * sizeof(Cut) + 2 * workers * ct * (dims + 2) * sizeof(float);
+}
 
-// PER_CU: workgroups a compute unit holds. MIN: the least steps of a share.
-template <class P, int NCW, int NKW, int H, int SLOTS, int PER_CU, int MIN>
-hipError_t launch_rows(RowsArgs a, void* workspace, hipStream_t stream) {
-  using S = Shape<P, NCW, NKW, H, SLOTS>;
-  constexpr int kEachEu = std::max(1, S::kWaves * PER_CU / 4);
-  a.workers = std::min(stream_compute_units(stream), kMaxCus) * PER_CU;
-  a.min_steps = MIN;
-  a.ws_o = static_cast<float*>(workspace);
+// Launches `kernel` on per_cu workgroups a compute unit, and the merge. min_steps: the least steps of a share.
+// whole: steps of the longest unit up to which units are not cut.
+template <class S, bool DENSE, class Kernel>
+hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, int whole, void* workspace, hipStream_t stream) {
+  a.workers = std::min(stream_compute_units(stream), kMaxCus) * per_cu;
+  a.min_steps = min_steps;
+  a.whole_units = ((int64_t)std::min<int64_t>(a.max_ctx, (int64_t)a.max_blocks_per_seq * kBlockSize) + S::KS - 1) / S::KS <= whole;
+  if (a.whole_units) a.min_steps = 1;
+  a.ws_cut = workspace;
+  a.ws_o = reinterpret_cast<float*>(static_cast<Cut*>(workspace) + a.workers);
   a.ws_ml = a.ws_o + 2 * (size_t)a.workers * S::kSlotFloats;
-  hipLaunchKernelGGL((rows_kernel<P, NCW, NKW, H, SLOTS, kEachEu>), dim3(a.workers), dim3(S::kThreads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(a.workers), dim3(S::kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((rows_merge_kernel<P, NCW, NKW, H, SLOTS>), dim3(std::max(1, a.workers - 1), NCW), dim3(256), 0, stream, a);
+  if (e != hipSuccess || a.whole_units) return e;
+  constexpr int kItems = S::CT / S::kLaneCols * S::kChunks / kMergeEach;
+  hipLaunchKernelGGL((rows_merge_kernel<S, DENSE>), dim3(std::max(1, a.workers - 1), kItems / kMergeWaves), dim3(kMergeWaves * kWave), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
-template <int NCW, int H, int MIN>
-hipError_t launch_latent_rows(RowsArgs a, void* workspace, hipStream_t stream) {
-  using S = LatentShape<NCW, H>;
-  a.workers = std::min(stream_compute_units(stream), kMaxCus);
-  a.min_steps = MIN;
-  a.ws_o = static_cast<float*>(workspace);
-  a.ws_ml = a.ws_o + 2 * (size_t)a.workers * S::kSlotFloats;
-  hipLaunchKernelGGL((latent_kernel<NCW, H, S::kWaves / 4>), dim3(a.workers), dim3(S::kThreads), 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((rows_merge_kernel<LatentPool, NCW, 1, H, 3>), dim3(std::max(1, a.workers - 1), NCW), dim3(256), 0, stream, a);
-  return hipGetLastError();
+template <class P, int NCW, int NKW, int SLOTS, int PER_CU>
+hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, void* workspace, hipStream_t stream) {
+  using S = Shape<P, NCW, NKW, SLOTS>;
+  constexpr int kEachEu = std::max(1, S::kWaves * PER_CU / 4);
+  return launch_shares<S, !P::kPaged>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu>, a, PER_CU, min_steps, whole, workspace, stream);
+}
+
+template <int NCW, int HV>
+hipError_t launch_latent_rows(const RowsArgs& a, int min_steps, int whole, void* workspace, hipStream_t stream) {
+  using S = LatentShape<NCW, HV>;
+  return launch_shares<S, false>(&latent_kernel<NCW, HV, S::kWaves / 4>, a, 1, min_steps, whole, workspace, stream);
 }
 
 }  // namespace ra

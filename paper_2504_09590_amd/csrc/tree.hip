@@ -75,9 +75,9 @@ size_t rows_workspace_bytes(bool latent) {
 
 hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * (a.num_q_heads / a.num_kv_heads);
-  if (columns <= 32) return ra::launch_rows<ra::KvPool, 1, 4, 1, 2, 1, 2>(a, workspace, stream);
-  if (columns <= 64) return ra::launch_rows<ra::KvPool, 2, 2, 1, 4, 1, 2>(a, workspace, stream);
-  return ra::launch_rows<ra::KvPool, 4, 1, 1, 4, 2, 4>(a, workspace, stream);
+  if (columns <= 32) return ra::launch_rows<ra::KvPool, 1, 4, 2, 1>(a, 2, 4, workspace, stream);
+  if (columns <= 64) return ra::launch_rows<ra::KvPool, 2, 2, 4, 1>(a, 2, 6, workspace, stream);
+  return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 8, workspace, stream);
 }
 
 hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream) {
