@@ -68,10 +68,11 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
   using S = LatentShape<NCW, HV>;
   constexpr int kDt = S::kDt / HV;                           // of this wave: 16-dim pieces of values
   constexpr int kQSteps = 18, kMainSteps = 16;               // 32-dim steps of score products
-  constexpr int kAhead = 4;                                  // operands read before the first product
+  constexpr int kAhead = HV == 1 ? 4 : 8;                    // operands read before the first product (as registers allow)
   constexpr int kRow = P::kMain + P::kRot;
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[S::SLOTS * S::kTile];
   __shared__ int32_t s_tab[S::kWaves][kTable];
+  __shared__ uint64_t s_word[S::kWaves][16];                 // the first mask word of each of a wave's columns
   __shared__ uint32_t s_bad[S::SLOTS][S::kWaves];            // of each row that a wave requested: something is not finite
   __shared__ int64_t s_scan[2 * S::kWaves];
   __shared__ Place s_place;
@@ -132,20 +133,33 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
     const int full_below = a.mask != nullptr ? min(ctx, q.c0) : min(ctx, q.c0 + t * S::CT / G + 1);
     const Table table{a.block_tables + (size_t)s * a.max_blocks_per_seq, s_tab[wave], (ctx + kBlockSize - 1) / kBlockSize, a.num_blocks};
 
+    // ---- Start: the first windows of the table, then queries and masks.
+    __syncthreads();   // (the ring's last use: the segment before this one)
+    const int e_first = (2 * first) & ~63;
+    const int32_t win0 = table.get(e_first), win1 = table.get(e_first + 64);
+    const int dir_all = seq_direction(a.dir, a.cls, s);   // (read where entries have no directions of their own)
     bf16x8_t qf[kQSteps];
     {
       // (columns behind the last row take that row's values: nothing is made of them)
-      const uint16_t* qp = static_cast<const uint16_t*>(a.q) + column().orow * (kRow / 2) + 8 * quarter;
+      const Column my = column();
+      if (a.mask != nullptr && quarter == 0) s_word[wave][col] = first_word(a, q, my.j);
+      const uint16_t* qp = static_cast<const uint16_t*>(a.q) + my.orow * (kRow / 2) + 8 * quarter;
 #pragma unroll
       for (int i = 0; i < kQSteps; ++i) qf[i] = as_bf16x8(*reinterpret_cast<const v4u_t*>(qp + 32 * i));
     }
 
-    uint32_t holes = 0;   // bit step % 32: a block of that step is missing
+    uint32_t holes = 0;               // bit step % 32: a block of that step is missing
+    int32_t word_a = 0, word_b = 0;   // the next request's entries
+    auto ask = [&](int step) __attribute__((always_inline)) {
+      word_a = table.word(2 * step);
+      word_b = table.word(2 * step + 1);
+    };
     // Requests the wave's rows of a step.
     auto request = [&](int step) __attribute__((always_inline)) {
       const int e = 2 * step;
-      if ((e & 63) == 0 && step > first) table.load(e + 64);
-      const int b0 = table(e), b1 = table(e + 1);
+      const int b0 = table.entry(e, word_a), b1 = table.entry(e + 1, word_b);
+      if ((e & 63) == 2 * Table::kLag) table.load((e & ~63) + 64);
+      ask(step + 1);
       const int row0 = S::kRows * wave, b = row0 >= kBlockSize ? b1 : b0;
       const uint8_t* src = static_cast<const uint8_t*>(a.k_pool) + ((size_t)max(b, 0) * kBlockSize + (row0 & 15)) * kRow;
       uint8_t* dst = s_ring + (step % S::SLOTS) * S::kTile;
@@ -159,7 +173,14 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
       holes = (holes & ~(1u << (step & 31))) | ((b0 < 0 || b1 < 0 ? 1u : 0u) << (step & 31));
     };
     auto masked = [&](int step) -> bool { return ((holes >> (step & 31)) & 1) || (step + 1) * kKeys > full_below; };
-    auto blocks_of = [&](int step) -> TileBlocks { return tile_blocks(a, table.tbl, table.nblk, s, step * kKeys, true); };
+    auto blocks_of = [&](int step) __attribute__((always_inline)) -> TileBlocks {   // (of a step whose entries are still in LDS)
+      const int e = 2 * step;
+      TileBlocks tb;
+      tb.ok0 = table.entry(e, table.word(e)) >= 0;
+      tb.ok1 = table.entry(e + 1, table.word(e + 1)) >= 0;
+      directions(a, s, e, dir_all, tb);
+      return tb;
+    };
     // Waits for the wave's rows of a step (those of the next SLOTS - 2 may be in flight) and, where the step
     // is masked, puts them in order: zeros for rows that are no context and for values that are not
     // finite, which it notes (a row that sees such a key becomes NaN). Then the barrier.
@@ -201,14 +222,17 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
     for (int i = 0; i < kDt; ++i) o[i] = floatx4{};
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
 
-    // ---- Start: the first windows of the table, the first SLOTS - 1 steps' rows.
-    __syncthreads();   // (the ring's last use: the segment before this one)
-    table.load((2 * first) & ~63);
-    table.load(((2 * first) & ~63) + 64);
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): a wait the compiler sees, q's included
+    // ---- The first step's rows as soon as the windows are there; the next ones' behind a wait that the compiler
+    // sees: it then knows that the queries have come, and adds no waits for them among the steps.
+    table.put(e_first, win0);
+    table.put(e_first + 64, win1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ask(first);
+    request(first);
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < S::SLOTS - 1; ++i)
+    for (int i = 1; i < S::SLOTS - 1; ++i)
       if (first + i < last) request(first + i);
     publish(first);
 
@@ -228,15 +252,15 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
               return c < kMainSteps ? lds_read((k ^ ((c & 3) << 6)) + (c >> 2) * 256 + h * 16 * P::kMain)
                                     : lds_read((r ^ ((c - kMainSteps) << 6)) + h * 16 * P::kRot);
             },
-            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
+            [&](int i, v4u_t x) __attribute__((always_inline)) {
               const int c = i >> 1, h = i & 1;
-              cur[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[c], c == 0 ? floatx4{} : cur[h], 0, 0, 0);
+              cur[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x), qf[c], c == 0 ? floatx4{} : cur[h], 0, 0, 0);
             });
       }
       if (masked(step)) {
         const TileBlocks tb = blocks_of(step);
         const Column my = column();
-        const uint32_t win = row_window(a, q, ctx, my.j, my.valid, step * kKeys);
+        const uint32_t win = row_window(a, q, ctx, my.j, my.valid, step * kKeys, s_word[wave][col]);
         uint32_t bad = 0;
 #pragma unroll
         for (int w = 0; w < S::kWaves; ++w) bad |= s_bad[slot][w] << (S::kRows * w);
@@ -283,8 +307,8 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
               const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned(at_v + 16 * P::kMain);
               return v4u_t{x0.x, x0.y, x1.x, x1.y};
             },
-            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
-              o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf8, o[i], 0, 0, 0);
+            [&](int i, v4u_t x) __attribute__((always_inline)) {
+              o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x), pf8, o[i], 0, 0, 0);
             });
       }
       publish(step + 1);

@@ -149,29 +149,28 @@ struct TileBlocks {
   bool ok0, ok1;
   int dir0, dir1;
 };
-__device__ __forceinline__ TileBlocks tile_blocks(const RowsArgs& a, const int32_t* tbl, int nblk, int s, int pos0, bool paged) {
-  const int e = pos0 / kBlockSize, em = max(nblk - 1, 0);
-  const int v0 = tbl[min(e, em)], v1 = tbl[min(e + 1, em)];
-  const bool ok0 = e < nblk && v0 >= 0 && v0 < a.num_blocks, ok1 = e + 1 < nblk && v1 >= 0 && v1 < a.num_blocks;
-  if (!paged) return TileBlocks{ok0, ok1, 1, 1};   // (dense rows lie in the order of their positions)
-  return TileBlocks{ok0, ok1, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e, em)),
-                    entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, min(e + 1, em))};
-}
 // Bits 15 and 31: the halves that are infinite or NaN, as bf16.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
-// Bits of the positions pos0 .. + 31 that row j of a sequence sees, of a context of ctx.
-__device__ __forceinline__ uint32_t row_window(const RowsArgs& a, const Seq& q, int ctx, int j, bool valid, int pos0) {
+// The first word of row j's mask (of one that is not there: of the last).
+__device__ __forceinline__ uint64_t first_word(const RowsArgs& a, const Seq& q, int j) {
+  return a.mask == nullptr ? 0 : a.mask[(size_t)(q.q0 + min(j, q.n - 1)) * a.mask_words];
+}
+// Bits of the positions pos0 .. + 31 that row j of a sequence sees, of a context of ctx. word0: its mask's first.
+__device__ __forceinline__ uint32_t row_window(const RowsArgs& a, const Seq& q, int ctx, int j, bool valid, int pos0, uint64_t word0) {
   const auto below = [](int k) -> uint32_t { return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u; };
   uint32_t win;
   if (a.mask != nullptr) {
     const int i0 = pos0 - q.c0;   // draft of position pos0 (negative: before the drafts)
     win = below(-i0);
-    const uint64_t* bits = a.mask + (size_t)(q.q0 + min(j, q.n - 1)) * a.mask_words;
     // the 64 bits from draft max(i0, 0) on
     const int f = max(i0, 0), wd = f >> 6, sh = f & 63;
-    uint64_t b = wd < a.mask_words ? bits[wd] >> sh : 0;
-    if (sh != 0 && wd + 1 < a.mask_words) b |= bits[wd + 1] << (64 - sh);
+    uint64_t b = wd == 0 ? word0 >> sh : 0;
+    if (a.mask_words > 1) {
+      const uint64_t* bits = a.mask + (size_t)(q.q0 + min(j, q.n - 1)) * a.mask_words;
+      if (wd > 0 && wd < a.mask_words) b = bits[wd] >> sh;
+      if (sh != 0 && wd + 1 < a.mask_words) b |= bits[wd + 1] << (64 - sh);
+    }
     if (q.n - f < 64) b &= q.n - f <= 0 ? 0 : (1ull << (q.n - f)) - 1;
     if (i0 > -32) win |= i0 < 0 ? (uint32_t)b << -i0 : (uint32_t)b;
   } else {
@@ -321,26 +320,41 @@ __device__ __forceinline__ void pipelined(Operand operand, Product product) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     __builtin_amdgcn_sched_barrier(0);
-    product(i, as_bf16x8(x[i % DEPTH]));
+    product(i, x[i % DEPTH]);
     if (i + DEPTH < N) x[i % DEPTH] = operand(i + DEPTH);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// The table entries of a sequence as a wave keeps them: two windows of 64 in LDS, the next requested when the
-// loads enter the one before it.
+// The table entries of a sequence as a wave keeps them: two windows of 64 in LDS. The next window is requested
+// kLag steps after the requests of rows have entered the one before it: until then steps may still look at
+// entries of the window that it replaces.
 struct Table {
+  static constexpr int kLag = 4;   // more than the steps between a step's request and its masks
   const int32_t* tbl;
   int32_t* lds;      // [kTable]
   int nblk, num_blocks;
+  __device__ __forceinline__ int32_t get(int e0) const { return tbl[max(0, min(e0 + lane_here(), nblk - 1))]; }
+  __device__ __forceinline__ void put(int e0, int32_t v) const { lds[(e0 & (kTable - 1)) + lane_here()] = v; }
   __device__ __forceinline__ void load(int e0) const {   // entries e0 .. + 63
     load_word_to_lds(tbl, 4u * (uint32_t)max(0, min(e0 + lane_here(), nblk - 1)), lds + (e0 & (kTable - 1)));
   }
-  __device__ __forceinline__ int operator()(int e) const {   // -1: none
-    const int v = __builtin_amdgcn_readfirstlane(lds_word(lds + (e & (kTable - 1))));
+  // A word of LDS that holds entry e (asked for before it is needed), and the entry that it is, -1: none.
+  __device__ __forceinline__ int32_t word(int e) const { return lds_word(lds + (e & (kTable - 1))); }
+  __device__ __forceinline__ int entry(int e, int32_t word) const {
+    const int v = __builtin_amdgcn_readfirstlane(word);
     return (e < nblk && v >= 0 && v < num_blocks) ? v : -1;
   }
 };
+// Direction of entries e and e + 1 of sequence s; `all`: that of a sequence whose entries have none of their own.
+__device__ __forceinline__ void directions(const RowsArgs& a, int s, int e, int all, TileBlocks& tb) {
+  tb.dir0 = tb.dir1 = all;
+  if (a.dir != nullptr && a.dir_per_entry) {
+    const int8_t* d = a.dir + (size_t)s * a.max_blocks_per_seq;
+    tb.dir0 = d[min(e, a.max_blocks_per_seq - 1)] < 0 ? -1 : 1;
+    tb.dir1 = d[min(e + 1, a.max_blocks_per_seq - 1)] < 0 ? -1 : 1;
+  }
+}
 
 // A unit cut between shares, as its first share notes it for the merge: its last share (-1: none).
 struct Cut {
@@ -373,7 +387,11 @@ template <class P, int NCW, int NKW, int SLOTS, int OCC>
 __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   using S = Shape<P, NCW, NKW, SLOTS>;
   constexpr int kDt = S::kDt, kMainSteps = P::kMain / 32, kQSteps = S::kQDims / 16, kR = S::kRows;
-  constexpr int kAhead = 4;   // operands read before the first product
+  constexpr int kAhead = 6;   // operands read before the first product
+  // With one key group, the scores of a step are formed beside the softmax of the one before it, whose values
+  // follow: the matrix cores and the vector units then work at the same time.
+  constexpr bool kOverlap = NKW == 1;
+  static_assert(!kOverlap || SLOTS >= 3, "two steps' rows are in use");
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[S::kRing];
   __shared__ int32_t s_tab[S::kWaves][kTable];
   __shared__ int64_t s_scan[2 * S::kWaves];
@@ -432,6 +450,13 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     const int full_below = a.mask != nullptr ? min(ctx, q.c0) : min(ctx, q.c0 + t * S::CT / G + 1);
     const Table table{a.block_tables + (size_t)s * a.max_blocks_per_seq, s_tab[wave], (ctx + kBlockSize - 1) / kBlockSize, a.num_blocks};
 
+    // ---- Start: the first windows of the table, then queries and masks.
+    __syncthreads();   // (the ring's last use: the segment before this one)
+    if (tid == 0) s_odd = 0;
+    const int e_first = 2 * (first * NKW + kg) & ~63;
+    const int32_t win0 = table.get(e_first), win1 = table.get(e_first + 64);
+    const int dir_all = P::kPaged ? seq_direction(a.dir, a.cls, s) : 1;   // (read where entries have no directions of their own)
+    const uint64_t word0 = first_word(a, q, j);
     bf16x8_t qf[kQSteps];
     {
       // (columns behind the last row take that row's values: nothing is made of them)
@@ -440,12 +465,19 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       for (int i = 0; i < kQSteps; ++i) qf[i] = as_bf16x8(*reinterpret_cast<const v4u_t*>(qp + 16 * i));
     }
 
-    uint32_t holes = 0;   // bit step % 32: a block of that step's tile is missing
+    uint32_t holes = 0;         // bit step % 32: a block of that step's tile is missing
+    int32_t word_a = 0, word_b = 0;   // the next request's entries
+    auto ask = [&](int step) __attribute__((always_inline)) {
+      const int e = 2 * (step * NKW + kg);
+      word_a = table.word(e);
+      word_b = table.word(e + 1);
+    };
     // Requests the wave's part of the rows of a step.
     auto request = [&](int step) __attribute__((always_inline)) {
       const int e = 2 * (step * NKW + kg);
-      if ((e & 63) < 2 * NKW && step > first) table.load((e & ~63) + 64);
-      const int b0 = table(e), b1 = table(e + 1);
+      const int b0 = table.entry(e, word_a), b1 = table.entry(e + 1, word_b);
+      if ((e & 63) / (2 * NKW) == Table::kLag) table.load((e & ~63) + 64);
+      ask(step + 1);
       holes = (holes & ~(1u << (step & 31))) | ((b0 < 0 || b1 < 0 ? 1u : 0u) << (step & 31));
       uint8_t* dst = ring + (step % SLOTS) * S::kTile;
       const int ln = lane_here();
@@ -473,7 +505,15 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     // The first position of the wave's tile in a step; whether the step needs masks there.
     auto pos_of = [&](int step) -> int { return step * S::KS + kKeys * kg; };
     auto masked = [&](int step) -> bool { return ((holes >> (step & 31)) & 1) || pos_of(step) + kKeys > full_below; };
-    auto blocks_of = [&](int pos0) -> TileBlocks { return tile_blocks(a, table.tbl, table.nblk, s, pos0, P::kPaged); };
+    auto blocks_of = [&](int pos0) __attribute__((always_inline)) -> TileBlocks {   // (of a step whose entries are still in LDS)
+      const int e = pos0 / kBlockSize;
+      TileBlocks tb;
+      tb.ok0 = table.entry(e, table.word(e)) >= 0;
+      tb.ok1 = table.entry(e + 1, table.word(e + 1)) >= 0;
+      if constexpr (P::kPaged) directions(a, s, e, dir_all, tb);
+      else tb.dir0 = tb.dir1 = 1;   // (dense rows lie in the order of their positions)
+      return tb;
+    };
 
     floatx16 o[kDt];
 #pragma unroll
@@ -481,12 +521,13 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
     uint32_t odd = 0;   // a value that is not finite was left out of a product
 
-    // Waits for the wave's rows of a step (those of the next SLOTS - 2 may be in flight) and, where the step is
+    // Waits for the wave's rows of a step (those of the next `most` may be in flight) and, where the step is
     // masked, puts its values in order: zeros where no context is, and for values that are not finite. Then
     // the waves that share a tile meet.
-    auto publish = [&](int step) __attribute__((always_inline)) {
+    constexpr int kLater = kOverlap ? SLOTS - 3 : SLOTS - 2;
+    auto publish = [&](int step, int most) __attribute__((always_inline)) {
       if (step < last) {
-        const int later = min(SLOTS - 2, last - 1 - step);
+        const int later = min(most, last - 1 - step);
         if (later >= 2) wait_vmem<2 * S::kLoads>();
         else if (later == 1) wait_vmem<S::kLoads>();
         else wait_vmem<0>();
@@ -514,41 +555,28 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (a wave's own rows: what was read is read, what was written is there)
     };
 
-    // ---- Start: the first windows of the table, the first SLOTS - 1 steps' rows.
-    __syncthreads();   // (the ring's last use: the segment before this one)
-    if (tid == 0) s_odd = 0;
-    {
-      const int e = 2 * (first * NKW + kg) & ~63;
-      table.load(e);
-      table.load(e + 64);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): a wait the compiler sees, q's included
+    // ---- The first step's rows as soon as the windows are there; the next ones' behind a wait that the compiler
+    // sees: it then knows that queries and masks have come, and adds no waits for them among the steps.
+    table.put(e_first, win0);
+    table.put(e_first + 64, win1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ask(first);
+    request(first);
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < SLOTS - 1; ++i)
+    for (int i = 1; i < SLOTS - 1; ++i)
       if (first + i < last) request(first + i);
-    publish(first);
+    publish(first, SLOTS - 2);
 
-#pragma unroll 1
-    for (int step = first; step < last; ++step) {
-      // (every wave is past the step before: its slot is free)
-      if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
-      const uint32_t tile = ring0 + (step % SLOTS) * S::kTile;
-
-      // ---- Scores.
-      floatx16 cur;
-      {
-        const uint32_t k = tile + k_lane, r = tile + r_lane;
-        pipelined<kQSteps, kAhead>(
-            [&](int i) __attribute__((always_inline)) { return i < kMainSteps ? lds_read(k ^ (i << 5)) : lds_read(r ^ ((i - kMainSteps) << 5)); },
-            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
-              cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
-            });
-      }
+    const auto slot_of = [&](int step) -> uint32_t { return ring0 + (step % SLOTS) * S::kTile; };
+    // Masks a tile's scores and moves the running maximum (lazily); gives the factor that the sums take for it.
+    float m_prev = kNoMax;
+    auto mask_max = [&](floatx16& cur, int step) __attribute__((always_inline)) {
       if (masked(step)) {
         const int pos0 = pos_of(step);
         const TileBlocks tb = blocks_of(pos0);
-        const uint32_t win = row_window(a, q, ctx, j, valid, pos0);
+        const uint32_t win = row_window(a, q, ctx, j, valid, pos0, word0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int k = 8 * (i >> 2) + 4 * half + (i & 3);
@@ -556,22 +584,24 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           cur[i] = ((i >> 3) ? tb.ok1 : tb.ok0) && ((win >> off) & 1u) ? cur[i] : -INFINITY;
         }
       }
-      // ---- Running maximum (moved lazily) and weights, rounded to bf16 for the second
-      // product; the totals add the rounded weights.
       float mr = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 16; ++i) mr = fmaxf(mr, cur[i]);
       const float mx = pair_max(mr) * sl2;
-      const float m_new = mx > m_run + kRescaleSlack ? mx : m_run;
-      if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
-        const float alpha = fast_exp2(m_run - m_new);
+      m_prev = m_run;
+      m_run = mx > m_run + kRescaleSlack ? mx : m_run;
+    };
+    auto rescale = [&]() __attribute__((always_inline)) {
+      if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
+        const float alpha = fast_exp2(m_prev - m_run);
 #pragma unroll
         for (int i = 0; i < kDt; ++i) o[i] *= alpha;
         l0 *= alpha;
         l1 *= alpha;
-        m_run = m_new;
       }
-      bf16x8_t pfr[2];
+    };
+    // Weights, rounded to bf16 for the second product; the totals add the rounded weights.
+    auto weights = [&](const floatx16& cur, bf16x8_t (&pfr)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int c2 = 0; c2 < 2; ++c2) {
         bf16x2_t pw[4];
@@ -587,21 +617,85 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
                           __builtin_bit_cast(uint32_t, pw[2]), __builtin_bit_cast(uint32_t, pw[3])};
         pfr[c2] = as_bf16x8(pk);
       }
-      // ---- Values.
-      {
-        const uint32_t v = tile + v_lane;
-        pipelined<2 * kDt, kAhead>(
-            [&](int i) __attribute__((always_inline)) {
-              const uint32_t at_v = (v ^ ((i % kDt) << 6)) + 16 * (i / kDt) * P::kVal;
-              // (keys 8 on: another bit of the row's permutation)
-              const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned((at_v ^ 16) + 8 * P::kVal);
-              return v4u_t{x0.x, x0.y, x1.x, x1.y};
-            },
-            [&](int i, bf16x8_t x) __attribute__((always_inline)) {
-              o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pfr[i / kDt], o[i % kDt], 0, 0, 0);
-            });
+    };
+    const auto key_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
+      return i < kMainSteps ? lds_read((tile + k_lane) ^ (i << 5)) : lds_read((tile + r_lane) ^ ((i - kMainSteps) << 5));
+    };
+    const auto value_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
+      const uint32_t at_v = ((tile + v_lane) ^ ((i % kDt) << 6)) + 16 * (i / kDt) * P::kVal;
+      // (keys 8 on: another bit of the row's permutation)
+      const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned((at_v ^ 16) + 8 * P::kVal);
+      return v4u_t{x0.x, x0.y, x1.x, x1.y};
+    };
+    const auto score = [&](floatx16& cur, int i, v4u_t x) __attribute__((always_inline)) {
+      cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
+    };
+    const auto value = [&](const bf16x8_t (&pfr)[2], int i, v4u_t x) __attribute__((always_inline)) {
+      o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), pfr[i / kDt], o[i % kDt], 0, 0, 0);
+    };
+
+    if constexpr (kOverlap) {
+      // Step i: the scores of step i + 1 (from `in`'s successor's rows) while the vector units turn those of
+      // step i into weights, then its values. The compiler interleaves them.
+      auto turn = [&](int step, const floatx16& in, floatx16& next) __attribute__((always_inline)) {
+        publish(step + 1, kLater);
+        if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
+        const uint32_t tile = slot_of(step), tile1 = slot_of(step + 1);
+        v4u_t kv[kQSteps], v0[kDt], v1[kDt];
+#pragma unroll
+        for (int i = 0; i < kQSteps; ++i) kv[i] = key_operand(tile1, i);
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) v0[i] = value_operand(tile, i);
+        bf16x8_t pfr[2];
+#pragma unroll
+        for (int i = 0; i < kQSteps; ++i) score(next, i, kv[i]);
+        weights(in, pfr);
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) v1[i] = value_operand(tile, kDt + i);
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) value(pfr, i, v0[i]);
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) value(pfr, kDt + i, v1[i]);
+        mask_max(next, step + 1);
+        rescale();
+      };
+      floatx16 sa, sb;
+#pragma unroll
+      for (int i = 0; i < kQSteps; ++i) score(sa, i, key_operand(slot_of(first), i));
+      mask_max(sa, first);
+      int step = first;
+#pragma unroll 1
+      for (; step + 2 < last; step += 2) {
+        turn(step, sa, sb);
+        turn(step + 1, sb, sa);
       }
-      publish(step + 1);
+      if (step + 1 < last) {
+        turn(step, sa, sb);
+        sa = sb;
+        ++step;
+      }
+      bf16x8_t pfr[2];
+      weights(sa, pfr);
+      const uint32_t tile = slot_of(step);
+#pragma unroll
+      for (int i = 0; i < 2 * kDt; ++i) value(pfr, i, value_operand(tile, i));
+    } else {
+#pragma unroll 1
+      for (int step = first; step < last; ++step) {
+        // (every wave is past the step before: its slot is free)
+        if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
+        const uint32_t tile = slot_of(step);
+        floatx16 cur;
+        pipelined<kQSteps, kAhead>([&](int i) __attribute__((always_inline)) { return key_operand(tile, i); },
+                                   [&](int i, v4u_t x) __attribute__((always_inline)) { score(cur, i, x); });
+        mask_max(cur, step);
+        rescale();
+        bf16x8_t pfr[2];
+        weights(cur, pfr);
+        pipelined<2 * kDt, kAhead>([&](int i) __attribute__((always_inline)) { return value_operand(tile, i); },
+                                   [&](int i, v4u_t x) __attribute__((always_inline)) { value(pfr, i, x); });
+        publish(step + 1, kLater);
+      }
     }
 
     // ---- The end of the segment.
@@ -678,10 +772,12 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       const int tiles = cnt * NKW;
 #pragma unroll 1
       for (int ti = 0; ti < tiles; ++ti) {
-        const int pos0 = first * S::KS + kKeys * ti;
-        const TileBlocks tb = blocks_of(pos0);
+        const int pos0 = first * S::KS + kKeys * ti, e0 = pos0 / kBlockSize;
+        const auto there = [&](int e) { return e < table.nblk && table.tbl[e] >= 0 && table.tbl[e] < a.num_blocks; };
+        TileBlocks tb{there(e0), there(e0 + 1), 1, 1};
+        if constexpr (P::kPaged) directions(a, s, e0, dir_all, tb);
         if (pos0 + kKeys <= full_below && tb.ok0 && tb.ok1) continue;
-        const uint32_t win = row_window(a, q, ctx, j, valid, pos0);
+        const uint32_t win = row_window(a, q, ctx, j, valid, pos0, word0);
         // value row of tile row r, or null where no context is
         const auto value_row = [&](int r) -> const uint8_t* {
           const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
