@@ -7,6 +7,7 @@
 // memory, 128 by memory and matrix cores alike. Expanded: each head's 128 key and 128
 // value dims are made from c once (2 * 512 * 256 operations a key and head) and then cost
 // 2 (192 + 128) a (key, row, head): less from about 170 rows a context on.
+#include "plan.h"
 #include "rows_launch.h"
 
 namespace bros {
@@ -339,10 +340,13 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
 
 hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * a.num_q_heads;
-  if (columns <= 16) return ra::launch_latent_rows<1, 4>(a, 4, 6, workspace, stream);
-  if (columns <= 32) return ra::launch_latent_rows<2, 2>(a, 4, 6, workspace, stream);
-  if (columns <= 64) return ra::launch_latent_rows<4, 2>(a, 4, 6, workspace, stream);
-  return ra::launch_latent_rows<8, 1>(a, 6, 6, workspace, stream);
+  const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
+  switch (pick_rows_way(kLatentWays, columns, a.num_seqs, keys, stream_compute_units(stream))) {
+    case 0: return ra::launch_latent_rows<1, 4>(a, 4, 6, workspace, stream);
+    case 1: return ra::launch_latent_rows<2, 2>(a, 4, 6, workspace, stream);
+    case 2: return ra::launch_latent_rows<4, 1>(a, 4, 6, workspace, stream);
+    default: return ra::launch_latent_rows<8, 1>(a, 6, 6, workspace, stream);
+  }
 }
 
 hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {

@@ -194,22 +194,24 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
           const TileBlocks tb = blocks_of(step);
           uint8_t* tile = s_ring + (step % S::SLOTS) * S::kTile;
           uint32_t noted = 0;
-#pragma unroll 1
+          v4u_t w[S::kRows];
+#pragma unroll
+          for (int i = 0; i < S::kRows; ++i) w[i] = reinterpret_cast<const v4u_t*>(tile + (S::kRows * wave + i) * P::kMain)[lane];
+#pragma unroll
           for (int i = 0; i < S::kRows; ++i) {
             const int r = S::kRows * wave + i;
             const int pos = step * kKeys + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
-            const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;
-            v4u_t* v = reinterpret_cast<v4u_t*>(tile + r * P::kMain) + lane;
-            v4u_t w = there ? *v : v4u_t{0, 0, 0, 0};
+            const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;   // (uniform)
             uint32_t any = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t bad = not_finite(w[e]);
+              const uint32_t bad = not_finite(w[i][e]);
               any |= bad;
-              w[e] &= ~((bad >> 15) * 0xffffu);
+              w[i][e] = there ? w[i][e] & ~((bad >> 15) * 0xffffu) : 0;
             }
-            *v = w;
-            noted |= (__builtin_amdgcn_ballot_w64(any != 0) != 0 ? 1u : 0u) << i;
+            const bool odd = there && __builtin_amdgcn_ballot_w64(any != 0) != 0;
+            if (!there || odd) reinterpret_cast<v4u_t*>(tile + r * P::kMain)[lane] = w[i];
+            noted |= (odd ? 1u : 0u) << i;
           }
           if (lane == 0) s_bad[step % S::SLOTS][wave] = noted;
         }

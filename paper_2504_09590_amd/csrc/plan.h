@@ -291,4 +291,39 @@ inline bool plan_q8_decode(int64_t segments, int32_t group, int64_t blocks, int3
   return false;
 }
 
+// A way to run the attention of few rows (rows_device.h, latent_device.h): the columns of a unit, what 32 of its keys
+// take on a compute unit (microseconds, all of them busy), and what it costs that units are cut: their
+// partial sums, written and read again, grow with the columns.
+struct RowsWay {
+  int32_t columns;
+  double keys32_us, cut_us;
+};
+// Rows over a K/V pool: two workgroups a compute unit, of two waves, of four as two pairs, or of four.
+constexpr RowsWay kTreeWays[] = {{32, 0.52, 3.0}, {64, 0.53, 6.0}, {128, 0.73, 12.0}};
+// Over a latent pool: one workgroup a compute unit, of four waves, or of eight with 128 columns.
+constexpr RowsWay kLatentWays[] = {{16, 1.7, 0.0}, {32, 1.7, 2.0}, {64, 2.4, 9.0}, {128, 3.4, 30.0}};
+
+// The index of the way that is expected to end first: wide units read each key for more columns, narrow ones
+// leave work for more compute units and smaller partials where there is little of it. Contexts count as 0.6 of the longest.
+//
+// Us by columns of a unit (256 compute units), the one taken first. K/V pool, 32 / 8 heads: 16 trees of 32 rows on up
+// to 8192 tokens 67 (128), 87, 151; of 16 rows 55 (64), 76 (32); two of 30 rows on 3000 32 (64), 27 (32), 35 (128). Latent
+// pool, one row: 128 heads, 96 contexts up to 16384 304 (128), 417, 682; five of 10000 53 (64), 55, 70 (128); one of 30000
+// 71 (32), 77 (16), 86, 95; 64 heads, 64 of 8192 99 (64), 139, 232.
+template <int N>
+inline int pick_rows_way(const RowsWay (&ways)[N], int64_t columns, int64_t segments, int64_t keys, int32_t compute_units) {
+  int best = 0;
+  double best_us = 0.0;
+  for (int i = 0; i < N; ++i) {
+    if (i > 0 && ways[i - 1].columns >= columns) break;   // (no wider than the columns ask for)
+    const double units = (double)((columns + ways[i].columns - 1) / ways[i].columns) * (double)segments;
+    const double us = units * (0.6 / 32.0) * (double)keys * ways[i].keys32_us / compute_units + ways[i].cut_us;
+    if (i == 0 || us < best_us) {
+      best = i;
+      best_us = us;
+    }
+  }
+  return best;
+}
+
 }  // namespace bros

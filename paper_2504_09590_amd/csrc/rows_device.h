@@ -388,10 +388,9 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   using S = Shape<P, NCW, NKW, SLOTS>;
   constexpr int kDt = S::kDt, kMainSteps = P::kMain / 32, kQSteps = S::kQDims / 16, kR = S::kRows;
   constexpr int kAhead = 6;   // operands read before the first product
-  // With one key group, the scores of a step are formed beside the softmax of the one before it, whose values
-  // follow: the matrix cores and the vector units then work at the same time.
-  constexpr bool kOverlap = NKW == 1;
-  static_assert(!kOverlap || SLOTS >= 3, "two steps' rows are in use");
+  // With three steps' rows in LDS or more, the scores of a step are formed beside the softmax of the one before it,
+  // whose values follow: the matrix cores and the vector units then work at the same time.
+  constexpr bool kOverlap = SLOTS >= 3;
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[S::kRing];
   __shared__ int32_t s_tab[S::kWaves][kTable];
   __shared__ int64_t s_scan[2 * S::kWaves];
@@ -531,23 +530,26 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         if (later >= 2) wait_vmem<2 * S::kLoads>();
         else if (later == 1) wait_vmem<S::kLoads>();
         else wait_vmem<0>();
-        if (masked(step)) {
+        if (masked(step) && (NCW > 1 || pos_of(step) < ctx)) {
           const int pos0 = pos_of(step);
           const TileBlocks tb = blocks_of(pos0);
           uint8_t* vt = ring + (step % SLOTS) * S::kTile + S::kValAt;
-          for (int i = lane; i < kR * (P::kVal / 16); i += kWave) {
-            const int r = kR * cw + i / (P::kVal / 16);
+          constexpr int kMine = kR * (P::kVal / 16) / kWave;   // 16-byte chunks of a lane
+          v4u_t w[kMine];
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) w[i] = reinterpret_cast<const v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + lane];
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) {
+            const int r = kR * cw + (i * kWave + lane) / (P::kVal / 16);
             const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
             const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;
-            v4u_t* at_v = reinterpret_cast<v4u_t*>(vt + r * P::kVal) + i % (P::kVal / 16);
-            v4u_t w = there ? *at_v : v4u_t{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t bad = not_finite(w[e]);
+              const uint32_t bad = there ? not_finite(w[i][e]) : 0;
               odd |= bad;
-              w[e] &= ~((bad >> 15) * 0xffffu);
+              w[i][e] = there ? w[i][e] & ~((bad >> 15) * 0xffffu) : 0;
             }
-            *at_v = w;
+            reinterpret_cast<v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + lane] = w[i];
           }
         }
       }
@@ -685,6 +687,11 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         // (every wave is past the step before: its slot is free)
         if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
         const uint32_t tile = slot_of(step);
+        // (a wave alone on its tile passes over one without context)
+        if (NCW == 1 && pos_of(step) >= ctx) {
+          publish(step + 1, kLater);
+          continue;
+        }
         floatx16 cur;
         pipelined<kQSteps, kAhead>([&](int i) __attribute__((always_inline)) { return key_operand(tile, i); },
                                    [&](int i, v4u_t x) __attribute__((always_inline)) { score(cur, i, x); });

@@ -4,6 +4,7 @@
 // head) a key of 512 bytes takes 512 M operations: few columns are bound by memory, from about
 // 150 on by the matrix cores. The columns a unit holds follow the longest tree: 32 with four
 // waves along the keys, 64 with two, 128 with none.
+#include "plan.h"
 #include "rows_launch.h"
 
 namespace bros {
@@ -75,9 +76,12 @@ size_t rows_workspace_bytes(bool latent) {
 
 hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * (a.num_q_heads / a.num_kv_heads);
-  if (columns <= 32) return ra::launch_rows<ra::KvPool, 1, 4, 2, 1>(a, 2, 4, workspace, stream);
-  if (columns <= 64) return ra::launch_rows<ra::KvPool, 2, 2, 4, 1>(a, 2, 6, workspace, stream);
-  return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 8, workspace, stream);
+  const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
+  switch (pick_rows_way(kTreeWays, columns, (int64_t)a.num_seqs * a.num_kv_heads, keys, stream_compute_units(stream))) {
+    case 0: return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
+    case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, workspace, stream);
+    default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);
+  }
 }
 
 hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream) {
