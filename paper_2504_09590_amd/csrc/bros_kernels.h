@@ -154,6 +154,7 @@ struct RowsArgs {
   const void* k_pool;         // latent: the only pool; expanded: keys [heads][dense_rows][128]
   const void* v_pool;
   const void* rot_rows;       // expanded: [dense_rows][64]
+  const int32_t* exps;        // expanded: [heads][dense_rows / 32] exponents of the values
   int64_t dense_rows;
   const int32_t* block_tables;
   const int8_t* dir;
@@ -231,10 +232,11 @@ struct LatentAppendArgs {
 struct ExpandArgs {
   const void* pool;
   const void* w;              // [heads][256][512] of this group
-  void* latents;              // [dense_rows][512]
   void* rot_rows;             // [dense_rows][64]
-  void* k_rows;               // [heads][dense_rows][128]
-  void* v_rows;
+  void* k_rows;               // [heads][dense_rows][128] bf16
+  void* v_rows;               // fp16, each 2^-e of the value
+  int32_t* exps;              // [heads][dense_rows / 32]: e
+  int32_t with_rot;           // write rot_rows too
   int64_t dense_rows;
   const int32_t* block_tables;
   const int8_t* dir;
@@ -298,7 +300,6 @@ hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream);
 hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream);
 hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream);
 hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream);
-hipError_t launch_latent_gather(const ExpandArgs& a, hipStream_t stream);
 hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream);
 hipError_t launch_kv_move(const KvMoveArgs& a, bool gather, hipStream_t stream);
 // bf16 rows over an 8-bit pool (a.k_pool and a.v_pool unused), with the bf16 decode's workspace.

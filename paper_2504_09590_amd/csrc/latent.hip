@@ -179,12 +179,42 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
 // expansion
 // ---------------------------------------------------------------------------
 
-// Latent rows of every sequence side by side, each sequence's to whole tiles of 32, zeros where there
-// is no context. A workgroup takes one tile.
-__global__ __launch_bounds__(kThreads) void latent_gather_kernel(ExpandArgs a) {
+// Dense rows: those of every sequence side by side, each sequence's to whole tiles of 32. Rows [128 y, + 128) of the
+// keys (even x) or values (odd x) of head x / 2: latents times weights, 128 x 128 values to a
+// workgroup, four waves of 64 x 64, 64 latent dims a step. Latent rows come straight from their
+// slots. Both operands' rows go to LDS as they lie, 128 bytes a row and step, chunks permuted so that an
+// operand read meets no bank conflict. (Keys that are no context are made of whatever a slot holds:
+// the attention masks them.)
+//
+// Keys are rounded to bf16, as the queries that they meet. Values are rounded to fp16, like the softmax weights that
+// they meet: three bits more (with both in bf16 the result is 1.65 times as far from 64 bits as one that is
+// rounded once, so 1.2). fp16's range is made up for by an exponent for each tile of 32 rows and head,
+// 2^e off: 0 where the tile's largest magnitude lies within 2^-6 .. 2^15, as nearly always.
+constexpr int kStepDims = 64, kTileRows = 128;
+constexpr int kHalfTile = kTileRows * kStepDims * 2;
+
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 half2_t;
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {   // round to nearest even
+  const pf::float2_t f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, half2_t));
+}
+// 16 bytes from each lane's own address to LDS at dst + 16 * lane.
+__device__ __forceinline__ void load_rows_to_lds(const uint8_t* lane_src, const uint8_t* dst) {
+  const uint32_t m0 = (uint32_t)(uintptr_t)dst;
+  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(lane_src), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
+}
+
+__global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2][2 * kHalfTile];
   __shared__ int64_t s_scan[kThreads / kWave];
-  __shared__ int s_seq, s_first;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
+  __shared__ int s_seq[4], s_pos[4];         // of each tile of 32 rows: its sequence (-1: none) and first position
+  __shared__ float s_max[2][4];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
+  const int half = lane >> 5, col = lane & 31;
+  const int64_t row0 = (int64_t)blockIdx.y * kTileRows;
+  const int head = blockIdx.x >> 1, which = blockIdx.x & 1;
+
+  // ---- The tiles' sequences.
   RowsArgs ra_{};
   ra_.cu_q = a.cu_q;
   ra_.ctx_lens = a.ctx_lens;
@@ -196,69 +226,61 @@ __global__ __launch_bounds__(kThreads) void latent_gather_kernel(ExpandArgs a) {
   int64_t mine = 0;
   for (int s = s0; s < s1; ++s) mine += ra::dense_rows(ra::seq_of(ra_, s).ctx);
   const int64_t inc = ra::wave_scan64(mine, lane);
-  if (lane == kWave - 1) s_scan[w] = inc;
-  if (tid == 0) s_seq = -1;
+  if (lane == kWave - 1) s_scan[wave] = inc;
+  if (tid < 4) s_seq[tid] = -1;
   __syncthreads();
   int64_t first = inc - mine;
-  for (int i = 0; i < w; ++i) first += s_scan[i];
-  const int64_t row0 = (int64_t)blockIdx.x * ra::kKeys;
-  if (row0 >= first && row0 < first + mine) {
+  for (int i = 0; i < wave; ++i) first += s_scan[i];
+  if (first < row0 + kTileRows && first + mine > row0) {
     for (int s = s0; s < s1; ++s) {
       const int rows = ra::dense_rows(ra::seq_of(ra_, s).ctx);
-      if (row0 < first + rows) {
-        s_seq = s;
-        s_first = (int)(row0 - first);   // position of the tile's first row
-        break;
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + 32 * i;
+        if (r >= first && r < first + rows) {
+          s_seq[i] = s;
+          s_pos[i] = (int)(r - first);
+        }
       }
       first += rows;
     }
   }
   __syncthreads();
-  const int s = s_seq;
-  if (s < 0) return;   // behind the last sequence
-  const int ctx = ra::seq_of(ra_, s).ctx;
-  constexpr int kChunks = kRow / 8;
-  for (int i = tid; i < ra::kKeys * kChunks; i += kThreads) {
-    const int r = i / kChunks, ch = i % kChunks, pos = s_first + r;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (pos < ctx) {
-      const int b = a.block_tables[(size_t)s * a.max_blocks_per_seq + (pos >> 4)];
-      if (b >= 0 && b < a.num_blocks) {
-        const int slot = slot_of_offset(pos & 15, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, pos >> 4));
-        v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.pool) + ((size_t)b * kBlockSize + slot) * kRow)[ch];
-      }
-    }
-    const size_t row = (size_t)row0 + r;
-    if (ch < kLatent / 8) reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.latents) + row * kLatent)[ch] = v;
-    else reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.rot_rows) + row * kRot)[ch - kLatent / 8] = v;
-  }
-}
+  if (s_seq[0] < 0) return;   // behind the last sequence (uniform)
+  // Row r of the workgroup's 128, in the pool (one that is not there: the first row of the pool).
+  const auto pool_row = [&](int r) -> const uint8_t* {
+    const uint8_t* pool = static_cast<const uint8_t*>(a.pool);
+    const int s = s_seq[r >> 5], pos = s_pos[r >> 5] + (r & 31);
+    if (s < 0 || (pos >> 4) >= a.max_blocks_per_seq) return pool;
+    const int b = a.block_tables[(size_t)s * a.max_blocks_per_seq + (pos >> 4)];
+    if (b < 0 || b >= a.num_blocks) return pool;
+    const int slot = slot_of_offset(pos & 15, entry_direction(a.dir, a.cls, a.dir_per_entry, a.max_blocks_per_seq, s, pos >> 4));
+    return pool + ((size_t)b * kBlockSize + slot) * (kRow * 2);
+  };
 
-// Rows [128 y, + 128) of the keys (even x) or values (odd x) of head x / 2: latents times
-// weights, 128 x 128 values to a workgroup, four waves of 64 x 64, 64 latent dims a step.
-// Both operands' rows go to LDS as they lie, 128 bytes a row and step, chunks permuted so that
-// an operand read meets no bank conflict.
-constexpr int kStepDims = 64, kTileRows = 128;
-constexpr int kHalfTile = kTileRows * kStepDims * 2;
-__global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a, int64_t rows) {
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2][2 * kHalfTile];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
-  const int half = lane >> 5, col = lane & 31;
-  const size_t row0 = (size_t)blockIdx.y * kTileRows;
-  const int head = blockIdx.x >> 1, which = blockIdx.x & 1;
+  const auto is_context = [&](int r) -> bool {
+    const int s = s_seq[r >> 5], pos = s_pos[r >> 5] + (r & 31);
+    if (s < 0 || pos >= ra::seq_of(ra_, s).ctx) return false;   // (ctx: within the table's width)
+    const int b = a.block_tables[(size_t)s * a.max_blocks_per_seq + (pos >> 4)];
+    return b >= 0 && b < a.num_blocks;
+  };
+
   const uint8_t* wsrc = static_cast<const uint8_t*>(a.w) + ((size_t)head * 256 + 128 * which) * kLatent * 2;
-  const uint8_t* csrc = static_cast<const uint8_t*>(a.latents);
-
   // a wave loads rows 32 wave .. + 31 of both tiles, eight rows of 128 bytes to a load
+  const uint8_t* csrc[4];
+  uint32_t woff[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 32 * wave + 8 * i + (lane >> 3);
+    const uint32_t chunk = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) << 4);
+    csrc[i] = pool_row(r) + chunk;
+    woff[i] = (uint32_t)r * (kLatent * 2) + chunk;
+  }
   auto issue = [&](int step, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r8 = 32 * wave + 8 * i, r = r8 + (lane >> 3);
-      const uint32_t chunk = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) << 4);
-      pf::load_to_lds(wsrc + step * 128, (uint32_t)r * (kLatent * 2) + chunk, s_tile[buf] + r8 * 128);
-      // (rows behind the buffer's end: its last row again)
-      const size_t cr = min(row0 + r, (size_t)a.dense_rows - 1);
-      pf::load_to_lds(csrc + row0 * (kLatent * 2) + step * 128, (uint32_t)(cr - row0) * (kLatent * 2) + chunk, s_tile[buf] + kHalfTile + r8 * 128);
+      const int r8 = 32 * wave + 8 * i;
+      pf::load_to_lds(wsrc + step * 128, woff[i], s_tile[buf] + r8 * 128);
+      load_rows_to_lds(csrc[i] + step * 128, s_tile[buf] + kHalfTile + r8 * 128);
     }
   };
   const int wd = wave & 1, wr = wave >> 1;   // the wave's 64 dims and 64 rows
@@ -270,6 +292,7 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
   }
   const int r_lane = (col >> 1) * 256 + ((col & 1) << 7), r_sw = (col >> 1) & 7;
   constexpr int kSteps = kLatent / kStepDims;
+  // (the addresses come from loads that the compiler sees: they are there before the first request)
   issue(0, 0);
 #pragma unroll 1
   for (int step = 0; step < kSteps; ++step) {
@@ -295,22 +318,63 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
       }
     }
   }
-  // (the expanded keys and values are rounded to bf16 once: the second operand type of the
-  // matrix cores' products, as the rows of a K/V pool are)
+  // The values' exponents: of the largest finite magnitude of 32 rows and 128 dims. Rows that are no context
+  // do not count, and are zeros.
+  float mul[2] = {1.0f, 1.0f};
+  if (which == 1) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const bool there = is_context(64 * wr + 32 * k + col);
+      float m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          o[i][k][e] = there ? o[i][k][e] : 0.0f;
+          const float x = fabsf(o[i][k][e]);
+          m = fmaxf(m, x < INFINITY ? x : 0.0f);
+        }
+      }
+#pragma unroll
+      for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+      if (lane == 0) s_max[wd][2 * wr + k] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float m = fmaxf(s_max[0][2 * wr + k], s_max[1][2 * wr + k]);
+      int e = 0;
+      if (m > 0.0f && (m < 0x1p-6f || m >= 0x1p15f)) e = max(-120, min(120, ilogbf(m) - 13));
+      mul[k] = ldexpf(1.0f, -e);
+      const int64_t tile = row0 / 32 + 2 * wr + k;
+      if (wd == 0 && lane == 0 && 32 * tile < a.dense_rows) a.exps[(size_t)head * (a.dense_rows / 32) + tile] = e;
+    }
+  }
   uint16_t* dst = static_cast<uint16_t*>(which == 0 ? a.k_rows : a.v_rows) + (size_t)head * a.dense_rows * 128;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const size_t r = row0 + 64 * wr + 32 * k + col;
-    if (r >= (size_t)rows) continue;
+    const int64_t r = row0 + 64 * wr + 32 * k + col;
+    if (r >= a.dense_rows) continue;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int jq = 0; jq < 4; ++jq) {
+        const float x[4] = {o[i][k][4 * jq], o[i][k][4 * jq + 1], o[i][k][4 * jq + 2], o[i][k][4 * jq + 3]};
         uint2 v;
-        v.x = pf::pack2_bf16(o[i][k][4 * jq], o[i][k][4 * jq + 1]);
-        v.y = pf::pack2_bf16(o[i][k][4 * jq + 2], o[i][k][4 * jq + 3]);
+        if (which == 0) v = make_uint2(pf::pack2_bf16(x[0], x[1]), pf::pack2_bf16(x[2], x[3]));
+        else v = make_uint2(pack2_f16(x[0] * mul[k], x[1] * mul[k]), pack2_f16(x[2] * mul[k], x[3] * mul[k]));
         *reinterpret_cast<uint2*>(dst + r * 128 + 64 * wd + 32 * i + 8 * jq + 4 * half) = v;
       }
+    }
+  }
+  // The rotated keys' dense rows, once a call.
+  if (blockIdx.x == 0 && a.with_rot) {
+    const int r = tid >> 1;
+    if (row0 + r < a.dense_rows) {
+      const uint4* src = reinterpret_cast<const uint4*>(pool_row(r) + kLatent * 2) + 4 * (tid & 1);
+      uint4* to = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.rot_rows) + (row0 + r) * (kRot * 2)) + 4 * (tid & 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = src[i];
     }
   }
 }
@@ -327,14 +391,9 @@ hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_latent_gather(const ExpandArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(latent_gather_kernel, dim3((unsigned)(a.dense_rows / ra::kKeys)), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
-}
-
 hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
   const unsigned tiles = (unsigned)((a.dense_rows + kTileRows - 1) / kTileRows);
-  hipLaunchKernelGGL(latent_expand_kernel, dim3(2 * a.heads, tiles), dim3(kThreads), 0, stream, a, a.dense_rows);
+  hipLaunchKernelGGL(latent_expand_kernel, dim3(2 * a.heads, tiles), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -85,15 +85,15 @@ __device__ __forceinline__ int32_t lds_word(const int32_t* p) {
 // kVal: bytes of a value row, or 0 where the first part is the value.
 struct KvPool {          // 128 dims each, [blocks][Hkv][16][128]
   static constexpr int kMain = 256, kRot = 0, kVal = 256;
-  static constexpr bool kPaged = true, kCausalUnits = false;
+  static constexpr bool kPaged = true, kCausalUnits = false, kHalf = false;
 };
 struct LatentPool {      // 512 shared dims and 64 rotated ones, [blocks][16][576]
   static constexpr int kMain = 1024, kRot = 128, kVal = 0;
   static constexpr bool kPaged = true, kCausalUnits = false;
 };
-struct Expanded {        // dense rows: keys of 128 dims and 64 rotated ones shared by the heads, values of 128
+struct Expanded {        // dense rows: keys of 128 dims and 64 rotated ones shared by the heads, values of 128 in fp16
   static constexpr int kMain = 256, kRot = 128, kVal = 256;
-  static constexpr bool kPaged = false, kCausalUnits = true;
+  static constexpr bool kPaged = false, kCausalUnits = true, kHalf = true;
 };
 
 // A sequence as the kernels see it. n = 0: nothing to do. ctx: its visible context
@@ -149,8 +149,22 @@ struct TileBlocks {
   bool ok0, ok1;
   int dir0, dir1;
 };
-// Bits 15 and 31: the halves that are infinite or NaN, as bf16.
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// Bits 15 and 31: the halves that are infinite or NaN, as bf16 or (HALF) fp16.
+template <bool HALF = false>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return HALF ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 half2_t;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 half8_t;
+// The two values of a word, as bf16 or fp16.
+template <bool HALF>
+__device__ __forceinline__ float2_t two_values(uint32_t w) {
+  if constexpr (HALF) {
+    const half2_t h = __builtin_bit_cast(half2_t, w);
+    return float2_t{(float)h[0], (float)h[1]};
+  }
+  return float2_t{bf16_lo(w), bf16_hi(w)};
+}
 
 // The first word of row j's mask (of one that is not there: of the last).
 __device__ __forceinline__ uint64_t first_word(const RowsArgs& a, const Seq& q, int j) {
@@ -379,6 +393,7 @@ struct Shape {
   static constexpr int kChunks = kDims / 8;                         // of a wave's partial, 1 KiB each
   // first of the four dims that a lane has in chunk i
   static __device__ __forceinline__ int dim_of(int i, int lane) { return 8 * i + 4 * (lane >> 5); }
+  static_assert(P::kMain == 256 && (P::kRot == 0 || P::kRot == 128), "");
   static_assert(kRows % 4 == 0, "a load takes four rows of 256 bytes");
   static_assert((NKW - 1) * NCW * 32 * kDims * 4 <= kRing, "the key groups' sums meet in the ring");
 };
@@ -425,6 +440,10 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   const uint32_t r_lane = S::kRotAt + (col >> 1) * 256 + ((col & 1) << 7) + ((half ^ ((col >> 1) & 7)) << 4);
   const int v_key = 4 * half + ((lane >> 2) & 3);
   const uint32_t v_lane = S::kValAt + v_key * P::kVal + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz(v_key)) << 4) + (lane & 1) * 8;
+  // Requests: a lane's byte of four rows of 256, and of eight of 128. The first row's other bits of the
+  // permutation are the same for every lane: a xor.
+  const uint32_t main_off = (uint32_t)((lane >> 4) * 256 + (((lane & 15) ^ ((lane >> 4) << 2)) << 4));
+  const uint32_t rot_off = (uint32_t)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 4)) << 4));
   uint8_t* const ring = s_ring + kg * SLOTS * S::kTile;
   const uint32_t ring0 = lds_address(ring);
 
@@ -479,7 +498,6 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       ask(step + 1);
       holes = (holes & ~(1u << (step & 31))) | ((b0 < 0 || b1 < 0 ? 1u : 0u) << (step & 31));
       uint8_t* dst = ring + (step % SLOTS) * S::kTile;
-      const int ln = lane_here();
       // (dense rows: of the tile, whose place is known)
       const size_t row0 = P::kPaged || !fits ? 0 : (size_t)(at.row0 + (int64_t)step * S::KS + kKeys * kg);
 #pragma unroll
@@ -488,16 +506,16 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         size_t src;
         if constexpr (P::kPaged) src = ((size_t)max((row >> 4) ? b1 : b0, 0) * Hkv + g) * (kBlockSize * P::kMain) + (row & 15) * P::kMain;
         else src = ((size_t)g * a.dense_rows + row0 + row) * P::kMain;
-        const uint32_t off = (uint32_t)((ln >> 4) * P::kMain + (((ln & 15) ^ swz(row + (ln >> 4))) << 4));
+        const uint32_t off = main_off ^ ((((row >> 2) & 1) << 1 | ((row >> 3) & 1)) << 4);
         load_to_lds(static_cast<const uint8_t*>(a.k_pool) + src, off, dst + row * P::kMain);
         load_to_lds(static_cast<const uint8_t*>(a.v_pool) + src, off, dst + S::kValAt + row * P::kVal);
       }
       if constexpr (P::kRot != 0) {
 #pragma unroll
         for (int i = 0; i < kR / 8; ++i) {
-          const int row = kR * cw + 8 * i, r = row + (ln >> 3);
-          load_to_lds(static_cast<const uint8_t*>(a.rot_rows) + (row0 + row) * P::kRot,
-                      (uint32_t)((ln >> 3) * P::kRot + (((ln & 7) ^ ((r >> 1) & 7)) << 4)), dst + S::kRotAt + row * P::kRot);
+          const int row = kR * cw + 8 * i;
+          load_to_lds(static_cast<const uint8_t*>(a.rot_rows) + (row0 + row) * P::kRot, rot_off ^ (((row >> 3) & 1) << 6),
+                      dst + S::kRotAt + row * P::kRot);
         }
       }
     };
@@ -518,12 +536,16 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < kDt; ++i) o[i] = floatx16{};
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
+    // Values that are 2^-e of what they stand for (nearly never any but e = 0): the sums are 2^-e_run of theirs, with the
+    // largest exponent so far, and a tile's weights are multiplied by 2^(e - e_run).
+    int e_run = 0, e_off = 0;
+    float e_scale = 1.0f;   // what the sums take for a larger exponent
+    const int32_t* exps = P::kHalf ? a.exps + (size_t)g * (a.dense_rows / kKeys) + at.row0 / kKeys : nullptr;
     uint32_t odd = 0;   // a value that is not finite was left out of a product
 
     // Waits for the wave's rows of a step (those of the next `most` may be in flight) and, where the step is
     // masked, puts its values in order: zeros where no context is, and for values that are not finite. Then
     // the waves that share a tile meet.
-    constexpr int kLater = kOverlap ? SLOTS - 3 : SLOTS - 2;
     auto publish = [&](int step, int most) __attribute__((always_inline)) {
       if (step < last) {
         const int later = min(most, last - 1 - step);
@@ -545,7 +567,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
             const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t bad = there ? not_finite(w[i][e]) : 0;
+              const uint32_t bad = there ? not_finite<P::kHalf>(w[i][e]) : 0;
               odd |= bad;
               w[i][e] = there ? w[i][e] & ~((bad >> 15) * 0xffffu) : 0;
             }
@@ -564,6 +586,12 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     ask(first);
     request(first);
+    bool scaled = false;   // any exponent of the segment's is not 0
+    if constexpr (P::kHalf) {
+      int any = 0;
+      for (int i = lane; i < cnt * NKW && fits; i += kWave) any |= exps[first * NKW + i];
+      scaled = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+    }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -572,140 +600,199 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     publish(first, SLOTS - 2);
 
     const auto slot_of = [&](int step) -> uint32_t { return ring0 + (step % SLOTS) * S::kTile; };
-    // Masks a tile's scores and moves the running maximum (lazily); gives the factor that the sums take for it.
+    // The steps; kScaled: with exponents of values. (Two loops, so that the usual one has no branches for them.)
     float m_prev = kNoMax;
-    auto mask_max = [&](floatx16& cur, int step) __attribute__((always_inline)) {
-      if (masked(step)) {
-        const int pos0 = pos_of(step);
-        const TileBlocks tb = blocks_of(pos0);
-        const uint32_t win = row_window(a, q, ctx, j, valid, pos0, word0);
+    auto steps = [&](auto scaledc) __attribute__((always_inline)) {
+      constexpr bool kScaled = decltype(scaledc)::value;
+      // Masks a tile's scores and moves the running maximum (lazily); gives the factor that the sums take for it.
+      auto mask_max = [&](floatx16& cur, int step) __attribute__((always_inline)) {
+        if (masked(step)) {
+          const int pos0 = pos_of(step);
+          const TileBlocks tb = blocks_of(pos0);
+          const uint32_t win = row_window(a, q, ctx, j, valid, pos0, word0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 8 * (i >> 2) + 4 * half + (i & 3);
-          const int off = (k & 16) + slot_of_offset(k & 15, (i >> 3) ? tb.dir1 : tb.dir0);
-          cur[i] = ((i >> 3) ? tb.ok1 : tb.ok0) && ((win >> off) & 1u) ? cur[i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) {
+            const int k = 8 * (i >> 2) + 4 * half + (i & 3);
+            const int off = (k & 16) + slot_of_offset(k & 15, (i >> 3) ? tb.dir1 : tb.dir0);
+            cur[i] = ((i >> 3) ? tb.ok1 : tb.ok0) && ((win >> off) & 1u) ? cur[i] : -INFINITY;
+          }
         }
-      }
-      float mr = -INFINITY;
+        float mr = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mr = fmaxf(mr, cur[i]);
-      const float mx = pair_max(mr) * sl2;
-      m_prev = m_run;
-      m_run = mx > m_run + kRescaleSlack ? mx : m_run;
-    };
-    auto rescale = [&]() __attribute__((always_inline)) {
-      if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
-        const float alpha = fast_exp2(m_prev - m_run);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) o[i] *= alpha;
-        l0 *= alpha;
-        l1 *= alpha;
-      }
-    };
-    // Weights, rounded to bf16 for the second product; the totals add the rounded weights.
-    auto weights = [&](const floatx16& cur, bf16x8_t (&pfr)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-        bf16x2_t pw[4];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float2_t pp = {fast_exp2(fmaf(cur[8 * c2 + 2 * w], sl2, -m_run)),
-                               fast_exp2(fmaf(cur[8 * c2 + 2 * w + 1], sl2, -m_run))};
-          pw[w] = __builtin_convertvector(pp, bf16x2_t);
-          if (w & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(pw[w], one2, l1, false);
-          else l0 = __builtin_amdgcn_fdot2_f32_bf16(pw[w], one2, l0, false);
+        for (int i = 0; i < 16; ++i) mr = fmaxf(mr, cur[i]);
+        const float mx = pair_max(mr) * sl2;
+        m_prev = m_run;
+        m_run = mx > m_run + kRescaleSlack ? mx : m_run;
+        if constexpr (kScaled) {
+          const int e = __builtin_amdgcn_readfirstlane(exps[pos_of(step) / kKeys]);
+          const int most = step == first ? e : max(e_run, e);
+          e_scale = step == first ? 1.0f : ldexpf(1.0f, max(e_run - most, -126));
+          e_run = most;
+          e_off = e - most;
         }
-        const v4u_t pk = {__builtin_bit_cast(uint32_t, pw[0]), __builtin_bit_cast(uint32_t, pw[1]),
-                          __builtin_bit_cast(uint32_t, pw[2]), __builtin_bit_cast(uint32_t, pw[3])};
-        pfr[c2] = as_bf16x8(pk);
-      }
-    };
-    const auto key_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
-      return i < kMainSteps ? lds_read((tile + k_lane) ^ (i << 5)) : lds_read((tile + r_lane) ^ ((i - kMainSteps) << 5));
-    };
-    const auto value_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
-      const uint32_t at_v = ((tile + v_lane) ^ ((i % kDt) << 6)) + 16 * (i / kDt) * P::kVal;
-      // (keys 8 on: another bit of the row's permutation)
-      const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned((at_v ^ 16) + 8 * P::kVal);
-      return v4u_t{x0.x, x0.y, x1.x, x1.y};
-    };
-    const auto score = [&](floatx16& cur, int i, v4u_t x) __attribute__((always_inline)) {
-      cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
-    };
-    const auto value = [&](const bf16x8_t (&pfr)[2], int i, v4u_t x) __attribute__((always_inline)) {
-      o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), pfr[i / kDt], o[i % kDt], 0, 0, 0);
-    };
-
-    if constexpr (kOverlap) {
-      // Step i: the scores of step i + 1 (from `in`'s successor's rows) while the vector units turn those of
-      // step i into weights, then its values. The compiler interleaves them.
-      auto turn = [&](int step, const floatx16& in, floatx16& next) __attribute__((always_inline)) {
-        publish(step + 1, kLater);
-        if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
-        const uint32_t tile = slot_of(step), tile1 = slot_of(step + 1);
-        v4u_t kv[kQSteps], v0[kDt], v1[kDt];
-#pragma unroll
-        for (int i = 0; i < kQSteps; ++i) kv[i] = key_operand(tile1, i);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) v0[i] = value_operand(tile, i);
-        bf16x8_t pfr[2];
-#pragma unroll
-        for (int i = 0; i < kQSteps; ++i) score(next, i, kv[i]);
-        weights(in, pfr);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) v1[i] = value_operand(tile, kDt + i);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) value(pfr, i, v0[i]);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) value(pfr, kDt + i, v1[i]);
-        mask_max(next, step + 1);
-        rescale();
       };
-      floatx16 sa, sb;
+      auto rescale = [&]() __attribute__((always_inline)) {
+        if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
+          const float alpha = fast_exp2(m_prev - m_run);
 #pragma unroll
-      for (int i = 0; i < kQSteps; ++i) score(sa, i, key_operand(slot_of(first), i));
-      mask_max(sa, first);
-      int step = first;
-#pragma unroll 1
-      for (; step + 2 < last; step += 2) {
-        turn(step, sa, sb);
-        turn(step + 1, sb, sa);
-      }
-      if (step + 1 < last) {
-        turn(step, sa, sb);
-        sa = sb;
-        ++step;
-      }
-      bf16x8_t pfr[2];
-      weights(sa, pfr);
-      const uint32_t tile = slot_of(step);
-#pragma unroll
-      for (int i = 0; i < 2 * kDt; ++i) value(pfr, i, value_operand(tile, i));
-    } else {
-#pragma unroll 1
-      for (int step = first; step < last; ++step) {
-        // (every wave is past the step before: its slot is free)
-        if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
-        const uint32_t tile = slot_of(step);
-        // (a wave alone on its tile passes over one without context)
-        if (NCW == 1 && pos_of(step) >= ctx) {
-          publish(step + 1, kLater);
-          continue;
+          for (int i = 0; i < kDt; ++i) o[i] *= alpha;
+          l0 *= alpha;
+          l1 *= alpha;
         }
-        floatx16 cur;
-        pipelined<kQSteps, kAhead>([&](int i) __attribute__((always_inline)) { return key_operand(tile, i); },
-                                   [&](int i, v4u_t x) __attribute__((always_inline)) { score(cur, i, x); });
-        mask_max(cur, step);
-        rescale();
+        if constexpr (kScaled) {
+          if (e_scale != 1.0f) {
+#pragma unroll
+            for (int i = 0; i < kDt; ++i) o[i] *= e_scale;
+          }
+        }
+      };
+      // Weights, rounded to 16 bits (bf16, or fp16 where the values are) for the second product; the totals add the
+      // rounded weights.
+      auto weights = [&](const floatx16& cur, bf16x8_t (&pfr)[2]) __attribute__((always_inline)) {
+        if constexpr (P::kHalf) {
+          float base = -m_run;
+          half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
+          if constexpr (kScaled) {   // (the totals count a weight whatever its values' exponent)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) l0 += fast_exp2(fmaf(cur[i], sl2, base));
+            base += (float)e_off;
+            ones = half2_t{(_Float16)0.0f, (_Float16)0.0f};
+          }
+#pragma unroll
+          for (int c2 = 0; c2 < 2; ++c2) {
+            half2_t pw[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float2_t pp = {fast_exp2(fmaf(cur[8 * c2 + 2 * w], sl2, base)), fast_exp2(fmaf(cur[8 * c2 + 2 * w + 1], sl2, base))};
+              pw[w] = __builtin_convertvector(pp, half2_t);
+              if (w & 1) l1 = __builtin_amdgcn_fdot2(pw[w], ones, l1, false);
+              else l0 = __builtin_amdgcn_fdot2(pw[w], ones, l0, false);
+            }
+            const v4u_t pk = {__builtin_bit_cast(uint32_t, pw[0]), __builtin_bit_cast(uint32_t, pw[1]),
+                              __builtin_bit_cast(uint32_t, pw[2]), __builtin_bit_cast(uint32_t, pw[3])};
+            pfr[c2] = as_bf16x8(pk);
+          }
+          return;
+        }
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) {
+          bf16x2_t pw[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2_t pp = {fast_exp2(fmaf(cur[8 * c2 + 2 * w], sl2, -m_run)),
+                                 fast_exp2(fmaf(cur[8 * c2 + 2 * w + 1], sl2, -m_run))};
+            pw[w] = __builtin_convertvector(pp, bf16x2_t);
+            if (w & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(pw[w], one2, l1, false);
+            else l0 = __builtin_amdgcn_fdot2_f32_bf16(pw[w], one2, l0, false);
+          }
+          const v4u_t pk = {__builtin_bit_cast(uint32_t, pw[0]), __builtin_bit_cast(uint32_t, pw[1]),
+                            __builtin_bit_cast(uint32_t, pw[2]), __builtin_bit_cast(uint32_t, pw[3])};
+          pfr[c2] = as_bf16x8(pk);
+        }
+      };
+      const auto key_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
+        return i < kMainSteps ? lds_read((tile + k_lane) ^ (i << 5)) : lds_read((tile + r_lane) ^ ((i - kMainSteps) << 5));
+      };
+      const auto value_operand = [&](uint32_t tile, int i) __attribute__((always_inline)) {
+        const uint32_t at_v = ((tile + v_lane) ^ ((i % kDt) << 6)) + 16 * (i / kDt) * P::kVal;
+        // (keys 8 on: another bit of the row's permutation)
+        const uint2 x0 = lds_read_turned(at_v), x1 = lds_read_turned((at_v ^ 16) + 8 * P::kVal);
+        return v4u_t{x0.x, x0.y, x1.x, x1.y};
+      };
+      const auto score = [&](floatx16& cur, int i, v4u_t x) __attribute__((always_inline)) {
+        cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), qf[i], i == 0 ? floatx16{} : cur, 0, 0, 0);
+      };
+      const auto value = [&](const bf16x8_t (&pfr)[2], int i, v4u_t x) __attribute__((always_inline)) {
+        if constexpr (P::kHalf)
+          o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, x), __builtin_bit_cast(half8_t, pfr[i / kDt]), o[i % kDt], 0, 0, 0);
+        else
+          o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), pfr[i / kDt], o[i % kDt], 0, 0, 0);
+      };
+
+      if constexpr (kOverlap && !kScaled) {
+        // Step i: the scores of step i + 1 (from `in`'s successor's rows) while the vector units turn those of
+        // step i into weights, then its values. The compiler interleaves them.
+        auto turn = [&](int step, const floatx16& in, floatx16& next) __attribute__((always_inline)) {
+          publish(step + 1, SLOTS - 3);
+          if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
+          const uint32_t tile = slot_of(step), tile1 = slot_of(step + 1);
+          v4u_t kv[kQSteps], v0[kDt], v1[kDt];
+#pragma unroll
+          for (int i = 0; i < kQSteps; ++i) kv[i] = key_operand(tile1, i);
+#pragma unroll
+          for (int i = 0; i < kDt; ++i) v0[i] = value_operand(tile, i);
+          bf16x8_t pfr[2];
+#pragma unroll
+          for (int i = 0; i < kQSteps; ++i) score(next, i, kv[i]);
+          weights(in, pfr);
+#pragma unroll
+          for (int i = 0; i < kDt; ++i) v1[i] = value_operand(tile, kDt + i);
+#pragma unroll
+          for (int i = 0; i < kDt; ++i) value(pfr, i, v0[i]);
+#pragma unroll
+          for (int i = 0; i < kDt; ++i) value(pfr, kDt + i, v1[i]);
+          mask_max(next, step + 1);
+          rescale();
+        };
+        floatx16 sa, sb;
+#pragma unroll
+        for (int i = 0; i < kQSteps; ++i) score(sa, i, key_operand(slot_of(first), i));
+        mask_max(sa, first);
+        int step = first;
+#pragma unroll 1
+        for (; step + 2 < last; step += 2) {
+          turn(step, sa, sb);
+          turn(step + 1, sb, sa);
+        }
+        if (step + 1 < last) {
+          turn(step, sa, sb);
+          sa = sb;
+          ++step;
+        }
         bf16x8_t pfr[2];
-        weights(cur, pfr);
-        pipelined<2 * kDt, kAhead>([&](int i) __attribute__((always_inline)) { return value_operand(tile, i); },
-                                   [&](int i, v4u_t x) __attribute__((always_inline)) { value(pfr, i, x); });
-        publish(step + 1, kLater);
+        weights(sa, pfr);
+        const uint32_t tile = slot_of(step);
+#pragma unroll
+        for (int i = 0; i < 2 * kDt; ++i) value(pfr, i, value_operand(tile, i));
+      } else {
+#pragma unroll 1
+        for (int step = first; step < last; ++step) {
+          // (every wave is past the step before: its slot is free)
+          if (step + SLOTS - 1 < last) request(step + SLOTS - 1);
+          const uint32_t tile = slot_of(step);
+          // (a wave alone on its tile passes over one without context)
+          if (NCW == 1 && pos_of(step) >= ctx) {
+            publish(step + 1, SLOTS - 2);
+            continue;
+          }
+          floatx16 cur;
+          pipelined<kQSteps, kAhead>([&](int i) __attribute__((always_inline)) { return key_operand(tile, i); },
+                                     [&](int i, v4u_t x) __attribute__((always_inline)) { score(cur, i, x); });
+          mask_max(cur, step);
+          rescale();
+          bf16x8_t pfr[2];
+          weights(cur, pfr);
+          pipelined<2 * kDt, kAhead>([&](int i) __attribute__((always_inline)) { return value_operand(tile, i); },
+                                     [&](int i, v4u_t x) __attribute__((always_inline)) { value(pfr, i, x); });
+          publish(step + 1, SLOTS - 2);
+        }
       }
+    };
+    if constexpr (P::kHalf) {
+      if (scaled) steps(std::true_type{});
+      else steps(std::false_type{});
+    } else {
+      steps(std::false_type{});
     }
 
     // ---- The end of the segment.
+    if constexpr (P::kHalf) {
+      if (scaled) {
+        const float f = ldexpf(1.0f, e_run);
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) o[i] *= f;
+      }
+    }
     float l = pair_sum(l0 + l1);
     if (odd != 0) s_odd = 1;
     if constexpr (NKW == 1) __syncthreads();   // (else the key groups' sums meet behind one)
@@ -798,7 +885,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           const uint8_t* row = value_row(i / (P::kVal / 16));
           if (row == nullptr) continue;
           const v4u_t w = *reinterpret_cast<const v4u_t*>(row + 16 * (i % (P::kVal / 16)));
-          any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
+          any |= not_finite<P::kHalf>(w[0]) | not_finite<P::kHalf>(w[1]) | not_finite<P::kHalf>(w[2]) | not_finite<P::kHalf>(w[3]);
         }
         if (__builtin_amdgcn_ballot_w64(any != 0) == 0) continue;
 #pragma unroll 1
@@ -811,8 +898,9 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           for (int i = 0; i < 4 * kDt; ++i) {
             const int d = 8 * i + 4 * half;   // four dims
             const uint2 w = *reinterpret_cast<const uint2*>(row + 2 * d);
-            if ((not_finite(w.x) | not_finite(w.y)) == 0) continue;
-            const float v[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+            if ((not_finite<P::kHalf>(w.x) | not_finite<P::kHalf>(w.y)) == 0) continue;
+            const float2_t v01 = two_values<P::kHalf>(w.x), v23 = two_values<P::kHalf>(w.y);
+            const float v[4] = {v01[0], v01[1], v23[0], v23[1]};
             if (whole) {
               uint2* at_out = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + orow * S::kDims + d);
               const uint2 y = *at_out;
