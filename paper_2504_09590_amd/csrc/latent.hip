@@ -179,19 +179,19 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
 // expansion
 // ---------------------------------------------------------------------------
 
-// Dense rows: those of every sequence side by side, each sequence's to whole tiles of 32. Rows [128 y, + 128) of the
-// keys (even x) or values (odd x) of head x / 2: latents times weights, 128 x 128 values to a
-// workgroup, four waves of 64 x 64, 64 latent dims a step. Latent rows come straight from their
-// slots. Both operands' rows go to LDS as they lie, 128 bytes a row and step, chunks permuted so that an
-// operand read meets no bank conflict. (Keys that are no context are made of whatever a slot holds:
-// the attention masks them.)
+// Dense rows: those of every sequence side by side, each sequence's to whole tiles of 32. A workgroup makes keys and
+// values of some heads for 128 rows, 128 dims at a time: four waves of 64 x 64, 64 latent dims a stage, two stages
+// in LDS, two workgroups a compute unit. Latent rows come straight from their slots. Both operands' rows go to
+// LDS as they lie, 128 bytes a row and stage, chunks permuted so that an operand read meets no bank conflict.
+// (Keys that are no context are made of whatever a slot holds: the attention masks them.)
 //
 // Keys are rounded to bf16, as the queries that they meet. Values are rounded to fp16, like the softmax weights that
 // they meet: three bits more (with both in bf16 the result is 1.65 times as far from 64 bits as one that is
 // rounded once, so 1.2). fp16's range is made up for by an exponent for each tile of 32 rows and head,
 // 2^e off: 0 where the tile's largest magnitude lies within 2^-6 .. 2^15, as nearly always.
-constexpr int kStepDims = 64, kTileRows = 128;
-constexpr int kHalfTile = kTileRows * kStepDims * 2;
+constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
+constexpr int kStageDims = 64, kStages = 2, kTileRows = 128;
+constexpr int kHalfTile = kTileRows * kStageDims * 2;
 
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 half2_t;
 __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {   // round to nearest even
@@ -204,15 +204,16 @@ __device__ __forceinline__ void load_rows_to_lds(const uint8_t* lane_src, const 
   asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(lane_src), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 
-__global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[2][2 * kHalfTile];
-  __shared__ int64_t s_scan[kThreads / kWave];
-  __shared__ int s_seq[4], s_pos[4];         // of each tile of 32 rows: its sequence (-1: none) and first position
-  __shared__ float s_max[2][4];
+__global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(ExpandArgs a, int items_each) {
+  constexpr int kTiles = kTileRows / ra::kKeys;   // of 32 rows
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tile[kStages][2 * kHalfTile];
+  __shared__ int64_t s_scan[kExpandWaves];
+  __shared__ int s_seq[kTiles], s_pos[kTiles];    // of each tile: its sequence (-1: none) and first position
+  __shared__ float s_max[2][kTiles];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
   const int half = lane >> 5, col = lane & 31;
   const int64_t row0 = (int64_t)blockIdx.y * kTileRows;
-  const int head = blockIdx.x >> 1, which = blockIdx.x & 1;
+  const int item0 = blockIdx.x * items_each, items = min(items_each, 2 * a.heads - item0);   // keys (even) or values of head item / 2
 
   // ---- The tiles' sequences.
   RowsArgs ra_{};
@@ -221,20 +222,20 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
   ra_.num_q_tokens = a.num_q_tokens;
   ra_.max_ctx = a.max_ctx;
   ra_.max_blocks_per_seq = a.max_blocks_per_seq;
-  const int per = (a.num_seqs + kThreads - 1) / kThreads;
+  const int per = (a.num_seqs + kExpandThreads - 1) / kExpandThreads;
   const int s0 = min(tid * per, a.num_seqs), s1 = min(s0 + per, a.num_seqs);
   int64_t mine = 0;
   for (int s = s0; s < s1; ++s) mine += ra::dense_rows(ra::seq_of(ra_, s).ctx);
   const int64_t inc = ra::wave_scan64(mine, lane);
   if (lane == kWave - 1) s_scan[wave] = inc;
-  if (tid < 4) s_seq[tid] = -1;
+  if (tid < kTiles) s_seq[tid] = -1;
   __syncthreads();
   int64_t first = inc - mine;
   for (int i = 0; i < wave; ++i) first += s_scan[i];
   if (first < row0 + kTileRows && first + mine > row0) {
     for (int s = s0; s < s1; ++s) {
       const int rows = ra::dense_rows(ra::seq_of(ra_, s).ctx);
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kTiles; ++i) {
         const int64_t r = row0 + 32 * i;
         if (r >= first && r < first + rows) {
           s_seq[i] = s;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
   }
   __syncthreads();
   if (s_seq[0] < 0) return;   // behind the last sequence (uniform)
-  // Row r of the workgroup's 128, in the pool (one that is not there: the first row of the pool).
+  // Row r of the workgroup's, in the pool (one that is not there: the first row of the pool).
   const auto pool_row = [&](int r) -> const uint8_t* {
     const uint8_t* pool = static_cast<const uint8_t*>(a.pool);
     const int s = s_seq[r >> 5], pos = s_pos[r >> 5] + (r & 31);
@@ -264,8 +265,8 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
     return b >= 0 && b < a.num_blocks;
   };
 
-  const uint8_t* wsrc = static_cast<const uint8_t*>(a.w) + ((size_t)head * 256 + 128 * which) * kLatent * 2;
-  // a wave loads rows 32 wave .. + 31 of both tiles, eight rows of 128 bytes to a load
+  // A wave loads rows 32 wave .. + 31 of both operands, eight rows of 128 bytes to a load: row r's chunk c lies at
+  // 128 r + 16 (c ^ (r / 2 % 8)), so that 16 rows' chunks of one operand read lie in 16 groups of banks.
   const uint8_t* csrc[4];
   uint32_t woff[4];
 #pragma unroll
@@ -275,101 +276,124 @@ __global__ __launch_bounds__(kThreads, 2) void latent_expand_kernel(ExpandArgs a
     csrc[i] = pool_row(r) + chunk;
     woff[i] = (uint32_t)r * (kLatent * 2) + chunk;
   }
-  auto issue = [&](int step, int buf) __attribute__((always_inline)) {
+  constexpr int kPerItem = kLatent / kStageDims;
+  const int stages = items * kPerItem;
+  auto issue = [&](int k) __attribute__((always_inline)) {   // stage k: latent dims 64 (k % 8) .. of item k / 8
+    const uint8_t* wsrc = static_cast<const uint8_t*>(a.w) + ((size_t)(item0 + k / kPerItem) * 128 * kLatent + (k % kPerItem) * kStageDims) * 2;
+    uint8_t* dst = s_tile[k % kStages];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r8 = 32 * wave + 8 * i;
-      pf::load_to_lds(wsrc + step * 128, woff[i], s_tile[buf] + r8 * 128);
-      load_rows_to_lds(csrc[i] + step * 128, s_tile[buf] + kHalfTile + r8 * 128);
+      pf::load_to_lds(wsrc, woff[i], dst + r8 * 128);
+      load_rows_to_lds(csrc[i] + (k % kPerItem) * (kStageDims * 2), dst + kHalfTile + r8 * 128);
     }
   };
   const int wd = wave & 1, wr = wave >> 1;   // the wave's 64 dims and 64 rows
+  uint32_t context = 0;                      // bit k: row 64 wr + 32 k + col is one
+#pragma unroll
+  for (int k = 0; k < 2; ++k) context |= (is_context(64 * wr + 32 * k + col) ? 1u : 0u) << k;
+  const int lane_at = (col >> 1) * 256 + ((col & 1) << 7), sw = (col >> 1) & 7;
   pf::floatx16 o[2][2];                      // [dims][rows]
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) o[i][k] = pf::floatx16{};
-  }
-  const int r_lane = (col >> 1) * 256 + ((col & 1) << 7), r_sw = (col >> 1) & 7;
-  constexpr int kSteps = kLatent / kStepDims;
   // (the addresses come from loads that the compiler sees: they are there before the first request)
-  issue(0, 0);
+  issue(0);
 #pragma unroll 1
-  for (int step = 0; step < kSteps; ++step) {
-    pf::wait_vmem<0>();
-    pf::lds_barrier();
-    if (step + 1 < kSteps) issue(step + 1, (step + 1) & 1);
-    const uint8_t* tw = s_tile[step & 1] + wd * 64 * 128;
-    const uint8_t* tc = s_tile[step & 1] + kHalfTile + wr * 64 * 128;
-#pragma unroll
-    for (int c = 0; c < kStepDims / 16; ++c) {
-      const int at = r_lane + (((2 * c + half) ^ r_sw) << 4);
-      pf::v4u_t x[2], y[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        x[i] = *reinterpret_cast<const pf::v4u_t*>(tw + 32 * 128 * i + at);
-        y[i] = *reinterpret_cast<const pf::v4u_t*>(tc + 32 * 128 * i + at);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          o[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf::as_bf16x8(x[i]), pf::as_bf16x8(y[k]), o[i][k], 0, 0, 0);
-      }
-    }
-  }
-  // The values' exponents: of the largest finite magnitude of 32 rows and 128 dims. Rows that are no context
-  // do not count, and are zeros.
-  float mul[2] = {1.0f, 1.0f};
-  if (which == 1) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const bool there = is_context(64 * wr + 32 * k + col);
-      float m = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          o[i][k][e] = there ? o[i][k][e] : 0.0f;
-          const float x = fabsf(o[i][k][e]);
-          m = fmaxf(m, x < INFINITY ? x : 0.0f);
-        }
-      }
-#pragma unroll
-      for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-      if (lane == 0) s_max[wd][2 * wr + k] = m;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float m = fmaxf(s_max[0][2 * wr + k], s_max[1][2 * wr + k]);
-      int e = 0;
-      if (m > 0.0f && (m < 0x1p-6f || m >= 0x1p15f)) e = max(-120, min(120, ilogbf(m) - 13));
-      mul[k] = ldexpf(1.0f, -e);
-      const int64_t tile = row0 / 32 + 2 * wr + k;
-      if (wd == 0 && lane == 0 && 32 * tile < a.dense_rows) a.exps[(size_t)head * (a.dense_rows / 32) + tile] = e;
-    }
-  }
-  uint16_t* dst = static_cast<uint16_t*>(which == 0 ? a.k_rows : a.v_rows) + (size_t)head * a.dense_rows * 128;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int64_t r = row0 + 64 * wr + 32 * k + col;
-    if (r >= a.dense_rows) continue;
+  for (int item = 0; item < items; ++item) {
+    const bool values = (item0 + item) & 1;
+    const int head = (item0 + item) >> 1;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int jq = 0; jq < 4; ++jq) {
-        const float x[4] = {o[i][k][4 * jq], o[i][k][4 * jq + 1], o[i][k][4 * jq + 2], o[i][k][4 * jq + 3]};
-        uint2 v;
-        if (which == 0) v = make_uint2(pf::pack2_bf16(x[0], x[1]), pf::pack2_bf16(x[2], x[3]));
-        else v = make_uint2(pack2_f16(x[0] * mul[k], x[1] * mul[k]), pack2_f16(x[2] * mul[k], x[3] * mul[k]));
-        *reinterpret_cast<uint2*>(dst + r * 128 + 64 * wd + 32 * i + 8 * jq + 4 * half) = v;
+      for (int k = 0; k < 2; ++k) o[i][k] = pf::floatx16{};
+    }
+#pragma unroll 1
+    for (int kk = 0; kk < kPerItem; ++kk) {
+      const int stage = item * kPerItem + kk;
+      pf::wait_vmem<0>();
+      pf::lds_barrier();
+      if (stage + 1 < stages) issue(stage + 1);
+      const uint8_t* tw = s_tile[stage % kStages] + wd * 64 * 128;
+      const uint8_t* tc = s_tile[stage % kStages] + kHalfTile + wr * 64 * 128;
+#pragma unroll
+      for (int c = 0; c < kStageDims / 16; ++c) {
+        const int at = lane_at + (((2 * c + half) ^ sw) << 4);
+        pf::v4u_t x[2], y[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[i] = *reinterpret_cast<const pf::v4u_t*>(tw + 32 * 128 * i + at);
+          y[i] = *reinterpret_cast<const pf::v4u_t*>(tc + 32 * 128 * i + at);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            o[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf::as_bf16x8(x[i]), pf::as_bf16x8(y[k]), o[i][k], 0, 0, 0);
+        }
+      }
+    }
+    // The values' exponents: of the largest finite magnitude of 32 rows and 128 dims. Rows that are no context
+    // do not count, and are zeros.
+    float mul[2] = {1.0f, 1.0f};
+    if (values) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool there = (context >> k) & 1u;
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            o[i][k][e] = there ? o[i][k][e] : 0.0f;
+            const float x = fabsf(o[i][k][e]);
+            m = fmaxf(m, x < INFINITY ? x : 0.0f);
+          }
+        }
+#pragma unroll
+        for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+        if (lane == 0) s_max[wd][2 * wr + k] = m;
+      }
+    }
+    pf::lds_barrier();   // (and every wave has read the last stage: its place takes the results)
+    if (values) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float m = fmaxf(s_max[0][2 * wr + k], s_max[1][2 * wr + k]);
+        int e = 0;
+        if (m > 0.0f && (m < 0x1p-6f || m >= 0x1p15f)) e = max(-120, min(120, ilogbf(m) - 13));
+        mul[k] = ldexpf(1.0f, -e);
+        const int64_t tile = row0 / 32 + 2 * wr + k;
+        if (wd == 0 && lane == 0 && 32 * tile < a.dense_rows) a.exps[(size_t)head * (a.dense_rows / 32) + tile] = e;
+      }
+    }
+    uint16_t* dst = static_cast<uint16_t*>(values ? a.v_rows : a.k_rows) + (size_t)head * a.dense_rows * 128 + 64 * wd;
+    // (through LDS to whole lines: as the products leave them, 16 bytes a row, the stores take as long as the products)
+    uint8_t* out = s_tile[(item * kPerItem + kPerItem - 1) % kStages] + wave * 4096;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // row `col`, 128 bytes: chunk c at 16 (c ^ (col % 8))
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int jq = 0; jq < 4; ++jq) {
+          const float x[4] = {o[i][k][4 * jq], o[i][k][4 * jq + 1], o[i][k][4 * jq + 2], o[i][k][4 * jq + 3]};
+          uint2 v;
+          if (values) v = make_uint2(pack2_f16(x[0] * mul[k], x[1] * mul[k]), pack2_f16(x[2] * mul[k], x[3] * mul[k]));
+          else v = make_uint2(pf::pack2_bf16(x[0], x[1]), pf::pack2_bf16(x[2], x[3]));
+          *reinterpret_cast<uint2*>(out + col * 128 + (((4 * i + jq) ^ (col & 7)) << 4) + 8 * half) = v;
+        }
+      }
+      // (the wave's own: reads follow its writes in order)
+      const int64_t r0 = row0 + 64 * wr + 32 * k;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3);
+        const uint4 v = *reinterpret_cast<const uint4*>(out + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+        if (r0 < a.dense_rows) *reinterpret_cast<uint4*>(dst + (r0 + r) * 128 + 8 * (lane & 7)) = v;
       }
     }
   }
   // The rotated keys' dense rows, once a call.
   if (blockIdx.x == 0 && a.with_rot) {
-    const int r = tid >> 1;
+    const int r = tid >> 1;   // (two threads a row)
     if (row0 + r < a.dense_rows) {
       const uint4* src = reinterpret_cast<const uint4*>(pool_row(r) + kLatent * 2) + 4 * (tid & 1);
       uint4* to = reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.rot_rows) + (row0 + r) * (kRot * 2)) + 4 * (tid & 1);
@@ -392,8 +416,20 @@ hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
-  const unsigned tiles = (unsigned)((a.dense_rows + kTileRows - 1) / kTileRows);
-  hipLaunchKernelGGL(latent_expand_kernel, dim3(2 * a.heads, tiles), dim3(kThreads), 0, stream, a);
+  const int64_t tiles = (a.dense_rows + kTileRows - 1) / kTileRows;
+  // Items (a head's keys, or its values) of a workgroup: the number whose rounds over the compute units, two workgroups
+  // each, end first; a workgroup's start (its rows' places) takes as long as two thirds of an item.
+  const int64_t slots = 2 * (int64_t)stream_compute_units(stream), all = 2 * (int64_t)a.heads;
+  int each = 1;
+  double best = 0.0;
+  for (int n = 1; n <= 32; ++n) {
+    const double us = (double)(((all + n - 1) / n * tiles + slots - 1) / slots) * (std::min<int64_t>(n, all) + 0.67);
+    if (n == 1 || us < best) {
+      each = n;
+      best = us;
+    }
+  }
+  hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)((all + each - 1) / each), (unsigned)tiles), dim3(kExpandThreads), 0, stream, a, each);
   return hipGetLastError();
 }
 
