@@ -94,15 +94,16 @@ int check_rope(const char* fn, const bros_rope* rope, const int32_t* rope_pos, i
 // the strides are equal, else by the whole ranges.
 bool rows_meet(const void* xp, int64_t sx, int64_t lx, const void* yp, int64_t sy, int64_t ly, int64_t tokens) {
   if (tokens <= 0 || lx <= 0 || ly <= 0) return false;
-  const int64_t x = (int64_t)reinterpret_cast<uintptr_t>(xp), y = (int64_t)reinterpret_cast<uintptr_t>(yp);
-  const int64_t last = tokens - 1;
+  using Wide = __int128;   // (a stride times 2^31 tokens passes 64 bits)
+  const Wide x = (Wide)reinterpret_cast<uintptr_t>(xp), y = (Wide)reinterpret_cast<uintptr_t>(yp);
+  const Wide last = tokens - 1;
   if (!(x < y + last * sy + ly && y < x + last * sx + lx)) return false;
   if (sx != sy || sx <= 0 || tokens == 1) return true;
   // some k in -last .. last with  -ly < (y - x) + k s < lx
-  const int64_t d = y - x;
-  const auto floor_div = [](int64_t a, int64_t b) { return a / b - ((a % b != 0 && (a < 0) != (b < 0)) ? 1 : 0); };
-  const int64_t k_lo = floor_div(-ly - d, sx) + 1;          // the least k with d + k s > -ly
-  const int64_t k = std::max(k_lo, -last);
+  const Wide d = y - x;
+  const auto floor_div = [](Wide a, Wide b) { return a / b - ((a % b != 0 && (a < 0) != (b < 0)) ? 1 : 0); };
+  const Wide k_lo = floor_div(-ly - d, sx) + 1;             // the least k with d + k s > -ly
+  const Wide k = std::max<Wide>(k_lo, -last);
   return k <= last && d + k * sx < lx;
 }
 

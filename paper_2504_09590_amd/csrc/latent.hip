@@ -212,8 +212,9 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
   __shared__ float s_max[2][kTiles];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
   const int half = lane >> 5, col = lane & 31;
-  const int64_t row0 = (int64_t)blockIdx.y * kTileRows;
-  const int item0 = blockIdx.x * items_each, items = min(items_each, 2 * a.heads - item0);   // keys (even) or values of head item / 2
+  const int shares = (2 * a.heads + items_each - 1) / items_each;   // workgroups of a tile of rows, one after another
+  const int64_t row0 = (int64_t)(blockIdx.x / shares) * kTileRows;
+  const int item0 = (int)(blockIdx.x % shares) * items_each, items = min(items_each, 2 * a.heads - item0);   // keys (even) or values of head item / 2
 
   // ---- The tiles' sequences.
   RowsArgs ra_{};
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
     }
   }
   // The rotated keys' dense rows, once a call.
-  if (blockIdx.x == 0 && a.with_rot) {
+  if (item0 == 0 && a.with_rot) {
     const int r = tid >> 1;   // (two threads a row)
     if (row0 + r < a.dense_rows) {
       const uint4* src = reinterpret_cast<const uint4*>(pool_row(r) + kLatent * 2) + 4 * (tid & 1);
@@ -429,7 +430,9 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
       best = us;
     }
   }
-  hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)((all + each - 1) / each), (unsigned)tiles), dim3(kExpandThreads), 0, stream, a, each);
+  // (a grid holds 2^32 - 1 threads)
+  while (each < all && (all + each - 1) / each * tiles > (1LL << 23)) each *= 2;
+  hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)((all + each - 1) / each * tiles)), dim3(kExpandThreads), 0, stream, a, each);
   return hipGetLastError();
 }
 

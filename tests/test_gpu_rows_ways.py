@@ -1,0 +1,204 @@
+"""Every way of running the attention of few rows (units' widths, whole units and cut ones) where it can go
+wrong: long contexts with blocks missing across the windows of table entries, masks' later words, values far from one, offsets."""
+
+import numpy as np
+import pytest
+
+from tests.gpu_helpers import announce, require_gpu
+from tests.rows_helpers import WAYS_LATENT, WAYS_TREE, bf16, check
+from tests.test_gpu_latent import LATENT, ROW, Absorbed, Chunks
+from tests.test_gpu_tree import D, Case
+
+pytestmark = pytest.mark.gpu
+
+
+def lose_blocks(b, seed):
+    """Takes entries out of every table: some alone, some side by side, each way that an entry is invalid."""
+    rng = np.random.default_rng(seed)
+    for s in range(b.S):
+        last = int(b.c0[s]) // 16            # (the drafts' own blocks stay)
+        if last < 8:
+            continue
+        at = rng.integers(0, last - 4, max(1, last // 24))
+        b.tables[s, at] = rng.choice([-1, b.num_blocks, -2 ** 31, 2 ** 31 - 1], at.size)
+        i = int(rng.integers(0, last - 6))
+        b.tables[s, i:i + 5] = -1
+
+
+@pytest.mark.parametrize("bits", ["tree", None])
+@pytest.mark.parametrize("way", WAYS_TREE, ids=lambda w: f"way{w[0]}")
+def test_drafts_take_every_way(way, bits):
+    torch = require_gpu()
+    w, n, c0, hq, hkv = way
+    c = Case(n, c0, hq, hkv, bits, seed=40 + w, directions="table")
+    lose_blocks(c.b, w)
+    got = c.check(f"tree way {w} {bits}")
+    assert torch.equal(got, c.run())
+
+
+@pytest.mark.parametrize("bits", ["tree", None])
+@pytest.mark.parametrize("way", WAYS_LATENT, ids=lambda w: f"way{w[0]}")
+def test_latent_rows_take_every_way(way, bits):
+    torch = require_gpu()
+    w, n, c0, hq = way
+    c = Absorbed(n, c0, hq, bits, seed=50 + w, directions="table")
+    lose_blocks(c.b, w)
+    got = c.check(f"latent way {w} {bits}")
+    assert torch.equal(got, c.run())
+
+
+@pytest.mark.parametrize("hq", [8, 64, 128])
+def test_one_long_sequence_beside_short_ones(hq):
+    """Shares that lie in one unit, and shares that hold many; a context without any valid block."""
+    require_gpu()
+    n = [1] * 40
+    c0 = [int(x) for x in np.random.default_rng(hq).integers(0, 200, 40)]
+    c0[7], c0[23] = 20000, 1000
+    c = Absorbed(n, c0, hq, None, seed=hq)
+    c.b.tables[23] = -1
+    got = c.check(f"latent, one long sequence, {hq} heads")
+    assert (got[23] == 0).all()
+    c = Case([3] * 40, c0, 8, 1, seed=hq)
+    c.b.tables[23] = -1
+    got = c.check("tree, one long sequence")
+    assert (got[69:72] == 0).all()
+
+
+def test_last_words_of_masks_over_long_contexts():
+    """Drafts of every word behind contexts that end inside a step of keys."""
+    require_gpu()
+    rng = np.random.default_rng(3)
+    n, c0 = [256, 200], [1999, 345]
+    rows = [sum(1 << int(x) for x in rng.integers(0, m, 3)) for m in n for _ in range(m)]
+    Case(n, c0, 8, 4, rows, seed=4, words=4).check("tree, masks of four words")
+    Absorbed(n, c0, 4, rows, seed=5, words=4).check("latent, masks of four words")
+
+
+def test_a_chunk_without_mask_of_many_rows():
+    require_gpu()
+    Case([700], [130], 8, 2, None, seed=7).check("tree, 700 rows without a mask")
+    Absorbed([333], [50], 6, None, seed=8).check("latent, 333 rows without a mask")
+
+
+def test_scale_and_scores_far_from_zero():
+    """A scale of the caller's; scores of hundreds, where one weight is all there is."""
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    c = Case([5, 20], [300, 700], 8, 2, seed=9)
+    c.q = (c.q.float() * 16).bfloat16()
+    c.check("tree, large scores")
+    a = Absorbed([2, 2], [300, 700], 20, "tree", seed=9)
+    a.q = (a.q.float() * 16).bfloat16()
+    a.check("latent, large scores")
+    announce("latent, a scale of the caller's")
+    tables, dirs, ctx, cu = a.b.cuda()
+    got = torch.empty((a.b.rows, a.hq, LATENT), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(bros.bros_attn_workspace_size(3, 1, 1, 1, ROW, 0), dtype=torch.uint8, device="cuda")
+    a.q = (a.q.float() / 16).bfloat16()       # (a power of two: the same scores from the scale)
+    bros.bros_attn_latent(got, a.q.cuda(), cu, 2, a.pool.cuda(), tables, dirs, None, ctx, a.b.max_ctx,
+                          mask=torch.from_numpy(a.bits).cuda(), scale=16 * 192 ** -0.5, workspace=ws)
+    torch.cuda.synchronize()
+    a.q = (a.q.float() * 16).bfloat16()
+    check(got, *a.want(), "latent, scale")
+
+
+@pytest.mark.parametrize("gain", [2.0 ** -40, 2.0 ** -9, 2.0 ** 12, 2.0 ** 60])
+def test_expanded_values_far_from_one(gain):
+    """The values' weights: all small or large. (The result grows with them, so the bounds do.)"""
+    torch = require_gpu()
+    c = Chunks([70, 33], [200, 0], 2, seed=31)
+    c.w[:, 128:] = (c.w[:, 128:].float() * gain).bfloat16()
+    c.check(f"latent prefill, values of {gain}")
+
+
+def test_expanded_rows_of_different_sizes():
+    """A row of 2^20 times the others': the rows before it share its tile of 32 values. Values are halves behind a
+    power of two that brings the tile's largest magnitude m to 2^13 or more; halves below their
+    normal range are off by at most 2^-25, which is 2^-38 of m. (From that row on, scores are in the millions,
+    and which row takes all of the weight is a matter of roundings: those are only to be finite.)"""
+    require_gpu()
+    b = Chunks([96], [0], 2, seed=32)
+    big = 70
+    blk, slot = b.b.places(0, [big])
+    b.pool[blk, slot, :LATENT] = (b.pool[blk, slot, :LATENT].float() * 2.0 ** 20).bfloat16()
+    announce("latent prefill, rows of different sizes")
+    got = b.run().double().cpu()
+    assert got.isfinite().all()
+    want, tol = b.want()
+    m = (b.pool[b.b.places(0, [big])].double()[:, :LATENT] @ b.w[:, 128:].double().transpose(1, 2)).abs().amax((1, 2))   # [heads]
+    tol[64:] += m[None, :, None] * 2.0 ** -38
+    check(got[:big], want[:big], tol[:big], "rows of different sizes")
+
+
+def test_expanded_slots_behind_the_context_hold_anything():
+    """What lies behind the contexts in their last blocks, finite and huge, counts nowhere (the poisoned
+    pool of the other tests holds NaN there)."""
+    torch = require_gpu()
+    c = Chunks([37, 5], [0, 90], 2, seed=33)
+    announce("latent prefill, huge values behind the contexts")
+    first = c.run()
+    blk, slot = np.nonzero(~c.b.owned())
+    c.pool[blk, slot] = 3.0e38
+    assert torch.equal(first, c.run())
+    c.pool[blk, slot] = 0.0
+    assert torch.equal(first, c.run())
+
+
+def test_latent_offsets_beyond_32_bits():
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    nb = 300000                               # 5.5e9 bytes
+    a = Absorbed([3], [900], 16, "tree", seed=34)
+    e = Chunks([40], [500], 2, seed=35)
+    announce("latent offsets")
+    pool = torch.empty((nb, 16, ROW), dtype=torch.bfloat16, device="cuda")
+    for c, call in ((a, "absorbed"), (e, "expanded")):
+        tables, dirs, ctx, cu = c.b.cuda()
+        pool[nb - c.b.num_blocks:] = c.pool.cuda()
+        tables = torch.where(tables >= 0, tables + (nb - c.b.num_blocks), tables)
+        q = c.q.cuda()
+        if call == "absorbed":
+            out = torch.empty((c.b.rows, c.hq, LATENT), dtype=torch.bfloat16, device="cuda")
+            ws = torch.empty(bros.bros_attn_workspace_size(3, 1, 1, 1, ROW, 0), dtype=torch.uint8, device="cuda")
+            bros.bros_attn_latent(out, q, cu, 3, pool, tables, dirs, None, ctx, c.b.max_ctx, mask=torch.from_numpy(c.bits).cuda(), workspace=ws)
+        else:
+            out = torch.empty((c.b.rows, c.hq, 128), dtype=torch.bfloat16, device="cuda")
+            ws = torch.empty(bros.bros_latent_prefill_workspace_size(1, 540, 2), dtype=torch.uint8, device="cuda")
+            bros.bros_attn_latent_prefill(out, q, cu, 40, c.w.cuda(), pool, tables, dirs, None, ctx, 540, 540, workspace=ws)
+        torch.cuda.synchronize()
+        check(out, *c.want(), f"latent offsets, {call}")
+    # the append to the last block, and a commit there
+    kv = bf16(np.random.default_rng(1), (3, ROW)).cuda()
+    tables = torch.tensor([[nb - 1]], dtype=torch.int32).cuda()
+    dirs, at, cu = torch.ones(1, dtype=torch.int8).cuda(), torch.tensor([5], dtype=torch.int32).cuda(), torch.tensor([0, 3], dtype=torch.int32).cuda()
+    bros.bros_latent_append(None, None, kv, pool, tables, dirs, None, at, cu)
+    torch.cuda.synchronize()
+    assert torch.equal(pool[nb - 1, 5:8], kv)
+    path = torch.tensor([[2]], dtype=torch.int32).cuda()
+    bros.bros_tree_commit(pool, None, tables, dirs, None, at + 3, cu, path, torch.tensor([1], dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(pool[nb - 1, 5], kv[2]) and torch.equal(pool[nb - 1, 6:8], kv[1:])
+
+
+def test_dirty_workspaces_and_two_streams():
+    """Two calls at once, each with a workspace of its own that held anything before."""
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    c = Case([20] * 3, [3000] * 3, 8, 2, seed=36)
+    a = Absorbed([2] * 3, [3000] * 3, 32, "tree", seed=37)
+    announce("two calls at once")
+    first_c, first_a = c.run(), a.run()
+    tc, ta = c.b.cuda(), a.b.cuda()
+    mc, ma = torch.from_numpy(c.bits).cuda(), torch.from_numpy(a.bits).cuda()
+    wc = torch.full((bros.bros_attn_workspace_size(2, 1, 1, 1, D, 0),), 127, dtype=torch.uint8, device="cuda")
+    wa = torch.full((bros.bros_attn_workspace_size(3, 1, 1, 1, ROW, 0),), 127, dtype=torch.uint8, device="cuda")
+    oc, oa = torch.empty_like(first_c), torch.empty_like(first_a)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        q, k, v = c.dev
+        bros.bros_attn_tree(oc, q, tc[3], 20, k, v, tc[0], tc[1], None, tc[2], c.b.max_ctx, mask=mc, workspace=wc, stream=s1)
+        q, pool = a.dev
+        bros.bros_attn_latent(oa, q, ta[3], 2, pool, ta[0], ta[1], None, ta[2], a.b.max_ctx, mask=ma, workspace=wa, stream=s2)
+    torch.cuda.synchronize()
+    assert torch.equal(oc, first_c) and torch.equal(oa, first_a)
