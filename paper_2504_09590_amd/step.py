@@ -32,6 +32,10 @@ max(t_exec, t_swap).
 
 QkvStep is the step one operator earlier: it takes the projection's rows, and
 the append's norms, rotation and writes stand in place of bros_kv_write.
+
+DraftStep is the decode step of drafted tokens: several new rows a sequence in a tree, and the
+accepted ones kept. LatentStep is the step over a latent pool: prompts' chunks in the expanded
+form, decode rows or drafts in the absorbed one.
 """
 
 from __future__ import annotations
@@ -272,3 +276,128 @@ class QkvStep:
             decode(dec, self.q[n:], *pools, d.block_tables[P:], d.dir[P:], d.cls[P:], d.ctx_lens[P:], self.max_ctx_dec,
                    workspace=self.workspace)
         return pre, dec
+
+
+def _advance(pos0, ctx_lens, drafts, path_lens, most):
+    """Lengths behind a commit: the kept drafts are context, the next ones lie behind them."""
+    kept = torch.minimum(path_lens.clamp(0, most), drafts)
+    pos0.add_(kept)
+    torch.add(pos0, drafts, out=ctx_lens)
+
+
+class DraftStep:
+    """One decode step of drafted tokens over a K/V pool, and the keeping of those accepted.
+
+    batch and dev are those of MixedStep without prefill chunks: sequence s has cu_new[s + 1] - cu_new[s]
+    drafts (at most BROS_TREE_MAX_DRAFTS, none is fine) behind pos0[s] tokens. dev.pos0 and dev.ctx_lens
+    are this step's to move on: every accept leaves them as the next run needs them, on the device, so that
+    run and accept can be captured. max_ctx bounds the contexts of every run (default: what the tables hold).
+
+    Order of one run:  bros_qkv_append (norms, rotation by rope_pos: a draft's depth, not its place)
+                       -> bros_attn_tree
+    and of accept:     bros_tree_commit -> the lengths, all on the current stream.
+    """
+
+    def __init__(self, batch, dev: bros.DeviceBatch, rope=None, norm=None, max_ctx: int | None = None):
+        if batch.num_prefill:
+            raise ValueError("a step of drafts has no prefill chunks")
+        if batch.dtype != "bf16":
+            raise ValueError(f"drafts' attention takes bf16 rows, not {batch.dtype}")
+        drafts = np.diff(batch.cu_new)
+        self.max_drafts = int(drafts.max()) if drafts.size else 0
+        if self.max_drafts > bros.BROS_TREE_MAX_DRAFTS:
+            raise ValueError(f"{self.max_drafts} drafts of a sequence; at most {bros.BROS_TREE_MAX_DRAFTS}")
+        self.batch, self.dev, self.rope, self.norm = batch, dev, rope, norm
+        device, rows = dev.k_pool.device, int(batch.cu_new[-1])
+        self.drafts = torch.from_numpy(drafts.astype(np.int32)).to(device)
+        self.max_ctx = 16 * dev.block_tables.shape[1] if max_ctx is None else int(max_ctx)
+        self.q = torch.empty((rows, batch.num_q_heads, batch.head_dim), dtype=torch.bfloat16, device=device)
+        self.out = torch.empty_like(self.q)
+        size = bros.bros_attn_workspace_size(bros.BROS_WS_TREE, bros.BROS_BF16, max(rows, 1), batch.num_q_heads, batch.head_dim,
+                                             self.max_ctx)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
+
+    def run(self, q, k, v, mask=None, rope_pos=None):
+        """q, k, v: the drafts' rows [Tn][heads][D]; mask: int64 [Tn][words] or None (chains). Returns the
+        drafts' outputs, which the next run overwrites. Runs of one step must not overlap in time."""
+        d = self.dev
+        bros.bros_qkv_append(self.q, q, k, v, d.k_pool, d.v_pool, d.block_tables, d.dir, d.cls, d.pos0, d.cu_new, rope=self.rope,
+                             rope_pos=rope_pos, norm=self.norm)
+        bros.bros_attn_tree(self.out, self.q, d.cu_new, self.max_drafts, d.k_pool, d.v_pool, d.block_tables, d.dir, d.cls, d.ctx_lens,
+                            self.max_ctx, mask=mask, workspace=self.workspace)
+        return self.out
+
+    def accept(self, path, path_lens):
+        """Keeps the drafts path[s][0 .. path_lens[s]) of every sequence (int32 [S][most] and [S], on the device)."""
+        d = self.dev
+        bros.bros_tree_commit(d.k_pool, d.v_pool, d.block_tables, d.dir, d.cls, d.ctx_lens, d.cu_new, path, path_lens)
+        _advance(d.pos0, d.ctx_lens, self.drafts, path_lens, path.shape[1])
+
+
+class LatentStep:
+    """One step over a latent pool: append, prompts' chunks in the expanded form, decode rows in the absorbed one.
+
+    Sequences [0, P) of batch are chunks, [P, S) have one new row each or several drafts. dev gives the
+    tables, directions, offsets and lengths (its pools are not used); pool is [num_blocks][16][576] and w_kv the
+    keys' and values' weights [Hq][256][512] (None without chunks). rope (of 64 dims) and norm (bf16 [512])
+    are kept for every run. pass_heads: heads whose keys and values the workspace holds at a time (default: all).
+
+    Order of one run:  bros_latent_append (chunks; their queries' rotated dims where they are)
+                       -> bros_attn_latent_prefill
+                       -> bros_latent_append (decode rows, likewise) -> bros_attn_latent
+    all on the current stream. accept keeps drafts as DraftStep does.
+    """
+
+    def __init__(self, batch, dev, pool, w_kv=None, rope=None, norm=None, eps: float = 1e-6, pass_heads: int | None = None,
+                 max_ctx: int | None = None):
+        P, S = batch.num_prefill, batch.num_seqs
+        counts = np.diff(batch.cu_new)
+        if P and w_kv is None:
+            raise ValueError("chunks need the weights of keys and values")
+        self.batch, self.dev, self.pool, self.w_kv, self.rope, self.norm, self.eps = batch, dev, pool, w_kv, rope, norm, eps
+        self.P, self.S, self.rows_prefill = P, S, int(batch.cu_new[P])
+        self.max_chunk = int(counts[:P].max()) if P else 0
+        self.max_rows = int(counts[P:].max()) if S > P else 0
+        device, hq = pool.device, batch.num_q_heads
+        rows = int(batch.cu_new[-1]) - self.rows_prefill
+        self.drafts = torch.from_numpy(counts[P:].astype(np.int32)).to(device)
+        self.cu_rows = torch.from_numpy((batch.cu_new[P:] - batch.cu_new[P]).astype(np.int32)).to(device)
+        self.max_ctx_pre = int(batch.ctx_lens[:P].max()) if P else 0
+        self.total_ctx = int(batch.ctx_lens[:P].sum()) if P else 0
+        self.max_ctx_rows = 16 * dev.block_tables.shape[1] if max_ctx is None else int(max_ctx)
+        self.out_chunks = torch.empty((self.rows_prefill, hq, 128), dtype=torch.bfloat16, device=device)
+        self.out_rows = torch.empty((rows, hq, 512), dtype=torch.bfloat16, device=device)
+        size = bros.bros_latent_prefill_workspace_size(P, self.total_ctx, pass_heads or hq) if P else 0
+        if rows:
+            size = max(size, bros.bros_attn_workspace_size(bros.BROS_WS_LATENT, bros.BROS_BF16, rows, hq, 576, self.max_ctx_rows))
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
+
+    def _append(self, q, kv, lo, hi, cu, rope_pos):
+        d = self.dev
+        turn = q[:, :, -64:]
+        bros.bros_latent_append(turn, turn, kv, self.pool, d.block_tables[lo:hi], d.dir[lo:hi], d.cls[lo:hi], d.pos0[lo:hi], cu,
+                                rope=self.rope, rope_pos=rope_pos, norm=self.norm, eps=self.eps)
+
+    def run(self, kv, q_chunks=None, q_rows=None, mask=None, rope_pos=None):
+        """kv: the new tokens' rows [Tn][576], the chunks' first; q_chunks: their queries [n][Hq][192]; q_rows: the
+        others' [Tn - n][Hq][576], (W_k^T q_n | q_r). The append turns both's last 64 dims in place. mask: int64
+        [Tn - n][words] or None; rope_pos: int32 [axes][Tn] (or [Tn]). Returns the outputs [n][Hq][128] and
+        [Tn - n][Hq][512], which the next run overwrites. Runs of one step must not overlap in time."""
+        d, P, S, n = self.dev, self.P, self.S, self.rows_prefill
+        pos = (lambda lo, hi: None) if rope_pos is None else (lambda lo, hi: rope_pos[..., lo:hi].contiguous())
+        if P:
+            self._append(q_chunks, kv[:n], 0, P, d.cu_new[:P + 1], pos(0, n))
+            bros.bros_attn_latent_prefill(self.out_chunks, q_chunks, d.cu_new[:P + 1], self.max_chunk, self.w_kv, self.pool,
+                                          d.block_tables[:P], d.dir[:P], d.cls[:P], d.ctx_lens[:P], self.max_ctx_pre, self.total_ctx,
+                                          workspace=self.workspace)
+        if S > P:
+            self._append(q_rows, kv[n:], P, S, self.cu_rows, pos(n, kv.shape[0]))
+            bros.bros_attn_latent(self.out_rows, q_rows, self.cu_rows, self.max_rows, self.pool, d.block_tables[P:], d.dir[P:],
+                                  d.cls[P:], d.ctx_lens[P:], self.max_ctx_rows, mask=mask, workspace=self.workspace)
+        return self.out_chunks, self.out_rows
+
+    def accept(self, path, path_lens):
+        """Keeps the drafts path[i][0 .. path_lens[i]) of sequence P + i (int32 [S - P][most] and [S - P])."""
+        d, P = self.dev, self.P
+        bros.bros_tree_commit(self.pool, None, d.block_tables[P:], d.dir[P:], d.cls[P:], d.ctx_lens[P:], self.cu_rows, path, path_lens)
+        _advance(d.pos0[P:], d.ctx_lens[P:], self.drafts, path_lens, path.shape[1])
