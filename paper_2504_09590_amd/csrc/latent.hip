@@ -436,6 +436,8 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+constexpr int kNarrowKeys = 1024;   // contexts of narrow units of the expanded form, at most
+
 hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * a.num_q_heads;
   const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
@@ -447,7 +449,16 @@ hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   }
 }
 
+// Units of 128 rows over steps of 32 keys, cut into shares; where contexts are short and units few, whole units of 64
+// rows over steps of 64 keys, a workgroup each: half the steps one after another, and no merge. Us of a whole call, wide
+// and narrow: one prompt of 301 rows and 32 heads 44 and 30, of 1000 and 16 heads 50 and 42, of 500 and 64 heads 62 and 54;
+// four of 200 and 16 heads 37 and 28. With more units the wide ones read less: 700 rows behind 100 and 128 heads
+// 130 and 156; with longer contexts shares are even: 301 rows behind 700 and 16 heads 43 and 45, 150 behind 3000 89
+// and 84 (cut), with 32 heads.
 hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {
+  const int64_t units = (int64_t)a.num_seqs * a.num_kv_heads * ((a.max_q_len + 63) / 64);
+  if (16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq) <= kNarrowKeys && units <= 2 * (int64_t)stream_compute_units(stream))
+    return ra::launch_rows<ra::Expanded, 2, 2, 3, 1>(a, 4, kNarrowKeys / 64, workspace, stream);
   return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, workspace, stream);
 }
 

@@ -498,8 +498,8 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       ask(step + 1);
       holes = (holes & ~(1u << (step & 31))) | ((b0 < 0 || b1 < 0 ? 1u : 0u) << (step & 31));
       uint8_t* dst = ring + (step % SLOTS) * S::kTile;
-      // (dense rows: of the tile, whose place is known)
-      const size_t row0 = P::kPaged || !fits ? 0 : (size_t)(at.row0 + (int64_t)step * S::KS + kKeys * kg);
+      // (dense rows: of the tile, whose place is known; of one behind the context, which nothing is made of, within the buffer)
+      const size_t row0 = P::kPaged || !fits ? 0 : (size_t)min(at.row0 + (int64_t)step * S::KS + kKeys * kg, a.dense_rows - kKeys);
 #pragma unroll
       for (int i = 0; i < kR / 4; ++i) {
         const int row = kR * cw + 4 * i;   // the first of four
@@ -589,7 +589,8 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     bool scaled = false;   // any exponent of the segment's is not 0
     if constexpr (P::kHalf) {
       int any = 0;
-      for (int i = lane; i < cnt * NKW && fits; i += kWave) any |= exps[first * NKW + i];
+      const int tiles = min(last * NKW, (ctx + kKeys - 1) / kKeys);
+      for (int i = first * NKW + lane; i < tiles; i += kWave) any |= exps[i];
       scaled = __builtin_amdgcn_ballot_w64(any != 0) != 0;
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
@@ -624,7 +625,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         m_prev = m_run;
         m_run = mx > m_run + kRescaleSlack ? mx : m_run;
         if constexpr (kScaled) {
-          const int e = __builtin_amdgcn_readfirstlane(exps[pos_of(step) / kKeys]);
+          const int e = pos_of(step) < ctx ? __builtin_amdgcn_readfirstlane(exps[pos_of(step) / kKeys]) : 0;
           const int most = step == first ? e : max(e_run, e);
           e_scale = step == first ? 1.0f : ldexpf(1.0f, max(e_run - most, -126));
           e_run = most;

@@ -102,13 +102,45 @@ def test_scale_and_scores_far_from_zero():
     check(got, *a.want(), "latent, scale")
 
 
+@pytest.mark.parametrize("c0", [[200, 0], [1200, 90]])
 @pytest.mark.parametrize("gain", [2.0 ** -40, 2.0 ** -9, 2.0 ** 12, 2.0 ** 60])
-def test_expanded_values_far_from_one(gain):
-    """The values' weights: all small or large. (The result grows with them, so the bounds do.)"""
-    torch = require_gpu()
-    c = Chunks([70, 33], [200, 0], 2, seed=31)
+def test_expanded_values_far_from_one(gain, c0):
+    """The values' weights: all small or large. (The result grows with them, so the bounds do.) Contexts of narrow
+    units of rows and of wide ones."""
+    require_gpu()
+    c = Chunks([70, 33], c0, 2, seed=31)
     c.w[:, 128:] = (c.w[:, 128:].float() * gain).bfloat16()
     c.check(f"latent prefill, values of {gain}")
+
+
+@pytest.mark.parametrize("n,c0,hq", [([301], [0], 3), ([20] * 90, [40] * 90, 6), ([64, 1, 65, 128, 129], [0, 900, 33, 64, 0], 2),
+                                     ([65, 64], [1000, 7], 2), ([100] * 3, [950] * 3, 2)])
+def test_expanded_units(n, c0, hq):
+    """Narrow units and wide ones, whole and cut; contexts that end inside a step, and in the last tile of the dense rows."""
+    torch = require_gpu()
+    c = Chunks(n, c0, hq, seed=len(n), directions="table")
+    got = c.check(f"latent prefill units {n[:5]} {c0[:5]}")
+    assert torch.equal(got, c.run())
+
+
+def test_expanded_sequences_without_context_behind_a_full_buffer():
+    """The dense rows end where the second sequence would begin, which has more rows than tokens: zeros."""
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    for n0, c0 in ((64, 0), (64, 1216)):
+        c = Chunks([n0, 5], [c0, 0], 2, seed=36)
+        announce(f"latent prefill, nothing behind a full buffer, {c0}")
+        tables, dirs, ctx, cu = c.b.cuda()
+        ctx[1] = 3
+        total = n0 + c0 - 62                      # dense rows for two sequences: rounded up, n0 + c0 of them
+        q, pool, w = c.q.cuda(), c.pool.cuda(), c.w.cuda()
+        out = torch.full((n0 + 5, 2, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        ws = torch.full((bros.bros_latent_prefill_workspace_size(2, total, 2),), 255, dtype=torch.uint8, device="cuda")
+        bros.bros_attn_latent_prefill(out, q, cu, n0, w, pool, tables, dirs, None, ctx, n0 + c0, total, workspace=ws)
+        torch.cuda.synchronize()
+        want, tol = c.want()
+        check(out[:n0], want[:n0], tol[:n0], "the first sequence")
+        assert (out[n0:] == 0).all()
 
 
 def test_expanded_rows_of_different_sizes():
