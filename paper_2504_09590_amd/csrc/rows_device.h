@@ -552,7 +552,8 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         if (later >= 2) wait_vmem<2 * S::kLoads>();
         else if (later == 1) wait_vmem<S::kLoads>();
         else wait_vmem<0>();
-        if (masked(step) && (NCW > 1 || pos_of(step) < ctx)) {
+        // (a wave alone on its tile passes over one without context, unless the loop takes every tile)
+        if (masked(step) && (NCW > 1 || kOverlap || pos_of(step) < ctx)) {
           const int pos0 = pos_of(step);
           const TileBlocks tb = blocks_of(pos0);
           uint8_t* vt = ring + (step % SLOTS) * S::kTile + S::kValAt;

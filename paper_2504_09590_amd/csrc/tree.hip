@@ -77,8 +77,15 @@ size_t rows_workspace_bytes(bool latent) {
 hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = (int64_t)a.max_q_len * (a.num_q_heads / a.num_kv_heads);
   const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
-  switch (pick_rows_way(kTreeWays, columns, (int64_t)a.num_seqs * a.num_kv_heads, keys, stream_compute_units(stream))) {
-    case 0: return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
+  const int64_t segments = (int64_t)a.num_seqs * a.num_kv_heads;
+  switch (pick_rows_way(kTreeWays, columns, segments, keys, stream_compute_units(stream))) {
+    case 0:
+      // Short contexts and no more units than compute units: a unit has one to itself, with a third step's rows in LDS.
+      // Us, so and two to a compute unit: one sequence of four rows on 300, 8 / 2 heads 12.6 and 13.8; 32 / 8 heads:
+      // four of 4 on 500 16.8 and 18.5, 32 of 6 19.6 and 27; but 64 of 4 on 300, 512 units, 26 and 20.4.
+      if (keys <= 8 * 64 && segments * ((columns + 31) / 32) <= stream_compute_units(stream))
+        return ra::launch_rows<ra::KvPool, 1, 2, 3, 1>(a, 4, 8, workspace, stream);
+      return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
     case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, workspace, stream);
     default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);
   }

@@ -124,5 +124,5 @@ def check(got, want, tol, what):
 
 # Shapes that take each way of running the attention of few rows on a card of 256 compute units (index of the way,
 # narrowest units first): drafts (n, c0, hq, hkv) over a K/V pool, rows (n, c0, hq) over a latent pool.
-WAYS_TREE = [(0, [20], [2000], 8, 2), (1, [16] * 8, [4000] * 8, 16, 4), (2, [30] * 16, [8000] * 16, 16, 4)]
+WAYS_TREE = [(0, [6] * 3, [480, 17, 300], 8, 2), (0, [2] * 150, [240] * 150, 8, 2), (0, [20], [2000], 8, 2), (1, [16] * 8, [4000] * 8, 16, 4), (2, [30] * 16, [8000] * 16, 16, 4)]
 WAYS_LATENT = [(0, [1] * 2, [600] * 2, 64), (1, [1] * 8, [5000] * 8, 64), (2, [2] * 40, [4000] * 40, 32), (3, [1] * 90, [4000] * 90, 128)]

@@ -26,7 +26,7 @@ def lose_blocks(b, seed):
 
 
 @pytest.mark.parametrize("bits", ["tree", None])
-@pytest.mark.parametrize("way", WAYS_TREE, ids=lambda w: f"way{w[0]}")
+@pytest.mark.parametrize("way", WAYS_TREE, ids=lambda w: f"way{w[0]}-{len(w[1])}")
 def test_drafts_take_every_way(way, bits):
     torch = require_gpu()
     w, n, c0, hq, hkv = way
@@ -37,7 +37,7 @@ def test_drafts_take_every_way(way, bits):
 
 
 @pytest.mark.parametrize("bits", ["tree", None])
-@pytest.mark.parametrize("way", WAYS_LATENT, ids=lambda w: f"way{w[0]}")
+@pytest.mark.parametrize("way", WAYS_LATENT, ids=lambda w: f"way{w[0]}-{len(w[1])}")
 def test_latent_rows_take_every_way(way, bits):
     torch = require_gpu()
     w, n, c0, hq = way
