@@ -44,19 +44,30 @@ __device__ __forceinline__ uint4 narrow8(const float (&x)[8]) {   // the one rou
   return make_uint4(pf::pack2_bf16(x[0], x[1]), pf::pack2_bf16(x[2], x[3]), pf::pack2_bf16(x[4], x[5]), pf::pack2_bf16(x[6], x[7]));
 }
 
-// Turns pairs 8 l .. + 7 of token t at logical position pos. (Positions outside the table: row 0; the caller drops them.)
-template <bool ADJ>
-__device__ __forceinline__ void turn(const LatentAppendArgs& a, int t, int pos, int l, float (&xa)[8], float (&xb)[8]) {
-  float c[8], s[8];
+// Cosines and sines of pairs 8 l .. + 7 of token t at logical position pos. (Positions outside the table: row 0; the
+// caller drops them.)
+__device__ __forceinline__ void angles(const LatentAppendArgs& a, int t, int pos, int l, float (&c)[8], float (&s)[8]) {
+  const auto row_of = [&](int32_t at) -> const float* { return a.rope_table + (size_t)(at < 0 || at >= a.table_rows ? 0 : at) * kRot + 8 * l; };
+  if (a.rope_pos == nullptr || a.axes == 1) {   // one row of the table
+    const float4* row = reinterpret_cast<const float4*>(row_of(a.rope_pos == nullptr ? pos : a.rope_pos[t]));
+    const float4 x[4] = {row[0], row[1], row[kRot / 8], row[kRot / 8 + 1]};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c[4 * i] = x[i].x, c[4 * i + 1] = x[i].y, c[4 * i + 2] = x[i].z, c[4 * i + 3] = x[i].w;
+      s[4 * i] = x[2 + i].x, s[4 * i + 1] = x[2 + i].y, s[4 * i + 2] = x[2 + i].z, s[4 * i + 3] = x[2 + i].w;
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int pair = 8 * l + i;
-    int row = pos;
-    if (a.rope_pos != nullptr) row = a.rope_pos[(size_t)axis_of(a, pair) * a.num_new_tokens + t];
-    row = row < 0 || row >= a.table_rows ? 0 : row;
-    c[i] = a.rope_table[(size_t)row * kRot + pair];
-    s[i] = a.rope_table[(size_t)row * kRot + kRot / 2 + pair];
+    const float* row = row_of(a.rope_pos[(size_t)axis_of(a, 8 * l + i) * a.num_new_tokens + t]);
+    c[i] = row[i];
+    s[i] = row[kRot / 2 + i];
   }
+}
+// Turns those pairs.
+template <bool ADJ>
+__device__ __forceinline__ void turn(const float (&c)[8], const float (&s)[8], float (&xa)[8], float (&xb)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float& u = ADJ ? (i < 4 ? xa[2 * (i & 3)] : xb[2 * (i & 3)]) : xa[i];
@@ -66,46 +77,64 @@ __device__ __forceinline__ void turn(const LatentAppendArgs& a, int t, int pos, 
     v = fmaf(v0, c[i], u0 * s[i]);
   }
 }
+// Whether token t's position lies outside the table.
+__device__ __forceinline__ bool outside(const LatentAppendArgs& a, int t, int pos) {
+  if (a.rope_table == nullptr) return false;
+  if (a.rope_pos == nullptr) return pos < 0 || pos >= a.table_rows;
+  bool off = false;
+  for (int x = 0; x < a.axes; ++x) {
+    const int r = a.rope_pos[(size_t)x * a.num_new_tokens + t];
+    off |= r < 0 || r >= a.table_rows;
+  }
+  return off;
+}
 
-// ADJ: pairs (2 i, 2 i + 1) instead of (i, i + 32).
-template <bool ADJ>
+// ADJ: pairs (2 i, 2 i + 1) instead of (i, i + 32). EACH: query rows of a thread; those of one token share its angles.
+template <bool ADJ, int EACH>
 __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArgs a, int kv_groups) {
-  __shared__ int s_seq[kHeads], s_pos[kHeads];
+  constexpr int kItems = kHeads * EACH;
+  __shared__ int s_seq[kItems], s_pos[kItems];
   const int tid = threadIdx.x;
   const bool kv = (int)blockIdx.x < kv_groups;
   // the workgroup's tokens t0 .. t0 + n_tok - 1
-  int64_t item0 = 0;
-  int t0, n_tok;
+  int t0, n_tok, h0 = 0;
   if (kv) {
     t0 = blockIdx.x * kTokens;
     n_tok = min(kTokens, a.num_new_tokens - t0);
   } else {
-    item0 = (int64_t)(blockIdx.x - kv_groups) * kHeads;
+    const int64_t item0 = (int64_t)(blockIdx.x - kv_groups) * kItems;
     t0 = (int)(item0 / a.num_q_heads);
-    n_tok = min((int)((item0 + kHeads - 1) / a.num_q_heads) - t0 + 1, a.num_new_tokens - t0);
+    h0 = (int)(item0 - (int64_t)t0 * a.num_q_heads);
+    n_tok = min((h0 + kItems - 1) / a.num_q_heads + 1, a.num_new_tokens - t0);
   }
-  // this thread's row, requested before its position is known
-  const int lane = tid & (kWave - 1), l4 = tid & 3;
-  const int64_t item = item0 + tid / 4;
-  const int t = kv ? t0 + tid / kWave : (int)min(item / a.num_q_heads, (int64_t)a.num_new_tokens - 1);
-  const int h = kv ? 0 : (int)(item % a.num_q_heads);
-  const bool live = kv ? t < a.num_new_tokens : item < (int64_t)a.num_new_tokens * a.num_q_heads;
-  uint4 w0{}, w1{}, w2{};
-  if (live) {
-    if (kv) {
-      const uint4* row = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.kv) + (size_t)t * a.kv_stride);
-      w0 = row[lane];
-      if (lane < 4) {
-        w1 = row[kLatent / 8 + chunk_a(ADJ, lane)];
-        w2 = row[kLatent / 8 + chunk_b(ADJ, lane)];
-      }
-    } else {
-      const uint4* row = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (size_t)t * a.q_stride + (size_t)h * a.q_head_stride);
-      w1 = row[chunk_a(ADJ, l4)];
-      w2 = row[chunk_b(ADJ, l4)];
+  // this thread's rows, requested before their positions are known
+  const int lane = tid & (kWave - 1), l = kv ? lane & 3 : tid & 3;
+  const int t = t0 + tid / kWave;                // of a latent row
+  int tq[EACH], hq[EACH];                        // of query rows (tq: behind t0)
+  bool live[EACH];
+  uint4 w0{}, w1[EACH] = {}, w2[EACH] = {};
+  if (kv) {
+    live[0] = t < a.num_new_tokens;
+    tq[0] = t - t0;
+    const uint4* row = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.kv) + (size_t)min(t, a.num_new_tokens - 1) * a.kv_stride);
+    w0 = row[lane];
+    w1[0] = row[kLatent / 8 + chunk_a(ADJ, l)];
+    w2[0] = row[kLatent / 8 + chunk_b(ADJ, l)];
+  } else {
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) {
+      const int item = h0 + kHeads * r + tid / 4;
+      tq[r] = item / a.num_q_heads;
+      hq[r] = item - tq[r] * a.num_q_heads;
+      live[r] = tq[r] < n_tok;
+      const uint4* row = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (size_t)(t0 + min(tq[r], n_tok - 1)) * a.q_stride +
+                                                        (size_t)hq[r] * a.q_head_stride);
+      w1[r] = row[chunk_a(ADJ, l)];
+      w2[r] = row[chunk_b(ADJ, l)];
     }
   }
-  if (tid < kHeads) s_seq[tid] = -1;
+#pragma unroll
+  for (int r = 0; r < EACH; ++r) s_seq[kHeads * r + (tid & (kHeads - 1))] = -1;
   __syncthreads();
   for (int j = tid; j < a.num_seqs; j += kThreads) {
     const int lo = a.cu_new[j], hi = a.cu_new[j + 1], p0 = a.pos0[j];
@@ -116,31 +145,36 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
     }
   }
   __syncthreads();
-  if (!live) return;
-  const int seq = s_seq[t - t0];
-  if (seq < 0) return;   // in no sequence: left as it was
-  const int pos = s_pos[t - t0];
-  bool off = false;      // a position outside the table
-  if (a.rope_table != nullptr) {
-    if (a.rope_pos == nullptr) off = pos < 0 || pos >= a.table_rows;
-    else {
-      for (int x = 0; x < a.axes; ++x) {
-        const int r = a.rope_pos[(size_t)x * a.num_new_tokens + t];
-        off |= r < 0 || r >= a.table_rows;
-      }
-    }
-  }
-  float xa[8], xb[8];
+  float xa[8], xb[8], c[8], s[8];
   if (!kv) {
-    widen8(w1, xa);
-    widen8(w2, xb);
-    if (a.rope_table != nullptr) turn<ADJ>(a, t, pos, l4, xa, xb);
-    uint4* row = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.q_out) + (size_t)t * a.out_stride + (size_t)h * a.out_head_stride);
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    row[chunk_a(ADJ, l4)] = off ? zero : a.rope_table != nullptr ? narrow8(xa) : w1;
-    row[chunk_b(ADJ, l4)] = off ? zero : a.rope_table != nullptr ? narrow8(xb) : w2;
+    int last = -1;
+    bool off = false;
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) {
+      if (!live[r] || s_seq[tq[r]] < 0) continue;   // (in no sequence: left as it was)
+      const int tr = t0 + tq[r];
+      if (tq[r] != last) {
+        off = outside(a, tr, s_pos[tq[r]]);
+        if (a.rope_table != nullptr) angles(a, tr, s_pos[tq[r]], l, c, s);
+        last = tq[r];
+      }
+      if (a.rope_table != nullptr) {
+        widen8(w1[r], xa);
+        widen8(w2[r], xb);
+        turn<ADJ>(c, s, xa, xb);
+        w1[r] = off ? make_uint4(0, 0, 0, 0) : narrow8(xa);
+        w2[r] = off ? make_uint4(0, 0, 0, 0) : narrow8(xb);
+      }
+      uint4* row = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.q_out) + (size_t)tr * a.out_stride + (size_t)hq[r] * a.out_head_stride);
+      row[chunk_a(ADJ, l)] = w1[r];
+      row[chunk_b(ADJ, l)] = w2[r];
+    }
     return;
   }
+  const int seq = live[0] ? s_seq[t - t0] : -1;
+  if (seq < 0) return;   // (uniform in a wave)
+  const int pos = s_pos[t - t0];
+  const bool off = outside(a, t, pos);
   // the latent's norm: every lane of the wave takes part
   if (a.norm != nullptr) {
     float x[8], g[8];
@@ -164,14 +198,15 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
   row[lane] = w0;
   if (lane < 4) {
     if (a.rope_table != nullptr) {
-      widen8(w1, xa);
-      widen8(w2, xb);
-      turn<ADJ>(a, t, pos, lane, xa, xb);
-      w1 = narrow8(xa);
-      w2 = narrow8(xb);
+      angles(a, t, pos, lane, c, s);
+      widen8(w1[0], xa);
+      widen8(w2[0], xb);
+      turn<ADJ>(c, s, xa, xb);
+      w1[0] = narrow8(xa);
+      w2[0] = narrow8(xb);
     }
-    row[kLatent / 8 + chunk_a(ADJ, lane)] = w1;
-    row[kLatent / 8 + chunk_b(ADJ, lane)] = w2;
+    row[kLatent / 8 + chunk_a(ADJ, lane)] = w1[0];
+    row[kLatent / 8 + chunk_b(ADJ, lane)] = w2[0];
   }
 }
 
@@ -406,14 +441,24 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
 
 }  // namespace
 
-hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream) {
+template <int EACH>
+static hipError_t append_rows(const LatentAppendArgs& a, hipStream_t stream) {
   const int64_t kv = ((int64_t)a.num_new_tokens + kTokens - 1) / kTokens;
-  const int64_t q = ((int64_t)a.num_new_tokens * a.num_q_heads + kHeads - 1) / kHeads;
+  const int64_t q = ((int64_t)a.num_new_tokens * a.num_q_heads + kHeads * EACH - 1) / (kHeads * EACH);
   if ((kv + q) * kThreads > 0xffffffffLL) return hipErrorInvalidValue;
   if (kv + q == 0) return hipSuccess;
-  if (a.adjacent) hipLaunchKernelGGL(latent_append_kernel<true>, dim3((unsigned)(kv + q)), dim3(kThreads), 0, stream, a, (int)kv);
-  else hipLaunchKernelGGL(latent_append_kernel<false>, dim3((unsigned)(kv + q)), dim3(kThreads), 0, stream, a, (int)kv);
+  if (a.adjacent) hipLaunchKernelGGL((latent_append_kernel<true, EACH>), dim3((unsigned)(kv + q)), dim3(kThreads), 0, stream, a, (int)kv);
+  else hipLaunchKernelGGL((latent_append_kernel<false, EACH>), dim3((unsigned)(kv + q)), dim3(kThreads), 0, stream, a, (int)kv);
   return hipGetLastError();
+}
+
+hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream) {
+  // Query rows of a thread: more from two workgroups a compute unit on (fewer workgroups each look their tokens up), four
+  // where heads enough share a token's angles. Us with 1, 2 and 4: 32 tokens of 128 heads 3.8, 4.2, 5.2; 256 5.4, 4.9, 5.8;
+  // 1024 15.3, 10.6, 10.0; 4000 of 16 heads 12.3, 12.0, 13.0; 8000 21.1, 19.1, 20.0; 6000 of 128 86, 65, 63 (with 8: 66).
+  const int64_t rows = (int64_t)a.num_new_tokens * a.num_q_heads, wide = 2 * kHeads * (int64_t)stream_compute_units(stream);
+  if (rows >= 2 * wide && a.num_q_heads >= 64) return append_rows<4>(a, stream);
+  return rows >= wide ? append_rows<2>(a, stream) : append_rows<1>(a, stream);
 }
 
 hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {

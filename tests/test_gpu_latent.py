@@ -325,11 +325,22 @@ def turned(x, cos, sin, adjacent):
 @pytest.mark.parametrize("hq", [1, 6, 128])
 @pytest.mark.parametrize("place", ["absorbed", "itself"])
 def test_append(hq, axes, adjacent, place):
+    append_case(hq, axes, adjacent, place, [1, 7, 0, 40, 1])
+
+
+@pytest.mark.parametrize("hq,n", [(1, 33000), (16, 2100), (48, 1500), (128, 700)])
+@pytest.mark.parametrize("axes", [1, 3])
+def test_append_of_many_rows(hq, n, axes):
+    """Threads of several query rows, of one token and of several."""
+    append_case(hq, axes, False, "itself", [1, n, 0, 40, 1])
+
+
+def append_case(hq, axes, adjacent, place, n):
     """Values are rounded once (2^-8 of each, and 32-bit arithmetic before it); slots that get nothing keep their bits."""
     torch = require_gpu()
     from paper_2504_09590_amd import bros
     rng = np.random.default_rng(hq + axes)
-    b = Rows([1, 7, 0, 40, 1], [0, 30, 5, 3, 100], hq, "table" if axes else "sequence")
+    b = Rows(n, [0, 30, 5, 3, 100], hq, "table" if axes else "sequence")
     tn, pad = b.rows, 3                       # rows of padding behind the last sequence
     kv_all = bf16(rng, (tn + pad, 704))
     kv = kv_all.cuda()[:, 104:680] if axes != 1 else kv_all.cuda()[:, 104:680].contiguous()
@@ -351,7 +362,7 @@ def test_append(hq, axes, adjacent, place):
         q_out = buf[:, :, LATENT:]
     else:
         q_out = q[:, :, 128:]
-    announce(f"latent append {hq} {axes} {adjacent} {place}")
+    announce(f"latent append {hq} {axes} {adjacent} {place} {n}")
     tables, dirs, _, cu = b.cuda()
     bros.bros_latent_append(q_out, q[:, :, 128:], kv, pool, tables, dirs, None, torch.from_numpy(b.c0.astype(np.int32)).cuda(), cu,
                             rope=rope, rope_pos=given, norm=None if norm is None else norm.cuda(), eps=1e-5)
