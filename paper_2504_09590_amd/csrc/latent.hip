@@ -236,7 +236,7 @@ __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {   // round t
 // 16 bytes from each lane's own address to LDS at dst + 16 * lane.
 __device__ __forceinline__ void load_rows_to_lds(const uint8_t* lane_src, const uint8_t* dst) {
   const uint32_t m0 = (uint32_t)(uintptr_t)dst;
-  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(lane_src), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(lane_src), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 
 __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(ExpandArgs a, int items_each) {
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r8 = 32 * wave + 8 * i;
-      pf::load_to_lds(wsrc, woff[i], dst + r8 * 128);
+      ra::load_to_lds(wsrc, woff[i], dst + r8 * 128);
       load_rows_to_lds(csrc[i] + (k % kPerItem) * (kStageDims * 2), dst + kHalfTile + r8 * 128);
     }
   };

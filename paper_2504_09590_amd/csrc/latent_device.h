@@ -6,9 +6,11 @@
 // wave, two to a SIMD, and no wave needs another's scores. Up to 128 columns are eight such waves; with
 // fewer columns HV waves share a column group, each computing all its scores and a part of
 // the value dims. The price is LDS: every operand of 1 KiB serves 16 columns, 544 KiB a step and
-// compute unit with 128 columns, 4250 cycles at 128 bytes, twice the products' 2176. (32 columns to a wave
-// and the dims in two halves, whose score sums waves exchange in LDS, read 336 KiB, but two barriers and
-// the exchange a step cost more: 96 contexts up to 16384 with 128 heads 370 us.)
+// compute unit with 128 columns, twice what the products take. Tried instead, and slower over 96 contexts up to 16384
+// with 128 heads (302 us): 32 columns to a wave and the dims in two halves whose score sums waves exchange, 336 KiB but two
+// barriers a step, 370; four waves of 32 columns and 512 registers, one block of the step's keys each, that exchange
+// weights, 136 KiB for 64 columns, 387, and two such workgroups on the same keys 350: LDS no longer binds, but nothing runs
+// beside one wave's softmax and barrier.
 //
 // Rows are requested three steps ahead; each wave waits for those it requested itself, and puts in
 // order what it finds there (rows that are no context, values that are not finite),
