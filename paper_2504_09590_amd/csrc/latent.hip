@@ -504,7 +504,11 @@ hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t units = (int64_t)a.num_seqs * a.num_kv_heads * ((a.max_q_len + 63) / 64);
   if (16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq) <= kNarrowKeys && units <= 2 * (int64_t)stream_compute_units(stream))
     return ra::launch_rows<ra::Expanded, 2, 2, 3, 1>(a, 4, kNarrowKeys / 64, workspace, stream);
-  return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, workspace, stream);
+  switch (rows_team(((int64_t)a.max_q_len + 127) / 128, a.num_q_tokens, a.max_q_len, a.num_seqs)) {
+    case 4: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 4>(a, 4, 8, workspace, stream);
+    case 2: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 2>(a, 4, 8, workspace, stream);
+    default: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, workspace, stream);
+  }
 }
 
 }  // namespace bros

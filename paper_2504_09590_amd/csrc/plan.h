@@ -326,4 +326,16 @@ inline int pick_rows_way(const RowsWay (&ways)[N], int64_t columns, int64_t segm
   return best;
 }
 
+// Workgroups side by side (a team) for units that share their keys: `tiles` units of the longest sequence. The second
+// and later ones find the keys in their die's L2, but a team whose last units are missing leaves them idle.
+// Us by one, two and four to a team, 128 columns to a unit. Drafts over a K/V pool: six trees of 64 with 64 / 8 heads on
+// 8000 to 32000 tokens (four units) 338, 284, 268; 16 of 40 to 64 with 32 / 8 on up to 8000 (two) 148, 125, 186; 32 of 20 to
+// 64 with 64 / 8 on up to 3000 163, 163, 196; four of 33 to 48 (three) 76, 82, 82. Expanded chunks: one of 2000 rows and
+// 32 heads 134, 126, 122; four of 601 to 1400 behind up to 6000, 64 heads, 1387, 1291, 1337; eight of 256 564, 557, 657.
+inline int rows_team(int64_t tiles, int64_t rows, int64_t max_rows, int64_t num_seqs) {
+  const double filled = (double)rows / ((double)max_rows * (double)num_seqs);
+  if (tiles % 4 == 0 && filled >= 0.9) return 4;
+  return (tiles % 2 == 0 && filled >= 0.75) || tiles >= 5 ? 2 : 1;
+}
+
 }  // namespace bros

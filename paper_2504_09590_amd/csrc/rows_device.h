@@ -22,6 +22,10 @@
 // sums (fp32, with their maximum and total) that a merge folds. Where no unit is long,
 // whole units are shared out instead, and nothing is merged.
 //
+// Teams. Where a sequence has several tiles of columns, TEAM workgroups of a die take them side by side, step by step: the
+// shares are those of teams, and the keys come from memory once (drafts of four tiles read 1.6 GB where the pool's rows
+// are 0.44, at the rate that binds).
+//
 // Masks. A row sees the keys before the drafts, and of those the ones its bits name (or the
 // causal ones). Only steps that reach the drafts, the context's end or an invalid table
 // entry look at masks: a row's 32 bits of the tile's positions. In such tiles a value that is
@@ -407,7 +411,7 @@ struct Shape {
   static_assert((NKW - 1) * NCW * 32 * kDims * 4 <= kRing, "the key groups' sums meet in the ring");
 };
 
-template <class P, int NCW, int NKW, int SLOTS, int OCC>
+template <class P, int NCW, int NKW, int SLOTS, int OCC, int TEAM>
 __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   using S = Shape<P, NCW, NKW, SLOTS>;
   constexpr int kDt = S::kDt, kMainSteps = P::kMain / 32, kQSteps = S::kQDims / 16, kR = S::kRows;
@@ -428,18 +432,19 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   // neighbouring shares to one die
   const int nb = gridDim.x;
   const int me = nb % pf::kXcds == 0 ? (blockIdx.x % pf::kXcds) * (nb / pf::kXcds) + blockIdx.x / pf::kXcds : blockIdx.x;
+  const int team = me / TEAM, member = me % TEAM;
   Cut* cut = reinterpret_cast<Cut*>(a.ws_cut) + me;
   if (tid == 0) cut->last = -1;
 
-  Place at = find_place<P, S::CT, S::KS, S::kThreads>(
+  Place at = find_place<P, S::CT * TEAM, S::KS, S::kThreads>(
       a, G, [&](int64_t total) -> int64_t {
         const Shares sh(a, total);
-        return me < sh.n ? sh.begin(me) : -1;
+        return team < sh.n ? sh.begin(team) : -1;
       }, s_scan, &s_place);
   if (at.s < 0) return;   // (uniform: no step left for this workgroup)
   const Shares shares(a, at.total);
-  int64_t x = shares.begin(me);
-  const int64_t x_end = shares.begin(me + 1);
+  int64_t x = shares.begin(team);
+  const int64_t x_end = shares.begin(team + 1);
 
   const float sl2 = a.scale_log2;
   const bf16x2_t one2 = {(__bf16)1.0f, (__bf16)1.0f};
@@ -457,15 +462,18 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   const uint32_t ring0 = lds_address(ring);
 
   while (x < x_end) {
-    // ---- The segment: steps [first, last) of unit (s, g, t).
-    const int s = at.s, g = at.g, t = at.t;
+    // ---- The segment: steps [first, last) of unit (s, g, t), of those of the team's units side by side [first, first + taken).
+    const int s = at.s, g = at.g, t = at.t * TEAM + member;
     const Seq q = seq_of(a, s);
-    const Steps<P, S::CT, S::KS> st(a, q, G);
-    const int usteps = __builtin_amdgcn_readfirstlane(st.of(t));
+    const Steps<P, S::CT * TEAM, S::KS> st(a, q, G);
+    const Steps<P, S::CT, S::KS> own(a, q, G);
+    const int tsteps = __builtin_amdgcn_readfirstlane(st.of(at.t));
     const int first = st.whole ? 0 : at.step;
-    const int cnt = st.whole ? usteps : (int)min((int64_t)(usteps - first), x_end - x);
-    const int last = first + cnt;
+    const int taken = st.whole ? tsteps : (int)min((int64_t)(tsteps - first), x_end - x);
+    const int usteps = TEAM == 1 ? tsteps : t < own.tiles ? __builtin_amdgcn_readfirstlane(own.of(t)) : 0;
+    const int last = min(first + taken, usteps), cnt = last - first;
     const bool whole = cnt == usteps;
+    if (TEAM == 1 || cnt > 0) {   // (a team's last units may not be there, and causal ones end one before the other)
     // (dense keys that do not fit their buffer: the sequence's rows see nothing)
     const bool fits = P::kPaged || at.row0 + dense_rows(q.ctx) <= a.dense_rows;
     const int ctx = fits ? q.ctx : 0, n = q.n;
@@ -868,7 +876,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           ml[0] = m_run;
           ml[1] = l;
         }
-        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x + usteps - 1)};
+        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x + usteps - 1) * TEAM + member};
       }
     }
     // ---- Values that were left out and are seen: added to the rows that see them, where
@@ -930,8 +938,10 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
       }
     }
 
+    }
+
     // ---- The next unit.
-    x += st.whole ? 1 : cnt;
+    x += st.whole ? 1 : taken;
     at.step = 0;
     if (x < x_end) {
       if (++at.t >= st.tiles) {
@@ -951,7 +961,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 // Folds the partials of the units cut between shares: workgroup (w, y) the chunks kWaves kEach y .. of the unit
 // that share w noted. A chunk is 1 KiB of a partial: a wave's columns, four dims to a lane.
 constexpr int kMergeWaves = 4, kMergeEach = 2;   // waves of a workgroup, chunks of a wave
-template <class S, bool DENSE>
+template <class S, bool DENSE, int TEAM>
 __global__ __launch_bounds__(kMergeWaves * kWave) void rows_merge_kernel(RowsArgs a) {
   constexpr int kGroups = S::CT / S::kLaneCols;            // column waves of a partial
   constexpr int kParts = S::kChunks / kMergeEach;          // waves to one of them
@@ -962,8 +972,8 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void rows_merge_kernel(RowsArg
   const int item = blockIdx.y * kMergeWaves + wave_id_uniform();
   const int cw = item / kParts, i0 = (item % kParts) * kMergeEach;
   const int col = S::kLaneCols * cw + lane % S::kLaneCols;
-  const int pieces = cut.last - w0 + 1;
-  const auto slot = [&](int p) -> size_t { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };
+  const int pieces = (cut.last - w0) / TEAM + 1;
+  const auto slot = [&](int p) -> size_t { return 2 * (size_t)(w0 + p * TEAM) + (p == 0 ? 1 : 0); };
   const auto ml = [&](int p) -> float2 { return reinterpret_cast<const float2*>(a.ws_ml)[slot(p) * S::CT + col]; };
 
   float m = kNoMax;

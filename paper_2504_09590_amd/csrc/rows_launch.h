@@ -18,29 +18,30 @@ constexpr size_t partial_bytes(size_t workers, size_t ct, size_t dims) {
 
 // Launches `kernel` on per_cu workgroups a compute unit, and the merge. min_steps: the least steps of a share.
 // whole: steps of the longest unit up to which units are not cut.
-template <class S, bool DENSE, class Kernel>
+template <class S, bool DENSE, int TEAM = 1, class Kernel>
 hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, int whole, void* workspace, hipStream_t stream) {
-  a.workers = std::min(stream_compute_units(stream), kMaxCus) * per_cu;
+  a.workers = std::max(1, std::min(stream_compute_units(stream), kMaxCus) * per_cu / TEAM);
+  const int groups = a.workers * TEAM;
   a.min_steps = min_steps;
   a.whole_units = ((int64_t)std::min<int64_t>(a.max_ctx, (int64_t)a.max_blocks_per_seq * kBlockSize) + S::KS - 1) / S::KS <= whole;
   if (a.whole_units) a.min_steps = 1;
   a.ws_cut = workspace;
-  a.ws_o = reinterpret_cast<float*>(static_cast<Cut*>(workspace) + a.workers);
-  a.ws_ml = a.ws_o + 2 * (size_t)a.workers * S::kSlotFloats;
-  hipLaunchKernelGGL(kernel, dim3(a.workers), dim3(S::kThreads), 0, stream, a);
+  a.ws_o = reinterpret_cast<float*>(static_cast<Cut*>(workspace) + groups);
+  a.ws_ml = a.ws_o + 2 * (size_t)groups * S::kSlotFloats;
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(S::kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.whole_units) return e;
   constexpr int kItems = S::CT / S::kLaneCols * S::kChunks / kMergeEach;
-  hipLaunchKernelGGL((rows_merge_kernel<S, DENSE>), dim3(std::max(1, a.workers - 1), kItems / kMergeWaves), dim3(kMergeWaves * kWave), 0,
+  hipLaunchKernelGGL((rows_merge_kernel<S, DENSE, TEAM>), dim3(std::max(1, groups - 1), kItems / kMergeWaves), dim3(kMergeWaves * kWave), 0,
                      stream, a);
   return hipGetLastError();
 }
 
-template <class P, int NCW, int NKW, int SLOTS, int PER_CU>
+template <class P, int NCW, int NKW, int SLOTS, int PER_CU, int TEAM = 1>
 hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, void* workspace, hipStream_t stream) {
   using S = Shape<P, NCW, NKW, SLOTS>;
   constexpr int kEachEu = std::max(1, S::kWaves * PER_CU / 4);
-  return launch_shares<S, !P::kPaged>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu>, a, PER_CU, min_steps, whole, workspace, stream);
+  return launch_shares<S, !P::kPaged, TEAM>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu, TEAM>, a, PER_CU, min_steps, whole, workspace, stream);
 }
 
 template <int NCW, int HV>

@@ -87,7 +87,12 @@ hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
         return ra::launch_rows<ra::KvPool, 1, 2, 3, 1>(a, 4, 8, workspace, stream);
       return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
     case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, workspace, stream);
-    default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);
+    default:
+      switch (rows_team((columns + 127) / 128, a.num_q_tokens, a.max_q_len, a.num_seqs)) {
+        case 4: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 4>(a, 4, 12, workspace, stream);
+        case 2: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 2>(a, 4, 12, workspace, stream);
+        default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);
+      }
   }
 }
 

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests.gpu_helpers import announce, require_gpu
-from tests.rows_helpers import WAYS_LATENT, WAYS_TREE, bf16, check
+from tests.rows_helpers import TEAMS_CHUNKS, TEAMS_TREE, WAYS_LATENT, WAYS_TREE, bf16, check
 from tests.test_gpu_latent import LATENT, ROW, Absorbed, Chunks
 from tests.test_gpu_tree import D, Case
 
@@ -44,6 +44,28 @@ def test_latent_rows_take_every_way(way, bits):
     c = Absorbed(n, c0, hq, bits, seed=50 + w, directions="table")
     lose_blocks(c.b, w)
     got = c.check(f"latent way {w} {bits}")
+    assert torch.equal(got, c.run())
+
+
+@pytest.mark.parametrize("bits", ["tree", None])
+@pytest.mark.parametrize("case", TEAMS_TREE, ids=lambda c: f"team{c[0]}-{len(c[1])}")
+def test_drafts_in_teams(case, bits):
+    """Units that share their keys side by side: all there, the last missing, sequences without rows; cut and whole."""
+    torch = require_gpu()
+    team, n, c0, hq, hkv = case
+    c = Case(n, c0, hq, hkv, bits, seed=60 + team, directions="table")
+    lose_blocks(c.b, team)
+    got = c.check(f"tree teams of {team} {n[:4]} {bits}")
+    assert torch.equal(got, c.run())
+
+
+@pytest.mark.parametrize("case", TEAMS_CHUNKS, ids=lambda c: f"team{c[0]}-{c[1][0]}")
+def test_chunks_in_teams(case):
+    """Likewise for chunks, of which one unit ends some steps before its neighbour."""
+    torch = require_gpu()
+    team, n, c0, hq = case
+    c = Chunks(n, c0, hq, seed=70 + team)
+    got = c.check(f"latent prefill teams of {team} {n} {c0}")
     assert torch.equal(got, c.run())
 
 

@@ -10,7 +10,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.rows_helpers import WAYS_LATENT, WAYS_TREE
+from tests.rows_helpers import TEAMS_CHUNKS, TEAMS_TREE, WAYS_LATENT, WAYS_TREE
 
 bros = pytest.importorskip("paper_2504_09590_amd.bros", reason="libbros_attn.so not built")
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -145,22 +145,34 @@ def ways(tmp_path_factory):
 extern "C" int way(int latent, long long columns, long long segments, long long keys, int cus) {
   return latent ? bros::pick_rows_way(bros::kLatentWays, columns, segments, keys, cus) : bros::pick_rows_way(bros::kTreeWays, columns, segments, keys, cus);
 }
+extern "C" int team(long long tiles, long long rows, long long max_rows, long long seqs) { return bros::rows_team(tiles, rows, max_rows, seqs); }
 """)
     subprocess.run([gxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-ftrapv", "-shared", "-fPIC", "-I", CSRC, str(d / "ways.cpp"),
                     "-o", str(d / "ways.so")], check=True)
     lib = ctypes.CDLL(str(d / "ways.so"))
     L = ctypes.c_longlong
     lib.way.argtypes = [ctypes.c_int, L, L, L, ctypes.c_int]
-    return lib.way
+    lib.team.argtypes = [L, L, L, L]
+    return lib
 
 
 def test_the_gpu_tests_shapes_take_every_way(ways):
     """Card of 256 compute units; a context counts by its last block."""
     blocks = lambda c0, n: 16 * max((c + m + 15) // 16 for c, m in zip(c0, n))  # noqa: E731
-    got = [ways(0, max(n) * hq // hkv, len(n) * hkv, blocks(c0, n), 256) for _, n, c0, hq, hkv in WAYS_TREE]
+    got = [ways.way(0, max(n) * hq // hkv, len(n) * hkv, blocks(c0, n), 256) for _, n, c0, hq, hkv in WAYS_TREE]
     assert got == [w for w, *_ in WAYS_TREE] and set(got) == {0, 1, 2}
-    got = [ways(1, max(n) * hq, len(n), blocks(c0, n), 256) for _, n, c0, hq in WAYS_LATENT]
+    got = [ways.way(1, max(n) * hq, len(n), blocks(c0, n), 256) for _, n, c0, hq in WAYS_LATENT]
     assert got == [w for w, *_ in WAYS_LATENT] and set(got) == {0, 1, 2, 3}
+
+
+def test_the_gpu_tests_shapes_take_every_team(ways):
+    blocks = lambda c0, n: 16 * max((c + m + 15) // 16 for c, m in zip(c0, n))  # noqa: E731
+    for team, n, c0, hq, hkv in TEAMS_TREE:
+        columns = max(n) * hq // hkv
+        assert ways.way(0, columns, len(n) * hkv, blocks(c0, n), 256) == 2 and ways.team(-(-columns // 128), sum(n), max(n), len(n)) == team
+    for team, n, c0, hq in TEAMS_CHUNKS:
+        assert max(a + b for a, b in zip(n, c0)) > 1024 and ways.team(-(-max(n) // 128), sum(n), max(n), len(n)) == team
+    assert ways.team(1, 5, 5, 1) == 1 and ways.team(3, 300, 300, 1) == 1 and ways.team(2, 300, 256, 2) == 1
 
 
 def test_ways_hold_for_any_sizes(ways):
@@ -168,10 +180,10 @@ def test_ways_hold_for_any_sizes(ways):
     for latent, widths in ((0, (32, 64, 128)), (1, (16, 32, 64, 128))):
         for _ in range(2000):
             columns, segments, keys = (int(2 ** rng.uniform(0, 31)) for _ in range(3))
-            w = ways(latent, columns, segments, keys, int(rng.integers(1, 257)))
+            w = ways.way(latent, columns, segments, keys, int(rng.integers(1, 257)))
             assert 0 <= w < len(widths) and (w == 0 or widths[w - 1] < columns)
-        assert ways(latent, 1, 1, 0, 256) == 0
-        big = ways(latent, 2 ** 30, 2 ** 31 - 1, 2 ** 31 - 1, 1)
+        assert ways.way(latent, 1, 1, 0, 256) == 0
+        big = ways.way(latent, 2 ** 30, 2 ** 31 - 1, 2 ** 31 - 1, 1)
         assert widths[big] == 128
 
 
