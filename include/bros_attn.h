@@ -508,8 +508,8 @@ int bros_kv_read_q8(const void* k_pool, const void* v_pool, const uint8_t* kv_sc
  *   workspace  : bros_attn_workspace_size(BROS_WS_TREE, BROS_BF16, ...) bytes, 16-byte aligned,
  *                required; contents undefined after the call. Two calls that share it
  *                must not overlap in time (two captured graphs neither).
- * bf16 only (BROS_E_UNSUPPORTED otherwise). Softmax weights are rounded to bf16 before the
- * value product, as in the prefill; sums and statistics are fp32. Keys and values that are
+ * bf16 only, head groups of 1, 2, 4 or 8, at most 1024 query heads (BROS_E_UNSUPPORTED otherwise).
+ * Softmax weights are rounded to bf16 before the value product, as in the prefill; sums and statistics are fp32. Keys and values that are
  * not finite reach the rows that see them and no others. Rows behind cu_q[num_seqs], and those of a
  * sequence whose range is not within num_q_tokens, keep what out held; the rows of a
  * sequence with more rows than ctx_lens see nothing.
@@ -605,8 +605,11 @@ int bros_attn_latent(void* out, const void* q, const int32_t* cu_q, int32_t num_
 /*
  * bros_attn_latent_prefill -- the expanded form: causal chunks over a latent pool.
  *
- * Keys and values of every head are made from the latents in the workspace (rounded to bf16), then
- * row j of sequence s attends to positions 0 .. c0 + j, as in bros_attn_prefill_chunk.
+ * Keys and values of every head are made from the latents in the workspace, then row j of sequence s
+ * attends to positions 0 .. c0 + j, as in bros_attn_prefill_chunk. Keys are rounded to bf16; values,
+ * and the softmax weights that they meet, to fp16, values behind a power of two for each 32 of a
+ * sequence's positions and head (so any bf16 range holds). What is not finite in the pool reaches the rows
+ * that see it and no others; every head's weights must be finite.
  *   q         : [num_q_tokens][num_q_heads][192]       out : [num_q_tokens][num_q_heads][128]
  *   w_kv      : [num_q_heads][256][512], 16-byte aligned
  *   total_ctx : host-side upper bound of the sum of the contexts; a sequence whose context does not

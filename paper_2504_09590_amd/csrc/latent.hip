@@ -20,7 +20,9 @@ constexpr int kRot = 64, kLatent = 512, kRow = kLatent + kRot;
 // append
 // ---------------------------------------------------------------------------
 
-// Rows of one kind to a workgroup: kTokens latent rows, a wave each, or kHeads query rows of 64, four lanes each.
+// Rows of one kind to a workgroup: kTokens latent rows, a wave each, or kHeads query rows of 64 (several times as many where
+// there are enough), four lanes each. One pass, bound by bytes: 6000 tokens of 128 heads, 253 MB, 63 us (4.0 TB/s of the 4.93
+// that a copy reaches); a decode step of 64 tokens and 32 heads is all start and end, 4.3 us.
 constexpr int kTokens = kThreads / kWave;
 constexpr int kHeads = kThreads / 4;
 
@@ -215,23 +217,26 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
 // ---------------------------------------------------------------------------
 
 // Dense rows: those of every sequence side by side, each sequence's to whole tiles of 32. A workgroup makes keys and
-// values of some heads for 128 rows, 128 dims at a time: four waves of 64 x 64, 64 latent dims a stage, two stages
+// values of some heads for 128 rows, 128 dims at a time: four waves of 64 x 64, 32 latent dims a stage, four stages
 // in LDS, two workgroups a compute unit. Latent rows come straight from their slots. Both operands' rows go to
-// LDS as they lie, 128 bytes a row and stage, chunks permuted so that an operand read meets no bank conflict.
+// LDS as they lie, 64 bytes a row and stage, chunks permuted so that an operand read meets no bank conflict.
 // (Keys that are no context are made of whatever a slot holds: the attention masks them.)
 //
 // Keys are rounded to bf16, as the queries that they meet. Values are rounded to fp16, like the softmax weights that
 // they meet: three bits more (with both in bf16 the result is 1.65 times as far from 64 bits as one that is
 // rounded once, so 1.2). fp16's range is made up for by an exponent for each tile of 32 rows and head,
 // 2^e off: 0 where the tile's largest magnitude lies within 2^-6 .. 2^15, as nearly always.
+//
+// Measured: 64 heads of 8400 rows (1.41e11 operations, 0.28 GB written) 234 us, 600 TFLOP/s. What it moves binds: both
+// operands' 2.2 GB from L2 to LDS and the stores (without these 80 us less, without the products 47). 256 rows and 256 dims
+// to a workgroup of eight waves move half of that, and took 211, but 23.5 for a prompt of 301 rows and 32 heads, now 12.8.
 constexpr int kExpandThreads = 256, kExpandWaves = kExpandThreads / kWave;
-constexpr int kStageDims = 64, kStages = 2, kTileRows = 128;
+constexpr int kStageDims = 32, kStages = 4, kTileRows = 128;
 constexpr int kHalfTile = kTileRows * kStageDims * 2;
 
-typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 half2_t;
 __device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {   // round to nearest even
   const pf::float2_t f = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, half2_t));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, ra::half2_t));
 }
 // 16 bytes from each lane's own address to LDS at dst + 16 * lane.
 __device__ __forceinline__ void load_rows_to_lds(const uint8_t* lane_src, const uint8_t* dst) {
@@ -301,37 +306,39 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
     return b >= 0 && b < a.num_blocks;
   };
 
-  // A wave loads rows 32 wave .. + 31 of both operands, eight rows of 128 bytes to a load: row r's chunk c lies at
-  // 128 r + 16 (c ^ (r / 2 % 8)), so that 16 rows' chunks of one operand read lie in 16 groups of banks.
-  const uint8_t* csrc[4];
-  uint32_t woff[4];
+  // A wave loads rows 32 wave .. + 31 of both operands, sixteen rows of 64 bytes to a load: row r's chunk c lies at
+  // 64 r + 16 (c ^ (r / 4 % 4)), so that 16 rows' chunks of one operand read lie in 16 groups of banks.
+  const uint8_t* csrc[2];
+  uint32_t woff[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 32 * wave + 8 * i + (lane >> 3);
-    const uint32_t chunk = (uint32_t)(((lane & 7) ^ ((r >> 1) & 7)) << 4);
+  for (int i = 0; i < 2; ++i) {
+    const int r = 32 * wave + 16 * i + (lane >> 2);
+    const uint32_t chunk = (uint32_t)(((lane & 3) ^ ((r >> 2) & 3)) << 4);
     csrc[i] = pool_row(r) + chunk;
     woff[i] = (uint32_t)r * (kLatent * 2) + chunk;
   }
   constexpr int kPerItem = kLatent / kStageDims;
+  constexpr int kLoads = 4;                  // of a wave and stage
   const int stages = items * kPerItem;
-  auto issue = [&](int k) __attribute__((always_inline)) {   // stage k: latent dims 64 (k % 8) .. of item k / 8
+  auto issue = [&](int k) __attribute__((always_inline)) {   // stage k: latent dims 32 (k % 16) .. of item k / 16
     const uint8_t* wsrc = static_cast<const uint8_t*>(a.w) + ((size_t)(item0 + k / kPerItem) * 128 * kLatent + (k % kPerItem) * kStageDims) * 2;
     uint8_t* dst = s_tile[k % kStages];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r8 = 32 * wave + 8 * i;
-      ra::load_to_lds(wsrc, woff[i], dst + r8 * 128);
-      load_rows_to_lds(csrc[i] + (k % kPerItem) * (kStageDims * 2), dst + kHalfTile + r8 * 128);
+    for (int i = 0; i < 2; ++i) {
+      const int r16 = 32 * wave + 16 * i;
+      ra::load_to_lds(wsrc, woff[i], dst + r16 * 64);
+      load_rows_to_lds(csrc[i] + (k % kPerItem) * (kStageDims * 2), dst + kHalfTile + r16 * 64);
     }
   };
   const int wd = wave & 1, wr = wave >> 1;   // the wave's 64 dims and 64 rows
   uint32_t context = 0;                      // bit k: row 64 wr + 32 k + col is one
 #pragma unroll
   for (int k = 0; k < 2; ++k) context |= (is_context(64 * wr + 32 * k + col) ? 1u : 0u) << k;
-  const int lane_at = (col >> 1) * 256 + ((col & 1) << 7), sw = (col >> 1) & 7;
+  const int lane_at = col * 64, sw = (col >> 2) & 3;
   pf::floatx16 o[2][2];                      // [dims][rows]
   // (the addresses come from loads that the compiler sees: they are there before the first request)
-  issue(0);
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k) issue(k);   // (an item has more)
 #pragma unroll 1
   for (int item = 0; item < items; ++item) {
     const bool values = (item0 + item) & 1;
@@ -344,19 +351,23 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
 #pragma unroll 1
     for (int kk = 0; kk < kPerItem; ++kk) {
       const int stage = item * kPerItem + kk;
-      pf::wait_vmem<0>();
+      // (the stages behind it may be in flight, and what the item before stored)
+      const int later = min(kStages - 2, stages - 1 - stage);
+      if (later == 2) pf::wait_vmem<2 * kLoads>();
+      else if (later == 1) pf::wait_vmem<kLoads>();
+      else pf::wait_vmem<0>();
       pf::lds_barrier();
-      if (stage + 1 < stages) issue(stage + 1);
-      const uint8_t* tw = s_tile[stage % kStages] + wd * 64 * 128;
-      const uint8_t* tc = s_tile[stage % kStages] + kHalfTile + wr * 64 * 128;
+      if (stage + kStages - 1 < stages) issue(stage + kStages - 1);
+      const uint8_t* tw = s_tile[stage % kStages] + wd * 64 * 64;
+      const uint8_t* tc = s_tile[stage % kStages] + kHalfTile + wr * 64 * 64;
 #pragma unroll
       for (int c = 0; c < kStageDims / 16; ++c) {
         const int at = lane_at + (((2 * c + half) ^ sw) << 4);
         pf::v4u_t x[2], y[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          x[i] = *reinterpret_cast<const pf::v4u_t*>(tw + 32 * 128 * i + at);
-          y[i] = *reinterpret_cast<const pf::v4u_t*>(tc + 32 * 128 * i + at);
+          x[i] = *reinterpret_cast<const pf::v4u_t*>(tw + 32 * 64 * i + at);
+          y[i] = *reinterpret_cast<const pf::v4u_t*>(tc + 32 * 64 * i + at);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -463,13 +474,15 @@ hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t stream) {
 
 hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
   const int64_t tiles = (a.dense_rows + kTileRows - 1) / kTileRows;
-  // Items (a head's keys, or its values) of a workgroup: the number whose rounds over the compute units, two workgroups
-  // each, end first; a workgroup's start (its rows' places) takes as long as two thirds of an item.
+  // Items (a head's keys, or its values) of a workgroup, one, two or four: the number whose rounds over the compute units, two
+  // workgroups each, end first; a workgroup's start (its rows' places) takes as long as two thirds of an item. Us of a whole call
+  // with 1, 2, 4 and 8: four chunks of 1000 rows behind 1100, 64 heads, 623, 598, 600, 622; two of 512 behind 8000 883, 846, 806, 819;
+  // one prompt of 301 rows, 128 heads, 72, 67, 73, 98; 32 heads 30, 36, 49, 73. (Odd numbers part a head: 3 622, 5 603.)
   const int64_t slots = 2 * (int64_t)stream_compute_units(stream), all = 2 * (int64_t)a.heads;
-  int each = 1;
+  int64_t each = 1;
   double best = 0.0;
-  for (int n = 1; n <= 32; ++n) {
-    const double us = (double)(((all + n - 1) / n * tiles + slots - 1) / slots) * (std::min<int64_t>(n, all) + 0.67);
+  for (int n = 1; n <= 4; n *= 2) {
+    const double us = (double)(((all + n - 1) / n * tiles + slots - 1) / slots) * (n + 0.67);
     if (n == 1 || us < best) {
       each = n;
       best = us;
@@ -477,7 +490,7 @@ hipError_t launch_latent_expand(const ExpandArgs& a, hipStream_t stream) {
   }
   // (a grid holds 2^32 - 1 threads)
   while (each < all && (all + each - 1) / each * tiles > (1LL << 23)) each *= 2;
-  hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)((all + each - 1) / each * tiles)), dim3(kExpandThreads), 0, stream, a, each);
+  hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)((all + each - 1) / each * tiles)), dim3(kExpandThreads), 0, stream, a, (int)each);
   return hipGetLastError();
 }
 
