@@ -326,8 +326,15 @@ inline int pick_rows_way(const RowsWay (&ways)[N], int64_t columns, int64_t segm
   return best;
 }
 
+// The longest sequence's rows as units are planned for them: the caller's bound, or twice the mean where that is
+// less (a bound may be far too high, and wide units of few columns cost what full ones do).
+inline int64_t planned_rows(int64_t max_rows, int64_t rows, int64_t num_seqs) {
+  return std::min(max_rows, 2 * ((rows + num_seqs - 1) / num_seqs));
+}
+
 // Workgroups side by side (a team) for units that share their keys: `tiles` units of the longest sequence. The second
-// and later ones find the keys in their die's L2, but a team whose last units are missing leaves them idle.
+// and later ones find the keys in their die's L2, but a team whose last units are missing leaves them idle (so does a
+// bound of the rows that is too high: hence the rows there are against those that the bound allows).
 // Us by one, two and four to a team, 128 columns to a unit. Drafts over a K/V pool: six trees of 64 with 64 / 8 heads on
 // 8000 to 32000 tokens (four units) 338, 284, 268; 16 of 40 to 64 with 32 / 8 on up to 8000 (two) 148, 125, 186; 32 of 20 to
 // 64 with 64 / 8 on up to 3000 163, 163, 196; four of 33 to 48 (three) 76, 82, 82. Expanded chunks: one of 2000 rows and
@@ -335,7 +342,7 @@ inline int pick_rows_way(const RowsWay (&ways)[N], int64_t columns, int64_t segm
 inline int rows_team(int64_t tiles, int64_t rows, int64_t max_rows, int64_t num_seqs) {
   const double filled = (double)rows / ((double)max_rows * (double)num_seqs);
   if (tiles % 4 == 0 && filled >= 0.9) return 4;
-  return (tiles % 2 == 0 && filled >= 0.75) || tiles >= 5 ? 2 : 1;
+  return (tiles % 2 == 0 && filled >= 0.75) || (tiles >= 5 && filled >= 0.6) ? 2 : 1;
 }
 
 }  // namespace bros

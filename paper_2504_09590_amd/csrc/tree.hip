@@ -81,7 +81,7 @@ size_t rows_workspace_bytes(bool latent) {
 }
 
 hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
-  const int64_t columns = (int64_t)a.max_q_len * (a.num_q_heads / a.num_kv_heads);
+  const int64_t rows = planned_rows(a.max_q_len, a.num_q_tokens, a.num_seqs), columns = rows * (a.num_q_heads / a.num_kv_heads);
   const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
   const int64_t segments = (int64_t)a.num_seqs * a.num_kv_heads;
   switch (pick_rows_way(kTreeWays, columns, segments, keys, stream_compute_units(stream))) {
@@ -94,7 +94,7 @@ hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
       return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
     case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, workspace, stream);
     default:
-      switch (rows_team((columns + 127) / 128, a.num_q_tokens, a.max_q_len, a.num_seqs)) {
+      switch (rows_team((columns + 127) / 128, a.num_q_tokens, rows, a.num_seqs)) {
         case 4: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 4>(a, 4, 12, workspace, stream);
         case 2: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 2>(a, 4, 12, workspace, stream);
         default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);

@@ -390,7 +390,7 @@ class LatentStep:
             bros.bros_attn_latent_prefill(self.out_chunks, q_chunks, d.cu_new[:P + 1], self.max_chunk, self.w_kv, self.pool,
                                           d.block_tables[:P], d.dir[:P], d.cls[:P], d.ctx_lens[:P], self.max_ctx_pre, self.total_ctx,
                                           workspace=self.workspace)
-        if S > P:
+        if self.max_rows:
             self._append(q_rows, kv[n:], P, S, self.cu_rows, pos(n, kv.shape[0]))
             bros.bros_attn_latent(self.out_rows, q_rows, self.cu_rows, self.max_rows, self.pool, d.block_tables[P:], d.dir[P:],
                                   d.cls[P:], d.ctx_lens[P:], self.max_ctx_rows, mask=mask, workspace=self.workspace)

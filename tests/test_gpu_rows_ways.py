@@ -102,6 +102,25 @@ def test_a_chunk_without_mask_of_many_rows():
     Absorbed([333], [50], 6, None, seed=8).check("latent, 333 rows without a mask")
 
 
+def test_bounds_far_above_the_rows_there_are():
+    """max_q_len is a bound: whatever it says, the rows are those of the offsets."""
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    c = Case([5, 1, 8], [700, 20, 2000], 8, 2, seed=41)
+    a = Absorbed([5, 1, 8], [700, 20, 2000], 16, seed=41)
+    e = Chunks([40, 3], [700, 20], 2, seed=42)
+    announce("bounds far above")
+    for k, most in ((c, 256), (a, 64), (e, 2 ** 31 - 1)):
+        k.b.max_n = most
+        if k is not e:
+            k.bits = np.concatenate([k.bits, np.zeros((k.b.rows, 3), dtype=np.int64)], 1)
+        check(k.run(), *k.want(), f"bound {most}")
+    # one sequence with all of the rows, among many with one
+    Case([1] * 30 + [120], [90] * 31, 32, 8, None, seed=43).check("tree, one of many rows")
+    Absorbed([1] * 30 + [60], [90] * 31, 16, None, seed=44).check("latent, one of many rows")
+    Chunks([1] * 10 + [700], [1200] * 11, 2, seed=45).check("latent prefill, one of many rows")
+
+
 def test_scale_and_scores_far_from_zero():
     """A scale of the caller's; scores of hundreds, where one weight is all there is."""
     torch = require_gpu()

@@ -145,6 +145,7 @@ def ways(tmp_path_factory):
 extern "C" int way(int latent, long long columns, long long segments, long long keys, int cus) {
   return latent ? bros::pick_rows_way(bros::kLatentWays, columns, segments, keys, cus) : bros::pick_rows_way(bros::kTreeWays, columns, segments, keys, cus);
 }
+extern "C" long long planned(long long max_rows, long long rows, long long seqs) { return bros::planned_rows(max_rows, rows, seqs); }
 extern "C" int team(long long tiles, long long rows, long long max_rows, long long seqs) { return bros::rows_team(tiles, rows, max_rows, seqs); }
 """)
     subprocess.run([gxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-ftrapv", "-shared", "-fPIC", "-I", CSRC, str(d / "ways.cpp"),
@@ -153,25 +154,29 @@ extern "C" int team(long long tiles, long long rows, long long max_rows, long lo
     L = ctypes.c_longlong
     lib.way.argtypes = [ctypes.c_int, L, L, L, ctypes.c_int]
     lib.team.argtypes = [L, L, L, L]
+    lib.planned.argtypes, lib.planned.restype = [L, L, L], L
     return lib
 
 
 def test_the_gpu_tests_shapes_take_every_way(ways):
     """Card of 256 compute units; a context counts by its last block."""
     blocks = lambda c0, n: 16 * max((c + m + 15) // 16 for c, m in zip(c0, n))  # noqa: E731
-    got = [ways.way(0, max(n) * hq // hkv, len(n) * hkv, blocks(c0, n), 256) for _, n, c0, hq, hkv in WAYS_TREE]
+    got = [ways.way(0, ways.planned(max(n), sum(n), len(n)) * hq // hkv, len(n) * hkv, blocks(c0, n), 256) for _, n, c0, hq, hkv in WAYS_TREE]
     assert got == [w for w, *_ in WAYS_TREE] and set(got) == {0, 1, 2}
-    got = [ways.way(1, max(n) * hq, len(n), blocks(c0, n), 256) for _, n, c0, hq in WAYS_LATENT]
+    got = [ways.way(1, ways.planned(max(n), sum(n), len(n)) * hq, len(n), blocks(c0, n), 256) for _, n, c0, hq in WAYS_LATENT]
     assert got == [w for w, *_ in WAYS_LATENT] and set(got) == {0, 1, 2, 3}
 
 
 def test_the_gpu_tests_shapes_take_every_team(ways):
     blocks = lambda c0, n: 16 * max((c + m + 15) // 16 for c, m in zip(c0, n))  # noqa: E731
     for team, n, c0, hq, hkv in TEAMS_TREE:
-        columns = max(n) * hq // hkv
-        assert ways.way(0, columns, len(n) * hkv, blocks(c0, n), 256) == 2 and ways.team(-(-columns // 128), sum(n), max(n), len(n)) == team
+        columns = ways.planned(max(n), sum(n), len(n)) * hq // hkv
+        assert ways.way(0, columns, len(n) * hkv, blocks(c0, n), 256) == 2 and ways.team(-(-columns // 128), sum(n), ways.planned(max(n), sum(n), len(n)), len(n)) == team
     for team, n, c0, hq in TEAMS_CHUNKS:
-        assert max(a + b for a, b in zip(n, c0)) > 1024 and ways.team(-(-max(n) // 128), sum(n), max(n), len(n)) == team
+        assert max(a + b for a, b in zip(n, c0)) > 1024 and ways.team(-(-ways.planned(max(n), sum(n), len(n)) // 128), sum(n), ways.planned(max(n), sum(n), len(n)), len(n)) == team
+    assert ways.planned(256, 8 * 16, 16) == 16 and ways.planned(32, 400, 16) == 32 and ways.planned(1, 7, 9) == 1
+    assert ways.planned(2 ** 31 - 1, 2 ** 31 - 1, 1) == 2 ** 31 - 1
+    assert ways.team(16, 16 * 4, 256, 16) == 1      # a bound far above the rows there are
     assert ways.team(1, 5, 5, 1) == 1 and ways.team(3, 300, 300, 1) == 1 and ways.team(2, 300, 256, 2) == 1
 
 
