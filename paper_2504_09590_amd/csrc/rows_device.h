@@ -976,29 +976,38 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void rows_merge_kernel(RowsArg
   const auto slot = [&](int p) -> size_t { return 2 * (size_t)(w0 + p * TEAM) + (p == 0 ? 1 : 0); };
   const auto ml = [&](int p) -> float2 { return reinterpret_cast<const float2*>(a.ws_ml)[slot(p) * S::CT + col]; };
 
-  float m = kNoMax;
-  for (int p = 0; p < pieces; p += 4) {   // (past the end: the last again)
-    float2 y[4];
+  // (all that the first four pieces need is asked for at once: most units have no more)
+  const Seq q = seq_of(a, cut.s);
+  float2 y[4];
+  float4 z[4][kMergeEach];
+  const auto load_ml = [&](int p) __attribute__((always_inline)) {   // (past the end: the last again)
 #pragma unroll
     for (int u = 0; u < 4; ++u) y[u] = ml(min(p + u, pieces - 1));
+  };
+  const auto load_sums = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) m = fmaxf(m, y[u].x);
+    for (int u = 0; u < 4; ++u) {
+      const float4* po = reinterpret_cast<const float4*>(a.ws_o + slot(min(p + u, pieces - 1)) * S::kSlotFloats) + (cw * S::kChunks + i0) * kWave + lane;
+#pragma unroll
+      for (int i = 0; i < kMergeEach; ++i) z[u][i] = po[i * kWave];
+    }
+  };
+  load_ml(0);
+  load_sums(0);
+  float m = fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x));
+  for (int p = 4; p < pieces; p += 4) {
+    float2 w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = ml(min(p + u, pieces - 1));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m = fmaxf(m, w[u].x);
   }
+  m = fmaxf(m, kNoMax);   // (a maximum that is not a number)
   float l = 0.0f;
   float4 o[kMergeEach];
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int p = 0; p < pieces; p += 4) {
-    float2 y[4];
-    float4 z[4][kMergeEach];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int pu = min(p + u, pieces - 1);
-      y[u] = ml(pu);
-      const float4* po = reinterpret_cast<const float4*>(a.ws_o + slot(pu) * S::kSlotFloats) + (cw * S::kChunks + i0) * kWave + lane;
-#pragma unroll
-      for (int i = 0; i < kMergeEach; ++i) z[u][i] = po[i * kWave];
-    }
+  for (int p = 0;;) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (p + u >= pieces) break;
@@ -1012,9 +1021,12 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void rows_merge_kernel(RowsArg
         o[i].w = fmaf(z[u][i].w, f, o[i].w);
       }
     }
+    p += 4;
+    if (p >= pieces) break;
+    load_ml(p);
+    load_sums(p);
   }
   const int G = DENSE ? 1 : a.num_q_heads / a.num_kv_heads;
-  const Seq q = seq_of(a, cut.s);
   const int c = cut.t * S::CT + col, j = c / G;
   if (j >= q.n) return;
   const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // (NaN stays)
