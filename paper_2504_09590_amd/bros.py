@@ -509,14 +509,15 @@ def bros_tree_commit(k_pool, v_pool, block_tables, dir, cls, ctx_lens, cu_q, pat
         nb, bs, d = _latent_pool(k_pool)
         hkv = 1
     else:
-        nb, hkv, bs, d = k_pool.shape
-        if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype:
+        shape = nb, hkv, bs, d = k_pool.shape
+        if v_pool.shape != shape or v_pool.dtype is not k_pool.dtype:
             raise ValueError("k_pool and v_pool must have one shape and type")
-    if path.dtype is not _I32 or path.dim() != 2 or path.shape[0] != S:
+    paths = path.shape
+    if path.dtype is not _I32 or len(paths) != 2 or paths[0] != S:
         raise ValueError(f"path must be int32 [{S}][most]")
     width, per_entry = _check_meta(S, block_tables, dir, cls, (ctx_lens, S), (cu_q, S + 1), (path_lens, S))
     kp, vp, bt, dr, cl, cx, cu, pa, pl = _addresses(k_pool, v_pool, block_tables, dir, cls, ctx_lens, cu_q, path, path_lens)
-    _check(LIB.bros_tree_commit(kp, vp, nb, bt, width, dr, cl, per_entry, cx, cu, pa, pl, path.shape[1], S, hkv, d, bs,
+    _check(LIB.bros_tree_commit(kp, vp, nb, bt, width, dr, cl, per_entry, cx, cu, pa, pl, paths[1], S, hkv, d, bs,
                                 _dtype_code(k_pool), _stream(stream)))
 
 
@@ -536,16 +537,17 @@ def bros_latent_append(q_out, q, kv, pool, block_tables, dir, cls, pos0, cu_new,
     of a latent pool; the queries' last 64 dims, q [Tn][Hq][64] (a view will do), turned into q_out (q itself,
     or a view of other queries; both None: no queries)."""
     nb, bs, d = _latent_pool(pool)
-    tn = kv.shape[0]
-    if kv.dtype is not _BF16 or kv.dim() != 2 or kv.shape[1] != d or kv.stride(1) != 1:
+    rows, stride = kv.shape, kv.stride()
+    tn = rows[0]
+    if kv.dtype is not _BF16 or len(rows) != 2 or rows[1] != d or stride[1] != 1:
         raise ValueError(f"kv must be bfloat16 [tokens][{d}], a token's values contiguous")
     if (q is None) != (q_out is None):
         raise ValueError("give both q and q_out, or neither")
     qp = qs = qh = op = os_ = oh = hq = 0
     if q is not None:
         qp, qs, qh, hq = _turned_rows(q, "q", tn)
-        op, os_, oh, _ = _turned_rows(q_out, "q_out", tn)
-        if q_out.shape != q.shape:
+        op, os_, oh, heads = _turned_rows(q_out, "q_out", tn)
+        if heads != hq:
             raise ValueError("q_out must have q's shape")
     device = kv.get_device()
     if norm is not None and (norm.dtype is not _BF16 or norm.numel() != d - 64):
@@ -560,7 +562,7 @@ def bros_latent_append(q_out, q, kv, pool, block_tables, dir, cls, pos0, cu_new,
     S = cu_new.numel() - 1
     width, per_entry = _check_meta(S, block_tables, dir, cls, (cu_new, S + 1), (pos0, S))
     pl, nm, bt, dr, cl, p0, cu, rp = _addresses(pool, norm, block_tables, dir, cls, pos0, cu_new, rope_pos, strided=(q, q_out, kv))
-    _check(LIB.bros_latent_append(op or None, qp or None, os_, oh, qs, qh, kv.data_ptr(), kv.stride(0) if tn > 1 else d, tn, hq, nm,
+    _check(LIB.bros_latent_append(op or None, qp or None, os_, oh, qs, qh, kv.data_ptr(), stride[0] if tn > 1 else d, tn, hq, nm,
                                   eps, None if rope is None else rope.ref, rp, pl, nb, bt, width, dr, cl, per_entry, p0, cu, S,
                                   d, bs, BROS_BF16, _stream(stream)))
 
