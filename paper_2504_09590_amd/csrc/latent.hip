@@ -500,10 +500,10 @@ hipError_t launch_latent(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t columns = planned_rows(a.max_q_len, a.num_q_tokens, a.num_seqs) * a.num_q_heads;
   const int64_t keys = 16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq);
   switch (pick_rows_way(kLatentWays, columns, a.num_seqs, keys, stream_compute_units(stream))) {
-    case 0: return ra::launch_latent_rows<1, 4>(a, 4, 6, workspace, stream);
-    case 1: return ra::launch_latent_rows<2, 2>(a, 4, 6, workspace, stream);
-    case 2: return ra::launch_latent_rows<4, 1>(a, 4, 6, workspace, stream);
-    default: return ra::launch_latent_rows<8, 1>(a, 6, 6, workspace, stream);
+    case 0: return ra::launch_latent_rows<1, 4>(a, 4, 6, 6, workspace, stream);
+    case 1: return ra::launch_latent_rows<2, 2>(a, 4, 6, 6, workspace, stream);
+    case 2: return ra::launch_latent_rows<4, 1>(a, 4, 6, 6, workspace, stream);
+    default: return ra::launch_latent_rows<8, 1>(a, 6, 6, 6, workspace, stream);
   }
 }
 
@@ -517,11 +517,11 @@ hipError_t launch_expanded(RowsArgs a, void* workspace, hipStream_t stream) {
   const int64_t rows = planned_rows(a.max_q_len, a.num_q_tokens, a.num_seqs);
   const int64_t units = (int64_t)a.num_seqs * a.num_kv_heads * ((rows + 63) / 64);
   if (16 * (int64_t)longest_blocks(a.max_ctx, a.max_blocks_per_seq) <= kNarrowKeys && units <= 2 * (int64_t)stream_compute_units(stream))
-    return ra::launch_rows<ra::Expanded, 2, 2, 3, 1>(a, 4, kNarrowKeys / 64, workspace, stream);
+    return ra::launch_rows<ra::Expanded, 2, 2, 3, 1>(a, 4, kNarrowKeys / 64, 4, workspace, stream);
   switch (rows_team((rows + 127) / 128, a.num_q_tokens, rows, a.num_seqs)) {
-    case 4: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 4>(a, 4, 8, workspace, stream);
-    case 2: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 2>(a, 4, 8, workspace, stream);
-    default: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, workspace, stream);
+    case 4: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 4>(a, 4, 8, 4, workspace, stream);
+    case 2: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2, 2>(a, 4, 8, 4, workspace, stream);
+    default: return ra::launch_rows<ra::Expanded, 4, 1, 3, 2>(a, 4, 8, 4, workspace, stream);
   }
 }
 

@@ -17,8 +17,8 @@
 // for those it requested itself, and puts in order what it finds there, before the barrier
 // that publishes them.
 //
-// Work. The steps of all units are laid end to end and cut into equal shares, one per
-// workgroup, whatever the sequences' lengths; a unit cut between workgroups leaves partial
+// Work. The steps of all units, each with some for its start (offsets, table, queries, first rows), are laid end to end and
+// cut into equal shares, one per workgroup, whatever the sequences' lengths; a unit cut between workgroups leaves partial
 // sums (fp32, with their maximum and total) that a merge folds. Where no unit is long,
 // whole units are shared out instead, and nothing is merged.
 //
@@ -133,11 +133,13 @@ struct Steps {
   int tiles, each;   // units per KV head; steps of one (causal units: of the last)
   int before;        // causal units: steps of the keys before the new rows
   bool whole;        // shares are of whole units
+  int start;         // what a unit's start counts: its steps are those from `start` on in what is shared out
   __device__ __forceinline__ Steps(const RowsArgs& a, const Seq& q, int group) {
     tiles = (int)(((int64_t)q.n * group + CT - 1) / CT);
     each = max(1, (q.ctx + KS - 1) / KS);
     before = (max(q.c0, 0) + KS - 1) / KS;
     whole = a.whole_units != 0;
+    start = a.start_steps;
   }
   // Steps of unit t. Causal units (one column a row): those of its last row's keys.
   __device__ __forceinline__ int of(int t) const {
@@ -150,9 +152,9 @@ struct Steps {
     if constexpr (P::kCausalUnits) {
       // (the context may be cut short by max_ctx: units beyond it have `each` steps)
       const int free = min(t, min(tiles - 1, max(0, (each - before) / (CT / KS))));   // units whose `of` is not cut
-      return (int64_t)free * before + (int64_t)(CT / KS) * free * (free + 1) / 2 + (int64_t)(t - free) * each;
+      return (int64_t)free * before + (int64_t)(CT / KS) * free * (free + 1) / 2 + (int64_t)(t - free) * each + (int64_t)t * start;
     }
-    return (int64_t)t * each;
+    return (int64_t)t * (each + start);
   }
   __device__ __forceinline__ int64_t per_head() const { return first(tiles); }
 };
@@ -462,18 +464,19 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   const uint32_t ring0 = lds_address(ring);
 
   while (x < x_end) {
-    // ---- The segment: steps [first, last) of unit (s, g, t), of those of the team's units side by side [first, first + taken).
+    // ---- The segment: steps [first, last) of unit (s, g, t), of what is shared out `taken` from number at.step of the unit on.
     const int s = at.s, g = at.g, t = at.t * TEAM + member;
     const Seq q = seq_of(a, s);
     const Steps<P, S::CT * TEAM, S::KS> st(a, q, G);
     const Steps<P, S::CT, S::KS> own(a, q, G);
     const int tsteps = __builtin_amdgcn_readfirstlane(st.of(at.t));
-    const int first = st.whole ? 0 : at.step;
-    const int taken = st.whole ? tsteps : (int)min((int64_t)(tsteps - first), x_end - x);
+    const int taken = st.whole ? 0 : (int)min((int64_t)(st.start + tsteps - at.step), x_end - x);
+    const int first = st.whole ? 0 : max(0, at.step - st.start);
     const int usteps = TEAM == 1 ? tsteps : t < own.tiles ? __builtin_amdgcn_readfirstlane(own.of(t)) : 0;
-    const int last = min(first + taken, usteps), cnt = last - first;
+    const int last = st.whole ? usteps : min(at.step + taken - st.start, usteps), cnt = last - first;
+    x += st.whole ? 1 : taken;
     const bool whole = cnt == usteps;
-    if (TEAM == 1 || cnt > 0) {   // (a team's last units may not be there, and causal ones end one before the other)
+    if (cnt > 0) {   // (a share may end within a unit's start; a team's last units may not be there, and causal ones end one before the other)
     // (dense keys that do not fit their buffer: the sequence's rows see nothing)
     const bool fits = P::kPaged || at.row0 + dense_rows(q.ctx) <= a.dense_rows;
     const int ctx = fits ? q.ctx : 0, n = q.n;
@@ -876,7 +879,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           ml[0] = m_run;
           ml[1] = l;
         }
-        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x + usteps - 1) * TEAM + member};
+        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x - last + usteps - 1) * TEAM + member};
       }
     }
     // ---- Values that were left out and are seen: added to the rows that see them, where
@@ -941,7 +944,6 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     }
 
     // ---- The next unit.
-    x += st.whole ? 1 : taken;
     at.step = 0;
     if (x < x_end) {
       if (++at.t >= st.tiles) {

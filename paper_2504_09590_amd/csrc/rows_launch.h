@@ -17,13 +17,16 @@ constexpr size_t partial_bytes(size_t workers, size_t ct, size_t dims) {
 }
 
 // Launches `kernel` on per_cu workgroups a compute unit, and the merge. min_steps: the least steps of a share.
-// whole: steps of the longest unit up to which units are not cut.
+// whole: steps of the longest unit up to which units are not cut. start: steps that a unit's start counts as
+// in a share (us with 0, 3 and 6: decode of 16 heads, 64 contexts up to 8192, 77, 69, 64; of 64 heads 101, 93, 85; of 128 heads, 96 up to
+// 16384, 351, 341, 332; drafts of 32 heads 42, 38, 36; with 0, 4 and 8: 16 trees of 17 to 32 on up to 8192, 32 / 8 heads, 77, 69, 68).
 template <class S, bool DENSE, int TEAM = 1, class Kernel>
-hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, int whole, void* workspace, hipStream_t stream) {
+hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, int whole, int start, void* workspace, hipStream_t stream) {
   a.workers = std::max(1, std::min(stream_compute_units(stream), kMaxCus) * per_cu / TEAM);
   const int groups = a.workers * TEAM;
   a.min_steps = min_steps;
   a.whole_units = ((int64_t)std::min<int64_t>(a.max_ctx, (int64_t)a.max_blocks_per_seq * kBlockSize) + S::KS - 1) / S::KS <= whole;
+  a.start_steps = start;
   if (a.whole_units) a.min_steps = 1;
   a.ws_cut = workspace;
   a.ws_o = reinterpret_cast<float*>(static_cast<Cut*>(workspace) + groups);
@@ -38,16 +41,16 @@ hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, i
 }
 
 template <class P, int NCW, int NKW, int SLOTS, int PER_CU, int TEAM = 1>
-hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, void* workspace, hipStream_t stream) {
+hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, int start, void* workspace, hipStream_t stream) {
   using S = Shape<P, NCW, NKW, SLOTS>;
   constexpr int kEachEu = std::max(1, S::kWaves * PER_CU / 4);
-  return launch_shares<S, !P::kPaged, TEAM>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu, TEAM>, a, PER_CU, min_steps, whole, workspace, stream);
+  return launch_shares<S, !P::kPaged, TEAM>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu, TEAM>, a, PER_CU, min_steps, whole, start, workspace, stream);
 }
 
 template <int NCW, int HV>
-hipError_t launch_latent_rows(const RowsArgs& a, int min_steps, int whole, void* workspace, hipStream_t stream) {
+hipError_t launch_latent_rows(const RowsArgs& a, int min_steps, int whole, int start, void* workspace, hipStream_t stream) {
   using S = LatentShape<NCW, HV>;
-  return launch_shares<S, false>(&latent_kernel<NCW, HV, S::kWaves / 4>, a, 1, min_steps, whole, workspace, stream);
+  return launch_shares<S, false>(&latent_kernel<NCW, HV, S::kWaves / 4>, a, 1, min_steps, whole, start, workspace, stream);
 }
 
 }  // namespace ra

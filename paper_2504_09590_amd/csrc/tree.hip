@@ -90,14 +90,14 @@ hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
       // Us, so and two to a compute unit: one sequence of four rows on 300, 8 / 2 heads 12.6 and 13.8; 32 / 8 heads:
       // four of 4 on 500 16.8 and 18.5, 32 of 6 19.6 and 27; but 64 of 4 on 300, 512 units, 26 and 20.4.
       if (keys <= 8 * 64 && segments * ((columns + 31) / 32) <= stream_compute_units(stream))
-        return ra::launch_rows<ra::KvPool, 1, 2, 3, 1>(a, 4, 8, workspace, stream);
-      return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, workspace, stream);
-    case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, workspace, stream);
+        return ra::launch_rows<ra::KvPool, 1, 2, 3, 1>(a, 4, 8, 4, workspace, stream);
+      return ra::launch_rows<ra::KvPool, 1, 2, 2, 2>(a, 4, 8, 4, workspace, stream);
+    case 1: return ra::launch_rows<ra::KvPool, 2, 2, 2, 2>(a, 4, 8, 4, workspace, stream);
     default:
       switch (rows_team((columns + 127) / 128, a.num_q_tokens, rows, a.num_seqs)) {
-        case 4: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 4>(a, 4, 12, workspace, stream);
-        case 2: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 2>(a, 4, 12, workspace, stream);
-        default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, workspace, stream);
+        case 4: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 4>(a, 4, 12, 8, workspace, stream);
+        case 2: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2, 2>(a, 4, 12, 8, workspace, stream);
+        default: return ra::launch_rows<ra::KvPool, 4, 1, 4, 2>(a, 4, 12, 8, workspace, stream);
       }
   }
 }
