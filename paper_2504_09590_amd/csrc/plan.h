@@ -299,17 +299,18 @@ struct RowsWay {
   double keys32_us, cut_us;
 };
 // Rows over a K/V pool: two workgroups a compute unit, of two waves, of four as two pairs, or of four.
-constexpr RowsWay kTreeWays[] = {{32, 0.52, 3.0}, {64, 0.53, 6.0}, {128, 0.73, 12.0}};
+constexpr RowsWay kTreeWays[] = {{32, 0.52, 3.0}, {64, 0.53, 6.0}, {128, 0.73, 18.0}};
 // Over a latent pool: one workgroup a compute unit, of four waves, or of eight with 128 columns.
-constexpr RowsWay kLatentWays[] = {{16, 1.7, 0.0}, {32, 1.7, 2.0}, {64, 2.4, 9.0}, {128, 3.4, 30.0}};
+constexpr RowsWay kLatentWays[] = {{16, 1.7, 0.0}, {32, 1.7, 2.0}, {64, 2.4, 8.0}, {128, 3.4, 20.0}};
 
 // The index of the way that is expected to end first: wide units read each key for more columns, narrow ones
 // leave work for more compute units and smaller partials where there is little of it. Contexts count as 0.6 of the longest.
 //
-// Us by columns of a unit (256 compute units), the one taken first. K/V pool, 32 / 8 heads: 16 trees of 32 rows on up
-// to 8192 tokens 67 (128), 87, 151; of 16 rows 55 (64), 76 (32); two of 30 rows on 3000 32 (64), 27 (32), 35 (128). Latent
-// pool, one row: 128 heads, 96 contexts up to 16384 304 (128), 417, 682; five of 10000 53 (64), 55, 70 (128); one of 30000
-// 71 (32), 77 (16), 86, 95; 64 heads, 64 of 8192 99 (64), 139, 232.
+// Us by columns of a unit, from the narrowest on (256 compute units; 25 such calls were swept, of which the one taken is the
+// fastest, or within 6 % of it, in all). K/V pool: 16 trees of 32 rows on up to 8192 tokens, 32 / 8 heads, 126, 73, 59; of 16 rows 71, 49, 56;
+// 64 of 8 rows on 500 to 4000 124, 131, 143; one of 64 rows on 8000, 64 / 8 heads, 58, 41, 53. Latent pool, one row: 128 heads, 96
+// contexts up to 16384 1234, 654, 395, 293; five of 6000 to 10000 67, 46, 43, 53; one of 30000 63, 51, 60, 73; 64 heads, 64 of up
+// to 8192 198, 117, 83, 115; 16 heads, two drafts' sequences of 4 on 1000 21, 23, 25, 33; of 64 on 8000 199, 115, 83, 75.
 template <int N>
 inline int pick_rows_way(const RowsWay (&ways)[N], int64_t columns, int64_t segments, int64_t keys, int32_t compute_units) {
   int best = 0;

@@ -960,7 +960,8 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   }
 }
 
-// Folds the partials of the units cut between shares: workgroup (w, y) the chunks kWaves kEach y .. of the unit
+// Folds the partials of the units cut between shares, in the order of their keys: bound by the chain of the note, maxima and sums (5
+// us at least), for wide units by the partials' bytes (19 us for 64 MB). Workgroup (w, y) takes the chunks kWaves kEach y .. of the unit
 // that share w noted. A chunk is 1 KiB of a partial: a wave's columns, four dims to a lane.
 constexpr int kMergeWaves = 4, kMergeEach = 2;   // waves of a workgroup, chunks of a wave
 template <class S, bool DENSE, int TEAM>

@@ -5,9 +5,9 @@
 // 150 on by the matrix cores. A unit holds 32 columns (two waves along the keys), 64 (two by two) or 128 (four waves, each with
 // columns of its own), as plan.h expects them to end first; units of 128 that share their keys run side by side.
 //
-// Measured, kernel and merge: 16 trees of 17 to 32 drafts on up to 8192 tokens, 32 / 8 heads, 72 + 11 us, 271 MB at 3.8 TB/s
+// Measured, kernel and merge: 16 trees of 17 to 32 drafts on up to 8192 tokens, 32 / 8 heads, 67 + 11 us, 271 MB at 4.0 TB/s
 // (loads alone take 50: starts of shares and masked steps are the rest); six of 64 drafts on 8000 to 32000, 64 / 8 heads,
-// 276 + 13 us, 790 TFLOP/s, 0.44 GB read; one chain of four on 300 tokens, 8 / 2 heads, 12.8 us, a chain of latencies: offsets,
+// 266 + 13 us, 820 TFLOP/s, 0.44 GB read; one chain of four on 300 tokens, 8 / 2 heads, 12.8 us, a chain of latencies: offsets,
 // table, rows, three steps a wave, the masked one, the groups' sums.
 #include "plan.h"
 #include "rows_launch.h"

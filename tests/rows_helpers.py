@@ -128,7 +128,7 @@ WAYS_TREE = [(0, [6] * 3, [480, 17, 300], 8, 2), (0, [2] * 150, [240] * 150, 8, 
 WAYS_LATENT = [(0, [1] * 2, [600] * 2, 64), (1, [1] * 8, [5000] * 8, 64), (2, [2] * 40, [4000] * 40, 32), (3, [1] * 90, [4000] * 90, 128)]
 # Shapes whose units of 128 columns stand side by side in teams (workgroups of a team; the rest as above, chunks of a
 # latent cache as (n, c0, heads)).
-TEAMS_TREE = [(4, [64] * 3, [9000, 12000, 700], 64, 8), (4, [128] * 40, [300] * 40, 16, 4), (2, [64, 50, 41, 60] * 6, [4000, 900, 6000, 33] * 6, 16, 4),
+TEAMS_TREE = [(4, [64] * 3, [9000, 12000, 700], 64, 8), (4, [128] * 100, [250] * 100, 16, 4), (2, [64, 50, 41, 60] * 6, [4000, 900, 6000, 33] * 6, 16, 4),
               (2, [150, 0, 160], [9000, 5, 8000], 32, 8)]
 TEAMS_CHUNKS = [(4, [512, 512], [1000, 1300], 2), (4, [1024], [1100], 3), (2, [256, 250], [1500, 40], 3), (2, [700, 600, 1], [900, 1100, 1024], 2),
                 (2, [641], [2000], 2)]
