@@ -306,8 +306,8 @@ constexpr RowsWay kLatentWays[] = {{16, 1.7, 0.0}, {32, 1.7, 2.0}, {64, 2.4, 8.0
 // The index of the way that is expected to end first: wide units read each key for more columns, narrow ones
 // leave work for more compute units and smaller partials where there is little of it. Contexts count as 0.6 of the longest.
 //
-// Us by columns of a unit, from the narrowest on (256 compute units; 25 such calls were swept, of which the one taken is the
-// fastest, or within 6 % of it, in all). K/V pool: 16 trees of 32 rows on up to 8192 tokens, 32 / 8 heads, 126, 73, 59; of 16 rows 71, 49, 56;
+// Us by columns of a unit, from the narrowest on (256 compute units; 25 such calls were swept, and the one taken is the
+// fastest in each). K/V pool: 16 trees of 32 rows on up to 8192 tokens, 32 / 8 heads, 126, 73, 59; of 16 rows 71, 49, 56;
 // 64 of 8 rows on 500 to 4000 124, 131, 143; one of 64 rows on 8000, 64 / 8 heads, 58, 41, 53. Latent pool, one row: 128 heads, 96
 // contexts up to 16384 1234, 654, 395, 293; five of 6000 to 10000 67, 46, 43, 53; one of 30000 63, 51, 60, 73; 64 heads, 64 of up
 // to 8192 198, 117, 83, 115; 16 heads, two drafts' sequences of 4 on 1000 21, 23, 25, 33; of 64 on 8000 199, 115, 83, 75.
