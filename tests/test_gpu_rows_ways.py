@@ -275,3 +275,60 @@ def test_dirty_workspaces_and_two_streams():
         bros.bros_attn_latent(oa, q, ta[3], 2, pool, ta[0], ta[1], None, ta[2], a.b.max_ctx, mask=ma, workspace=wa, stream=s2)
     torch.cuda.synchronize()
     assert torch.equal(oc, first_c) and torch.equal(oa, first_a)
+
+
+@pytest.mark.parametrize("units", [32, 96])
+def test_on_a_share_of_the_compute_units(units):
+    """Fewer workgroups, other widths and cuts: within the same bounds."""
+    require_gpu()
+    from paper_2504_09590_amd import bros
+    stream = bros.bros_stream_create_cu_share(0, units)
+    try:
+        for c in (Case([20, 3, 64], [3000, 500, 900], 16, 4, seed=51), Case([64] * 3, [5000, 400, 3000], 64, 8, seed=52),
+                  Absorbed([2] * 3, [3000, 50, 700], 32, "tree", seed=53), Absorbed([1] * 20, [1500] * 20, 128, None, seed=54),
+                  Chunks([256, 250], [1500, 40], 3, seed=55), Chunks([300], [0], 4, seed=56)):
+            c.check(f"a share of {units} compute units, {type(c).__name__}", stream=stream)
+    finally:
+        bros.bros_stream_destroy(stream)
+
+
+def test_directions_by_class():
+    """Without directions a sequence's class gives them: 0 from the left, 1 from the right."""
+    torch = require_gpu()
+    from paper_2504_09590_amd import bros
+    for c in (Case([20, 3, 9], [300, 500, 0], 16, 4, seed=61), Absorbed([2, 3, 1], [300, 50, 700], 16, "tree", seed=62),
+              Chunks([70, 33, 5], [1500, 40, 3], 2, seed=63)):
+        announce(f"directions by class, {type(c).__name__}")
+        first = c.run()
+        tables, dirs, ctx, cu = c.b.cuda()
+        cls = (dirs < 0).to(torch.uint8)
+        out = torch.full_like(first, 7.0)
+        if isinstance(c, Chunks):
+            q, pool, w = c.dev
+            total = int(c.b.ctx.sum())
+            ws = torch.empty(bros.bros_latent_prefill_workspace_size(3, total, 2), dtype=torch.uint8, device="cuda")
+            bros.bros_attn_latent_prefill(out, q, cu, c.b.max_n, w, pool, tables, None, cls, ctx, c.b.max_ctx, total, workspace=ws)
+        else:
+            mask = torch.from_numpy(c.bits).cuda()
+            latent = isinstance(c, Absorbed)
+            ws = torch.empty(bros.bros_attn_workspace_size(3 if latent else 2, 1, 1, 1, ROW if latent else D, 0), dtype=torch.uint8, device="cuda")
+            call = bros.bros_attn_latent if latent else bros.bros_attn_tree
+            q, *pools = c.dev
+            call(out, q, cu, c.b.max_n, *pools, tables, None, cls, ctx, c.b.max_ctx, mask=mask, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
+    # the append and the commit, into a pool of zeros: the same slots either way
+    rng = np.random.default_rng(64)
+    b = Absorbed([6, 3, 8], [30, 5, 100], 4, None, seed=64).b
+    tables, dirs, ctx, cu = b.cuda()
+    cls, kv = (dirs < 0).to(torch.uint8), bf16(rng, (17, ROW)).cuda()
+    at = torch.from_numpy(b.c0.astype(np.int32)).cuda()
+    path, lens = torch.tensor([[4, 2], [2, 0], [7, 3]], dtype=torch.int32).cuda(), torch.tensor([2, 2, 1], dtype=torch.int32).cuda()
+    pools = []
+    for way in ((dirs, None), (None, cls)):
+        pool = torch.zeros((b.num_blocks, 16, ROW), dtype=torch.bfloat16, device="cuda")
+        bros.bros_latent_append(None, None, kv, pool, tables, *way, at, cu)
+        bros.bros_tree_commit(pool, None, tables, *way, ctx, cu, path, lens)
+        pools.append(pool)
+    torch.cuda.synchronize()
+    assert torch.equal(*pools) and int((pools[0] != 0).any(-1).sum()) == 17
