@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "rows_units.h"
+
 namespace bros {
 
 struct KvWriteArgs {
@@ -141,43 +143,6 @@ struct PrefillArgs {
   float* ws_o;
   float* ws_ml;
   int32_t* ws_list;
-};
-
-// Attention of a few new rows of each sequence (rows_device.h): drafts over a K/V pool, latent
-// queries over a pool of latent rows, causal chunks over expanded keys and values.
-struct RowsArgs {
-  void* out;
-  const void* q;
-  const int32_t* cu_q;        // null: one row per sequence
-  const uint64_t* mask;       // [num_q_tokens][mask_words], or null: causal
-  int32_t mask_words;
-  const void* k_pool;         // latent: the only pool; expanded: keys [heads][dense_rows][128]
-  const void* v_pool;
-  const void* rot_rows;       // expanded: [dense_rows][64]
-  const int32_t* exps;        // expanded: [heads][dense_rows / 32] exponents of the values
-  int64_t dense_rows;
-  const int32_t* block_tables;
-  const int8_t* dir;
-  const uint8_t* cls;
-  const int32_t* ctx_lens;
-  int32_t dir_per_entry;      // dir is [S][max_blocks_per_seq] (else [S])
-  int32_t num_q_tokens;
-  int32_t max_q_len;          // host bound of a sequence's rows
-  int32_t num_seqs;
-  int32_t num_blocks;
-  int32_t max_blocks_per_seq;
-  int32_t max_ctx;
-  int32_t num_q_heads;
-  int32_t num_kv_heads;       // expanded: heads of this pass
-  int32_t head0;              // expanded: the first of them (else 0)
-  float scale_log2;
-  int32_t workers;            // shares the work is cut into, at most (set by the launch)
-  int32_t min_steps;          // the least steps of a share (set by the launch)
-  int32_t whole_units;        // shares are of whole units (set by the launch)
-  int32_t start_steps;        // what a unit's start counts among its steps (set by the launch)
-  void* ws_cut;               // [workers] notes of cut units
-  float* ws_o;                // [2 workers] x (columns of a unit x value dims) partial sums
-  float* ws_ml;               // [2 workers][columns of a unit][2] maximum (log2 units) and total
 };
 
 // Accepted drafts moved to their final positions (tree.hip).

@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kExpandThreads, 2) void latent_expand_kernel(Expand
   for (int i = 0; i < wave; ++i) first += s_scan[i];
   if (first < row0 + kTileRows && first + mine > row0) {
     for (int s = s0; s < s1; ++s) {
-      const int rows = ra::dense_rows(ra::seq_of(ra_, s).ctx);
+      const int64_t rows = ra::dense_rows(ra::seq_of(ra_, s).ctx);
       for (int i = 0; i < kTiles; ++i) {
         const int64_t r = row0 + 32 * i;
         if (r >= first && r < first + rows) {

@@ -114,16 +114,12 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
 
   while (x < x_end) {
     // ---- The segment: steps [first, last) of unit (s, t).
-    const int s = at.s, t = at.t;
-    const Seq q = seq_of(a, s);
-    const Steps<P, S::CT, S::KS> st(a, q, G);
-    const int usteps = __builtin_amdgcn_readfirstlane(st.of(t));
-    const int taken = st.whole ? 0 : (int)min((int64_t)(st.start + usteps - at.step), x_end - x);
-    const int first = st.whole ? 0 : max(0, at.step - st.start);
-    const int last = st.whole ? usteps : at.step + taken - st.start, cnt = last - first;
-    x += st.whole ? 1 : taken;
-    const bool whole = cnt == usteps;
-    if (cnt > 0) {   // (a share may end within a unit's start)
+    const Segment<P, S::CT, S::KS, 1> seg(a, at, G, 0, x, x_end);
+    const int s = at.s, t = seg.t, first = seg.first, last = seg.last;
+    const Seq q = seg.q;
+    const bool whole = seg.whole;
+    x = seg.next;
+    if (seg.count > 0) {   // (a share may end within a unit's start)
     const int ctx = q.ctx, n = q.n;
     // The lane's column: its row, whether there is one, and the place of both in q and out. (Formed anew at
     // each use: the loop needs the registers.)
@@ -341,17 +337,13 @@ __global__ __launch_bounds__(64 * NCW * HV, OCC) void latent_kernel(RowsArgs a) 
         ml[0] = m_run;
         ml[1] = l;
       }
-      if (threadIdx.x == 0 && first == 0) *cut = Cut{s, 0, t, shares.of(x - last + usteps - 1)};
+      if (threadIdx.x == 0 && first == 0) *cut = Cut{s, 0, t, seg.last_share(shares)};
     }
     }
 
     // ---- The next unit.
     at.step = 0;
-    if (x < x_end && ++at.t >= st.tiles) {
-      at.t = 0;
-      do ++at.s;
-      while (seq_of(a, at.s).n <= 0);   // (steps are left, so a sequence with rows follows)
-    }
+    if (x < x_end) next_unit<P>(a, at, seg.tiles);
   }
 }
 

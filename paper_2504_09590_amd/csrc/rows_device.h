@@ -17,7 +17,7 @@
 // for those it requested itself, and puts in order what it finds there, before the barrier
 // that publishes them.
 //
-// Work. The steps of all units, each with some for its start (offsets, table, queries, first rows), are laid end to end and
+// Work (rows_units.h). The steps of all units, each with some for its start (offsets, table, queries, first rows), are laid end to end and
 // cut into equal shares, one per workgroup, whatever the sequences' lengths; a unit cut between workgroups leaves partial
 // sums (fp32, with their maximum and total) that a merge folds. Where no unit is long,
 // whole units are shared out instead, and nothing is merged.
@@ -35,6 +35,7 @@
 
 #include "bros_device.h"
 #include "bros_kernels.h"
+#include "rows_units.h"
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Wunneeded-internal-declaration"   // (its planning is not used here)
 #include "prefill_device.h"
@@ -59,7 +60,6 @@ using pf::swz;
 using pf::v4u_t;
 using pf::wait_vmem;
 
-constexpr int kKeys = 32;                // keys of a wave's tile
 constexpr float kRescaleSlack = 8.0f;    // log2 units: weights stay <= 2^8
 constexpr float kNoMax = -1.0e30f;       // finite "no score yet" reference
 constexpr int kTable = 128;              // staged table entries of a wave: two windows of 64
@@ -93,71 +93,6 @@ __device__ __forceinline__ int lane_here() {
 __device__ __forceinline__ int32_t lds_word(const int32_t* p) {
   return *(const volatile int32_t __attribute__((address_space(3)))*)(uintptr_t)lds_address(p);
 }
-
-// What is read. kMain: bytes of a key row's first part, kRot: of its second (0: none);
-// kVal: bytes of a value row, or 0 where the first part is the value.
-struct KvPool {          // 128 dims each, [blocks][Hkv][16][128]
-  static constexpr int kMain = 256, kRot = 0, kVal = 256;
-  static constexpr bool kPaged = true, kCausalUnits = false, kHalf = false;
-};
-struct LatentPool {      // 512 shared dims and 64 rotated ones, [blocks][16][576]
-  static constexpr int kMain = 1024, kRot = 128, kVal = 0;
-  static constexpr bool kPaged = true, kCausalUnits = false;
-};
-struct Expanded {        // dense rows: keys of 128 dims and 64 rotated ones shared by the heads, values of 128 in fp16
-  static constexpr int kMain = 256, kRot = 128, kVal = 256;
-  static constexpr bool kPaged = false, kCausalUnits = true, kHalf = true;
-};
-
-// A sequence as the kernels see it. n = 0: nothing to do. ctx: its visible context
-// (0 where lengths are inconsistent: its rows see nothing); c0: position of its first new row.
-struct Seq {
-  int q0, n, c0, ctx;
-};
-__device__ __forceinline__ Seq seq_of(const RowsArgs& a, int s) {
-  Seq r;
-  r.q0 = a.cu_q != nullptr ? a.cu_q[s] : s;
-  const int end = a.cu_q != nullptr ? a.cu_q[s + 1] : s + 1;
-  r.n = (r.q0 < 0 || end > a.num_q_tokens || end < r.q0) ? 0 : end - r.q0;
-  const int ctx = a.ctx_lens[s];
-  r.c0 = ctx - r.n;
-  const int64_t room = (int64_t)a.max_blocks_per_seq * kBlockSize;
-  r.ctx = r.c0 < 0 ? 0 : (int)min((int64_t)min(ctx, a.max_ctx), room);
-  return r;
-}
-
-// Steps of a sequence's units. CT columns to a unit, KS keys to a step. Every unit has one
-// at least: its rows are written even where they see nothing.
-template <class P, int CT, int KS>
-struct Steps {
-  int tiles, each;   // units per KV head; steps of one (causal units: of the last)
-  int before;        // causal units: steps of the keys before the new rows
-  bool whole;        // shares are of whole units
-  int start;         // what a unit's start counts: its steps are those from `start` on in what is shared out
-  __device__ __forceinline__ Steps(const RowsArgs& a, const Seq& q, int group) {
-    tiles = (int)(((int64_t)q.n * group + CT - 1) / CT);
-    each = max(1, (q.ctx + KS - 1) / KS);
-    before = (max(q.c0, 0) + KS - 1) / KS;
-    whole = a.whole_units != 0;
-    start = a.start_steps;
-  }
-  // Steps of unit t. Causal units (one column a row): those of its last row's keys.
-  __device__ __forceinline__ int of(int t) const {
-    if constexpr (P::kCausalUnits) return t + 1 < tiles ? min(before + (CT / KS) * (t + 1), each) : each;
-    return each;
-  }
-  // What units 0 .. t - 1 (t <= tiles) count, in what is shared out.
-  __device__ __forceinline__ int64_t first(int t) const {
-    if (whole) return t;
-    if constexpr (P::kCausalUnits) {
-      // (the context may be cut short by max_ctx: units beyond it have `each` steps)
-      const int free = min(t, min(tiles - 1, max(0, (each - before) / (CT / KS))));   // units whose `of` is not cut
-      return (int64_t)free * before + (int64_t)(CT / KS) * free * (free + 1) / 2 + (int64_t)(t - free) * each + (int64_t)t * start;
-    }
-    return (int64_t)t * (each + start);
-  }
-  __device__ __forceinline__ int64_t per_head() const { return first(tiles); }
-};
 
 // The two blocks of a tile: whether their entries are valid, and their directions.
 struct TileBlocks {
@@ -208,13 +143,6 @@ __device__ __forceinline__ uint32_t row_window(const RowsArgs& a, const Seq& q, 
   return valid ? win & below(ctx - pos0) : 0u;
 }
 
-// Where a workgroup's share begins.
-struct Place {
-  int s, g, t, step;
-  int64_t total;        // steps of all units
-  int64_t row0;         // dense keys: row of sequence s's position 0
-};
-
 __device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -224,9 +152,6 @@ __device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
   return v;
 }
 
-// Rows that a sequence's keys take in the dense buffers: whole tiles.
-__device__ __forceinline__ int dense_rows(int ctx) { return (ctx + kKeys - 1) / kKeys * kKeys; }
-
 // The steps of all units, and the unit and step of number `at(total)` (at: a function of the
 // total, the same for every thread; -1: no place wanted). All THREADS threads call it; `scratch` is 2 x (waves + 1) numbers of
 // LDS and s_place a Place.
@@ -234,16 +159,9 @@ template <class P, int CT, int KS, int THREADS, class At>
 __device__ __forceinline__ Place find_place(const RowsArgs& a, int group, At at, int64_t* scratch, Place* s_place) {
   constexpr int kW = THREADS / kWave;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
-  // a thread's run of sequences
-  const int per = (a.num_seqs + THREADS - 1) / THREADS;
-  const int s0 = min(tid * per, a.num_seqs), s1 = min(s0 + per, a.num_seqs);
-  int64_t mine = 0, rows = 0;
-  for (int s = s0; s < s1; ++s) {
-    const Seq q = seq_of(a, s);
-    const Steps<P, CT, KS> st(a, q, group);
-    mine += st.per_head() * a.num_kv_heads;
-    if constexpr (!P::kPaged) rows += dense_rows(q.ctx);
-  }
+  const Run run(a.num_seqs, THREADS, tid);
+  int64_t mine, rows;
+  count_run<P, CT, KS>(a, group, run, mine, rows);
   const int64_t inc = wave_scan64(mine, lane);
   int64_t rinc = 0;
   if constexpr (!P::kPaged) rinc = wave_scan64(rows, lane);
@@ -261,33 +179,7 @@ __device__ __forceinline__ Place find_place(const RowsArgs& a, int group, At at,
     total += scratch[i];
   }
   const int64_t x = at(total);
-  if (x >= first && x < first + mine) {
-    int64_t left = x - first;
-    for (int s = s0; s < s1; ++s) {
-      const Seq q = seq_of(a, s);
-      const Steps<P, CT, KS> st(a, q, group);
-      const int64_t ph = st.per_head();
-      if (left < ph * a.num_kv_heads) {
-        Place p;
-        p.s = s;
-        p.g = (int)(left / ph);
-        left -= p.g * ph;
-        int lo = 0, hi = st.tiles - 1;   // the last unit that begins at or before it
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (st.first(mid) <= left) lo = mid; else hi = mid - 1;
-        }
-        p.t = lo;
-        p.step = (int)(left - st.first(lo));
-        p.total = total;
-        p.row0 = rfirst;
-        *s_place = p;
-        break;
-      }
-      left -= ph * a.num_kv_heads;
-      if constexpr (!P::kPaged) rfirst += dense_rows(q.ctx);
-    }
-  }
+  if (x >= first && x < first + mine) *s_place = place_in_run<P, CT, KS>(a, group, run, x - first, rfirst, total);
   __syncthreads();
   Place p = *s_place;
   p.s = __builtin_amdgcn_readfirstlane(p.s);
@@ -297,31 +189,6 @@ __device__ __forceinline__ Place find_place(const RowsArgs& a, int group, At at,
   p.total = total;
   return p;
 }
-
-// How `total` steps are shared out: n shares, the first `more` of them one step longer than `per`.
-struct Shares {
-  int n;
-  int64_t per, more;
-  __device__ __forceinline__ Shares(const RowsArgs& a, int64_t total) {
-    // (32-bit division is a tenth of the other, and nearly every call's steps fit)
-    if (total < (1 << 30)) {
-      const uint32_t x = (uint32_t)total;
-      n = max(1u, min((uint32_t)a.workers, (x + a.min_steps - 1) / a.min_steps));
-      per = x / (uint32_t)n;
-    } else {
-      n = a.workers;
-      per = total / n;
-    }
-    more = total - per * n;
-  }
-  __device__ __forceinline__ int64_t begin(int w) const { return per * w + min((int64_t)w, more); }
-  // The share that step x lies in.
-  __device__ __forceinline__ int of(int64_t x) const {
-    const int64_t longer = more * (per + 1);
-    if (x < longer) return (int)(x / (per + 1));
-    return (int)(more + (x - longer) / per);
-  }
-};
 
 // Writes a wave's normalised columns: lane l holds column l % 32, accumulators 4 jq .. + 3 of o[i] are dims
 // 32 (dt0 + i) + 8 jq + 4 (l / 32) .. + 3.
@@ -464,19 +331,13 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   const uint32_t ring0 = lds_address(ring);
 
   while (x < x_end) {
-    // ---- The segment: steps [first, last) of unit (s, g, t), of what is shared out `taken` from number at.step of the unit on.
-    const int s = at.s, g = at.g, t = at.t * TEAM + member;
-    const Seq q = seq_of(a, s);
-    const Steps<P, S::CT * TEAM, S::KS> st(a, q, G);
-    const Steps<P, S::CT, S::KS> own(a, q, G);
-    const int tsteps = __builtin_amdgcn_readfirstlane(st.of(at.t));
-    const int taken = st.whole ? 0 : (int)min((int64_t)(st.start + tsteps - at.step), x_end - x);
-    const int first = st.whole ? 0 : max(0, at.step - st.start);
-    const int usteps = TEAM == 1 ? tsteps : t < own.tiles ? __builtin_amdgcn_readfirstlane(own.of(t)) : 0;
-    const int last = st.whole ? usteps : min(at.step + taken - st.start, usteps), cnt = last - first;
-    x += st.whole ? 1 : taken;
-    const bool whole = cnt == usteps;
-    if (cnt > 0) {   // (a share may end within a unit's start; a team's last units may not be there, and causal ones end one before the other)
+    // ---- The segment: steps [first, last) of unit (s, g, t).
+    const Segment<P, S::CT, S::KS, TEAM> seg(a, at, G, member, x, x_end);
+    const int s = at.s, g = at.g, t = seg.t, first = seg.first, last = seg.last, cnt = seg.count;
+    const Seq q = seg.q;
+    const bool whole = seg.whole;
+    x = seg.next;
+    if (cnt > 0) {
     // (dense keys that do not fit their buffer: the sequence's rows see nothing)
     const bool fits = P::kPaged || at.row0 + dense_rows(q.ctx) <= a.dense_rows;
     const int ctx = fits ? q.ctx : 0, n = q.n;
@@ -879,7 +740,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           ml[0] = m_run;
           ml[1] = l;
         }
-        if (tid == 0 && first == 0) *cut = Cut{s, g, t, shares.of(x - last + usteps - 1) * TEAM + member};
+        if (tid == 0 && first == 0) *cut = Cut{s, g, t, seg.last_share(shares) * TEAM + member};
       }
     }
     // ---- Values that were left out and are seen: added to the rows that see them, where
@@ -945,18 +806,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 
     // ---- The next unit.
     at.step = 0;
-    if (x < x_end) {
-      if (++at.t >= st.tiles) {
-        at.t = 0;
-        if (++at.g >= Hkv) {
-          at.g = 0;
-          do {
-            if constexpr (!P::kPaged) at.row0 += dense_rows(seq_of(a, at.s).ctx);
-            ++at.s;
-          } while (seq_of(a, at.s).n <= 0);   // (steps are left, so a sequence with rows follows)
-        }
-      }
-    }
+    if (x < x_end) next_unit<P>(a, at, seg.tiles);
   }
 }
 
