@@ -607,8 +607,10 @@ int bros_attn_latent(void* out, const void* q, const int32_t* cu_q, int32_t num_
  *
  * Keys and values of every head are made from the latents in the workspace, then row j of sequence s
  * attends to positions 0 .. c0 + j, as in bros_attn_prefill_chunk. Keys are rounded to bf16; values,
- * and the softmax weights that they meet, to fp16, values behind a power of two for each 32 of a
- * sequence's positions and head (so any bf16 range holds). What is not finite in the pool reaches the rows
+ * and the softmax weights that they meet, to fp16. A position's values of a head stand behind a power of two
+ * of their own wherever some of the 32 positions around it have a largest value outside 2^-6 .. 2^5 (other
+ * than zero), and weights then count from the largest weight times that power: what is lost is
+ * measured by the positions that a row sees, of whatever size they are. What is not finite in the pool reaches the rows
  * that see it and no others; every head's weights must be finite.
  *   q         : [num_q_tokens][num_q_heads][192]       out : [num_q_tokens][num_q_heads][128]
  *   w_kv      : [num_q_heads][256][512], 16-byte aligned

@@ -860,14 +860,14 @@ int bros_attn_latent(void* out, const void* q, const int32_t* cu_q, int32_t num_
   return launch_status(fn, bros::launch_latent(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
-// The workspace of an expanded call: partials, rotated keys, then K, V and the values' exponents of some heads.
+// The workspace of an expanded call: partials, rotated keys, then K, V and the values' exponents (a word a tile, a byte a row) of some heads.
 namespace {
 struct ExpandSizes {
   int64_t rows;          // of every dense buffer
   size_t partials, rot, head;
   ExpandSizes(int32_t num_seqs, int32_t total_ctx)
       : rows(((int64_t)total_ctx + 31 * (int64_t)num_seqs + 31) / 32 * 32), partials(bros::rows_workspace_bytes(false)),
-        rot((size_t)rows * kRotDims * 2), head((size_t)rows * 2 * 128 * 2 + (size_t)rows / 32 * sizeof(int32_t)) {}
+        rot((size_t)rows * kRotDims * 2), head((size_t)rows * 2 * 128 * 2 + (size_t)rows / 32 * sizeof(int32_t) + (size_t)rows) {}
   size_t bytes(size_t heads) const { return partials + rot + heads * head; }
 };
 }  // namespace
@@ -930,13 +930,15 @@ int bros_attn_latent_prefill(void* out, const void* q, const int32_t* cu_q, int3
     e.heads = std::min(heads, num_q_heads - h);
     e.w = static_cast<const uint16_t*>(w_kv) + (size_t)h * 256 * kLatentDims;
     e.v_rows = static_cast<uint8_t*>(e.k_rows) + (size_t)e.heads * sizes.rows * 256;
-    e.exps = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(e.v_rows) + (size_t)e.heads * sizes.rows * 256);
+    e.scaled = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(e.v_rows) + (size_t)e.heads * sizes.rows * 256);
+    e.exps = reinterpret_cast<int8_t*>(e.scaled + (size_t)e.heads * (sizes.rows / 32));
     e.with_rot = h == 0;
     err = bros::launch_latent_expand(e, s);
     if (err != hipSuccess) break;
     a.head0 = h;
     a.num_kv_heads = e.heads;
     a.v_pool = e.v_rows;
+    a.scaled = e.scaled;
     a.exps = e.exps;
     err = bros::launch_expanded(a, workspace, s);
   }

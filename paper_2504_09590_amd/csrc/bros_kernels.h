@@ -200,8 +200,9 @@ struct ExpandArgs {
   const void* w;              // [heads][256][512] of this group
   void* rot_rows;             // [dense_rows][64]
   void* k_rows;               // [heads][dense_rows][128] bf16
-  void* v_rows;               // fp16, each 2^-e of the value
-  int32_t* exps;              // [heads][dense_rows / 32]: e
+  void* v_rows;               // fp16, each 2^-e of the value in tiles that are scaled
+  int32_t* scaled;            // [heads][dense_rows / 32]: whether a tile of 32 rows is
+  int8_t* exps;               // [heads][dense_rows]: e of such a tile's rows
   int32_t with_rot;           // write rot_rows too
   int64_t dense_rows;
   const int32_t* block_tables;

@@ -63,6 +63,7 @@ using pf::wait_vmem;
 constexpr float kRescaleSlack = 8.0f;    // log2 units: weights stay <= 2^8
 constexpr float kNoMax = -1.0e30f;       // finite "no score yet" reference
 constexpr int kTable = 128;              // staged table entries of a wave: two windows of 64
+constexpr int kNoExponent = -128;        // of a value row of zeros (a row that is not zeros has -120 .. 120)
 
 typedef const v4u_t __attribute__((address_space(3)))* lds_v4u_ptr;
 typedef short v4s_t __attribute__((ext_vector_type(4)));
@@ -327,6 +328,9 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   // permutation are the same for every lane: a xor.
   const uint32_t main_off = (uint32_t)((lane >> 4) * 256 + (((lane & 15) ^ ((lane >> 4) << 2)) << 4));
   const uint32_t rot_off = (uint32_t)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 4)) << 4));
+  // The lane where it is seldom needed: with expanded keys the usual loop needs the registers that places made of it would
+  // hold (42 of them went to scratch memory, and chunks took 790 us instead of 710).
+  const auto lane_again = [&]() __attribute__((always_inline)) -> int { return P::kHalf ? lane_here() : lane; };
   uint8_t* const ring = s_ring + kg * SLOTS * S::kTile;
   const uint32_t ring0 = lds_address(ring);
 
@@ -417,11 +421,16 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < kDt; ++i) o[i] = floatx16{};
     float m_run = kNoMax, l0 = 0.0f, l1 = 0.0f;
-    // Values that are 2^-e of what they stand for (nearly never any but e = 0): the sums are 2^-e_run of theirs, with the
-    // largest exponent so far, and a tile's weights are multiplied by 2^(e - e_run).
-    int e_run = 0, e_off = 0;
-    float e_scale = 1.0f;   // what the sums take for a larger exponent
-    const int32_t* exps = P::kHalf ? a.exps + (size_t)g * (a.dense_rows / kKeys) + at.row0 / kKeys : nullptr;
+    // Values that stand behind exponents e of their rows (nearly never any). An fp16 weight must not take them up: it has no
+    // room below 2^-24 for a tile of small values, nor may a row that a column does not see set what is lost in it. So a tile's products are
+    // made of weights 2^(score + e - r), r being the column's largest score + e in this tile, and are added to the sums in fp32, which
+    // stand in units of 2^r_run, with the largest r so far. A loop of its own, without overlap: a call that is all of such values takes 1.39
+    // times as long (four chunks of 700 to 1400 rows behind up to 5000, 64 heads, 1030 and 1430 us).
+    // (Places are formed anew at each use: the usual loop needs the registers.)
+    const auto scaled_tile = [&](int tile) __attribute__((always_inline)) -> int32_t { return a.scaled[((size_t)g * a.dense_rows + at.row0) / kKeys + tile]; };
+    const auto exps_of = [&](int pos) __attribute__((always_inline)) -> uint32_t {   // of four positions
+      return *reinterpret_cast<const uint32_t*>(a.exps + (size_t)g * a.dense_rows + at.row0 + pos);
+    };
     uint32_t odd = 0;   // a value that is not finite was left out of a product
 
     // Waits for the wave's rows of a step (those of the next `most` may be in flight) and, where the step is
@@ -437,14 +446,15 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         if (masked(step) && (NCW > 1 || kOverlap || pos_of(step) < ctx)) {
           const int pos0 = pos_of(step);
           const TileBlocks tb = blocks_of(pos0);
+          const int ln = lane_again();
           uint8_t* vt = ring + (step % SLOTS) * S::kTile + S::kValAt;
           constexpr int kMine = kR * (P::kVal / 16) / kWave;   // 16-byte chunks of a lane
           v4u_t w[kMine];
 #pragma unroll
-          for (int i = 0; i < kMine; ++i) w[i] = reinterpret_cast<const v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + lane];
+          for (int i = 0; i < kMine; ++i) w[i] = reinterpret_cast<const v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + ln];
 #pragma unroll
           for (int i = 0; i < kMine; ++i) {
-            const int r = kR * cw + (i * kWave + lane) / (P::kVal / 16);
+            const int r = kR * cw + (i * kWave + ln) / (P::kVal / 16);
             const int pos = pos0 + (r & 16) + slot_of_offset(r & 15, r < 16 ? tb.dir0 : tb.dir1);
             const bool there = (r < 16 ? tb.ok0 : tb.ok1) && pos < ctx;
 #pragma unroll
@@ -453,7 +463,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
               odd |= bad;
               w[i][e] = there ? w[i][e] & ~((bad >> 15) * 0xffffu) : 0;
             }
-            reinterpret_cast<v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + lane] = w[i];
+            reinterpret_cast<v4u_t*>(vt + kR * cw * P::kVal)[i * kWave + ln] = w[i];
           }
         }
       }
@@ -468,11 +478,11 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     ask(first);
     request(first);
-    bool scaled = false;   // any exponent of the segment's is not 0
+    bool scaled = false;   // any of the segment's tiles is
     if constexpr (P::kHalf) {
       int any = 0;
       const int tiles = min(last * NKW, (ctx + kKeys - 1) / kKeys);
-      for (int i = first * NKW + lane; i < tiles; i += kWave) any |= exps[i];
+      for (int i = first * NKW + lane_here(); i < tiles; i += kWave) any |= scaled_tile(i);
       scaled = __builtin_amdgcn_ballot_w64(any != 0) != 0;
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
@@ -493,9 +503,10 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           const int pos0 = pos_of(step);
           const TileBlocks tb = blocks_of(pos0);
           const uint32_t win = row_window(a, q, ctx, j, valid, pos0, word0);
+          const int half_here = lane_again() >> 5;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int k = 8 * (i >> 2) + 4 * half + (i & 3);
+            const int k = 8 * (i >> 2) + 4 * half_here + (i & 3);
             const int off = (k & 16) + slot_of_offset(k & 15, (i >> 3) ? tb.dir1 : tb.dir0);
             cur[i] = ((i >> 3) ? tb.ok1 : tb.ok0) && ((win >> off) & 1u) ? cur[i] : -INFINITY;
           }
@@ -506,47 +517,29 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         const float mx = pair_max(mr) * sl2;
         m_prev = m_run;
         m_run = mx > m_run + kRescaleSlack ? mx : m_run;
-        if constexpr (kScaled) {
-          const int e = pos_of(step) < ctx ? __builtin_amdgcn_readfirstlane(exps[pos_of(step) / kKeys]) : 0;
-          const int most = step == first ? e : max(e_run, e);
-          e_scale = step == first ? 1.0f : ldexpf(1.0f, max(e_run - most, -126));
-          e_run = most;
-          e_off = e - most;
-        }
       };
       auto rescale = [&]() __attribute__((always_inline)) {
         if (__builtin_amdgcn_ballot_w64(m_run != m_prev) != 0) {
           const float alpha = fast_exp2(m_prev - m_run);
+          if constexpr (!kScaled) {
 #pragma unroll
-          for (int i = 0; i < kDt; ++i) o[i] *= alpha;
+            for (int i = 0; i < kDt; ++i) o[i] *= alpha;
+          }
           l0 *= alpha;
           l1 *= alpha;
-        }
-        if constexpr (kScaled) {
-          if (e_scale != 1.0f) {
-#pragma unroll
-            for (int i = 0; i < kDt; ++i) o[i] *= e_scale;
-          }
         }
       };
       // Weights, rounded to 16 bits (bf16, or fp16 where the values are) for the second product; the totals add the
       // rounded weights.
       auto weights = [&](const floatx16& cur, bf16x8_t (&pfr)[2]) __attribute__((always_inline)) {
         if constexpr (P::kHalf) {
-          float base = -m_run;
-          half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
-          if constexpr (kScaled) {   // (the totals count a weight whatever its values' exponent)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) l0 += fast_exp2(fmaf(cur[i], sl2, base));
-            base += (float)e_off;
-            ones = half2_t{(_Float16)0.0f, (_Float16)0.0f};
-          }
+          const half2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
           for (int c2 = 0; c2 < 2; ++c2) {
             half2_t pw[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-              const float2_t pp = {fast_exp2(fmaf(cur[8 * c2 + 2 * w], sl2, base)), fast_exp2(fmaf(cur[8 * c2 + 2 * w + 1], sl2, base))};
+              const float2_t pp = {fast_exp2(fmaf(cur[8 * c2 + 2 * w], sl2, -m_run)), fast_exp2(fmaf(cur[8 * c2 + 2 * w + 1], sl2, -m_run))};
               pw[w] = __builtin_convertvector(pp, half2_t);
               if (w & 1) l1 = __builtin_amdgcn_fdot2(pw[w], ones, l1, false);
               else l0 = __builtin_amdgcn_fdot2(pw[w], ones, l0, false);
@@ -590,6 +583,42 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, x), __builtin_bit_cast(half8_t, pfr[i / kDt]), o[i % kDt], 0, 0, 0);
         else
           o[i % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), pfr[i / kDt], o[i % kDt], 0, 0, 0);
+      };
+
+      // A tile's values behind exponents (the totals count a weight whatever its exponent).
+      float r_run = kNoMax;
+      const auto scaled_values = [&](floatx16& cur, int step, uint32_t tile) __attribute__((always_inline)) {
+        const int pos0 = pos_of(step), half_here = lane_here() >> 5;
+        const bool is = pos0 < ctx && __builtin_amdgcn_readfirstlane(scaled_tile(pos0 / kKeys)) != 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {   // keys 8 c + 4 half .. + 3
+          const uint32_t e4 = is ? exps_of(pos0 + 8 * c + 4 * half_here) : 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            l0 += fast_exp2(fmaf(cur[4 * c + i], sl2, -m_run));
+            cur[4 * c + i] = fmaf(cur[4 * c + i], sl2, (float)(int8_t)(e4 >> (8 * i)));
+          }
+        }
+        float r = kNoMax;   // (nothing seen: weights of 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r = fmaxf(r, cur[i]);
+        r = pair_max(r);
+        const float r_new = fmaxf(r_run, r), f_run = fast_exp2(r_run - r_new), f = fast_exp2(r - r_new);
+        r_run = r_new;
+        v4u_t pw[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2_t pp = {fast_exp2(cur[2 * i] - r), fast_exp2(cur[2 * i + 1] - r)};
+          pw[i >> 2][i & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pp, half2_t));
+        }
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) {
+          floatx16 y{};
+#pragma unroll
+          for (int c2 = 0; c2 < 2; ++c2)
+            y = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, value_operand(tile, kDt * c2 + i)), __builtin_bit_cast(half8_t, pw[c2]), y, 0, 0, 0);
+          o[i] = o[i] * f_run + y * f;
+        }
       };
 
       if constexpr (kOverlap && !kScaled) {
@@ -653,12 +682,26 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
                                      [&](int i, v4u_t x) __attribute__((always_inline)) { score(cur, i, x); });
           mask_max(cur, step);
           rescale();
-          bf16x8_t pfr[2];
-          weights(cur, pfr);
-          pipelined<2 * kDt, kAhead>([&](int i) __attribute__((always_inline)) { return value_operand(tile, i); },
-                                     [&](int i, v4u_t x) __attribute__((always_inline)) { value(pfr, i, x); });
+          if constexpr (kScaled) {
+            scaled_values(cur, step, tile);
+          } else {
+            bf16x8_t pfr[2];
+            weights(cur, pfr);
+            pipelined<2 * kDt, kAhead>([&](int i) __attribute__((always_inline)) { return value_operand(tile, i); },
+                                       [&](int i, v4u_t x) __attribute__((always_inline)) { value(pfr, i, x); });
+          }
           publish(step + 1, SLOTS - 2);
         }
+      }
+      if constexpr (kScaled) {
+        // from units of 2^r_run to those of the totals; the totals' move up where the sums would not fit into fp32 (they are
+        // below 2^33 here, and values, as what the totals divide them to, may be near 2^128)
+        const float up = fmaxf(0.0f, r_run - m_run - 90.0f), f = fast_exp2(r_run - m_run - up), fl = fast_exp2(-up);
+        m_run += up;
+        l0 *= fl;
+        l1 *= fl;
+#pragma unroll
+        for (int i = 0; i < kDt; ++i) o[i] *= f;
       }
     };
     if constexpr (P::kHalf) {
@@ -669,13 +712,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     }
 
     // ---- The end of the segment.
-    if constexpr (P::kHalf) {
-      if (scaled) {
-        const float f = ldexpf(1.0f, e_run);
-#pragma unroll
-        for (int i = 0; i < kDt; ++i) o[i] *= f;
-      }
-    }
+    const int lane_e = lane_again(), half_e = lane_e >> 5, col_e = lane_e & 31;
     float l = pair_sum(l0 + l1);
     if (odd != 0) s_odd = 1;
     if constexpr (NKW == 1) __syncthreads();   // (else the key groups' sums meet behind one)
@@ -690,11 +727,11 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
         for (int i = 0; i < kDt; ++i) {
 #pragma unroll
           for (int jq = 0; jq < 4; ++jq)
-            xo[(w * kDt * 4 + 4 * i + jq) * kWave + lane] = make_float4(o[i][4 * jq], o[i][4 * jq + 1], o[i][4 * jq + 2], o[i][4 * jq + 3]);
+            xo[(w * kDt * 4 + 4 * i + jq) * kWave + lane_e] = make_float4(o[i][4 * jq], o[i][4 * jq + 1], o[i][4 * jq + 2], o[i][4 * jq + 3]);
         }
-        if (half == 0) {
-          s_ml[2 * (w * 32 + col)] = m_run;
-          s_ml[2 * (w * 32 + col) + 1] = l;
+        if (half_e == 0) {
+          s_ml[2 * (w * 32 + col_e)] = m_run;
+          s_ml[2 * (w * 32 + col_e) + 1] = l;
         }
       }
       __syncthreads();
@@ -702,7 +739,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 #pragma unroll 1
         for (int k = 1; k < NKW; ++k) {
           const int w = (k - 1) * NCW + cw;
-          const float m2 = s_ml[2 * (w * 32 + col)], l2 = s_ml[2 * (w * 32 + col) + 1];
+          const float m2 = s_ml[2 * (w * 32 + col_e)], l2 = s_ml[2 * (w * 32 + col_e) + 1];
           const float m = fmaxf(m_run, m2);
           const float f1 = fast_exp2(m_run - m), f2 = fast_exp2(m2 - m);
           m_run = m;
@@ -711,7 +748,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           for (int i = 0; i < kDt; ++i) {
 #pragma unroll
             for (int jq = 0; jq < 4; ++jq) {
-              const float4 y = xo[(w * kDt * 4 + 4 * i + jq) * kWave + lane];
+              const float4 y = xo[(w * kDt * 4 + 4 * i + jq) * kWave + lane_e];
               o[i][4 * jq] = o[i][4 * jq] * f1 + y.x * f2;
               o[i][4 * jq + 1] = o[i][4 * jq + 1] * f1 + y.y * f2;
               o[i][4 * jq + 2] = o[i][4 * jq + 2] * f1 + y.z * f2;
@@ -725,18 +762,18 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     if (kg == 0) {
       if (whole) {
         const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // (NaN stays)
-        if (valid) write_columns<kDt>(static_cast<uint16_t*>(a.out) + orow * S::kDims, 0, o, inv, half);
+        if (valid) write_columns<kDt>(static_cast<uint16_t*>(a.out) + orow * S::kDims, 0, o, inv, half_e);
       } else {
         // the accumulators as they lie: every store of the wave is 1 KiB contiguous
-        float4* po = reinterpret_cast<float4*>(a.ws_o + ws * S::kSlotFloats) + cw * kDt * 4 * kWave + lane;
+        float4* po = reinterpret_cast<float4*>(a.ws_o + ws * S::kSlotFloats) + cw * kDt * 4 * kWave + lane_e;
 #pragma unroll
         for (int i = 0; i < kDt; ++i) {
 #pragma unroll
           for (int jq = 0; jq < 4; ++jq)
             po[(4 * i + jq) * kWave] = make_float4(o[i][4 * jq], o[i][4 * jq + 1], o[i][4 * jq + 2], o[i][4 * jq + 3]);
         }
-        if (half == 0) {
-          float* ml = a.ws_ml + (ws * S::CT + 32 * cw + col) * 2;
+        if (half_e == 0) {
+          float* ml = a.ws_ml + (ws * S::CT + 32 * cw + col_e) * 2;
           ml[0] = m_run;
           ml[1] = l;
         }
@@ -764,7 +801,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           return static_cast<const uint8_t*>(a.v_pool) + ((size_t)g * a.dense_rows + at.row0 + pos0 + r) * P::kVal;
         };
         uint32_t any = 0;
-        for (int i = lane; i < kKeys * (P::kVal / 16); i += kWave) {
+        for (int i = lane_e; i < kKeys * (P::kVal / 16); i += kWave) {
           const uint8_t* row = value_row(i / (P::kVal / 16));
           if (row == nullptr) continue;
           const v4u_t w = *reinterpret_cast<const v4u_t*>(row + 16 * (i % (P::kVal / 16)));
@@ -779,7 +816,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
           if (!((win >> off) & 1u)) continue;
 #pragma unroll 1
           for (int i = 0; i < 4 * kDt; ++i) {
-            const int d = 8 * i + 4 * half;   // four dims
+            const int d = 8 * i + 4 * half_e;   // four dims
             const uint2 w = *reinterpret_cast<const uint2*>(row + 2 * d);
             if ((not_finite<P::kHalf>(w.x) | not_finite<P::kHalf>(w.y)) == 0) continue;
             const float2_t v01 = two_values<P::kHalf>(w.x), v23 = two_values<P::kHalf>(w.y);
@@ -792,7 +829,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
               for (int e = 0; e < 4; ++e) z[e] = fabsf(v[e]) < INFINITY ? z[e] : z[e] + v[e];
               *at_out = make_uint2(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]));
             } else {
-              float* at_ws = a.ws_o + ws * S::kSlotFloats + (cw * kDt * 4 + i) * (4 * kWave) + 4 * lane;
+              float* at_ws = a.ws_o + ws * S::kSlotFloats + (cw * kDt * 4 + i) * (4 * kWave) + 4 * lane_e;
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (!(fabsf(v[e]) < INFINITY)) at_ws[e] += v[e];

@@ -26,7 +26,8 @@ struct RowsArgs {
   const void* k_pool;         // latent: the only pool; expanded: keys [heads][dense_rows][128]
   const void* v_pool;
   const void* rot_rows;       // expanded: [dense_rows][64]
-  const int32_t* exps;        // expanded: [heads][dense_rows / 32] exponents of the values
+  const int32_t* scaled;      // expanded: [heads][dense_rows / 32], of a tile: its values stand behind exponents
+  const int8_t* exps;         // expanded: [heads][dense_rows], the exponents of such tiles' rows
   int64_t dense_rows;
   const int32_t* block_tables;
   const int8_t* dir;
