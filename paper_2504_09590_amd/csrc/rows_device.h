@@ -180,7 +180,7 @@ __device__ __forceinline__ Place find_place(const RowsArgs& a, int group, At at,
     total += scratch[i];
   }
   const int64_t x = at(total);
-  if (x >= first && x < first + mine) *s_place = place_in_run<P, CT, KS>(a, group, run, x - first, rfirst, total);
+  if (x >= first && x < first + mine) place_in_run<P, CT, KS>(a, group, run, x - first, rfirst, total, s_place);
   __syncthreads();
   Place p = *s_place;
   p.s = __builtin_amdgcn_readfirstlane(p.s);

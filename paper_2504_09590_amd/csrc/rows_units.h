@@ -196,7 +196,7 @@ BROS_UNITS void count_run(const RowsArgs& a, int group, Run run, int64_t& steps,
 }
 // The unit and step of number `left` (of `total`) of a run, before which lie `rows` dense rows.
 template <class P, int CT, int KS>
-BROS_UNITS Place place_in_run(const RowsArgs& a, int group, Run run, int64_t left, int64_t rows, int64_t total) {
+BROS_UNITS void place_in_run(const RowsArgs& a, int group, Run run, int64_t left, int64_t rows, int64_t total, Place* out) {
   Place p{-1, 0, 0, 0, total, rows};
   for (int s = run.s0; s < run.s1; ++s) {
     const Seq q = seq_of(a, s);
@@ -213,12 +213,12 @@ BROS_UNITS Place place_in_run(const RowsArgs& a, int group, Run run, int64_t lef
       }
       p.t = lo;
       p.step = (int)(left - st.first(lo));
-      break;
+      *out = p;
+      return;
     }
     left -= ph * a.num_kv_heads;
     if constexpr (!P::kPaged) p.row0 += dense_rows(q.ctx);
   }
-  return p;
 }
 
 // What a workgroup (member of a team of TEAM) does of the unit at `at`, its share being [x, x_end): steps [first, last) of

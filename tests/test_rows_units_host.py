@@ -68,7 +68,7 @@ int walk(const RowsArgs& a, int group, char* msg) {
     int64_t first = 0, row = 0;
     for (int i = 0; i < THREADS; ++i) {
       if (wanted >= first && wanted < first + steps[i])
-        at = place_in_run<P, CT * TEAM, KS>(a, group, Run(S, THREADS, i), wanted - first, row, total);
+        place_in_run<P, CT * TEAM, KS>(a, group, Run(S, THREADS, i), wanted - first, row, total, &at);
       first += steps[i];
       row += rows[i];
     }
