@@ -142,16 +142,20 @@ __device__ __forceinline__ uint2 lds_read_tr(const uint8_t* p) {   // ds_read_b6
 // kernel's explicit waits (wait_vmem) and barriers order every access.
 // The source is a wave-uniform base (scalar registers) plus a per-lane byte
 // offset.
+// The compiler sees to wait states for its own loads only: M0 may be read one
+// state after a scalar instruction has written it, and a scalar register that a
+// vector instruction has written (a base that was spilled into the lanes of a
+// vector register and is read back) five states later. Hence the s_nop.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t lane_off, const uint8_t* dst) {
   // the LDS aperture is 4 GiB aligned: the low half of a generic pointer into
   // LDS is the LDS address
   const uint32_t m0 = (uint32_t)(uintptr_t)dst;
-  asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 // The same for 4 bytes per lane, at dst + 4 * lane.
 __device__ __forceinline__ void load_word_to_lds(const void* base, uint32_t lane_off, const void* dst) {
   const uint32_t m0 = (uint32_t)(uintptr_t)dst;
-  asm volatile("global_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
+  asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 // A load the compiler may issue as a scalar (uniform) load.
 typedef const int32_t __attribute__((address_space(4)))* scalar_i32_ptr;

@@ -53,6 +53,8 @@ using pf::float2_t;
 using pf::floatx16;
 using pf::lds_barrier;
 using pf::lds_read_tr;
+using pf::load_to_lds;
+using pf::load_word_to_lds;
 using pf::pack2_bf16;
 using pf::pair_max;
 using pf::pair_sum;
@@ -72,17 +74,6 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_
 __device__ __forceinline__ v4u_t lds_read(uint32_t at) { return *(lds_v4u_ptr)(uintptr_t)at; }
 __device__ __forceinline__ uint2 lds_read_turned(uint32_t at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)at));
-}
-// 16 or 4 bytes from base + lane_off of each lane to LDS at dst + 16 or 4 * lane. A scalar register that a vector instruction
-// has written (a base that was spilled into lanes of a vector register and is read back) may be read as an address five wait
-// states later, which the compiler sees to for its own loads only.
-__device__ __forceinline__ void load_to_lds(const void* base, uint32_t lane_off, const uint8_t* dst) {
-  const uint32_t m0 = (uint32_t)(uintptr_t)dst;   // (the LDS aperture is 4 GiB aligned)
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
-}
-__device__ __forceinline__ void load_word_to_lds(const void* base, uint32_t lane_off, const void* dst) {
-  const uint32_t m0 = (uint32_t)(uintptr_t)dst;
-  asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(m0)));
 }
 // Lane id that is computed where it is used (values made of it are not held in registers over a loop).
 __device__ __forceinline__ int lane_here() {
