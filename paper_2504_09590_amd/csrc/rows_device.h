@@ -284,7 +284,8 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
   __shared__ int32_t s_tab[S::kWaves][kTable];
   __shared__ int64_t s_scan[2 * S::kWaves];
   __shared__ Place s_place;
-  __shared__ int s_odd;
+  __shared__ __attribute__((aligned(4))) uint8_t s_odd[4];   // of each wave: it left out a value that is not finite
+  static_assert(S::kWaves <= 4, "their notes are read as one word");
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = wave_id_uniform();
   const int cw = wave % NCW, kg = wave / NCW;
@@ -346,7 +347,6 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
 
     // ---- Start: the first windows of the table, then queries and masks.
     __syncthreads();   // (the ring's last use: the segment before this one)
-    if (tid == 0) s_odd = 0;
     const int e_first = 2 * (first * NKW + kg) & ~63;
     const int32_t win0 = table.get(e_first), win1 = table.get(e_first + 64);
     const int dir_all = P::kPaged ? seq_direction(a.dir, a.cls, s) : 1;   // (read where entries have no directions of their own)
@@ -705,7 +705,9 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     // ---- The end of the segment.
     const int lane_e = lane_again(), half_e = lane_e >> 5, col_e = lane_e & 31;
     float l = pair_sum(l0 + l1);
-    if (odd != 0) s_odd = 1;
+    // (every wave writes its note, before a barrier that the readers wait for and, at the next segment's start, behind one)
+    const bool any_odd = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+    if (lane_e == 0) s_odd[wave] = any_odd;
     if constexpr (NKW == 1) __syncthreads();   // (else the key groups' sums meet behind one)
     if constexpr (NKW > 1) {
       // the key groups' sums meet in the ring
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(64 * NCW * NKW, OCC) void rows_kernel(RowsArgs a) {
     }
     // ---- Values that were left out and are seen: added to the rows that see them, where
     // those now lie. (Every key of the segment's masked tiles is looked at again, in memory.)
-    if (kg == 0 && s_odd != 0) {
+    if (kg == 0 && (*reinterpret_cast<const uint32_t*>(s_odd) & (0xffffffffu >> (32 - 8 * S::kWaves))) != 0) {
       const int tiles = cnt * NKW;
 #pragma unroll 1
       for (int ti = 0; ti < tiles; ++ti) {
