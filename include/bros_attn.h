@@ -535,7 +535,7 @@ int bros_attn_tree(void* out, const void* q, const int32_t* cu_q, int32_t num_q_
  * is, and so does a position without a valid table entry on either side. Bytes move unchanged;
  * nothing else changes.
  *
- *   k_pool, v_pool : a pool of BROS_F32 or BROS_BF16 rows, row_dim 128; or a latent pool
+ *   k_pool, v_pool : a pool of BROS_F32 or BROS_BF16 rows, row_dim 128, of at most 16384 KV heads; or a latent pool
  *                    (below): row_dim 576, num_kv_heads 1, BROS_BF16 and v_pool NULL
  *   path           : int32 [num_seqs][max_path], device; max_path at most BROS_TREE_MAX_DRAFTS
  *   path_lens      : int32 [num_seqs], device

@@ -20,7 +20,7 @@ constexpr int kCommitThreads = 256;
 constexpr int kCommitRows = kCommitThreads / 16;   // rows a workgroup moves at once, 16 lanes each
 constexpr int kCommitRounds = 16;                  // so many times at most
 
-// Sequence blockIdx.x, 256 bytes (16 chunks) blockIdx.y of its slots' rows. Every row is in
+// Sequence blockIdx.x, 256 bytes (16 chunks) blockIdx.y of its slots' rows in pool blockIdx.z (K's, V's). Every row is in
 // registers before the first is written, so a path may go any way. Bound by its chain of loads (offsets, path,
 // table entries, rows): 64 sequences of a bf16 pool with 8 heads 4.6 us, 256 of a latent pool 6.4 us, for 2.3 and 2.8 MB.
 __global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitArgs a) {
@@ -29,13 +29,10 @@ __global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitArgs a) {
   const int c0 = a.ctx_lens[s] - n;
   if (n <= 0 || c0 < 0) return;
   const int len = min(a.path_lens[s], min(n, a.max_path));
-  // 256-byte pieces of a (slot, head) row, K's heads then V's
+  // 256-byte pieces of a (slot, head) row
   const int pieces = (a.row_bytes + 255) / 256;
-  int y = blockIdx.y;
-  const int piece = y % pieces;
-  y /= pieces;
-  const int head = y % a.num_heads;
-  uint8_t* pool = static_cast<uint8_t*>(y / a.num_heads == 0 ? a.k_pool : a.v_pool);
+  const int piece = blockIdx.y % pieces, head = blockIdx.y / pieces;
+  uint8_t* pool = static_cast<uint8_t*>(blockIdx.z == 0 ? a.k_pool : a.v_pool);
   const int at = 256 * piece + 16 * (threadIdx.x & 15);
   const int r0 = threadIdx.x >> 4;
   if (len <= 0) return;
@@ -103,9 +100,9 @@ hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
 }
 
 hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t stream) {
-  const int64_t pieces = (int64_t)((a.row_bytes + 255) / 256) * a.num_heads * (a.v_pool != nullptr ? 2 : 1);
-  if (pieces > 65535) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(commit_kernel, dim3(a.num_seqs, (unsigned)pieces), dim3(kCommitThreads), 0, stream, a);
+  // (16384 heads of two pieces at most: within a grid's 65535)
+  const unsigned pieces = (unsigned)((a.row_bytes + 255) / 256) * a.num_heads;
+  hipLaunchKernelGGL(commit_kernel, dim3(a.num_seqs, pieces, a.v_pool != nullptr ? 2 : 1), dim3(kCommitThreads), 0, stream, a);
   return hipGetLastError();
 }
 
