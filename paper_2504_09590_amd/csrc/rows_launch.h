@@ -11,10 +11,12 @@ namespace ra {
 
 constexpr int kMaxCus = 256;   // compute units whose shares' partials the workspace holds
 
-// Bytes of the notes and partials of `workers` shares of units of CT columns and `dims` dims.
-constexpr size_t partial_bytes(size_t workers, size_t ct, size_t dims) {
-  return workers * sizeof(Cut) + 2 * workers * ct * (dims + 2) * sizeof(float);
+// Bytes of the notes and partials of `groups` workgroups whose units have CT columns and `dims` dims.
+constexpr size_t partial_bytes(size_t groups, size_t ct, size_t dims) {
+  return groups * sizeof(Cut) + 2 * groups * ct * (dims + 2) * sizeof(float);
 }
+// The workspaces: what the widest units take. (Every launch is checked against them where it is compiled.)
+constexpr size_t kRowsWorkspace = partial_bytes(2 * kMaxCus, 128, 128), kLatentWorkspace = partial_bytes(kMaxCus, 128, 512);
 
 // Launches `kernel` on per_cu workgroups a compute unit, and the merge. min_steps: the least steps of a share.
 // whole: steps of the longest unit up to which units are not cut. start: steps that a unit's start counts as
@@ -43,6 +45,7 @@ hipError_t launch_shares(Kernel kernel, RowsArgs a, int per_cu, int min_steps, i
 template <class P, int NCW, int NKW, int SLOTS, int PER_CU, int TEAM = 1>
 hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, int start, void* workspace, hipStream_t stream) {
   using S = Shape<P, NCW, NKW, SLOTS>;
+  static_assert(partial_bytes(kMaxCus * PER_CU, S::CT, S::kDims) <= kRowsWorkspace && PER_CU * kMaxCus % TEAM == 0, "");
   constexpr int kEachEu = std::max(1, S::kWaves * PER_CU / 4);
   return launch_shares<S, !P::kPaged, TEAM>(&rows_kernel<P, NCW, NKW, SLOTS, kEachEu, TEAM>, a, PER_CU, min_steps, whole, start, workspace, stream);
 }
@@ -50,6 +53,7 @@ hipError_t launch_rows(const RowsArgs& a, int min_steps, int whole, int start, v
 template <int NCW, int HV>
 hipError_t launch_latent_rows(const RowsArgs& a, int min_steps, int whole, int start, void* workspace, hipStream_t stream) {
   using S = LatentShape<NCW, HV>;
+  static_assert(partial_bytes(kMaxCus, S::CT, S::kDims) <= kLatentWorkspace, "");
   return launch_shares<S, false>(&latent_kernel<NCW, HV, S::kWaves / 4>, a, 1, min_steps, whole, start, workspace, stream);
 }
 

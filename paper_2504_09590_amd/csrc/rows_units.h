@@ -44,13 +44,14 @@ struct RowsArgs {
   int32_t num_kv_heads;       // expanded: heads of this pass
   int32_t head0;              // expanded: the first of them (else 0)
   float scale_log2;
-  int32_t workers;            // shares the work is cut into, at most (set by the launch)
+  int32_t workers;            // shares the work is cut into, at most: those of workgroups or of teams (set by the launch)
   int32_t min_steps;          // the least steps of a share (set by the launch)
   int32_t whole_units;        // shares are of whole units (set by the launch)
   int32_t start_steps;        // what a unit's start counts among its steps (set by the launch)
-  void* ws_cut;               // [workers] notes of cut units
-  float* ws_o;                // [2 workers] x (columns of a unit x value dims) partial sums
-  float* ws_ml;               // [2 workers][columns of a unit][2] maximum (log2 units) and total
+  // (workgroups: workers times those of a team)
+  void* ws_cut;               // [workgroups] notes of cut units
+  float* ws_o;                // [2 workgroups] x (columns of a unit x value dims) partial sums
+  float* ws_ml;               // [2 workgroups][columns of a unit][2] maximum (log2 units) and total
 };
 
 namespace ra {

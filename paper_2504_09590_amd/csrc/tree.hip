@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitArgs a) {
 }  // namespace
 
 size_t rows_workspace_bytes(bool latent) {
-  return latent ? ra::partial_bytes(ra::kMaxCus, 128, 512) : ra::partial_bytes(2 * ra::kMaxCus, 128, 128);
+  return latent ? ra::kLatentWorkspace : ra::kRowsWorkspace;
 }
 
 hipError_t launch_tree(RowsArgs a, void* workspace, hipStream_t stream) {
