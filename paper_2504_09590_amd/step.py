@@ -342,6 +342,12 @@ class LatentStep:
     keys' and values' weights [Hq][256][512] (None without chunks). rope (of 64 dims) and norm (bf16 [512])
     are kept for every run. pass_heads: heads whose keys and values the workspace holds at a time (default: all).
 
+    The lengths in dev may change from run to run (a prompt's next chunk of as many rows), within bounds that are taken here,
+    for the device's lengths are not read back: max_ctx bounds the contexts of the rows (default: what the tables hold),
+    max_ctx_chunks that of every chunk and total_ctx their sum (default of both: batch's lengths, so that a step whose chunks
+    go on has to be given them). Beyond them a chunk sees its context cut short at max_ctx_chunks, and chunks that total_ctx has no room for
+    get zero rows, as in bros_attn_latent_prefill.
+
     Order of one run:  bros_latent_append (chunks; their queries' rotated dims where they are)
                        -> bros_attn_latent_prefill
                        -> bros_latent_append (decode rows, likewise) -> bros_attn_latent
@@ -349,7 +355,7 @@ class LatentStep:
     """
 
     def __init__(self, batch, dev, pool, w_kv=None, rope=None, norm=None, eps: float = 1e-6, pass_heads: int | None = None,
-                 max_ctx: int | None = None):
+                 max_ctx: int | None = None, max_ctx_chunks: int | None = None, total_ctx: int | None = None):
         P, S = batch.num_prefill, batch.num_seqs
         counts = np.diff(batch.cu_new)
         if P and w_kv is None:
@@ -362,8 +368,12 @@ class LatentStep:
         rows = int(batch.cu_new[-1]) - self.rows_prefill
         self.drafts = torch.from_numpy(counts[P:].astype(np.int32)).to(device)
         self.cu_rows = torch.from_numpy((batch.cu_new[P:] - batch.cu_new[P]).astype(np.int32)).to(device)
-        self.max_ctx_pre = int(batch.ctx_lens[:P].max()) if P else 0
-        self.total_ctx = int(batch.ctx_lens[:P].sum()) if P else 0
+        longest, total = (int(batch.ctx_lens[:P].max()), int(batch.ctx_lens[:P].sum())) if P else (0, 0)
+        self.max_ctx_pre = longest if max_ctx_chunks is None else int(max_ctx_chunks)
+        self.total_ctx = total if total_ctx is None else int(total_ctx)
+        if self.max_ctx_pre < longest or self.total_ctx < total:
+            raise ValueError(f"chunks of {longest} tokens at most and {total} in all are beyond max_ctx_chunks {self.max_ctx_pre} or "
+                             f"total_ctx {self.total_ctx}")
         self.max_ctx_rows = 16 * dev.block_tables.shape[1] if max_ctx is None else int(max_ctx)
         self.out_chunks = torch.empty((self.rows_prefill, hq, 128), dtype=torch.bfloat16, device=device)
         self.out_rows = torch.empty((rows, hq, 512), dtype=torch.bfloat16, device=device)
