@@ -6,7 +6,10 @@
 // wave, two to a SIMD, and no wave needs another's scores. Up to 128 columns are eight such waves; with
 // fewer columns HV waves share a column group, each computing all its scores and a part of
 // the value dims. The price is LDS: every operand of 1 KiB serves 16 columns, 544 KiB a step and
-// compute unit with 128 columns, twice what the products take. Tried instead, and slower over 96 contexts up to 16384
+// compute unit with 128 columns, twice what the products take; and the rows' permutation (swz, made for 32-row operands)
+// leaves the reads of the keys' 512 dims two-way bank conflicts: the lanes that are served together are of two quarters, and rows 4 to 7 of
+// one meet rows 12 to 15 of the other. They are 32 % of the LDS's active cycles with 128 columns, 37 with 32 and 41 with 16
+// (SQ_LDS_BANK_CONFLICT; the values' reads and the rotated dims' have none). Tried instead, and slower over 96 contexts up to 16384
 // with 128 heads (302 us then, 293 with shares that count starts): 32 columns to a wave and the dims in two halves whose score sums waves exchange, 336 KiB but two
 // barriers a step, 370; four waves of 32 columns and 512 registers, one block of the step's keys each, that exchange
 // weights, 136 KiB for 64 columns, 387, and two such workgroups on the same keys 350: LDS no longer binds, but nothing runs
@@ -16,8 +19,8 @@
 // order what it finds there (rows that are no context, values that are not finite),
 // before the barrier that publishes them, the only one of a step.
 //
-// Measured, kernel and merge: 16 heads, 64 contexts up to 8192, 64 + 5 us, 289 MB, bound by memory; 128 heads, 96 contexts up to 16384,
-// 315 + 19 us, 790 TFLOP/s, bound by LDS; five sequences of five to eight drafts, 32 heads, on up to 4000, 32 + 6 us.
+// Measured, kernel and merge: 16 heads, 64 contexts up to 8192, 65 + 5 us, 289 MB, bound by memory; 128 heads, 96 contexts up to 16384,
+// 315 + 19 us (410 + 22 in the middle of the first twelve calls), 790 TFLOP/s, bound by LDS; five sequences of five to eight drafts, 32 heads, on up to 4000, 32 + 6 us.
 #pragma once
 
 #include "rows_device.h"

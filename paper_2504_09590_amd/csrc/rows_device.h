@@ -24,7 +24,9 @@
 //
 // Teams. Where a sequence has several tiles of columns, TEAM workgroups of a die take them side by side, step by step: the
 // shares are those of teams, and the keys come from memory once (drafts of four tiles read 1.6 GB where the pool's rows
-// are 0.44, at the rate that binds).
+// are 0.44, at the rate that binds). Expanded keys are read again all the same where a (sequence, head) has more tiles than its team:
+// the team comes back to them for each pair, while the other teams of the die pass through other heads' (four
+// chunks of 601 to 1400 rows behind up to 6000, 64 heads: 1.97 GB read, where the dense rows are 0.28).
 //
 // Masks. A row sees the keys before the drafts, and of those the ones its bits name (or the
 // causal ones). Only steps that reach the drafts, the context's end or an invalid table

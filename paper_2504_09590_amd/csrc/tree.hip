@@ -7,7 +7,8 @@
 //
 // Measured, kernel and merge: 16 trees of 17 to 32 drafts on up to 8192 tokens, 32 / 8 heads, 67 + 11 us, 271 MB at 4.0 TB/s
 // (loads alone take 50: starts of shares and masked steps are the rest); six of 64 drafts on 8000 to 32000, 64 / 8 heads,
-// 266 + 13 us, 820 TFLOP/s, 0.44 GB read; one chain of four on 300 tokens, 8 / 2 heads, 12.8 us, a chain of latencies: offsets,
+// 266 + 13 us (306 + 15 in the middle of the first twelve calls), 820 TFLOP/s, 0.44 GB read, matrix cores busy 38 % of the cycles, waves waiting 25, no bank conflicts: what
+// the matrix cores wait for is not shown; one chain of four on 300 tokens, 8 / 2 heads, 12.8 us, a chain of latencies: offsets,
 // table, rows, three steps a wave, the masked one, the groups' sums.
 #include "plan.h"
 #include "rows_launch.h"
