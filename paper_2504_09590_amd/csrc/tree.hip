@@ -26,9 +26,10 @@ constexpr int kCommitRounds = 16;                  // so many times at most
 // table entries, rows): 64 sequences of a bf16 pool with 8 heads 4.6 us, 256 of a latent pool 6.4 us, for 2.3 and 2.8 MB.
 __global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitArgs a) {
   const int s = blockIdx.x;
-  const int n = a.cu_q[s + 1] - a.cu_q[s];
-  const int c0 = a.ctx_lens[s] - n;
-  if (n <= 0 || c0 < 0) return;
+  const int64_t drafts = (int64_t)a.cu_q[s + 1] - a.cu_q[s];
+  const int ctx = a.ctx_lens[s];
+  if (drafts <= 0 || drafts > ctx) return;   // (inconsistent offsets and lengths may be any numbers)
+  const int n = (int)drafts, c0 = ctx - n;
   const int len = min(a.path_lens[s], min(n, a.max_path));
   // 256-byte pieces of a (slot, head) row
   const int pieces = (a.row_bytes + 255) / 256;
